@@ -45,6 +45,28 @@ class AloraAttnDims(ctypes.Structure):
                 ("scale", ctypes.c_float)]
 
 
+class AloraHeadsDims(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("n_tokens", ctypes.c_int32), ("n_q_heads", ctypes.c_int32),
+                ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("norm", ctypes.c_int32), ("rope_positions", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("n_slots", ctypes.c_int64), ("q_stride", ctypes.c_int64),
+                ("q_out_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("k_out_stride", ctypes.c_int64),
+                ("v_stride", ctypes.c_int64), ("v_out_stride", ctypes.c_int64), ("dq_stride", ctypes.c_int64),
+                ("dk_stride", ctypes.c_int64)]
+
+
+class AloraRopeSpec(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("scaling", ctypes.c_int32), ("base", ctypes.c_double),
+                ("factor", ctypes.c_double), ("original", ctypes.c_double), ("low", ctypes.c_double),
+                ("high", ctypes.c_double), ("magnitude", ctypes.c_double)]
+
+
+class AloraCacheDims(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("n_layers", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("block_size", ctypes.c_int32), ("n_slots", ctypes.c_int64),
+                ("k_caches", ctypes.c_void_p), ("v_caches", ctypes.c_void_p)]
+
+
 class AloraError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -107,6 +129,15 @@ def lib() -> ctypes.CDLL:
         L.alora_paged_attention_workspace_bytes.argtypes = [ctypes.POINTER(AloraAttnDims), ctypes.POINTER(sz)]
         L.alora_paged_attention_suffix_split.argtypes = [vp, vp, vp, vp, vp, vp, vp, ctypes.POINTER(AloraAttnDims), vp, sz, vp]
         L.alora_paged_attention_suffix_workspace_bytes.argtypes = [ctypes.POINTER(AloraAttnDims), ctypes.POINTER(sz)]
+        heads, spec, cache = ctypes.POINTER(AloraHeadsDims), ctypes.POINTER(AloraRopeSpec), ctypes.POINTER(AloraCacheDims)
+        L.alora_qk_norm_rope.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, heads, vp]
+        L.alora_qk_norm_rope_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, heads, vp, sz, vp]
+        L.alora_qk_norm_rope_workspace_bytes.argtypes = [heads, ctypes.POINTER(sz)]
+        L.alora_qk_norm_rope_validate.argtypes = [vp, vp, heads]
+        L.alora_rope_tables.argtypes = [vp, vp, i64, i64, spec, vp]
+        L.alora_cache_copy_blocks.argtypes = [vp, vp, i32, cache, vp]
+        L.alora_cache_move_rows.argtypes = [vp, vp, vp, i32, vp, vp, i32, i32, i32, cache, vp]
+        L.alora_cache_move_rows_validate.argtypes = [vp, vp, vp, i32, i32, cache]
         L.alora_status_string.argtypes = [ctypes.c_int]
         L.alora_status_string.restype = ctypes.c_char_p
         L.alora_qkv_set_tuning.argtypes = [ctypes.c_int, ctypes.c_int]
@@ -120,7 +151,9 @@ def lib() -> ctypes.CDLL:
                      "alora_qkv_forward_ex", "alora_qkv_graph_create", "alora_qkv_graph_launch", "alora_qkv_graph_destroy",
                      "alora_paged_attention", "alora_paged_attention_validate", "alora_paged_attention_split", "alora_paged_attention_suffix",
                      "alora_paged_attention_workspace_bytes", "alora_paged_attention_suffix_split",
-                     "alora_paged_attention_suffix_workspace_bytes"):
+                     "alora_paged_attention_suffix_workspace_bytes", "alora_qk_norm_rope", "alora_qk_norm_rope_backward",
+                     "alora_qk_norm_rope_workspace_bytes", "alora_qk_norm_rope_validate", "alora_rope_tables", "alora_cache_copy_blocks",
+                     "alora_cache_move_rows", "alora_cache_move_rows_validate"):
             getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -400,3 +433,149 @@ def alora_paged_attention_suffix_split(q, k_cache, v_cache, block_tables, token_
                                                  _stream_handle(stream))
     if s:
         raise AloraError(s, "alora_paged_attention_suffix_split")
+
+
+# ---- norm and rotary embedding of heads, rotary tables (include/alora_heads.h) -------------------
+def _rows_stride(t, name: str, width: int) -> int:
+    """Elements from row to row of a tensor whose rows are dense; 0 for None."""
+    if t is None:
+        return 0
+    if t.dim() != 2 or t.stride(1) != 1 or t.shape[1] != width:
+        raise ValueError(f"{name}: two dimensions of rows of {width} dense elements expected, got {tuple(t.shape)} with strides {t.stride()}")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), width)
+
+
+def _check_rope(rope) -> None:
+    import torch
+    cos, sin = rope
+    if cos.dim() != 2 or cos.shape != sin.shape or cos.dtype != torch.float32 or sin.dtype != torch.float32 or not (cos.is_contiguous() and sin.is_contiguous()):
+        raise ValueError("rope: two contiguous fp32 tensors [positions, rotary_dim / 2] expected")
+
+
+def make_heads_dims(q, q_out, k, k_out, n_q_heads: int, n_kv_heads: int, head_dim: int, rope=None, interleaved: bool = False,
+                    norm: bool = True, eps: float = 1e-6, v=None, v_out=None, dq=None, dk=None) -> AloraHeadsDims:
+    """Description of alora_qk_norm_rope calls on these tensors, or on others of the same shapes and strides: q, q_out, k, v
+    rows (views of a fused buffer may be given), k_out and v_out the caches; k None: keys are turned where they lie in the cache.  For
+    the backward pass q_out and k_out are the outputs' gradients, and dq, dk the gradients where their strides are not q's and k's."""
+    nq, nkv = n_q_heads * head_dim, n_kv_heads * head_dim
+    if rope is not None:
+        _check_rope(rope)
+    for name, t in (("q_out", q_out), ("k", k), ("k_out", k_out), ("v", v), ("v_out", v_out), ("dq", dq), ("dk", dk)):
+        if t is not None and t.dtype != q.dtype:
+            raise ValueError(f"{name}: {t.dtype}, but q is {q.dtype}")
+    for name, t in (("q_out", q_out), ("k", k), ("v", v), ("dq", dq), ("dk", dk)):
+        if t is not None and t.shape[0] != q.shape[0]:
+            raise ValueError(f"{name}: {t.shape[0]} rows, but q has {q.shape[0]}")
+    if v_out is not None and v_out.shape[0] != k_out.shape[0]:
+        raise ValueError(f"v_out: {v_out.shape[0]} rows, but k_out has {k_out.shape[0]}")
+    return AloraHeadsDims(_dtype_code(q), q.shape[0], n_q_heads, n_kv_heads, head_dim, 0 if rope is None else 2 * rope[0].shape[1],
+                          1 if interleaved else 0, 1 if norm else 0, 0 if rope is None else rope[0].shape[0], eps, k_out.shape[0],
+                          _rows_stride(q, "q", nq), _rows_stride(q_out, "q_out", nq), _rows_stride(k, "k", nkv),
+                          _rows_stride(k_out, "k_out", nkv), _rows_stride(v, "v", nkv), _rows_stride(v_out, "v_out", nkv),
+                          _rows_stride(dq, "dq", nq), _rows_stride(dk, "dk", nkv))
+
+
+def alora_qk_norm_rope(q, q_out, k, k_cache, v, v_cache, wq, wk, rope, token_positions, slot_mapping, dims: AloraHeadsDims,
+                       stream=None) -> None:
+    """Enqueue norm and rotary embedding of the rows' heads (include/alora_heads.h): q to q_out, k (None: in place) to its slots of k_cache,
+    v, where given, to v_cache.  The tensors are those that dims was made from, or of the same shapes and strides; wq and wk are None
+    without norm, rope without rotation."""
+    p = [None if t is None else t.data_ptr() for t in (q, q_out, k, k_cache, v, v_cache, wq, wk, token_positions, slot_mapping)]
+    cos, sin = (None, None) if rope is None else (rope[0].data_ptr(), rope[1].data_ptr())
+    s = lib().alora_qk_norm_rope(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], cos, sin, p[8], p[9], ctypes.byref(dims), _stream_handle(stream))
+    if s:
+        raise AloraError(s, "alora_qk_norm_rope")
+
+
+def alora_qk_norm_rope_workspace_bytes(dims: AloraHeadsDims) -> int:
+    """Bytes of workspace of the backward pass."""
+    out = ctypes.c_size_t(0)
+    s = lib().alora_qk_norm_rope_workspace_bytes(ctypes.byref(dims), ctypes.byref(out))
+    if s:
+        raise AloraError(s, "alora_qk_norm_rope_workspace_bytes")
+    return int(out.value)
+
+
+def alora_qk_norm_rope_backward(q, dq_out, dq, k, dk_out, dk, wq, wk, dwq, dwk, rope, token_positions, dims: AloraHeadsDims,
+                                workspace=None, stream=None) -> None:
+    """Enqueue the backward pass of alora_qk_norm_rope: dq, dk and, with norm, the fp32 dwq, dwk from the gradients of its outputs."""
+    if dq.stride(0) != (dims.dq_stride or dims.q_stride) and dims.n_tokens > 1 or dk.stride(0) != (dims.dk_stride or dims.k_stride) and dims.n_tokens > 1:
+        raise ValueError("dq, dk: strides other than those of dims (make_heads_dims takes dq and dk)")
+    p = [None if t is None else t.data_ptr() for t in (q, dq_out, dq, k, dk_out, dk, wq, wk, dwq, dwk, token_positions, workspace)]
+    cos, sin = (None, None) if rope is None else (rope[0].data_ptr(), rope[1].data_ptr())
+    s = lib().alora_qk_norm_rope_backward(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9], cos, sin, p[10], ctypes.byref(dims), p[11],
+                                          0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_handle(stream))
+    if s:
+        raise AloraError(s, "alora_qk_norm_rope_backward")
+
+
+def alora_qk_norm_rope_validate(token_positions, slot_mapping, dims: AloraHeadsDims) -> int:
+    return int(lib().alora_qk_norm_rope_validate(_ptr(token_positions), _ptr(slot_mapping), ctypes.byref(dims)))
+
+
+ROPE_SCALINGS = {"none": 0, "linear": 1, "by_parts": 2}
+
+
+def make_rope_spec(rotary_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original: float = 0.0, low: float = 1.0,
+                   high: float = 32.0, magnitude: float = 1.0) -> AloraRopeSpec:
+    """Angles of alora_rope_tables: scaling "none", "linear" or "by_parts" (include/alora_heads.h)."""
+    if scaling not in ROPE_SCALINGS:
+        raise ValueError(f"scaling {scaling!r}: one of {', '.join(ROPE_SCALINGS)} expected")
+    return AloraRopeSpec(rotary_dim, ROPE_SCALINGS[scaling], base, factor, original, low, high, magnitude)
+
+
+def alora_rope_tables(cos, sin, spec: AloraRopeSpec, first: int = 0, stream=None) -> None:
+    """Fill the fp32 tensors cos, sin [rows, rotary_dim / 2] for positions first, first + 1, ..."""
+    _check_rope((cos, sin))
+    if 2 * cos.shape[1] != spec.rotary_dim:
+        raise ValueError(f"cos, sin: {cos.shape[1]} columns for a rotary_dim of {spec.rotary_dim}")
+    s = lib().alora_rope_tables(cos.data_ptr(), sin.data_ptr(), first, cos.shape[0], ctypes.byref(spec), _stream_handle(stream))
+    if s:
+        raise AloraError(s, "alora_rope_tables")
+
+
+# ---- what the cache holds, moved (include/alora_cache.h) -----------------------------------------
+def make_cache_dims(k_caches: Sequence, v_caches: Sequence, n_kv_heads: int, head_dim: int, block_size: int) -> AloraCacheDims:
+    """The layers' caches [n_slots, n_kv_heads * head_dim], as alora_cache_copy_blocks and alora_cache_move_rows take them; it keeps the tensors."""
+    if len(k_caches) != len(v_caches) or not k_caches:
+        raise ValueError(f"{len(k_caches)} K caches and {len(v_caches)} V caches")
+    first = k_caches[0]
+    for t in (*k_caches, *v_caches):
+        if t.dtype != first.dtype or t.shape != first.shape or not t.is_contiguous() or t.dim() != 2 or t.shape[1] != n_kv_heads * head_dim:
+            raise ValueError(f"caches: contiguous tensors [n_slots, {n_kv_heads * head_dim}] of one type expected")
+    k, v = _ptr_array(k_caches), _ptr_array(v_caches)
+    d = AloraCacheDims(_dtype_code(first), len(k_caches), n_kv_heads, head_dim, block_size, first.shape[0], _table(k), _table(v))
+    d.keep = (k, v, list(k_caches), list(v_caches))
+    return d
+
+
+def _host_int32(a, name: str) -> int:
+    if a.dtype != "int32" or a.ndim != 1 or not a.flags.c_contiguous:
+        raise ValueError(f"{name}: a contiguous int32 array on the host expected")
+    return a.__array_interface__["data"][0]
+
+
+def alora_cache_copy_blocks(src, dst, dims: AloraCacheDims, stream=None) -> None:
+    """Enqueue copies of blocks src[i] to dst[i] (src[i] = -1: cleared) in every layer; src, dst: int32 numpy arrays."""
+    if len(src) != len(dst):
+        raise ValueError(f"{len(src)} sources and {len(dst)} destinations")
+    s = lib().alora_cache_copy_blocks(_host_int32(src, "src"), _host_int32(dst, "dst"), len(src), ctypes.byref(dims), _stream_handle(stream))
+    if s:
+        raise AloraError(s, "alora_cache_copy_blocks")
+
+
+def alora_cache_move_rows(src, dst, shift, rope, dims: AloraCacheDims, interleaved: bool = False, stream=None) -> None:
+    """Enqueue moves of rows src[i] to dst[i] (int64 device tensors) in every layer, keys turned by shift[i] positions (int32, with the
+    tables rope; both None: rows are only copied)."""
+    n = src.shape[0]
+    if dst.shape[0] != n or (shift is not None and shift.shape[0] != n):
+        raise ValueError("src, dst, shift: one length expected")
+    cos, sin, positions, rot = (None, None, 0, 0) if rope is None else (rope[0].data_ptr(), rope[1].data_ptr(), rope[0].shape[0], 2 * rope[0].shape[1])
+    s = lib().alora_cache_move_rows(src.data_ptr(), dst.data_ptr(), None if shift is None else shift.data_ptr(), n, cos, sin, positions, rot,
+                                    1 if interleaved else 0, ctypes.byref(dims), _stream_handle(stream))
+    if s:
+        raise AloraError(s, "alora_cache_move_rows")
+
+
+def alora_cache_move_rows_validate(src, dst, shift, rope, dims: AloraCacheDims) -> int:
+    return int(lib().alora_cache_move_rows_validate(_ptr(src), _ptr(dst), _ptr(shift), src.shape[0], 0 if rope is None else rope[0].shape[0], ctypes.byref(dims)))

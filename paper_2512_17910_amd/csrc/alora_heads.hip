@@ -1,0 +1,521 @@
+// Norm of query and key heads with the rotary embedding, in one pass; its backward pass; rotary tables (include/alora_heads.h).
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <vector>
+#include "alora_heads.h"
+#include "alora_heads_core.h"
+
+namespace alora {
+
+struct HeadsArgs {
+    const char *q, *k, *v;
+    char *q_out, *kc, *vc;
+    const char *wq, *wk;
+    const float *cos, *sin;
+    const int32_t *pos;
+    const int64_t *slot;
+    long long q_row, qo_row, k_row, ko_row, v_row, vo_row;   // bytes from row to row
+    long long n_slots;
+    HeadShape s;
+    int T, hq, hkv, n_pos;
+    int uq, uk;              // units of 64 >> gshift heads: of queries, of keys
+    float eps, inv_d;
+};
+
+constexpr int HEADS_WAVES = 8;   // wavefronts of a workgroup, at most
+
+// One workgroup per row.  A wavefront takes U units at a time (their loads are requested together), the units of queries and
+// keys first, then the row of v in pieces of 2 KiB.
+template <bool BF16, int V, bool INTERLEAVED, bool NORM, int U>
+__global__ __launch_bounds__(64 * HEADS_WAVES) void heads_kernel(HeadsArgs g)
+{
+    typedef Chunk<BF16, V> C;
+    constexpr int E = BF16 ? 2 : 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, lane = threadIdx.x & 63;
+    const int gs = g.s.gshift, per = 64 >> gs;
+    const LanePlace p = lane_place<V, INTERLEAVED>(g.s, lane & ((1 << gs) - 1));
+    const long long row = (long long)blockIdx.y * ROWS_AT_ONCE + blockIdx.x;
+    if (row >= g.T) return;
+    const long long slot = g.slot[row];
+    const bool store = slot >= 0 && slot < g.n_slots;
+    const int units = g.uq + g.uk, batches = (units + U - 1) / U;
+    const int v_bytes = g.v ? g.hkv * g.s.d * E : 0, all = batches + (v_bytes + 2047) / 2048;
+
+    float c[V], s[V];
+    if (g.s.rot && wave < batches) {
+        const int at = min(max(g.pos[row], 0), g.n_pos - 1);
+        load_angles<V, INTERLEAVED>(g.cos, g.sin, (size_t)at * g.s.half, p, c, s);
+    }
+    for (int i0 = wave; i0 < all; i0 += waves) {
+        if (i0 >= batches) {
+            if (!store) break;
+            const char *from = g.v + row * g.v_row;
+            char *to = g.vc + slot * g.vo_row;
+            const int o = (i0 - batches) * 2048 + lane * 16;
+            u32x4 x, y;
+            if (o < v_bytes) x = *(const u32x4 *)(from + o);
+            if (o + 1024 < v_bytes) y = *(const u32x4 *)(from + o + 1024);
+            if (o < v_bytes) *(u32x4 *)(to + o) = x;
+            if (o + 1024 < v_bytes) *(u32x4 *)(to + o + 1024) = y;
+            continue;
+        }
+        C a[U], b[U], wa[U], wb[U];
+        char *to[U];
+        bool on[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const int unit = i0 * U + i;
+            const bool is_k = unit >= g.uq;
+            const int head = (is_k ? unit - g.uq : unit) * per + (lane >> gs);
+            const long long offset = (long long)head * (g.s.d * E);
+            on[i] = is_k ? store && head < g.hkv : head < g.hq;    // (units behind the last have no such head)
+            const char *from = is_k ? (g.k ? g.k + row * g.k_row : g.kc + slot * g.ko_row) : g.q + row * g.q_row;
+            to[i] = (is_k ? g.kc + slot * g.ko_row : g.q_out + row * g.qo_row) + offset;
+            a[i].zero();
+            b[i].zero();
+            if (on[i] && p.has_a) a[i].load(from + offset + p.a * E);
+            if (on[i] && p.has_b) b[i].load(from + offset + p.b * E);
+            if (NORM) {
+                const char *w = is_k ? g.wk : g.wq;
+                wa[i].zero();
+                wb[i].zero();
+                if (p.has_a) wa[i].load(w + p.a * E);
+                if (p.has_b) wb[i].load(w + p.b * E);
+            }
+        }
+        float r[U];
+        if (NORM) {
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                float x[V], y[V];
+                a[i].widen(x);
+                b[i].widen(y);
+                r[i] = 0.f;
+#pragma unroll
+                for (int e = 0; e < V; ++e) r[i] = fmaf(x[e], x[e], r[i]);
+#pragma unroll
+                for (int e = 0; e < V; ++e) r[i] = fmaf(y[e], y[e], r[i]);
+            }
+            head_sum<U>(r, gs);
+#pragma unroll
+            for (int i = 0; i < U; ++i) r[i] = rsqrtf(fmaf(r[i], g.inv_d, g.eps));
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            float x[V], y[V];
+            a[i].widen(x);
+            b[i].widen(y);
+            if (NORM) {
+                float w[V];
+                wa[i].widen(w);
+#pragma unroll
+                for (int e = 0; e < V; ++e) x[e] = x[e] * r[i] * w[e];
+                wb[i].widen(w);
+#pragma unroll
+                for (int e = 0; e < V; ++e) y[e] = y[e] * r[i] * w[e];
+            }
+            turn<V, INTERLEAVED, false>(x, y, c, s, p);
+            a[i].narrow(x);
+            b[i].narrow(y);
+            if (on[i] && p.has_a) a[i].store(to[i] + p.a * E);
+            if (on[i] && p.has_b) b[i].store(to[i] + p.b * E);
+        }
+    }
+}
+
+struct HeadsBackArgs {
+    const char *q, *k, *gq, *gk;
+    char *dq, *dk;
+    const char *wq, *wk;
+    const float *cos, *sin;
+    const int32_t *pos;
+    long long q_row, k_row, gq_row, gk_row, dq_row, dk_row;
+    float *partial;          // [workgroups][2][d]
+    HeadShape s;
+    int T, hq, hkv, n_pos;
+    int uq, uk, wq_waves;    // the first wq_waves wavefronts of a workgroup take the queries
+    float eps, inv_d;
+};
+
+// Rows blockIdx.x, blockIdx.x + gridDim.x, ...  A wavefront keeps to queries or to keys, so that its lanes' sums for the weights are of
+// one of the two.
+template <bool BF16, int V, bool INTERLEAVED, bool NORM>
+__global__ __launch_bounds__(64 * HEADS_WAVES) void heads_back_kernel(HeadsBackArgs g)
+{
+    typedef Chunk<BF16, V> C;
+    constexpr int E = BF16 ? 2 : 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, lane = threadIdx.x & 63;
+    const int gs = g.s.gshift, per = 64 >> gs;
+    const LanePlace p = lane_place<V, INTERLEAVED>(g.s, lane & ((1 << gs) - 1));
+    const bool is_k = wave >= g.wq_waves;
+    const int heads = is_k ? g.hkv : g.hq, units = is_k ? g.uk : g.uq;
+    const int first = is_k ? wave - g.wq_waves : wave, step = is_k ? waves - g.wq_waves : g.wq_waves;
+    const char *xs = is_k ? g.k : g.q, *gs_in = is_k ? g.gk : g.gq;
+    char *outs = is_k ? g.dk : g.dq;
+    const long long x_row = is_k ? g.k_row : g.q_row, g_row = is_k ? g.gk_row : g.gq_row, d_row = is_k ? g.dk_row : g.dq_row;
+
+    float w0[V], w1[V], dw0[V], dw1[V];
+    if (NORM) {
+        const char *w = is_k ? g.wk : g.wq;
+        C a, b;
+        a.zero();
+        b.zero();
+        if (p.has_a) a.load(w + p.a * E);
+        if (p.has_b) b.load(w + p.b * E);
+        a.widen(w0);
+        b.widen(w1);
+#pragma unroll
+        for (int e = 0; e < V; ++e) dw0[e] = dw1[e] = 0.f;
+    }
+    for (long long row = blockIdx.x; row < g.T; row += gridDim.x) {
+        float c[V], s[V];
+        if (g.s.rot) {
+            const int at = min(max(g.pos[row], 0), g.n_pos - 1);
+            load_angles<V, INTERLEAVED>(g.cos, g.sin, (size_t)at * g.s.half, p, c, s);
+        }
+        for (int unit = first; unit < units; unit += step) {
+            const int head = unit * per + (lane >> gs);
+            const bool on = head < heads;
+            const long long offset = (long long)head * (g.s.d * E);
+            C xa, xb, ga, gb;
+            xa.zero(); xb.zero(); ga.zero(); gb.zero();
+            if (on && p.has_a) {
+                ga.load(gs_in + row * g_row + offset + p.a * E);
+                if (NORM) xa.load(xs + row * x_row + offset + p.a * E);
+            }
+            if (on && p.has_b) {
+                gb.load(gs_in + row * g_row + offset + p.b * E);
+                if (NORM) xb.load(xs + row * x_row + offset + p.b * E);
+            }
+            float u[V], v[V];
+            ga.widen(u);
+            gb.widen(v);
+            turn<V, INTERLEAVED, true>(u, v, c, s, p);
+            if (NORM) {
+                float x[V], y[V], sums[2] = {0.f, 0.f};    // of x x, of x u
+                xa.widen(x);
+                xb.widen(y);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    sums[0] = fmaf(x[e], x[e], sums[0]);
+                    sums[0] = fmaf(y[e], y[e], sums[0]);
+                    sums[1] = fmaf(u[e] * w0[e], x[e], sums[1]);
+                    sums[1] = fmaf(v[e] * w1[e], y[e], sums[1]);
+                }
+                head_sum<2>(sums, gs);
+                const float r = rsqrtf(fmaf(sums[0], g.inv_d, g.eps)), m = r * r * r * (sums[1] * g.inv_d);
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    dw0[e] = fmaf(u[e] * x[e], r, dw0[e]);
+                    dw1[e] = fmaf(v[e] * y[e], r, dw1[e]);
+                    u[e] = r * (u[e] * w0[e]) - x[e] * m;
+                    v[e] = r * (v[e] * w1[e]) - y[e] * m;
+                }
+            }
+            ga.narrow(u);
+            gb.narrow(v);
+            if (on && p.has_a) ga.store(outs + row * d_row + offset + p.a * E);
+            if (on && p.has_b) gb.store(outs + row * d_row + offset + p.b * E);
+        }
+    }
+    if (NORM) {
+        __shared__ float red[HEADS_WAVES][256];
+        for (int m = 1 << gs; m < 64; m <<= 1) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                dw0[e] += __shfl_xor(dw0[e], m);
+                dw1[e] += __shfl_xor(dw1[e], m);
+            }
+        }
+        if (lane < (1 << gs)) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                if (p.has_a) red[wave][p.a + e] = dw0[e];
+                if (p.has_b) red[wave][p.b + e] = dw1[e];
+            }
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < 2 * g.s.d; i += blockDim.x) {
+            const int kind = i >= g.s.d, e = i - kind * g.s.d;
+            float sum = 0.f;
+            for (int w = kind ? g.wq_waves : 0; w < (kind ? waves : g.wq_waves); ++w) sum += red[w][e];
+            g.partial[(size_t)blockIdx.x * 2 * g.s.d + i] = sum;
+        }
+    }
+}
+
+// dw[i] = the workgroups' partial sums added in a fixed order; 16 columns a workgroup, 16 threads a column.
+__global__ __launch_bounds__(256) void heads_weights_kernel(const float *__restrict__ partial, int parts, int d, float *__restrict__ dwq,
+                                                            float *__restrict__ dwk)
+{
+    __shared__ float red[16][17];
+    const int col = threadIdx.x & 15, sl = threadIdx.x >> 4, i = blockIdx.x * 16 + col;
+    float sum = 0.f;
+    if (i < 2 * d) {
+#pragma unroll 8
+        for (int b = sl; b < parts; b += 16) sum += partial[(size_t)b * 2 * d + i];
+    }
+    red[sl][col] = sum;
+    __syncthreads();
+    if (sl == 0 && i < 2 * d) {
+        for (int k = 1; k < 16; ++k) sum += red[k][col];
+        (i < d ? dwq[i] : dwk[i - d]) = sum;
+    }
+}
+
+// Cosines and sines.  A thread keeps to one pair and steps through the rows: angles are added by multiplying exp(i angle) by exp(i step) in 64
+// bits, so that the sines themselves are computed twice a thread.
+__global__ __launch_bounds__(256) void rope_tables_kernel(float *__restrict__ cos, float *__restrict__ sin, long long first, long long rows,
+                                                          int half, int steps, int scaling, double log2_base, double factor, double original,
+                                                          double low, double high, double magnitude)
+{
+    const int at_once = 256 / half;      // rows of a pass
+    const int i = threadIdx.x % half, sub = threadIdx.x / half;
+    if (sub >= at_once) return;
+    constexpr double TWO_PI = 6.283185307179586476925;
+    double theta = exp2(-(double)i / half * log2_base);
+    if (scaling == ALORA_ROPE_LINEAR) theta /= factor;
+    if (scaling == ALORA_ROPE_BY_PARTS) {
+        const double keep = fmin(fmax((original * theta / TWO_PI - low) / (high - low), 0.0), 1.0);
+        theta *= keep + (1.0 - keep) / factor;
+    }
+    const double turns = theta / TWO_PI;
+    long long row = (long long)blockIdx.x * at_once * steps + sub;
+    double t = (double)(first + row) * turns, c, s, dc, ds;
+    sincospi(2.0 * (t - rint(t)), &s, &c);
+    t = at_once * turns;
+    sincospi(2.0 * (t - rint(t)), &ds, &dc);
+    c *= magnitude;
+    s *= magnitude;
+    for (int k = 0; k < steps && row < rows; ++k, row += at_once) {
+        cos[row * half + i] = (float)c;
+        sin[row * half + i] = (float)s;
+        const double n = c * dc - s * ds;
+        s = s * dc + c * ds;
+        c = n;
+    }
+}
+
+// ---- host ---------------------------------------------------------------------------------------
+static inline bool off16(const void *p) { return ((uintptr_t)p & 15) != 0; }
+
+static int check_heads(const alora_heads_dims *d)
+{
+    if (!d) return ALORA_EINVAL;
+    if (d->dtype != ALORA_F32 && d->dtype != ALORA_BF16) return ALORA_EINVAL;
+    if (d->n_tokens < 0 || d->n_q_heads < 1 || d->n_kv_heads < 1 || d->head_dim < 1 || d->rotary_dim < 0 || d->n_slots < 0) return ALORA_EINVAL;
+    if ((d->interleaved | 1) != 1 || (d->norm | 1) != 1 || !(d->eps >= 0.f) || std::isinf(d->eps)) return ALORA_EINVAL;
+    if (d->rotary_dim && d->rope_positions < 1) return ALORA_EINVAL;
+    if (d->head_dim > 256 || d->head_dim % (d->dtype == ALORA_BF16 ? 8 : 4) || d->rotary_dim % 4 || d->rotary_dim > d->head_dim) return ALORA_ESHAPE;
+    if (d->n_q_heads > 0x3fffffff / d->head_dim || d->n_kv_heads > 0x3fffffff / d->head_dim) return ALORA_ESHAPE;
+    if ((long long)d->n_tokens * (d->n_q_heads + 2ll * d->n_kv_heads) > 0x7fffffffll) return ALORA_ESHAPE;
+    return ALORA_OK;
+}
+
+// a stride that holds the row and keeps 16-byte alignment
+static bool bad_stride(int64_t stride, int64_t width, int dtype) { return stride < width || stride % (dtype == ALORA_BF16 ? 8 : 4) || stride > (1ll << 40); }
+
+// V and the layout as template arguments: f(integral_constant V, bool_constant bf16, bool_constant interleaved)
+template <typename F>
+static int with_layout(bool bf16, int V, bool interleaved, F f)
+{
+    using std::integral_constant;
+    using std::bool_constant;
+#define ALORA_CASE(B, N)                                                                                       \
+    if (bf16 == B && V == N)                                                                                   \
+        return interleaved ? f(bool_constant<B>(), integral_constant<int, N>(), bool_constant<true>())          \
+                           : f(bool_constant<B>(), integral_constant<int, N>(), bool_constant<false>());
+    ALORA_CASE(true, 8)
+    ALORA_CASE(true, 4)
+    ALORA_CASE(true, 2)
+    ALORA_CASE(false, 4)
+    ALORA_CASE(false, 2)
+#undef ALORA_CASE
+    return -1;
+}
+
+static int units_of(int heads, const HeadShape &s)
+{
+    const int per = 64 >> s.gshift;
+    return (heads + per - 1) / per;
+}
+
+static int launch_heads(const HeadsArgs &g, bool bf16, int V, bool norm, hipStream_t st)
+{
+    const int units = g.uq + g.uk, v_pieces = g.v ? (g.hkv * g.s.d * (bf16 ? 2 : 4) + 2047) / 2048 : 0;
+    const int U = (long long)g.T * units >= 8192 ? 2 : 1;
+    const int waves = std::min(HEADS_WAVES, (units + U - 1) / U + v_pieces);
+    return with_layout(bf16, V, g.s.interleaved, [&](auto b, auto v, auto il) {
+        const auto go = [&](auto kernel) {
+            launch_kernel(kernel, dim3(std::min(g.T, ROWS_AT_ONCE), (g.T - 1) / ROWS_AT_ONCE + 1), dim3(64 * waves), 0, st, g);
+            return launch_status();
+        };
+        if (norm) return U == 2 ? go(heads_kernel<b.value, v.value, il.value, true, 2>) : go(heads_kernel<b.value, v.value, il.value, true, 1>);
+        return U == 2 ? go(heads_kernel<b.value, v.value, il.value, false, 2>) : go(heads_kernel<b.value, v.value, il.value, false, 1>);
+    });
+}
+
+// Workgroups of the backward pass, each with a row of partial sums.
+static int back_workgroups(const alora_heads_dims *d) { return std::min(d->n_tokens, 1024); }
+
+static size_t back_workspace(const alora_heads_dims *d) { return d->norm ? (size_t)back_workgroups(d) * 2 * d->head_dim * sizeof(float) : 0; }
+
+}  // namespace alora
+
+using namespace alora;
+
+extern "C" {
+
+int alora_qk_norm_rope(const void *q, void *q_out, const void *k, void *k_cache, const void *v, void *v_cache, const void *wq, const void *wk,
+                       const float *cos, const float *sin, const int32_t *positions, const int64_t *slot_mapping, const alora_heads_dims *dims,
+                       void *hip_stream)
+{
+    const int st = check_heads(dims);
+    if (st) return st;
+    const alora_heads_dims &d = *dims;
+    if (d.n_tokens == 0) return ALORA_OK;
+    const int64_t Nq = (int64_t)d.n_q_heads * d.head_dim, Nkv = (int64_t)d.n_kv_heads * d.head_dim;
+    if (!q || !q_out || !slot_mapping || (d.n_slots && !k_cache)) return ALORA_EINVAL;
+    if (!v != !v_cache && d.n_slots) return ALORA_EINVAL;
+    if ((wq != nullptr) != (d.norm != 0) || (wk != nullptr) != (d.norm != 0)) return ALORA_EINVAL;
+    if ((cos != nullptr) != (d.rotary_dim > 0) || (sin != nullptr) != (d.rotary_dim > 0) || (d.rotary_dim && !positions)) return ALORA_EINVAL;
+    if (off16(q) || off16(q_out) || off16(k) || off16(k_cache) || off16(v) || off16(v_cache) || off16(wq) || off16(wk) || off16(cos) || off16(sin) ||
+        ((uintptr_t)positions & 3) || ((uintptr_t)slot_mapping & 7))
+        return ALORA_EINVAL;
+    if (bad_stride(d.q_stride, Nq, d.dtype) || bad_stride(d.q_out_stride, Nq, d.dtype) || bad_stride(d.k_out_stride, Nkv, d.dtype) ||
+        (k && bad_stride(d.k_stride, Nkv, d.dtype)) || (v && (bad_stride(d.v_stride, Nkv, d.dtype) || bad_stride(d.v_out_stride, Nkv, d.dtype))) ||
+        (q == q_out && d.q_stride != d.q_out_stride))
+        return ALORA_EINVAL;
+    const bool bf16 = d.dtype == ALORA_BF16;
+    const int E = bf16 ? 2 : 4, V = head_chunk(bf16, d.rotary_dim, d.interleaved);
+    HeadsArgs g;
+    g.q = (const char *)q; g.q_out = (char *)q_out; g.k = (const char *)k; g.kc = (char *)k_cache;
+    g.v = (const char *)v; g.vc = (char *)v_cache; g.wq = (const char *)wq; g.wk = (const char *)wk;
+    g.cos = cos; g.sin = sin; g.pos = positions; g.slot = slot_mapping;
+    g.q_row = d.q_stride * E; g.qo_row = d.q_out_stride * E; g.k_row = d.k_stride * E; g.ko_row = d.k_out_stride * E;
+    g.v_row = d.v_stride * E; g.vo_row = d.v_out_stride * E;
+    g.n_slots = d.n_slots;
+    g.s = head_shape(d.head_dim, d.rotary_dim, d.interleaved, V);
+    g.T = d.n_tokens; g.hq = d.n_q_heads; g.hkv = d.n_kv_heads; g.n_pos = d.rope_positions;
+    g.uq = units_of(g.hq, g.s); g.uk = units_of(g.hkv, g.s);
+    g.eps = d.eps; g.inv_d = 1.0f / (float)d.head_dim;
+    const int e = launch_heads(g, bf16, V, d.norm, (hipStream_t)hip_stream);
+    if (e) { note_hip_error(e); return ALORA_EHIP; }
+    return ALORA_OK;
+}
+
+int alora_qk_norm_rope_workspace_bytes(const alora_heads_dims *dims, size_t *out_bytes)
+{
+    if (!out_bytes) return ALORA_EINVAL;
+    const int st = check_heads(dims);
+    if (st) return st;
+    *out_bytes = back_workspace(dims);
+    return ALORA_OK;
+}
+
+int alora_qk_norm_rope_backward(const void *q, const void *dq_out, void *dq, const void *k, const void *dk_out, void *dk, const void *wq,
+                                const void *wk, float *dwq, float *dwk, const float *cos, const float *sin, const int32_t *positions,
+                                const alora_heads_dims *dims, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    const int st = check_heads(dims);
+    if (st) return st;
+    const alora_heads_dims &d = *dims;
+    const int64_t Nq = (int64_t)d.n_q_heads * d.head_dim, Nkv = (int64_t)d.n_kv_heads * d.head_dim;
+    if ((wq != nullptr) != (d.norm != 0) || (wk != nullptr) != (d.norm != 0) || (dwq != nullptr) != (d.norm != 0) || (dwk != nullptr) != (d.norm != 0))
+        return ALORA_EINVAL;
+    if (off16(wq) || off16(wk) || off16(dwq) || off16(dwk)) return ALORA_EINVAL;
+    const int64_t dq_stride = d.dq_stride ? d.dq_stride : d.q_stride, dk_stride = d.dk_stride ? d.dk_stride : d.k_stride;
+    if (d.n_tokens) {
+        if (!q || !dq_out || !dq || !k || !dk_out || !dk) return ALORA_EINVAL;
+        if ((cos != nullptr) != (d.rotary_dim > 0) || (sin != nullptr) != (d.rotary_dim > 0) || (d.rotary_dim && !positions)) return ALORA_EINVAL;
+        if (off16(q) || off16(dq_out) || off16(dq) || off16(k) || off16(dk_out) || off16(dk) || off16(cos) || off16(sin) || ((uintptr_t)positions & 3))
+            return ALORA_EINVAL;
+        if (bad_stride(d.q_stride, Nq, d.dtype) || bad_stride(d.q_out_stride, Nq, d.dtype) || bad_stride(d.k_stride, Nkv, d.dtype) ||
+            bad_stride(d.k_out_stride, Nkv, d.dtype) || bad_stride(dq_stride, Nq, d.dtype) || bad_stride(dk_stride, Nkv, d.dtype) ||
+            (dq == dq_out && dq_stride != d.q_out_stride) || (dk == dk_out && dk_stride != d.k_out_stride))
+            return ALORA_EINVAL;
+    }
+    const size_t need = back_workspace(dims);
+    if (need && (!workspace || off16(workspace) || workspace_bytes < need)) return ALORA_EWORKSPACE;
+    const bool bf16 = d.dtype == ALORA_BF16;
+    const int E = bf16 ? 2 : 4, V = head_chunk(bf16, d.rotary_dim, d.interleaved), groups = back_workgroups(dims);
+    HeadsBackArgs g;
+    g.q = (const char *)q; g.k = (const char *)k; g.gq = (const char *)dq_out; g.gk = (const char *)dk_out; g.dq = (char *)dq; g.dk = (char *)dk;
+    g.wq = (const char *)wq; g.wk = (const char *)wk;
+    g.cos = cos; g.sin = sin; g.pos = positions;
+    g.q_row = d.q_stride * E; g.k_row = d.k_stride * E; g.gq_row = d.q_out_stride * E; g.gk_row = d.k_out_stride * E;
+    g.dq_row = dq_stride * E; g.dk_row = dk_stride * E;
+    g.partial = (float *)workspace;
+    g.s = head_shape(d.head_dim, d.rotary_dim, d.interleaved, V);
+    g.T = d.n_tokens; g.hq = d.n_q_heads; g.hkv = d.n_kv_heads; g.n_pos = d.rope_positions;
+    g.uq = units_of(g.hq, g.s); g.uk = units_of(g.hkv, g.s);
+    g.eps = d.eps; g.inv_d = 1.0f / (float)d.head_dim;
+    // wavefronts by the share of the units, one for each kind at least
+    const int waves = std::min(HEADS_WAVES, g.uq + g.uk);
+    g.wq_waves = std::max(1, std::min(waves - 1, (int)((long long)waves * g.uq / (g.uq + g.uk))));
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    int e = 0;
+    if (groups)
+        e = with_layout(bf16, V, d.interleaved, [&](auto b, auto v, auto il) {
+            if (d.norm) launch_kernel(heads_back_kernel<b.value, v.value, il.value, true>, dim3(groups), dim3(64 * waves), 0, stream, g);
+            else launch_kernel(heads_back_kernel<b.value, v.value, il.value, false>, dim3(groups), dim3(64 * waves), 0, stream, g);
+            return launch_status();
+        });
+    if (!e && d.norm) {
+        launch_kernel(heads_weights_kernel, dim3((2 * d.head_dim + 15) / 16), dim3(256), 0, stream, (const float *)workspace, groups, (int)d.head_dim, dwq, dwk);
+        e = launch_status();
+    }
+    if (e) { note_hip_error(e); return ALORA_EHIP; }
+    return ALORA_OK;
+}
+
+int alora_qk_norm_rope_validate(const int32_t *positions, const int64_t *slot_mapping, const alora_heads_dims *dims)
+{
+    const int st = check_heads(dims);
+    if (st) return st;
+    const size_t T = (size_t)dims->n_tokens;
+    if (T == 0) return ALORA_OK;
+    if (!slot_mapping || (dims->rotary_dim && !positions)) return ALORA_EINVAL;
+    try {
+        std::vector<int32_t> pos(dims->rotary_dim ? T : 0);
+        std::vector<int64_t> slot(T);
+        hipError_t e = hipMemcpy(slot.data(), slot_mapping, 8 * T, hipMemcpyDeviceToHost);
+        if (!e && dims->rotary_dim) e = hipMemcpy(pos.data(), positions, 4 * T, hipMemcpyDeviceToHost);
+        if (e) { note_hip_error((int)e); return ALORA_EHIP; }
+        for (int32_t x : pos)
+            if (x < 0 || x >= dims->rope_positions) return ALORA_EDATA;
+        std::sort(slot.begin(), slot.end());
+        if (slot.front() < -1 || slot.back() >= dims->n_slots) return ALORA_EDATA;
+        for (size_t i = 1; i < T; ++i)
+            if (slot[i] >= 0 && slot[i] == slot[i - 1]) return ALORA_EDATA;
+        return ALORA_OK;
+    } catch (const std::bad_alloc &) {
+        return ALORA_ENOMEM;
+    }
+}
+
+int alora_rope_tables(float *cos, float *sin, int64_t first, int64_t rows, const alora_rope_spec *spec, void *hip_stream)
+{
+    if (!spec || first < 0 || rows < 0) return ALORA_EINVAL;
+    const alora_rope_spec &s = *spec;
+    if (s.scaling < ALORA_ROPE_PLAIN || s.scaling > ALORA_ROPE_BY_PARTS || !(s.base > 0.0) || std::isinf(s.base) || !std::isfinite(s.magnitude)) return ALORA_EINVAL;
+    if (s.scaling != ALORA_ROPE_PLAIN && (!(s.factor > 0.0) || std::isinf(s.factor))) return ALORA_EINVAL;
+    if (s.scaling == ALORA_ROPE_BY_PARTS && (!(s.original > 0.0) || std::isinf(s.original) || !std::isfinite(s.low) || !std::isfinite(s.high) || !(s.low < s.high)))
+        return ALORA_EINVAL;
+    if (s.rotary_dim < 2 || s.rotary_dim > 512 || s.rotary_dim % 2) return ALORA_ESHAPE;
+    if (first > (1 << 24) || rows > (1 << 24) - first) return ALORA_ESHAPE;
+    if (rows == 0) return ALORA_OK;
+    if (!cos || !sin || off16(cos) || off16(sin)) return ALORA_EINVAL;
+    const int half = s.rotary_dim / 2, at_once = 256 / half;
+    // rows per thread: about 2048 workgroups, at most 64 steps
+    const int steps = (int)std::max<int64_t>(1, std::min<int64_t>(64, rows / ((int64_t)at_once * 2048)));
+    const int64_t groups = (rows + (int64_t)at_once * steps - 1) / ((int64_t)at_once * steps);
+    launch_kernel(rope_tables_kernel, dim3((unsigned)groups), dim3(256), 0, (hipStream_t)hip_stream, cos, sin, (long long)first, (long long)rows, half, steps,
+                  (int)s.scaling, std::log2(s.base), s.factor, s.original, s.low, s.high, s.magnitude);
+    const int e = launch_status();
+    if (e) { note_hip_error(e); return ALORA_EHIP; }
+    return ALORA_OK;
+}
+
+}  // extern "C"

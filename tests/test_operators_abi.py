@@ -1,0 +1,193 @@
+"""Refusals of the head and cache operators, found on the host before anything is launched (CPU; dummy addresses that nothing
+dereferences), and the launches of calls, recorded without a GPU."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2512_17910_amd import binding as ab
+
+P = 0x100000
+OK, EINVAL, ESHAPE, EWORKSPACE, EDATA = ab.ALORA_OK, ab.ALORA_EINVAL, ab.ALORA_ESHAPE, ab.ALORA_EWORKSPACE, ab.ALORA_EDATA
+
+
+def heads_dims(**kw):
+    d = dict(dtype=1, n_tokens=7, n_q_heads=4, n_kv_heads=2, head_dim=64, rotary_dim=64, interleaved=0, norm=1, rope_positions=100, eps=1e-6,
+             n_slots=64, q_stride=256, q_out_stride=256, k_stride=128, k_out_stride=128, v_stride=128, v_out_stride=128, dq_stride=0, dk_stride=0)
+    d.update(kw)
+    return ab.AloraHeadsDims(**d)
+
+
+FORWARD = ("q", "q_out", "k", "kc", "v", "vc", "wq", "wk", "cos", "sin", "pos", "slot")
+
+
+def forward(dims, **kw):
+    a = {n: P for n in FORWARD}
+    a["q_out"] = P + 0x1000
+    a.update(kw)
+    return ab.lib().alora_qk_norm_rope(*[a[n] for n in FORWARD], ctypes.byref(dims), None)
+
+
+BACKWARD = ("q", "gq", "dq", "k", "gk", "dk", "wq", "wk", "dwq", "dwk", "cos", "sin", "pos")
+
+
+def backward(dims, ws=P, size=1 << 24, **kw):
+    a = {n: P + 0x1000 * i for i, n in enumerate(BACKWARD)}
+    a.update(kw)
+    return ab.lib().alora_qk_norm_rope_backward(*[a[n] for n in BACKWARD], ctypes.byref(dims), ws, size, None)
+
+
+SHAPES = [(dict(dtype=3), EINVAL), (dict(n_tokens=-1), EINVAL), (dict(n_q_heads=0), EINVAL), (dict(n_kv_heads=0), EINVAL), (dict(head_dim=0), EINVAL),
+          (dict(rotary_dim=-4), EINVAL), (dict(interleaved=2), EINVAL), (dict(norm=-1), EINVAL), (dict(eps=-1.0), EINVAL), (dict(eps=float("nan")), EINVAL),
+          (dict(eps=float("inf")), EINVAL), (dict(rope_positions=0), EINVAL), (dict(n_slots=-1), EINVAL), (dict(head_dim=60), ESHAPE),
+          (dict(dtype=0, head_dim=66), ESHAPE), (dict(head_dim=264), ESHAPE), (dict(rotary_dim=62), ESHAPE), (dict(rotary_dim=68), ESHAPE),
+          (dict(n_tokens=1 << 29), ESHAPE), (dict(n_q_heads=1 << 26), ESHAPE)]
+
+
+@pytest.mark.parametrize("kw,status", SHAPES)
+def test_shapes_are_refused(kw, status):
+    d = heads_dims(**kw)
+    n = ctypes.c_size_t(0)
+    assert forward(d) == backward(d) == status
+    assert ab.lib().alora_qk_norm_rope_workspace_bytes(ctypes.byref(d), ctypes.byref(n)) == status
+    assert ab.lib().alora_qk_norm_rope_validate(P, P, ctypes.byref(d)) == status
+
+
+def test_forward_arguments_are_refused():
+    d = heads_dims()
+    for name in ("q", "q_out", "kc", "vc", "wq", "wk", "cos", "sin", "pos", "slot"):
+        assert forward(d, **{name: None}) == EINVAL, name
+    for name in FORWARD:
+        assert forward(d, **{name: P + (4 if name == "slot" else 2 if name == "pos" else 8)}) == EINVAL, name
+    assert forward(heads_dims(norm=0)) == EINVAL and forward(heads_dims(rotary_dim=0)) == EINVAL       # weights, tables that no step takes
+    for name, bad in (("q_stride", 248), ("q_out_stride", 257), ("k_stride", 120), ("k_out_stride", 132), ("v_stride", -128), ("v_out_stride", 1 << 41)):
+        assert forward(heads_dims(**{name: bad})) == EINVAL, name
+    assert forward(heads_dims(q_stride=264), q_out=P) == EINVAL                                        # in place, strides differ
+    assert ab.lib().alora_qk_norm_rope(*[P] * 12, None, None) == EINVAL
+    assert forward(heads_dims(n_tokens=0), q=None, q_out=None, kc=None, slot=None) == OK
+
+
+def test_backward_arguments_are_refused():
+    d = heads_dims()
+    for name in BACKWARD:
+        assert backward(d, **{name: None}) == EINVAL, name
+        assert backward(d, **{name: P + (2 if name == "pos" else 8)}) == EINVAL, name
+    for name, bad in (("q_stride", 248), ("q_out_stride", 257), ("k_stride", 120), ("k_out_stride", 132), ("dq_stride", 128), ("dk_stride", 64)):
+        assert backward(heads_dims(**{name: bad})) == EINVAL, name
+    need = ab.alora_qk_norm_rope_workspace_bytes(d)
+    assert need == 7 * 2 * 64 * 4
+    assert backward(d, ws=None) == backward(d, ws=P + 8) == backward(d, size=need - 1) == EWORKSPACE
+    assert ab.alora_qk_norm_rope_workspace_bytes(heads_dims(norm=0)) == 0 == ab.alora_qk_norm_rope_workspace_bytes(heads_dims(n_tokens=0))
+    assert backward(heads_dims(norm=0, n_tokens=0), ws=None, size=0, wq=None, wk=None, dwq=None, dwk=None) == OK
+    assert backward(heads_dims(q_out_stride=264), dq=P + 0x1000) == EINVAL                             # dq in dq_out's place, strides differ
+
+
+def spec(**kw):
+    d = dict(rotary_dim=64, scaling=2, base=1e4, factor=4.0, original=2048.0, low=1.0, high=32.0, magnitude=1.0)
+    d.update(kw)
+    return ab.AloraRopeSpec(**d)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(scaling=3), EINVAL), (dict(base=0.0), EINVAL), (dict(base=float("nan")), EINVAL), (dict(base=float("inf")), EINVAL), (dict(factor=0.0), EINVAL),
+    (dict(factor=float("inf")), EINVAL), (dict(original=0.0), EINVAL), (dict(low=32.0), EINVAL), (dict(high=float("nan")), EINVAL),
+    (dict(magnitude=float("inf")), EINVAL), (dict(rotary_dim=0), ESHAPE), (dict(rotary_dim=7), ESHAPE), (dict(rotary_dim=514), ESHAPE)])
+def test_rope_specs_are_refused(kw, status):
+    assert ab.lib().alora_rope_tables(P, P, 0, 8, ctypes.byref(spec(**kw)), None) == status
+
+
+def test_rope_table_arguments_are_refused():
+    f = lambda cos=P, sin=P, first=0, rows=8, s=spec(): ab.lib().alora_rope_tables(cos, sin, first, rows, None if s is None else ctypes.byref(s), None)
+    assert f(cos=None) == f(sin=None) == f(cos=P + 4) == f(first=-1) == f(rows=-1) == f(s=None) == EINVAL
+    assert f(first=1 << 24, rows=1) == f(rows=(1 << 24) + 1) == f(first=1 << 62) == ESHAPE
+    assert f(rows=0, cos=None, sin=None) == OK
+    # what the scaling does not take is not looked at
+    assert f(rows=0, s=spec(scaling=0, factor=0.0, original=0.0)) == OK
+    with pytest.raises(ValueError):
+        ab.make_rope_spec(64, scaling="other")
+    with pytest.raises(ValueError):
+        ab.alora_rope_tables(torch.zeros(4, 31), torch.zeros(4, 31), ab.make_rope_spec(64))
+
+
+def cache_dims(n_layers=2, ptr=P, **kw):
+    d = dict(dtype=1, n_layers=n_layers, n_kv_heads=2, head_dim=64, block_size=16, n_slots=256)
+    d.update(kw)
+    tab = (ctypes.c_void_p * max(1, n_layers))(*[ptr] * n_layers)
+    c = ab.AloraCacheDims(**d, k_caches=ctypes.cast(tab, ctypes.c_void_p), v_caches=ctypes.cast(tab, ctypes.c_void_p))
+    c.keep = tab
+    return c
+
+
+def copy(src, dst, dims=None, n=None):
+    s, d = (None if x is None else np.array(x, np.int32) for x in (src, dst))
+    dims = dims or cache_dims()
+    return ab.lib().alora_cache_copy_blocks(None if s is None else s.ctypes.data, None if d is None else d.ctypes.data, len(s) if n is None else n,
+                                            ctypes.byref(dims), None)
+
+
+def move(dims=None, n=3, rot=64, pos=10, il=0, **kw):
+    a = dict(src=P, dst=P, shift=P, cos=P, sin=P)
+    a.update(kw)
+    dims = dims or cache_dims()
+    return ab.lib().alora_cache_move_rows(a["src"], a["dst"], a["shift"], n, a["cos"], a["sin"], pos, rot, il, ctypes.byref(dims), None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dtype=2), EINVAL), (dict(n_layers=-1), EINVAL), (dict(n_kv_heads=0), EINVAL), (dict(head_dim=0), EINVAL), (dict(block_size=0), EINVAL),
+    (dict(n_slots=-16), EINVAL), (dict(head_dim=60), ESHAPE), (dict(head_dim=264), ESHAPE), (dict(n_slots=250), ESHAPE), (dict(n_layers=4097), ESHAPE),
+    (dict(n_slots=1 << 50), ESHAPE), (dict(block_size=1 << 24, n_slots=1 << 24), ESHAPE), (dict(ptr=None), EINVAL), (dict(ptr=P + 8), EINVAL)])
+def test_caches_are_refused(kw, status):
+    if kw.get("n_layers") == -1:
+        d = cache_dims(1)
+        d.n_layers = -1
+    else:
+        d = cache_dims(**kw)
+    assert copy([0], [1], d) == move(d) == status
+    if "ptr" not in kw:
+        assert ab.lib().alora_cache_move_rows_validate(P, P, P, 3, 10, ctypes.byref(d)) == status
+
+
+@pytest.mark.parametrize("n", [0, 30])      # (short and long lists are checked in different ways)
+def test_lists_of_blocks_are_refused(n):
+    fill = lambda a, first: a + list(range(first, first + n))
+    d = cache_dims(n_slots=16 * 200)
+    for src, dst in (([0, 200], [1, 2]), ([0, -2], [1, 2]), ([0, 1], [3, 200]), ([0, 1], [3, -1]), ([0, 1], [3, 3]), ([0, 1], [1, 2]), ([5, 1], [5, 2]),
+                     ([-1, -1], [4, 4]), ([-1, 4], [4, 6])):
+        assert copy(fill(src, 40), fill(dst, 100), d) == EDATA, (src, dst)
+    assert copy(None, [1], d, 1) == copy([1], None, d, 1) == copy([1], [2], d, -1) == EINVAL
+    assert copy([], [], d) == OK and copy([1], [2], cache_dims(0)) == OK
+    assert copy([0], [1], cache_dims(n_slots=0)) == EDATA
+
+
+def test_move_arguments_are_refused():
+    for name in ("src", "dst", "shift", "cos", "sin"):
+        assert move(**{name: None}) == EINVAL, name
+        assert move(**{name: P + (2 if name == "shift" else 4)}) == EINVAL, name
+    assert move(n=-1) == move(rot=-4) == move(il=2) == move(pos=0) == move(rot=0) == EINVAL
+    assert move(rot=62) == move(rot=68) == ESHAPE
+    assert move(n=0) == move(dims=cache_dims(0)) == OK
+
+
+def test_binding_refuses_what_it_would_misread():
+    t = lambda *s: torch.zeros(*s)
+    q, k = t(4, 128), t(32, 64)
+    rope = (t(10, 16), t(10, 16))
+    ok = ab.make_heads_dims(q, q, None, k, 4, 2, 32, rope=rope)
+    assert (ok.rotary_dim, ok.q_stride, ok.k_stride, ok.k_out_stride, ok.rope_positions, ok.n_slots) == (32, 128, 0, 64, 10, 32)
+    for bad in (lambda: ab.make_heads_dims(q, q, None, k, 4, 2, 64, rope=rope), lambda: ab.make_heads_dims(q.t(), q, None, k, 4, 2, 32),
+                lambda: ab.make_heads_dims(q, q.bfloat16(), None, k, 4, 2, 32), lambda: ab.make_heads_dims(q, q[:2], None, k, 4, 2, 32),
+                lambda: ab.make_heads_dims(q, q, None, k, 4, 2, 32, rope=(rope[0].double(), rope[1])),
+                lambda: ab.make_heads_dims(q, q, None, k, 4, 2, 32, rope=(rope[0], rope[1][:9])),
+                lambda: ab.make_heads_dims(q, q, k[:4], k, 4, 2, 32, v=k[:4], v_out=k[:20]),
+                lambda: ab.make_cache_dims([k], [k[:16]], 2, 32, 16), lambda: ab.make_cache_dims([], [], 2, 32, 16),
+                lambda: ab.make_cache_dims([k], [k, k], 2, 32, 16), lambda: ab.make_cache_dims([k.t()], [k.t()], 2, 32, 16),
+                lambda: ab.alora_cache_copy_blocks(np.zeros(2, np.int64), np.ones(2, np.int32), ab.make_cache_dims([k], [k], 2, 32, 16)),
+                lambda: ab.alora_cache_copy_blocks(np.zeros(2, np.int32), np.ones(1, np.int32), ab.make_cache_dims([k], [k], 2, 32, 16)),
+                lambda: ab.alora_cache_move_rows(torch.zeros(2).long(), torch.zeros(3).long(), None, None, ab.make_cache_dims([k], [k], 2, 32, 16)),
+                lambda: ab.alora_qk_norm_rope_backward(q, q, t(4, 256)[:, :128], k[:4], k[:4], k[:4], None, None, None, None, rope, None,
+                                                       ab.make_heads_dims(q, q, k[:4], k[:4], 4, 2, 32, rope=rope, norm=False))):
+        with pytest.raises(ValueError):
+            bad()
+    one = ab.make_heads_dims(q[:1], q[:1], None, k, 4, 2, 32)
+    assert one.q_stride >= 128
