@@ -43,6 +43,7 @@ int alora_cache_copy_blocks(const int32_t *src, const int32_t *dst, int32_t n, c
  * R as in alora_qk_norm_rope, with cos, sin at |shift[i]| and the sine's sign that of the shift.  A key that was stored
  * for position p then stands for p + shift[i], whatever base and scaling the tables have, as long as p and the
  * shift count positions of the same tables.  The tables' magnitude has to be 1 (cached keys hold it already).
+ * Limit (ALORA_ESHAPE): n_rows * n_kv_heads <= 2^25.
  * fp32 products, one rounding; keys of rows with shift 0 are copied bit for bit.
  *   src, dst        [n_rows] int64; a row outside [0, n_slots) on either side is left alone
  *   shift           [n_rows] int32, NULL: rows are only copied (then cos and sin are NULL and rotary_dim is 0);

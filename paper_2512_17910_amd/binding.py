@@ -480,9 +480,13 @@ def alora_qk_norm_rope(q, q_out, k, k_cache, v, v_cache, wq, wk, rope, token_pos
     """Enqueue norm and rotary embedding of the rows' heads (include/alora_heads.h): q to q_out, k (None: in place) to its slots of k_cache,
     v, where given, to v_cache.  The tensors are those that dims was made from, or of the same shapes and strides; wq and wk are None
     without norm, rope without rotation."""
-    p = [None if t is None else t.data_ptr() for t in (q, q_out, k, k_cache, v, v_cache, wq, wk, token_positions, slot_mapping)]
-    cos, sin = (None, None) if rope is None else (rope[0].data_ptr(), rope[1].data_ptr())
-    s = lib().alora_qk_norm_rope(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], cos, sin, p[8], p[9], ctypes.byref(dims), _stream_handle(stream))
+    cos, sin = (None, None) if rope is None else rope
+    s = (_lib or lib()).alora_qk_norm_rope(q.data_ptr(), q_out.data_ptr(), None if k is None else k.data_ptr(), k_cache.data_ptr(),
+                                           None if v is None else v.data_ptr(), None if v_cache is None else v_cache.data_ptr(),
+                                           None if wq is None else wq.data_ptr(), None if wk is None else wk.data_ptr(),
+                                           None if cos is None else cos.data_ptr(), None if sin is None else sin.data_ptr(),
+                                           None if token_positions is None else token_positions.data_ptr(), slot_mapping.data_ptr(),
+                                           ctypes.byref(dims), _stream_handle(stream))
     if s:
         raise AloraError(s, "alora_qk_norm_rope")
 
@@ -499,12 +503,15 @@ def alora_qk_norm_rope_workspace_bytes(dims: AloraHeadsDims) -> int:
 def alora_qk_norm_rope_backward(q, dq_out, dq, k, dk_out, dk, wq, wk, dwq, dwk, rope, token_positions, dims: AloraHeadsDims,
                                 workspace=None, stream=None) -> None:
     """Enqueue the backward pass of alora_qk_norm_rope: dq, dk and, with norm, the fp32 dwq, dwk from the gradients of its outputs."""
-    if dq.stride(0) != (dims.dq_stride or dims.q_stride) and dims.n_tokens > 1 or dk.stride(0) != (dims.dk_stride or dims.k_stride) and dims.n_tokens > 1:
+    if dims.n_tokens > 1 and (dq.stride(0) != (dims.dq_stride or dims.q_stride) or dk.stride(0) != (dims.dk_stride or dims.k_stride)):
         raise ValueError("dq, dk: strides other than those of dims (make_heads_dims takes dq and dk)")
-    p = [None if t is None else t.data_ptr() for t in (q, dq_out, dq, k, dk_out, dk, wq, wk, dwq, dwk, token_positions, workspace)]
-    cos, sin = (None, None) if rope is None else (rope[0].data_ptr(), rope[1].data_ptr())
-    s = lib().alora_qk_norm_rope_backward(p[0], p[1], p[2], p[3], p[4], p[5], p[6], p[7], p[8], p[9], cos, sin, p[10], ctypes.byref(dims), p[11],
-                                          0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_handle(stream))
+    cos, sin = (None, None) if rope is None else rope
+    s = (_lib or lib()).alora_qk_norm_rope_backward(
+        q.data_ptr(), dq_out.data_ptr(), dq.data_ptr(), k.data_ptr(), dk_out.data_ptr(), dk.data_ptr(), None if wq is None else wq.data_ptr(),
+        None if wk is None else wk.data_ptr(), None if dwq is None else dwq.data_ptr(), None if dwk is None else dwk.data_ptr(),
+        None if cos is None else cos.data_ptr(), None if sin is None else sin.data_ptr(),
+        None if token_positions is None else token_positions.data_ptr(), ctypes.byref(dims), None if workspace is None else workspace.data_ptr(),
+        0 if workspace is None else workspace.nbytes, _stream_handle(stream))
     if s:
         raise AloraError(s, "alora_qk_norm_rope_backward")
 
@@ -526,10 +533,10 @@ def make_rope_spec(rotary_dim: int, base: float = 10000.0, scaling: str = "none"
 
 def alora_rope_tables(cos, sin, spec: AloraRopeSpec, first: int = 0, stream=None) -> None:
     """Fill the fp32 tensors cos, sin [rows, rotary_dim / 2] for positions first, first + 1, ..."""
-    _check_rope((cos, sin))
-    if 2 * cos.shape[1] != spec.rotary_dim:
-        raise ValueError(f"cos, sin: {cos.shape[1]} columns for a rotary_dim of {spec.rotary_dim}")
-    s = lib().alora_rope_tables(cos.data_ptr(), sin.data_ptr(), first, cos.shape[0], ctypes.byref(spec), _stream_handle(stream))
+    rows, pairs = cos.shape
+    if 2 * pairs != spec.rotary_dim or sin.shape != cos.shape or not (cos.is_contiguous() and sin.is_contiguous()) or _dtype_code(cos) or _dtype_code(sin):
+        raise ValueError(f"cos, sin: contiguous fp32 tensors [rows, {spec.rotary_dim // 2}] expected")
+    s = (_lib or lib()).alora_rope_tables(cos.data_ptr(), sin.data_ptr(), first, rows, ctypes.byref(spec), _stream_handle(stream))
     if s:
         raise AloraError(s, "alora_rope_tables")
 
@@ -539,18 +546,19 @@ def make_cache_dims(k_caches: Sequence, v_caches: Sequence, n_kv_heads: int, hea
     """The layers' caches [n_slots, n_kv_heads * head_dim], as alora_cache_copy_blocks and alora_cache_move_rows take them; it keeps the tensors."""
     if len(k_caches) != len(v_caches) or not k_caches:
         raise ValueError(f"{len(k_caches)} K caches and {len(v_caches)} V caches")
-    first = k_caches[0]
-    for t in (*k_caches, *v_caches):
-        if t.dtype != first.dtype or t.shape != first.shape or not t.is_contiguous() or t.dim() != 2 or t.shape[1] != n_kv_heads * head_dim:
-            raise ValueError(f"caches: contiguous tensors [n_slots, {n_kv_heads * head_dim}] of one type expected")
-    k, v = _ptr_array(k_caches), _ptr_array(v_caches)
-    d = AloraCacheDims(_dtype_code(first), len(k_caches), n_kv_heads, head_dim, block_size, first.shape[0], _table(k), _table(v))
-    d.keep = (k, v, list(k_caches), list(v_caches))
+    tensors = [*k_caches, *v_caches]
+    dtype, shape = tensors[0].dtype, (tensors[0].shape[0], n_kv_heads * head_dim)
+    if not all(t.shape == shape and t.dtype is dtype and t.is_contiguous() for t in tensors):
+        raise ValueError(f"caches: contiguous tensors [n_slots, {n_kv_heads * head_dim}] of one type expected")
+    ptrs, n = _ptr_array(tensors), len(k_caches)
+    at = _table(ptrs)
+    d = AloraCacheDims(_dtype_code(tensors[0]), n, n_kv_heads, head_dim, block_size, shape[0], at, at + 8 * n)
+    d.keep = (ptrs, tensors)
     return d
 
 
 def _host_int32(a, name: str) -> int:
-    if a.dtype != "int32" or a.ndim != 1 or not a.flags.c_contiguous:
+    if a.dtype.char != "i" or a.ndim != 1 or a.strides != (4,):
         raise ValueError(f"{name}: a contiguous int32 array on the host expected")
     return a.__array_interface__["data"][0]
 
@@ -559,7 +567,7 @@ def alora_cache_copy_blocks(src, dst, dims: AloraCacheDims, stream=None) -> None
     """Enqueue copies of blocks src[i] to dst[i] (src[i] = -1: cleared) in every layer; src, dst: int32 numpy arrays."""
     if len(src) != len(dst):
         raise ValueError(f"{len(src)} sources and {len(dst)} destinations")
-    s = lib().alora_cache_copy_blocks(_host_int32(src, "src"), _host_int32(dst, "dst"), len(src), ctypes.byref(dims), _stream_handle(stream))
+    s = (_lib or lib()).alora_cache_copy_blocks(_host_int32(src, "src"), _host_int32(dst, "dst"), len(src), ctypes.byref(dims), _stream_handle(stream))
     if s:
         raise AloraError(s, "alora_cache_copy_blocks")
 
@@ -571,7 +579,7 @@ def alora_cache_move_rows(src, dst, shift, rope, dims: AloraCacheDims, interleav
     if dst.shape[0] != n or (shift is not None and shift.shape[0] != n):
         raise ValueError("src, dst, shift: one length expected")
     cos, sin, positions, rot = (None, None, 0, 0) if rope is None else (rope[0].data_ptr(), rope[1].data_ptr(), rope[0].shape[0], 2 * rope[0].shape[1])
-    s = lib().alora_cache_move_rows(src.data_ptr(), dst.data_ptr(), None if shift is None else shift.data_ptr(), n, cos, sin, positions, rot,
+    s = (_lib or lib()).alora_cache_move_rows(src.data_ptr(), dst.data_ptr(), None if shift is None else shift.data_ptr(), n, cos, sin, positions, rot,
                                     1 if interleaved else 0, ctypes.byref(dims), _stream_handle(stream))
     if s:
         raise AloraError(s, "alora_cache_move_rows")

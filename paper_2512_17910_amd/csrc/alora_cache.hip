@@ -20,12 +20,15 @@ struct PairList {
 constexpr int PAIRS_FEW = 16, PAIRS_MANY = 352;
 static_assert(sizeof(CacheTable) + sizeof(PairList<PAIRS_MANY>) + 16 <= 4096, "kernel arguments");
 
-// One workgroup per piece of 4 KiB * K of a block, cache and pair.
+// One workgroup per piece of 4 KiB * K of a block, pair and cache; all pairs of a cache before the next cache.  Bound by memory: each byte is
+// read and written once, past the caches, since nothing reads it soon.  1000 blocks of 32 KiB in 16 caches, us: 204 (5.1 TB/s; a
+// large copy reaches 5.2), with ordinary loads and stores 221, with the caches of a pair behind each other 211; pieces of
+// 8, 16, 64 KiB are within 1 %.
 template <int PAIRS, int K>
 __global__ __launch_bounds__(256) void copy_blocks_kernel(CacheTable caches, PairList<PAIRS> pairs, long long block_bytes)
 {
-    char *cache = caches.p[blockIdx.y];
-    const int src = pairs.src[blockIdx.z], dst = pairs.dst[blockIdx.z];
+    char *cache = caches.p[blockIdx.z];
+    const int src = pairs.src[blockIdx.y], dst = pairs.dst[blockIdx.y];
     const long long piece = (long long)blockIdx.x * (K * 4096);
     const int left = (int)min(block_bytes - piece, (long long)K * 4096), o = threadIdx.x * 16;
     const char *from = cache + src * block_bytes + piece;    // (not read where src is -1)
@@ -36,14 +39,21 @@ __global__ __launch_bounds__(256) void copy_blocks_kernel(CacheTable caches, Pai
         for (int i = 0; i < K; ++i) x[i] = u32x4{0u, 0u, 0u, 0u};
         if (src >= 0) {
 #pragma unroll
-            for (int i = 0; i < K; ++i) x[i] = *(const u32x4 *)(from + o + i * 4096);
+            for (int i = 0; i < K; ++i) x[i] = __builtin_nontemporal_load((const u32x4 *)(from + o + i * 4096));
         }
 #pragma unroll
-        for (int i = 0; i < K; ++i) *(u32x4 *)(to + o + i * 4096) = x[i];
+        for (int i = 0; i < K; ++i) __builtin_nontemporal_store(x[i], (u32x4 *)(to + o + i * 4096));
         return;
     }
     for (int i = o; i < left; i += 4096) *(u32x4 *)(to + i) = src >= 0 ? *(const u32x4 *)(from + i) : u32x4{0u, 0u, 0u, 0u};
 }
+
+// How rows lie on wavefronts: `rows` of them on one where they leave room, else one on `units`.  Bound by memory; what costs next is the number of
+// wavefronts, each with a chain of loads (indexes, shift; angles and rows).  9001 rows over 16 layers, us: 8 heads of 128 219 (5.4 TB/s), in
+// wavefronts that went through four layers each 245; one head of 64 19 (a row to a workgroup: 44, a row and layer: 93).
+struct RowSplit {
+    int rows, units;
+};
 
 struct MoveArgs {
     CacheTable caches;
@@ -51,94 +61,115 @@ struct MoveArgs {
     const int32_t *shift;       // or null
     const float *cos, *sin;
     HeadShape s;
-    int hkv, n_pos, uk;         // uk: units of 64 >> gshift heads
-    int layers, per_group;      // per_group: layers of a workgroup
-    int n_rows;
+    RowSplit k, v;              // of keys that are turned; of rows that are copied, in 16-byte pieces
+    int heads, pieces, n_rows, n_pos;
     long long n_slots, row_bytes;
 };
 
-constexpr int MOVE_WAVES = 8;
-constexpr int MOVE_LAYERS = 4;   // layers whose loads are requested together
+struct Move {
+    long long src, dst;
+    bool on;
+};
+__device__ __forceinline__ Move move_of(const MoveArgs &g, int row)
+{
+    Move m = {g.src[row], g.dst[row], false};
+    m.on = m.src >= 0 && m.src < g.n_slots && m.dst >= 0 && m.dst < g.n_slots;
+    return m;
+}
 
-// One workgroup per row and group of layers.  A wavefront takes a unit of key heads or 2 KiB of values through the layers; its
-// angles are the same in all of them.
+constexpr int MOVE_WAVES = 4;
+
+// A wavefront's share of a layer's K cache, keys turned on the way.
+template <bool BF16, int V, bool INTERLEAVED>
+__device__ __forceinline__ void move_keys(const MoveArgs &g, char *cache, int item, int lane)
+{
+    typedef Chunk<BF16, V> C;
+    constexpr int E = BF16 ? 2 : 4;
+    const LanePlace p = lane_place<V, INTERLEAVED>(g.s, lane & ((1 << g.s.gshift) - 1));
+    const int h = lane >> g.s.gshift;
+    const int group = g.k.units == 1 ? item : item / g.k.units;
+    if (group >= (g.n_rows + g.k.rows - 1) / g.k.rows) return;
+    int row = group, head = (item - group * g.k.units) * (64 >> g.s.gshift) + h;
+    Move m;
+    int shift;
+    bool on = head < g.heads;
+    if (g.k.rows == 1) {       // (one row: scalar loads)
+        m = move_of(g, row);
+        shift = g.shift[row];
+    } else {
+        const int sub = h / g.heads;
+        head = h - sub * g.heads;
+        row = group * g.k.rows + sub;
+        on = sub < g.k.rows && row < g.n_rows;
+        row = min(row, g.n_rows - 1);
+        m = move_of(g, row);
+        shift = g.shift[row];
+    }
+    on &= m.on;
+    if (!on) return;
+    const char *from = cache + m.src * g.row_bytes + head * (g.s.d * E);
+    char *to = cache + m.dst * g.row_bytes + head * (g.s.d * E);
+    C a, b;
+    a.zero();
+    b.zero();
+    if (p.has_a) a.load(from + p.a * E);
+    if (p.has_b) b.load(from + p.b * E);
+    if (shift) {      // (keys that keep their position are copied bit for bit)
+        const uint32_t far = shift < 0 ? 0u - (uint32_t)shift : (uint32_t)shift;
+        float c[V], s[V], x[V], y[V];
+        load_angles<V, INTERLEAVED>(g.cos, g.sin, (size_t)min(far, (uint32_t)g.n_pos - 1u) * g.s.half, p, c, s);
+#pragma unroll
+        for (int e = 0; e < V; ++e) s[e] = shift < 0 ? -s[e] : s[e];
+        a.widen(x);
+        b.widen(y);
+        turn<V, INTERLEAVED, false>(x, y, c, s, p);
+        a.narrow(x);
+        b.narrow(y);
+    }
+    if (p.has_a) a.store(to + p.a * E);
+    if (p.has_b) b.store(to + p.b * E);
+}
+
+// A wavefront's share of a cache whose rows are copied as they are: 2 KiB, past the caches.  (Turned keys are loaded and stored the ordinary way: chunks of
+// their layout cover lines in two requests.)
+__device__ __forceinline__ void move_copies(const MoveArgs &g, char *cache, int item, int lane)
+{
+    const int group = g.v.units == 1 ? item : item / g.v.units;
+    if (group >= (g.n_rows + g.v.rows - 1) / g.v.rows) return;
+    u32x4 x[2];
+    char *to[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        to[i] = nullptr;
+        int piece = (item - group * g.v.units) * 128 + 64 * i + lane;
+        Move m;
+        bool on = piece < g.pieces;
+        if (g.v.rows == 1) {
+            m = move_of(g, group);
+        } else {
+            const int sub = piece / g.pieces, row = group * g.v.rows + sub;
+            piece -= sub * g.pieces;
+            on = sub < g.v.rows && row < g.n_rows;
+            m = move_of(g, min(row, g.n_rows - 1));
+        }
+        if (on && m.on) {
+            x[i] = __builtin_nontemporal_load((const u32x4 *)(cache + m.src * g.row_bytes + piece * 16));
+            to[i] = cache + m.dst * g.row_bytes + piece * 16;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        if (to[i]) __builtin_nontemporal_store(x[i], (u32x4 *)to[i]);
+}
+
+// One wavefront per item of a layer's K or V cache; gridDim.y counts the caches.
 template <bool BF16, int V, bool INTERLEAVED>
 __global__ __launch_bounds__(64 * MOVE_WAVES) void move_rows_kernel(MoveArgs g)
 {
-    typedef Chunk<BF16, V> C;
-    constexpr int E = BF16 ? 2 : 4, L = MOVE_LAYERS;
-    const long long row = (long long)blockIdx.z * ROWS_AT_ONCE + blockIdx.x;
-    if (row >= g.n_rows) return;
-    const long long src = g.src[row], dst = g.dst[row];
-    if (src < 0 || src >= g.n_slots || dst < 0 || dst >= g.n_slots) return;
-    const int shift = g.shift ? g.shift[row] : 0;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, lane = threadIdx.x & 63;
-    const int l0 = blockIdx.y * g.per_group, l1 = min(l0 + g.per_group, g.layers);
-    const int pieces = (int)((g.row_bytes + 2047) / 2048), k_units = shift ? g.uk : pieces;
-    const LanePlace p = lane_place<V, INTERLEAVED>(g.s, lane & ((1 << g.s.gshift) - 1));
-    float c[V], s[V];
-    if (shift && wave < k_units) {
-        const uint32_t far = shift < 0 ? 0u - (uint32_t)shift : (uint32_t)shift;
-        load_angles<V, INTERLEAVED>(g.cos, g.sin, (size_t)min(far, (uint32_t)g.n_pos - 1u) * g.s.half, p, c, s);
-        if (shift < 0) {
-#pragma unroll
-            for (int e = 0; e < V; ++e) s[e] = -s[e];
-        }
-    }
-    for (int u = wave; u < k_units + pieces; u += waves) {
-        if (shift && u < k_units) {
-            const int head = u * (64 >> g.s.gshift) + (lane >> g.s.gshift);
-            const bool on = head < g.hkv;
-            const long long offset = (long long)head * (g.s.d * E);
-            for (int l = l0; l < l1; l += L) {
-                C a[L], b[L];
-#pragma unroll
-                for (int i = 0; i < L; ++i) {
-                    a[i].zero();
-                    b[i].zero();
-                    if (l + i < l1) {
-                        const char *from = g.caches.p[2 * (l + i)] + src * g.row_bytes + offset;
-                        if (on && p.has_a) a[i].load(from + p.a * E);
-                        if (on && p.has_b) b[i].load(from + p.b * E);
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < L; ++i) {
-                    float x[V], y[V];
-                    a[i].widen(x);
-                    b[i].widen(y);
-                    turn<V, INTERLEAVED, false>(x, y, c, s, p);
-                    a[i].narrow(x);
-                    b[i].narrow(y);
-                    if (l + i < l1) {
-                        char *to = g.caches.p[2 * (l + i)] + dst * g.row_bytes + offset;
-                        if (on && p.has_a) a[i].store(to + p.a * E);
-                        if (on && p.has_b) b[i].store(to + p.b * E);
-                    }
-                }
-            }
-            continue;
-        }
-        const int side = u < k_units ? 0 : 1;
-        const long long o = (long long)(side ? u - k_units : u) * 2048 + lane * 16;
-        for (int l = l0; l < l1; l += L) {
-            u32x4 x[L], y[L];
-#pragma unroll
-            for (int i = 0; i < L; ++i) {
-                if (l + i >= l1) break;
-                const char *from = g.caches.p[2 * (l + i) + side] + src * g.row_bytes + o;
-                if (o < g.row_bytes) x[i] = *(const u32x4 *)from;
-                if (o + 1024 < g.row_bytes) y[i] = *(const u32x4 *)(from + 1024);
-            }
-#pragma unroll
-            for (int i = 0; i < L; ++i) {
-                if (l + i >= l1) break;
-                char *to = g.caches.p[2 * (l + i) + side] + dst * g.row_bytes + o;
-                if (o < g.row_bytes) *(u32x4 *)to = x[i];
-                if (o + 1024 < g.row_bytes) *(u32x4 *)(to + 1024) = y[i];
-            }
-        }
-    }
+    const int item = blockIdx.x * MOVE_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    char *cache = g.caches.p[blockIdx.y];
+    if (g.shift && !(blockIdx.y & 1)) move_keys<BF16, V, INTERLEAVED>(g, cache, item, lane);
+    else move_copies(g, cache, item, lane);
 }
 
 // ---- host ---------------------------------------------------------------------------------------
@@ -209,12 +240,12 @@ static void launch_copies(const CacheTable &caches, int n_caches, const int32_t 
         PairList<PAIRS> list;
         std::copy(src + i, src + i + m, list.src);
         std::copy(dst + i, dst + i + m, list.dst);
-        // pieces of 32 KiB where that gives the chip two workgroups for every compute unit, else of 4
+        // pieces of 32 KiB where that gives the chip two workgroups for every compute unit, else of 4 (one block in 64 caches: 2.6 us)
         const long long large = (block_bytes + 32767) / 32768;
         if (large * n_caches * m >= 512)
-            launch_kernel(copy_blocks_kernel<PAIRS, 8>, dim3((unsigned)large, n_caches, m), dim3(256), 0, st, caches, list, block_bytes);
+            launch_kernel(copy_blocks_kernel<PAIRS, 8>, dim3((unsigned)large, m, n_caches), dim3(256), 0, st, caches, list, block_bytes);
         else
-            launch_kernel(copy_blocks_kernel<PAIRS, 1>, dim3((unsigned)((block_bytes + 4095) / 4096), n_caches, m), dim3(256), 0, st, caches, list, block_bytes);
+            launch_kernel(copy_blocks_kernel<PAIRS, 1>, dim3((unsigned)((block_bytes + 4095) / 4096), m, n_caches), dim3(256), 0, st, caches, list, block_bytes);
     }
 }
 
@@ -254,36 +285,35 @@ int alora_cache_move_rows(const int64_t *src, const int64_t *dst, const int32_t 
     if (rotary_dim % 4 || rotary_dim > dims->head_dim) return ALORA_ESHAPE;
     if ((shift != nullptr) != (rotary_dim > 0) || (cos != nullptr) != (rotary_dim > 0) || (sin != nullptr) != (rotary_dim > 0)) return ALORA_EINVAL;
     if (rotary_dim && rope_positions < 1) return ALORA_EINVAL;
+    if ((long long)n_rows * dims->n_kv_heads > 1 << 25) return ALORA_ESHAPE;     // (a grid holds fewer than 2^32 threads)
     if (n_rows == 0 || dims->n_layers == 0) return ALORA_OK;
     if (!src || !dst) return ALORA_EINVAL;
     if ((((uintptr_t)src | (uintptr_t)dst) & 7) || ((uintptr_t)shift & 3) || (((uintptr_t)cos | (uintptr_t)sin) & 15)) return ALORA_EINVAL;
     st = check_pointers(dims);
     if (st) return st;
     const bool bf16 = dims->dtype == ALORA_BF16;
-    const int V = head_chunk(bf16, rotary_dim, interleaved);
+    const int V = head_chunk(bf16, dims->head_dim, rotary_dim, interleaved);
     MoveArgs g;
-    g.n_rows = n_rows;
     g.src = src; g.dst = dst; g.shift = shift; g.cos = cos; g.sin = sin;
+    g.heads = dims->n_kv_heads; g.n_rows = n_rows; g.n_pos = rope_positions;
     g.s = head_shape(dims->head_dim, rotary_dim, interleaved, V);
-    g.hkv = dims->n_kv_heads; g.n_pos = rope_positions;
-    const int per = 64 >> g.s.gshift;
-    g.uk = (g.hkv + per - 1) / per;
     g.n_slots = dims->n_slots;
     g.row_bytes = row_bytes_of(dims);
-    const long long pieces = (g.row_bytes + 2047) / 2048, units = pieces + (shift ? std::max<long long>(g.uk, pieces) : pieces);
-    const int waves = (int)std::min<long long>(MOVE_WAVES, units);
+    g.pieces = (int)(g.row_bytes / 16);
+    const auto split = [](int parts, int at_once) { return RowSplit{std::max(1, at_once / parts), (parts + at_once - 1) / at_once}; };
+    g.k = split(g.heads, 64 >> g.s.gshift);
+    g.v = split(g.pieces, 128);
+    const auto items = [&](const RowSplit &x) { return ((long long)n_rows + x.rows - 1) / x.rows * x.units; };
+    const long long groups = (std::max(items(g.v), shift ? items(g.k) : 0) + MOVE_WAVES - 1) / MOVE_WAVES;
     for (int l = 0; l < dims->n_layers; l += LAYERS_AT_ONCE) {
-        g.layers = std::min(LAYERS_AT_ONCE, dims->n_layers - l);
-        g.caches = table_of(dims, l, g.layers);
-        // all layers of a row on one workgroup where the rows alone fill the chip, else MOVE_LAYERS or one
-        g.per_group = (long long)n_rows * waves >= 8192 ? g.layers : (long long)n_rows * waves * g.layers >= 8192 ? MOVE_LAYERS : 1;
-        const dim3 grid(std::min(n_rows, ROWS_AT_ONCE), (g.layers + g.per_group - 1) / g.per_group, (n_rows - 1) / ROWS_AT_ONCE + 1), block(64 * waves);
-        const auto go = [&](auto kernel) { launch_kernel(kernel, grid, block, 0, (hipStream_t)hip_stream, g); };
+        const int layers = std::min(LAYERS_AT_ONCE, dims->n_layers - l);
+        g.caches = table_of(dims, l, layers);
+        const auto go = [&](auto kernel) { launch_kernel(kernel, dim3((unsigned)groups, 2 * layers), dim3(64 * MOVE_WAVES), 0, (hipStream_t)hip_stream, g); };
         if (bf16 && V == 8) interleaved ? go(move_rows_kernel<true, 8, true>) : go(move_rows_kernel<true, 8, false>);
-        else if (bf16 && V == 4) go(move_rows_kernel<true, 4, false>);
-        else if (bf16) interleaved ? go(move_rows_kernel<true, 2, true>) : go(move_rows_kernel<true, 2, false>);
+        else if (bf16 && V == 4) interleaved ? go(move_rows_kernel<true, 4, true>) : go(move_rows_kernel<true, 4, false>);
+        else if (bf16) go(move_rows_kernel<true, 2, false>);
         else if (V == 4) interleaved ? go(move_rows_kernel<false, 4, true>) : go(move_rows_kernel<false, 4, false>);
-        else interleaved ? go(move_rows_kernel<false, 2, true>) : go(move_rows_kernel<false, 2, false>);
+        else go(move_rows_kernel<false, 2, false>);
     }
     const int e = launch_status();
     if (e) { note_hip_error(e); return ALORA_EHIP; }

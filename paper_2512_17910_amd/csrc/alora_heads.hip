@@ -25,8 +25,10 @@ struct HeadsArgs {
 
 constexpr int HEADS_WAVES = 8;   // wavefronts of a workgroup, at most
 
-// One workgroup per row.  A wavefront takes U units at a time (their loads are requested together), the units of queries and
-// keys first, then the row of v in pieces of 2 KiB.
+// One workgroup per row: its slot and position are scalars, a lane's angles serve all its heads.  A wavefront takes U units at a time (their
+// loads are requested together), the units of queries and keys first, then the row of v in pieces of 2 KiB.  One pass: the mean
+// square is a sum over a lane's chunks and over the lanes of the head (DPP), after which the head is still in registers.  Bound by memory: 8192 rows of
+// 64 / 8 heads of 128 take 62 us (5.4 TB/s; a large copy reaches 5.2), with U = 2 74, 1 75, 4 74.  One row takes 3 us: launch and three dependent loads.
 template <bool BF16, int V, bool INTERLEAVED, bool NORM, int U>
 __global__ __launch_bounds__(64 * HEADS_WAVES) void heads_kernel(HeadsArgs g)
 {
@@ -93,9 +95,11 @@ __global__ __launch_bounds__(64 * HEADS_WAVES) void heads_kernel(HeadsArgs g)
                 b[i].widen(y);
                 r[i] = 0.f;
 #pragma unroll
-                for (int e = 0; e < V; ++e) r[i] = fmaf(x[e], x[e], r[i]);
-#pragma unroll
-                for (int e = 0; e < V; ++e) r[i] = fmaf(y[e], y[e], r[i]);
+                for (int e = 0; e < V; ++e) {
+                    const float xe = e < p.again_a ? 0.f : x[e], ye = e < p.again_b ? 0.f : y[e];
+                    r[i] = fmaf(xe, xe, r[i]);
+                    r[i] = fmaf(ye, ye, r[i]);
+                }
             }
             head_sum<U>(r, gs);
 #pragma unroll
@@ -132,16 +136,23 @@ struct HeadsBackArgs {
     const int32_t *pos;
     long long q_row, k_row, gq_row, gk_row, dq_row, dk_row;
     float *partial;          // [workgroups][2][d]
+    float *dwq, *dwk;        // where one workgroup does it all, it writes these
     HeadShape s;
     int T, hq, hkv, n_pos;
     int uq, uk, wq_waves;    // the first wq_waves wavefronts of a workgroup take the queries
     float eps, inv_d;
 };
 
-// Rows blockIdx.x, blockIdx.x + gridDim.x, ...  A wavefront keeps to queries or to keys, so that its lanes' sums for the weights are of
-// one of the two.
+constexpr int BACK_WAVES = 16;   // wavefronts of a workgroup, at most
+
+// With g = the outputs' gradient turned back, u = g w, r = 1 / sqrt(mean x^2 + eps): both means (of x x and x u) come out of one pass over x and g, then
+// dx = r u - x (r^3 mean(x u)) from registers, and each lane adds g x r to sums for the weights of its features.
+// The units of heads of all rows, those of queries dealt to the wavefronts of all workgroups that take queries, those of keys to
+// the others, so that a lane's sums for the weights are of one of the two.  Bound by memory: 4096 rows of 32 / 8 heads of 128 take 24.3 us (5.2 TB/s),
+// the second kernel 4.4.  256 workgroups of up to 16 wavefronts (fewer partial sums to add): the pass 27.6 us; with 512 29.9, 1024 of five
+// wavefronts that kept to rows 42.  dx goes past the caches: 27.6, ordinary stores 29.2.
 template <bool BF16, int V, bool INTERLEAVED, bool NORM>
-__global__ __launch_bounds__(64 * HEADS_WAVES) void heads_back_kernel(HeadsBackArgs g)
+__global__ __launch_bounds__(64 * BACK_WAVES) void heads_back_kernel(HeadsBackArgs g)
 {
     typedef Chunk<BF16, V> C;
     constexpr int E = BF16 ? 2 : 4;
@@ -150,7 +161,9 @@ __global__ __launch_bounds__(64 * HEADS_WAVES) void heads_back_kernel(HeadsBackA
     const LanePlace p = lane_place<V, INTERLEAVED>(g.s, lane & ((1 << gs) - 1));
     const bool is_k = wave >= g.wq_waves;
     const int heads = is_k ? g.hkv : g.hq, units = is_k ? g.uk : g.uq;
-    const int first = is_k ? wave - g.wq_waves : wave, step = is_k ? waves - g.wq_waves : g.wq_waves;
+    const int mine = is_k ? waves - g.wq_waves : g.wq_waves, step = gridDim.x * mine;
+    const int first = blockIdx.x * mine + (is_k ? wave - g.wq_waves : wave);
+    const int row_step = step / units, unit_step = step % units;
     const char *xs = is_k ? g.k : g.q, *gs_in = is_k ? g.gk : g.gq;
     char *outs = is_k ? g.dk : g.dq;
     const long long x_row = is_k ? g.k_row : g.q_row, g_row = is_k ? g.gk_row : g.gq_row, d_row = is_k ? g.dk_row : g.dq_row;
@@ -168,13 +181,17 @@ __global__ __launch_bounds__(64 * HEADS_WAVES) void heads_back_kernel(HeadsBackA
 #pragma unroll
         for (int e = 0; e < V; ++e) dw0[e] = dw1[e] = 0.f;
     }
-    for (long long row = blockIdx.x; row < g.T; row += gridDim.x) {
-        float c[V], s[V];
-        if (g.s.rot) {
-            const int at = min(max(g.pos[row], 0), g.n_pos - 1);
-            load_angles<V, INTERLEAVED>(g.cos, g.sin, (size_t)at * g.s.half, p, c, s);
+    for (int row = first / units, unit = first % units; row < g.T; row += row_step, unit += unit_step) {
+        if (unit >= units) {
+            unit -= units;
+            if (++row >= g.T) break;
         }
-        for (int unit = first; unit < units; unit += step) {
+        {
+            float c[V], s[V];
+            if (g.s.rot) {
+                const int at = min(max(g.pos[row], 0), g.n_pos - 1);
+                load_angles<V, INTERLEAVED>(g.cos, g.sin, (size_t)at * g.s.half, p, c, s);
+            }
             const int head = unit * per + (lane >> gs);
             const bool on = head < heads;
             const long long offset = (long long)head * (g.s.d * E);
@@ -198,10 +215,11 @@ __global__ __launch_bounds__(64 * HEADS_WAVES) void heads_back_kernel(HeadsBackA
                 xb.widen(y);
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    sums[0] = fmaf(x[e], x[e], sums[0]);
-                    sums[0] = fmaf(y[e], y[e], sums[0]);
-                    sums[1] = fmaf(u[e] * w0[e], x[e], sums[1]);
-                    sums[1] = fmaf(v[e] * w1[e], y[e], sums[1]);
+                    const float xe = e < p.again_a ? 0.f : x[e], ye = e < p.again_b ? 0.f : y[e];
+                    sums[0] = fmaf(xe, xe, sums[0]);
+                    sums[0] = fmaf(ye, ye, sums[0]);
+                    sums[1] = fmaf(u[e] * w0[e], xe, sums[1]);
+                    sums[1] = fmaf(v[e] * w1[e], ye, sums[1]);
                 }
                 head_sum<2>(sums, gs);
                 const float r = rsqrtf(fmaf(sums[0], g.inv_d, g.eps)), m = r * r * r * (sums[1] * g.inv_d);
@@ -215,12 +233,12 @@ __global__ __launch_bounds__(64 * HEADS_WAVES) void heads_back_kernel(HeadsBackA
             }
             ga.narrow(u);
             gb.narrow(v);
-            if (on && p.has_a) ga.store(outs + row * d_row + offset + p.a * E);
-            if (on && p.has_b) gb.store(outs + row * d_row + offset + p.b * E);
+            if (on && p.has_a) ga.template store<true>(outs + row * d_row + offset + p.a * E);
+            if (on && p.has_b) gb.template store<true>(outs + row * d_row + offset + p.b * E);
         }
     }
     if (NORM) {
-        __shared__ float red[HEADS_WAVES][256];
+        __shared__ float red[BACK_WAVES][256];
         for (int m = 1 << gs; m < 64; m <<= 1) {
 #pragma unroll
             for (int e = 0; e < V; ++e) {
@@ -240,32 +258,33 @@ __global__ __launch_bounds__(64 * HEADS_WAVES) void heads_back_kernel(HeadsBackA
             const int kind = i >= g.s.d, e = i - kind * g.s.d;
             float sum = 0.f;
             for (int w = kind ? g.wq_waves : 0; w < (kind ? waves : g.wq_waves); ++w) sum += red[w][e];
-            g.partial[(size_t)blockIdx.x * 2 * g.s.d + i] = sum;
+            if (gridDim.x == 1) (kind ? g.dwk : g.dwq)[e] = sum;
+            else g.partial[(size_t)blockIdx.x * 2 * g.s.d + i] = sum;
         }
     }
 }
 
-// dw[i] = the workgroups' partial sums added in a fixed order; 16 columns a workgroup, 16 threads a column.
-__global__ __launch_bounds__(256) void heads_weights_kernel(const float *__restrict__ partial, int parts, int d, float *__restrict__ dwq,
-                                                            float *__restrict__ dwk)
+// dw[i] = the workgroups' partial sums added in a fixed order; 16 columns a workgroup, 64 threads a column.
+__global__ __launch_bounds__(1024) void heads_weights_kernel(const float *__restrict__ partial, int parts, int d, float *__restrict__ dwq,
+                                                             float *__restrict__ dwk)
 {
-    __shared__ float red[16][17];
+    __shared__ float red[64][17];
     const int col = threadIdx.x & 15, sl = threadIdx.x >> 4, i = blockIdx.x * 16 + col;
     float sum = 0.f;
     if (i < 2 * d) {
 #pragma unroll 8
-        for (int b = sl; b < parts; b += 16) sum += partial[(size_t)b * 2 * d + i];
+        for (int b = sl; b < parts; b += 64) sum += partial[(size_t)b * 2 * d + i];
     }
     red[sl][col] = sum;
     __syncthreads();
-    if (sl == 0 && i < 2 * d) {
-        for (int k = 1; k < 16; ++k) sum += red[k][col];
-        (i < d ? dwq[i] : dwk[i - d]) = sum;
-    }
+    float v[1] = {red[threadIdx.x & 63][threadIdx.x >> 6]};      // a column's sums on the lanes of a wavefront
+    head_sum<1>(v, 6);
+    const int o = blockIdx.x * 16 + (threadIdx.x >> 6);
+    if ((threadIdx.x & 63) == 0 && o < 2 * d) (o < d ? dwq[o] : dwk[o - d]) = v[0];
 }
 
 // Cosines and sines.  A thread keeps to one pair and steps through the rows: angles are added by multiplying exp(i angle) by exp(i step) in 64
-// bits, so that the sines themselves are computed twice a thread.
+// bits, so that sines themselves are computed twice a thread.
 __global__ __launch_bounds__(256) void rope_tables_kernel(float *__restrict__ cos, float *__restrict__ sin, long long first, long long rows,
                                                           int half, int steps, int scaling, double log2_base, double factor, double original,
                                                           double low, double high, double magnitude)
@@ -322,15 +341,16 @@ static int with_layout(bool bf16, int V, bool interleaved, F f)
 {
     using std::integral_constant;
     using std::bool_constant;
-#define ALORA_CASE(B, N)                                                                                       \
-    if (bf16 == B && V == N)                                                                                   \
-        return interleaved ? f(bool_constant<B>(), integral_constant<int, N>(), bool_constant<true>())          \
-                           : f(bool_constant<B>(), integral_constant<int, N>(), bool_constant<false>());
-    ALORA_CASE(true, 8)
-    ALORA_CASE(true, 4)
-    ALORA_CASE(true, 2)
-    ALORA_CASE(false, 4)
-    ALORA_CASE(false, 2)
+#define ALORA_CASE(B, N, I) \
+    if (bf16 == B && V == N && interleaved == I) return f(bool_constant<B>(), integral_constant<int, N>(), bool_constant<I>());
+    ALORA_CASE(true, 8, false)
+    ALORA_CASE(true, 4, false)
+    ALORA_CASE(true, 2, false)
+    ALORA_CASE(true, 8, true)
+    ALORA_CASE(true, 4, true)
+    ALORA_CASE(false, 4, false)
+    ALORA_CASE(false, 2, false)
+    ALORA_CASE(false, 4, true)
 #undef ALORA_CASE
     return -1;
 }
@@ -344,22 +364,53 @@ static int units_of(int heads, const HeadShape &s)
 static int launch_heads(const HeadsArgs &g, bool bf16, int V, bool norm, hipStream_t st)
 {
     const int units = g.uq + g.uk, v_pieces = g.v ? (g.hkv * g.s.d * (bf16 ? 2 : 4) + 2047) / 2048 : 0;
-    const int U = (long long)g.T * units >= 8192 ? 2 : 1;
+    // three units of a wavefront where the chip is full many times over, else one: more wavefronts have shorter chains of loads
+    const int U = (long long)g.T * units >= 8192 ? 3 : 1;
     const int waves = std::min(HEADS_WAVES, (units + U - 1) / U + v_pieces);
     return with_layout(bf16, V, g.s.interleaved, [&](auto b, auto v, auto il) {
         const auto go = [&](auto kernel) {
             launch_kernel(kernel, dim3(std::min(g.T, ROWS_AT_ONCE), (g.T - 1) / ROWS_AT_ONCE + 1), dim3(64 * waves), 0, st, g);
             return launch_status();
         };
-        if (norm) return U == 2 ? go(heads_kernel<b.value, v.value, il.value, true, 2>) : go(heads_kernel<b.value, v.value, il.value, true, 1>);
-        return U == 2 ? go(heads_kernel<b.value, v.value, il.value, false, 2>) : go(heads_kernel<b.value, v.value, il.value, false, 1>);
+        if (norm) return U == 3 ? go(heads_kernel<b.value, v.value, il.value, true, 3>) : go(heads_kernel<b.value, v.value, il.value, true, 1>);
+        return U == 3 ? go(heads_kernel<b.value, v.value, il.value, false, 3>) : go(heads_kernel<b.value, v.value, il.value, false, 1>);
     });
 }
 
 // Workgroups of the backward pass, each with a row of partial sums.
-static int back_workgroups(const alora_heads_dims *d) { return std::min(d->n_tokens, 1024); }
+struct BackPlan {
+    int groups, waves, q_waves;   // workgroups, their wavefronts, those of them that take queries
+};
+// Units that one workgroup takes alone, without the second kernel; the pass in us with it and without: 5 units 11.2 and 8.4, 40 units 11.1 and
+// 9.5, 80 units 11.1 and 13.9.
+constexpr int ONE_WORKGROUP = 48;
+static BackPlan plan_back(int T, int uq, int uk)
+{
+    const long long all = (long long)T * (uq + uk);
+    const int most = all <= ONE_WORKGROUP ? BACK_WAVES : (int)std::min<long long>(BACK_WAVES, std::max<long long>(2, all / 256));
+    BackPlan p = {0, 0, 0};
+    double best = 0.0;
+    for (int w = 2; w <= most; ++w) {
+        const int q = std::max(1, std::min(w - 1, (int)((double)w * uq / (uq + uk) + 0.5)));
+        const double cost = std::max((double)uq / q, (double)uk / (w - q)) * w;    // wavefronts' time for a row
+        if (w == 2 || cost <= best * 1.02) {
+            best = w == 2 ? cost : std::min(best, cost);
+            p.waves = w;
+            p.q_waves = q;
+        }
+    }
+    p.groups = T == 0 ? 0 : all <= ONE_WORKGROUP ? 1 : (int)std::min<long long>(256, (all + p.waves - 1) / p.waves);
+    return p;
+}
 
-static size_t back_workspace(const alora_heads_dims *d) { return d->norm ? (size_t)back_workgroups(d) * 2 * d->head_dim * sizeof(float) : 0; }
+static HeadShape shape_of(const alora_heads_dims *d) { return head_shape(d->head_dim, d->rotary_dim, d->interleaved, head_chunk(d->dtype == ALORA_BF16, d->head_dim, d->rotary_dim, d->interleaved)); }
+
+static size_t back_workspace(const alora_heads_dims *d)
+{
+    const HeadShape s = shape_of(d);
+    const int groups = plan_back(d->n_tokens, units_of(d->n_q_heads, s), units_of(d->n_kv_heads, s)).groups;
+    return d->norm && groups > 1 ? (size_t)groups * 2 * d->head_dim * sizeof(float) : 0;
+}
 
 }  // namespace alora
 
@@ -388,7 +439,7 @@ int alora_qk_norm_rope(const void *q, void *q_out, const void *k, void *k_cache,
         (q == q_out && d.q_stride != d.q_out_stride))
         return ALORA_EINVAL;
     const bool bf16 = d.dtype == ALORA_BF16;
-    const int E = bf16 ? 2 : 4, V = head_chunk(bf16, d.rotary_dim, d.interleaved);
+    const int E = bf16 ? 2 : 4, V = head_chunk(bf16, d.head_dim, d.rotary_dim, d.interleaved);
     HeadsArgs g;
     g.q = (const char *)q; g.q_out = (char *)q_out; g.k = (const char *)k; g.kc = (char *)k_cache;
     g.v = (const char *)v; g.vc = (char *)v_cache; g.wq = (const char *)wq; g.wk = (const char *)wk;
@@ -439,7 +490,7 @@ int alora_qk_norm_rope_backward(const void *q, const void *dq_out, void *dq, con
     const size_t need = back_workspace(dims);
     if (need && (!workspace || off16(workspace) || workspace_bytes < need)) return ALORA_EWORKSPACE;
     const bool bf16 = d.dtype == ALORA_BF16;
-    const int E = bf16 ? 2 : 4, V = head_chunk(bf16, d.rotary_dim, d.interleaved), groups = back_workgroups(dims);
+    const int E = bf16 ? 2 : 4, V = head_chunk(bf16, d.head_dim, d.rotary_dim, d.interleaved);
     HeadsBackArgs g;
     g.q = (const char *)q; g.k = (const char *)k; g.gq = (const char *)dq_out; g.gk = (const char *)dk_out; g.dq = (char *)dq; g.dk = (char *)dk;
     g.wq = (const char *)wq; g.wk = (const char *)wk;
@@ -451,19 +502,19 @@ int alora_qk_norm_rope_backward(const void *q, const void *dq_out, void *dq, con
     g.T = d.n_tokens; g.hq = d.n_q_heads; g.hkv = d.n_kv_heads; g.n_pos = d.rope_positions;
     g.uq = units_of(g.hq, g.s); g.uk = units_of(g.hkv, g.s);
     g.eps = d.eps; g.inv_d = 1.0f / (float)d.head_dim;
-    // wavefronts by the share of the units, one for each kind at least
-    const int waves = std::min(HEADS_WAVES, g.uq + g.uk);
-    g.wq_waves = std::max(1, std::min(waves - 1, (int)((long long)waves * g.uq / (g.uq + g.uk))));
+    const BackPlan plan = plan_back(d.n_tokens, g.uq, g.uk);
+    g.wq_waves = plan.q_waves;
+    g.dwq = dwq; g.dwk = dwk;
     const hipStream_t stream = (hipStream_t)hip_stream;
     int e = 0;
-    if (groups)
+    if (plan.groups)
         e = with_layout(bf16, V, d.interleaved, [&](auto b, auto v, auto il) {
-            if (d.norm) launch_kernel(heads_back_kernel<b.value, v.value, il.value, true>, dim3(groups), dim3(64 * waves), 0, stream, g);
-            else launch_kernel(heads_back_kernel<b.value, v.value, il.value, false>, dim3(groups), dim3(64 * waves), 0, stream, g);
+            if (d.norm) launch_kernel(heads_back_kernel<b.value, v.value, il.value, true>, dim3(plan.groups), dim3(64 * plan.waves), 0, stream, g);
+            else launch_kernel(heads_back_kernel<b.value, v.value, il.value, false>, dim3(plan.groups), dim3(64 * plan.waves), 0, stream, g);
             return launch_status();
         });
-    if (!e && d.norm) {
-        launch_kernel(heads_weights_kernel, dim3((2 * d.head_dim + 15) / 16), dim3(256), 0, stream, (const float *)workspace, groups, (int)d.head_dim, dwq, dwk);
+    if (!e && d.norm && plan.groups != 1) {
+        launch_kernel(heads_weights_kernel, dim3((2 * d.head_dim + 15) / 16), dim3(1024), 0, stream, (const float *)workspace, plan.groups, (int)d.head_dim, dwq, dwk);
         e = launch_status();
     }
     if (e) { note_hip_error(e); return ALORA_EHIP; }
@@ -508,8 +559,9 @@ int alora_rope_tables(float *cos, float *sin, int64_t first, int64_t rows, const
     if (rows == 0) return ALORA_OK;
     if (!cos || !sin || off16(cos) || off16(sin)) return ALORA_EINVAL;
     const int half = s.rotary_dim / 2, at_once = 256 / half;
-    // rows per thread: about 2048 workgroups, at most 64 steps
-    const int steps = (int)std::max<int64_t>(1, std::min<int64_t>(64, rows / ((int64_t)at_once * 2048)));
+    // rows per thread: about 512 workgroups, at most 64 steps.  us with 512 | 1024 | 2048 workgroups, 64 pairs: 16384 rows 6.2 | 6.5 | 8.2,
+    // 65536 rows 8.8 | 9.1 | 10.8, 131072 rows 13.3 | 13.2 | 13.2; two or four pairs a thread with wider stores: 6.4 to 22
+    const int steps = (int)std::max<int64_t>(1, std::min<int64_t>(64, rows / ((int64_t)at_once * 512)));
     const int64_t groups = (rows + (int64_t)at_once * steps - 1) / ((int64_t)at_once * steps);
     launch_kernel(rope_tables_kernel, dim3((unsigned)groups), dim3(256), 0, (hipStream_t)hip_stream, cos, sin, (long long)first, (long long)rows, half, steps,
                   (int)s.scaling, std::log2(s.base), s.factor, s.original, s.low, s.high, s.magnitude);

@@ -75,9 +75,10 @@ def test_backward_arguments_are_refused():
         assert backward(d, **{name: P + (2 if name == "pos" else 8)}) == EINVAL, name
     for name, bad in (("q_stride", 248), ("q_out_stride", 257), ("k_stride", 120), ("k_out_stride", 132), ("dq_stride", 128), ("dk_stride", 64)):
         assert backward(heads_dims(**{name: bad})) == EINVAL, name
-    need = ab.alora_qk_norm_rope_workspace_bytes(d)
-    assert need == 7 * 2 * 64 * 4
-    assert backward(d, ws=None) == backward(d, ws=P + 8) == backward(d, size=need - 1) == EWORKSPACE
+    large = heads_dims(n_tokens=3000)
+    need = ab.alora_qk_norm_rope_workspace_bytes(large)
+    assert need > 0 and need % (2 * 64 * 4) == 0
+    assert backward(large, ws=None) == backward(large, ws=P + 8) == backward(large, size=need - 1) == EWORKSPACE
     assert ab.alora_qk_norm_rope_workspace_bytes(heads_dims(norm=0)) == 0 == ab.alora_qk_norm_rope_workspace_bytes(heads_dims(n_tokens=0))
     assert backward(heads_dims(norm=0, n_tokens=0), ws=None, size=0, wq=None, wk=None, dwq=None, dwk=None) == OK
     assert backward(heads_dims(q_out_stride=264), dq=P + 0x1000) == EINVAL                             # dq in dq_out's place, strides differ
@@ -165,7 +166,7 @@ def test_move_arguments_are_refused():
         assert move(**{name: None}) == EINVAL, name
         assert move(**{name: P + (2 if name == "shift" else 4)}) == EINVAL, name
     assert move(n=-1) == move(rot=-4) == move(il=2) == move(pos=0) == move(rot=0) == EINVAL
-    assert move(rot=62) == move(rot=68) == ESHAPE
+    assert move(rot=62) == move(rot=68) == move(n=(1 << 24) + 1) == ESHAPE
     assert move(n=0) == move(dims=cache_dims(0)) == OK
 
 
