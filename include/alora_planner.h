@@ -86,6 +86,37 @@ int alora_planner_commit(alora_planner *p, int64_t req_id);
 /* The request is over: its blocks return to the free pool (still reusable through their hash). */
 int alora_planner_finish(alora_planner *p, int64_t req_id);
 
+/*
+ * What a request holds, shared or moved (alora_cache.h moves the cache's contents).  The planner's state is that behind
+ * the moves: enqueue them on the stream of the projection before any later batch, and behind the batches planned so far.
+ *
+ * Fork: request new_req_id begins as request req_id is now (its tokens, its blocks), with an adapter of its own: an adapter is
+ * invoked on a conversation that goes on besides, or an answer is sampled twice.  Full blocks are shared; the partial one,
+ * if any, is to be copied: then *n_copies = 1 and *copy_src, *copy_dst are the block and the new request's own
+ * (alora_cache_copy_blocks), else *n_copies = 0.  ALORA_EINVAL where the cached K/V are not the new request's: its adapter would have been
+ * active at a position that req_id projected without it, or the other way round.
+ */
+int alora_planner_fork(alora_planner *p, int64_t req_id, int64_t new_req_id, int32_t adapter_id, int32_t activation_start,
+                       int32_t *copy_src, int32_t *copy_dst, int32_t *n_copies);
+
+/*
+ * The pool keeps blocks 0 .. n_blocks - 1 only (at most as many as it has).  Blocks in use behind those move to free ones: src, dst
+ * [cap], *n of them, as alora_cache_copy_blocks takes them.  Free blocks that hold nothing reusable are taken first, then the least
+ * recently freed; reusable blocks behind n_blocks are forgotten.  More blocks in use than n_blocks: ALORA_ENOBLOCKS;
+ * cap too small: ALORA_ESHAPE, with the number of moves in *n.
+ */
+int alora_planner_compact(alora_planner *p, int64_t n_blocks, int32_t *src, int32_t *dst, int32_t cap, int32_t *n);
+
+/*
+ * Tokens first .. first + n_drop - 1 of a request are dropped; what is behind them moves up.  Rows from the first one's block on
+ * move to fresh blocks (others may share the old ones): slots src to dst and the shift of the position, as alora_cache_move_rows
+ * takes them, *n_rows of them.  At least one token stays.  An activation point behind the dropped tokens moves with its token, one
+ * among them to `first`.  The moved keys and values were computed with the dropped tokens in view, so no block from there on is ever
+ * reused for another request.  cap too small: ALORA_ESHAPE, with the number of rows in *n_rows; too few free blocks: ALORA_ENOBLOCKS.
+ */
+int alora_planner_drop(alora_planner *p, int64_t req_id, int32_t first, int32_t n_drop, int64_t *src, int64_t *dst, int32_t *shift,
+                       int32_t cap, int32_t *n_rows);
+
 /* Physical blocks of the request's logical blocks 0,1,...: writes min(*n, cap) ids, sets *n. */
 int alora_planner_block_table(const alora_planner *p, int64_t req_id, int32_t *out, int32_t cap, int32_t *n);
 

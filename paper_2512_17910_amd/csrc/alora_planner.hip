@@ -47,6 +47,7 @@ struct Request {
     std::vector<uint64_t> hashes;     // chained hashes of the full blocks computed so far
     int32_t adapter = -1, start = 0;
     int32_t keyed = 0;                // leading blocks already registered in (or taken from) the cache
+    int64_t exact = INT64_MAX;        // leading blocks whose K/V are those of the tokens alone: none behind them is ever registered
 };
 
 }  // namespace
@@ -81,19 +82,28 @@ struct alora_planner {
     {
         const int32_t b = head;
         unlink_free(b);
-        if (keyed[b]) {
-            auto it = block_of.find(hash_of[b]);
-            if (it != block_of.end() && it->second == b) block_of.erase(it);
-            keyed[b] = 0;
-        }
+        forget(b);
         return b;
+    }
+    void forget(int32_t b)
+    {
+        if (!keyed[b]) return;
+        auto it = block_of.find(hash_of[b]);
+        if (it != block_of.end() && it->second == b) block_of.erase(it);
+        keyed[b] = 0;
+    }
+    // a request's blocks from logical block `first` on, last first
+    void release(const std::vector<int32_t> &table, size_t first)
+    {
+        for (size_t i = table.size(); i-- > first;)
+            if (--ref[table[i]] == 0) push_back_free(table[i]);
     }
     // the adapter id enters block b's hash iff the block holds a position at or after the activation point
     bool with_adapter(const Request &r, int64_t b) const { return r.adapter >= 0 && (b + 1) * (int64_t)bs > r.start; }
     // extend r.hashes to cover every full block of r.tokens
     void hash_full_blocks(Request &r) const
     {
-        const int64_t nfull = (int64_t)r.tokens.size() / bs;
+        const int64_t nfull = std::min<int64_t>((int64_t)r.tokens.size() / bs, r.exact);
         for (int64_t b = (int64_t)r.hashes.size(); b < nfull; ++b) {
             const uint64_t parent = b ? r.hashes[b - 1] : ROOT_HASH;
             r.hashes.push_back(block_hash(parent, r.tokens.data() + b * bs, bs, with_adapter(r, b), r.adapter));
@@ -266,12 +276,144 @@ int alora_planner_finish(alora_planner *p, int64_t req_id)
     if (!p) return ALORA_EINVAL;
     auto it = p->reqs.find(req_id);
     if (it == p->reqs.end()) return ALORA_EINVAL;
-    const Request &r = it->second;
-    for (size_t i = r.table.size(); i-- > 0;) {
-        const int32_t b = r.table[i];
-        if (--p->ref[b] == 0) p->push_back_free(b);
-    }
+    p->release(it->second.table, 0);
     p->reqs.erase(it);
+    return ALORA_OK;
+}
+
+int alora_planner_fork(alora_planner *p, int64_t req_id, int64_t new_req_id, int32_t adapter_id, int32_t activation_start,
+                       int32_t *copy_src, int32_t *copy_dst, int32_t *n_copies)
+{
+    if (!p || adapter_id < -1 || activation_start < 0 || !copy_src || !copy_dst || !n_copies) return ALORA_EINVAL;
+    auto it = p->reqs.find(req_id);
+    if (it == p->reqs.end() || p->reqs.count(new_req_id)) return ALORA_EINVAL;
+    const Request &from = it->second;
+    const int64_t n = (int64_t)from.tokens.size(), bs = p->bs;
+    const bool plain = from.adapter < 0 || from.start >= n, plain_new = adapter_id < 0 || activation_start >= n;
+    if (!(plain && plain_new) && !(adapter_id == from.adapter && activation_start == from.start)) return ALORA_EINVAL;
+    const bool partial = n % bs != 0;
+    if (partial && p->n_free < 1) return ALORA_ENOBLOCKS;
+    try {
+        Request r = from;
+        r.adapter = adapter_id;
+        r.start = activation_start;
+        auto to = p->reqs.emplace(new_req_id, Request());    // (may move the table of requests: `from` is not used behind it)
+        // nothing can fail from here on
+        for (size_t b = 0; b < r.table.size() - (partial ? 1 : 0); ++b) ++p->ref[r.table[b]];
+        if (partial) {
+            *copy_src = r.table.back();
+            *copy_dst = r.table.back() = p->take_free();
+            p->ref[r.table.back()] = 1;
+        }
+        *n_copies = partial ? 1 : 0;
+        to.first->second = std::move(r);
+    } catch (const std::bad_alloc &) {
+        return ALORA_ENOMEM;
+    }
+    return ALORA_OK;
+}
+
+int alora_planner_compact(alora_planner *p, int64_t n_blocks, int32_t *src, int32_t *dst, int32_t cap, int32_t *n)
+{
+    if (!p || !n || n_blocks < 0 || n_blocks > p->n_blocks || cap < 0 || (cap > 0 && (!src || !dst))) return ALORA_EINVAL;
+    const int32_t keep = (int32_t)n_blocks;
+    int64_t used = 0, moving = 0;
+    for (int64_t b = 0; b < p->n_blocks; ++b) {
+        used += p->ref[b] > 0;
+        moving += p->ref[b] > 0 && b >= keep;
+    }
+    if (used > keep) return ALORA_ENOBLOCKS;
+    if (moving > cap) {
+        *n = (int32_t)moving;
+        return ALORA_ESHAPE;
+    }
+    try {
+        std::vector<int32_t> to, where((size_t)(p->n_blocks - keep), -1);
+        to.reserve((size_t)moving);
+        // blocks that hold nothing worth keeping first, then the least recently freed
+        for (int pass = 0; pass < 2; ++pass)
+            for (int32_t b = p->head; b >= 0 && (int64_t)to.size() < moving; b = p->next[b])
+                if (b < keep && (p->keyed[b] != 0) == (pass != 0)) to.push_back(b);
+        // nothing can fail from here on (an entry of block_of is changed, none is added)
+        int32_t m = 0;
+        for (int64_t s = keep; s < p->n_blocks; ++s) {
+            if (p->ref[s] == 0) {
+                p->unlink_free((int32_t)s);
+                p->forget((int32_t)s);
+                continue;
+            }
+            const int32_t d = to[m];
+            p->unlink_free(d);
+            p->forget(d);
+            p->ref[d] = p->ref[s];
+            if (p->keyed[s]) {
+                p->keyed[d] = 1;
+                p->hash_of[d] = p->hash_of[s];
+                const auto entry = p->block_of.find(p->hash_of[s]);
+                if (entry != p->block_of.end()) entry->second = d;
+            }
+            where[s - keep] = d;
+            src[m] = (int32_t)s;
+            dst[m++] = d;
+        }
+        for (auto &r : p->reqs)
+            for (int32_t &b : r.second.table)
+                if (b >= keep) b = where[b - keep];
+        p->n_blocks = keep;
+        p->hash_of.resize(keep);
+        p->keyed.resize(keep);
+        p->ref.resize(keep);
+        p->prev.resize(keep);
+        p->next.resize(keep);
+        *n = m;
+    } catch (const std::bad_alloc &) {
+        return ALORA_ENOMEM;
+    }
+    return ALORA_OK;
+}
+
+int alora_planner_drop(alora_planner *p, int64_t req_id, int32_t first, int32_t n_drop, int64_t *src, int64_t *dst, int32_t *shift,
+                       int32_t cap, int32_t *n_rows)
+{
+    if (!p || !n_rows || first < 0 || n_drop < 1 || cap < 0 || (cap > 0 && (!src || !dst || !shift))) return ALORA_EINVAL;
+    auto it = p->reqs.find(req_id);
+    if (it == p->reqs.end()) return ALORA_EINVAL;
+    Request &r = it->second;
+    const int64_t bs = p->bs, n = (int64_t)r.tokens.size(), left = n - n_drop;
+    if (left < 1 || first > left) return ALORA_EINVAL;
+    const int64_t b0 = first / bs, rows = left - b0 * bs, fresh = (rows + bs - 1) / bs;
+    if (rows > cap) {
+        *n_rows = (int32_t)rows;
+        return ALORA_ESHAPE;
+    }
+    if (fresh > p->n_free) return ALORA_ENOBLOCKS;
+    try {
+        std::vector<int32_t> table(r.table.begin(), r.table.begin() + b0);
+        table.reserve((size_t)(b0 + fresh));
+        // nothing can fail from here on
+        for (int64_t i = 0; i < fresh; ++i) {
+            const int32_t b = p->take_free();
+            p->ref[b] = 1;
+            table.push_back(b);
+        }
+        for (int64_t i = 0; i < rows; ++i) {
+            const int64_t now = b0 * bs + i, was = now < first ? now : now + n_drop;
+            src[i] = (int64_t)r.table[was / bs] * bs + was % bs;
+            dst[i] = (int64_t)table[now / bs] * bs + now % bs;
+            shift[i] = (int32_t)(now - was);
+        }
+        p->release(r.table, (size_t)b0);
+        r.table = std::move(table);
+        r.tokens.erase(r.tokens.begin() + first, r.tokens.begin() + first + n_drop);
+        if (r.start >= first + n_drop) r.start -= n_drop;
+        else if (r.start > first) r.start = first;
+        r.exact = std::min(r.exact, b0);
+        r.keyed = (int32_t)std::min<int64_t>(r.keyed, b0);
+        if ((int64_t)r.hashes.size() > b0) r.hashes.resize((size_t)b0);
+        *n_rows = (int32_t)rows;
+    } catch (const std::bad_alloc &) {
+        return ALORA_ENOMEM;
+    }
     return ALORA_OK;
 }
 

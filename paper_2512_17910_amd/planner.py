@@ -7,7 +7,7 @@ from typing import Sequence
 
 import numpy as np
 
-from .binding import AloraError, lib
+from .binding import ALORA_ESHAPE, AloraError, lib
 
 ALORA_ENOBLOCKS = -7
 
@@ -45,7 +45,10 @@ def _L():
         L.alora_planner_block_table.argtypes = [vp, i64, vp, i32, ctypes.POINTER(i32)]
         L.alora_planner_free_blocks.argtypes = [vp]
         L.alora_planner_free_blocks.restype = i64
-        for n in ("create", "destroy", "admit", "append", "commit", "finish", "block_table"):
+        L.alora_planner_fork.argtypes = [vp, i64, i64, i32, i32, vp, vp, ctypes.POINTER(i32)]
+        L.alora_planner_compact.argtypes = [vp, i64, vp, vp, i32, ctypes.POINTER(i32)]
+        L.alora_planner_drop.argtypes = [vp, i64, i32, i32, vp, vp, vp, i32, ctypes.POINTER(i32)]
+        for n in ("create", "destroy", "admit", "append", "commit", "finish", "block_table", "fork", "compact", "drop"):
             getattr(L, "alora_planner_" + n).restype = ctypes.c_int
         _declared = True
     return L
@@ -124,6 +127,36 @@ class Planner:
         s = _L().alora_planner_finish(self._h, req_id)
         if s:
             raise AloraError(s, "alora_planner_finish")
+
+    def fork(self, req_id: int, new_req_id: int, adapter_id: int, activation_start: int):
+        """(src, dst) int32 arrays of the block copies the new request needs: one pair, or none (alora_cache_copy_blocks)."""
+        src, dst, n = np.zeros(1, np.int32), np.zeros(1, np.int32), ctypes.c_int32(0)
+        s = _L().alora_planner_fork(self._h, req_id, new_req_id, adapter_id, activation_start, src.ctypes.data, dst.ctypes.data, ctypes.byref(n))
+        if s:
+            raise AloraError(s, "alora_planner_fork")
+        return src[:n.value], dst[:n.value]
+
+    def compact(self, n_blocks: int):
+        """The pool keeps its first n_blocks blocks; (src, dst) int32 arrays of the block copies that takes."""
+        n = ctypes.c_int32(0)
+        s = _L().alora_planner_compact(self._h, n_blocks, None, None, 0, ctypes.byref(n))
+        src, dst = np.zeros(n.value, np.int32), np.zeros(n.value, np.int32)
+        if s == ALORA_ESHAPE:
+            s = _L().alora_planner_compact(self._h, n_blocks, src.ctypes.data, dst.ctypes.data, src.size, ctypes.byref(n))
+        if s:
+            raise AloraError(s, "alora_planner_compact")
+        return src, dst
+
+    def drop(self, req_id: int, first: int, n_drop: int):
+        """Tokens first .. first + n_drop - 1 leave the request; (src, dst, shift) arrays of the rows that move (alora_cache_move_rows)."""
+        n = ctypes.c_int32(0)
+        s = _L().alora_planner_drop(self._h, req_id, first, n_drop, None, None, None, 0, ctypes.byref(n))
+        src, dst, shift = np.zeros(n.value, np.int64), np.zeros(n.value, np.int64), np.zeros(n.value, np.int32)
+        if s == ALORA_ESHAPE:
+            s = _L().alora_planner_drop(self._h, req_id, first, n_drop, src.ctypes.data, dst.ctypes.data, shift.ctypes.data, n.value, ctypes.byref(n))
+        if s:
+            raise AloraError(s, "alora_planner_drop")
+        return src, dst, shift
 
     def block_table(self, req_id: int) -> np.ndarray:
         n = ctypes.c_int32(0)
