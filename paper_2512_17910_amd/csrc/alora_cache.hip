@@ -283,11 +283,11 @@ int alora_cache_move_rows(const int64_t *src, const int64_t *dst, const int32_t 
     if (st) return st;
     if (n_rows < 0 || rotary_dim < 0 || (interleaved | 1) != 1) return ALORA_EINVAL;
     if (rotary_dim % 4 || rotary_dim > dims->head_dim) return ALORA_ESHAPE;
-    if ((shift != nullptr) != (rotary_dim > 0) || (cos != nullptr) != (rotary_dim > 0) || (sin != nullptr) != (rotary_dim > 0)) return ALORA_EINVAL;
     if (rotary_dim && rope_positions < 1) return ALORA_EINVAL;
     if ((long long)n_rows * dims->n_kv_heads > 1 << 25) return ALORA_ESHAPE;     // (a grid holds fewer than 2^32 threads)
     if (n_rows == 0 || dims->n_layers == 0) return ALORA_OK;
     if (!src || !dst) return ALORA_EINVAL;
+    if ((shift != nullptr) != (rotary_dim > 0) || (cos != nullptr) != (rotary_dim > 0) || (sin != nullptr) != (rotary_dim > 0)) return ALORA_EINVAL;
     if ((((uintptr_t)src | (uintptr_t)dst) & 7) || ((uintptr_t)shift & 3) || (((uintptr_t)cos | (uintptr_t)sin) & 15)) return ALORA_EINVAL;
     st = check_pointers(dims);
     if (st) return st;

@@ -167,7 +167,7 @@ def test_move_arguments_are_refused():
         assert move(**{name: P + (2 if name == "shift" else 4)}) == EINVAL, name
     assert move(n=-1) == move(rot=-4) == move(il=2) == move(pos=0) == move(rot=0) == EINVAL
     assert move(rot=62) == move(rot=68) == move(n=(1 << 24) + 1) == ESHAPE
-    assert move(n=0) == move(dims=cache_dims(0)) == OK
+    assert move(n=0) == move(dims=cache_dims(0)) == move(n=0, src=None, dst=None, shift=None) == OK
 
 
 def test_binding_refuses_what_it_would_misread():
@@ -190,5 +190,10 @@ def test_binding_refuses_what_it_would_misread():
                                                        ab.make_heads_dims(q, q, k[:4], k[:4], 4, 2, 32, rope=rope, norm=False))):
         with pytest.raises(ValueError):
             bad()
+    dims = ab.make_cache_dims([k], [k], 2, 32, 16)
+    some = np.arange(4, dtype=np.int32)
+    with pytest.raises(ValueError):
+        ab.alora_cache_copy_blocks(some[::2], some[:2], dims)
+    ab._host_int32(some[:0], "src"), ab._host_int32(np.zeros(0, np.int32), "src")      # (an empty array's strides say nothing)
     one = ab.make_heads_dims(q[:1], q[:1], None, k, 4, 2, 32)
     assert one.q_stride >= 128
