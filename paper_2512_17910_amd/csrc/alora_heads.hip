@@ -20,10 +20,59 @@ struct HeadsArgs {
     HeadShape s;
     int T, hq, hkv, n_pos;
     int uq, uk;              // units of 64 >> gshift heads: of queries, of keys
+    int items_q, items_k;    // packed rows: wavefronts of queries, of keys
     float eps, inv_d;
 };
 
 constexpr int HEADS_WAVES = 8;   // wavefronts of a workgroup, at most
+
+// U loaded heads of every lane group, normalised, turned and stored where `on`; all 64 lanes take part.
+template <bool BF16, int V, bool INTERLEAVED, bool NORM, int U>
+__device__ __forceinline__ void norm_turn_store(const HeadsArgs &g, const LanePlace &p, Chunk<BF16, V> (&a)[U], Chunk<BF16, V> (&b)[U],
+                                                const Chunk<BF16, V> (&wa)[U], const Chunk<BF16, V> (&wb)[U], const float c[V], const float s[V],
+                                                const bool (&on)[U], char *const (&to)[U])
+{
+    constexpr int E = BF16 ? 2 : 4;
+    float r[U];
+    if (NORM) {
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            float x[V], y[V];
+            a[i].widen(x);
+            b[i].widen(y);
+            r[i] = 0.f;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float xe = e < p.again_a ? 0.f : x[e], ye = e < p.again_b ? 0.f : y[e];
+                r[i] = fmaf(xe, xe, r[i]);
+                r[i] = fmaf(ye, ye, r[i]);
+            }
+        }
+        head_sum<U>(r, g.s.gshift);
+#pragma unroll
+        for (int i = 0; i < U; ++i) r[i] = rsqrtf(fmaf(r[i], g.inv_d, g.eps));
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        float x[V], y[V];
+        a[i].widen(x);
+        b[i].widen(y);
+        if (NORM) {
+            float w[V];
+            wa[i].widen(w);
+#pragma unroll
+            for (int e = 0; e < V; ++e) x[e] = x[e] * r[i] * w[e];
+            wb[i].widen(w);
+#pragma unroll
+            for (int e = 0; e < V; ++e) y[e] = y[e] * r[i] * w[e];
+        }
+        turn<V, INTERLEAVED, false>(x, y, c, s, p);
+        a[i].narrow(x);
+        b[i].narrow(y);
+        if (on[i] && p.has_a) a[i].store(to[i] + p.a * E);
+        if (on[i] && p.has_b) b[i].store(to[i] + p.b * E);
+    }
+}
 
 // One workgroup per row: its slot and position are scalars, a lane's angles serve all its heads.  A wavefront takes U units at a time (their
 // loads are requested together), the units of queries and keys first, then the row of v in pieces of 2 KiB.  One pass: the mean
@@ -86,46 +135,72 @@ __global__ __launch_bounds__(64 * HEADS_WAVES) void heads_kernel(HeadsArgs g)
                 if (p.has_b) wb[i].load(w + p.b * E);
             }
         }
-        float r[U];
-        if (NORM) {
+        norm_turn_store<BF16, V, INTERLEAVED, NORM, U>(g, p, a, b, wa, wb, c, s, on, to);
+    }
+}
+
+// The same for rows of few heads (at most half a unit): a wavefront takes several rows' queries, keys or values, since what such calls cost is the number of
+// wavefronts.  8192 rows of 4 / 1 heads of 64 take 4.9 us, a workgroup for each row 14.0.
+template <bool BF16, int V, bool INTERLEAVED, bool NORM>
+__global__ __launch_bounds__(256) void heads_packed_kernel(HeadsArgs g)
+{
+    typedef Chunk<BF16, V> C;
+    constexpr int E = BF16 ? 2 : 4;
+    const int lane = threadIdx.x & 63;
+    int item = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (item >= g.items_q + g.items_k) {      // values: 2 KiB
+        item -= g.items_q + g.items_k;
+        const int pieces = g.hkv * g.s.d * E / 16, rows = 128 / pieces;
+        u32x4 x[2];
+        char *to[2];
 #pragma unroll
-            for (int i = 0; i < U; ++i) {
-                float x[V], y[V];
-                a[i].widen(x);
-                b[i].widen(y);
-                r[i] = 0.f;
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const float xe = e < p.again_a ? 0.f : x[e], ye = e < p.again_b ? 0.f : y[e];
-                    r[i] = fmaf(xe, xe, r[i]);
-                    r[i] = fmaf(ye, ye, r[i]);
+        for (int i = 0; i < 2; ++i) {
+            const int at = 64 * i + lane, sub = at / pieces, piece = at - sub * pieces;
+            const long long row = (long long)item * rows + sub;
+            to[i] = nullptr;
+            if (g.v && sub < rows && row < g.T) {
+                const long long slot = g.slot[row];
+                if (slot >= 0 && slot < g.n_slots) {
+                    x[i] = *(const u32x4 *)(g.v + row * g.v_row + piece * 16);
+                    to[i] = g.vc + slot * g.vo_row + piece * 16;
                 }
             }
-            head_sum<U>(r, gs);
-#pragma unroll
-            for (int i = 0; i < U; ++i) r[i] = rsqrtf(fmaf(r[i], g.inv_d, g.eps));
         }
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            float x[V], y[V];
-            a[i].widen(x);
-            b[i].widen(y);
-            if (NORM) {
-                float w[V];
-                wa[i].widen(w);
-#pragma unroll
-                for (int e = 0; e < V; ++e) x[e] = x[e] * r[i] * w[e];
-                wb[i].widen(w);
-#pragma unroll
-                for (int e = 0; e < V; ++e) y[e] = y[e] * r[i] * w[e];
-            }
-            turn<V, INTERLEAVED, false>(x, y, c, s, p);
-            a[i].narrow(x);
-            b[i].narrow(y);
-            if (on[i] && p.has_a) a[i].store(to[i] + p.a * E);
-            if (on[i] && p.has_b) b[i].store(to[i] + p.b * E);
-        }
+        for (int i = 0; i < 2; ++i)
+            if (to[i]) *(u32x4 *)to[i] = x[i];
+        return;
     }
+    const bool is_k = item >= g.items_q;
+    if (is_k) item -= g.items_q;
+    const int gs = g.s.gshift, heads = is_k ? g.hkv : g.hq, rows = (64 >> gs) / heads;
+    const LanePlace p = lane_place<V, INTERLEAVED>(g.s, lane & ((1 << gs) - 1));
+    const int sub = (lane >> gs) / heads, head = (lane >> gs) - sub * heads;
+    const long long row = (long long)item * rows + sub;
+    bool on[1] = {sub < rows && row < g.T};
+    long long slot = 0;
+    if (is_k && on[0]) {
+        slot = g.slot[row];
+        on[0] = slot >= 0 && slot < g.n_slots;
+    }
+    C a[1], b[1], wa[1], wb[1];
+    a[0].zero(); b[0].zero(); wa[0].zero(); wb[0].zero();
+    char *to[1] = {nullptr};
+    float c[V], s[V];
+    const char *w = is_k ? g.wk : g.wq;
+    if (on[0]) {
+        const long long offset = (long long)head * (g.s.d * E);
+        const char *from = (is_k ? (g.k ? g.k + row * g.k_row : g.kc + slot * g.ko_row) : g.q + row * g.q_row) + offset;
+        to[0] = (is_k ? g.kc + slot * g.ko_row : g.q_out + row * g.qo_row) + offset;
+        if (p.has_a) a[0].load(from + p.a * E);
+        if (p.has_b) b[0].load(from + p.b * E);
+        if (g.s.rot) load_angles<V, INTERLEAVED>(g.cos, g.sin, (size_t)min(max(g.pos[row], 0), g.n_pos - 1) * g.s.half, p, c, s);
+    }
+    if (NORM) {
+        if (p.has_a) wa[0].load(w + p.a * E);
+        if (p.has_b) wb[0].load(w + p.b * E);
+    }
+    norm_turn_store<BF16, V, INTERLEAVED, NORM, 1>(g, p, a, b, wa, wb, c, s, on, to);
 }
 
 struct HeadsBackArgs {
@@ -270,10 +345,11 @@ __global__ __launch_bounds__(1024) void heads_weights_kernel(const float *__rest
 {
     __shared__ float red[64][17];
     const int col = threadIdx.x & 15, sl = threadIdx.x >> 4, i = blockIdx.x * 16 + col;
-    float sum = 0.f;
-    if (i < 2 * d) {
-#pragma unroll 8
-        for (int b = sl; b < parts; b += 64) sum += partial[(size_t)b * 2 * d + i];
+    float x[4], sum = 0.f;
+    for (int first = sl; first < parts; first += 256) {      // (once: there are at most 256 workgroups)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x[u] = i < 2 * d && first + 64 * u < parts ? partial[(size_t)(first + 64 * u) * 2 * d + i] : 0.f;
+        sum += (x[0] + x[1]) + (x[2] + x[3]);
     }
     red[sl][col] = sum;
     __syncthreads();
@@ -361,11 +437,25 @@ static int units_of(int heads, const HeadShape &s)
     return (heads + per - 1) / per;
 }
 
-static int launch_heads(const HeadsArgs &g, bool bf16, int V, bool norm, hipStream_t st)
+static int launch_heads(HeadsArgs &g, bool bf16, int V, bool norm, hipStream_t st)
 {
     const int units = g.uq + g.uk, v_pieces = g.v ? (g.hkv * g.s.d * (bf16 ? 2 : 4) + 2047) / 2048 : 0;
     // three units of a wavefront where the chip is full many times over, else one: more wavefronts have shorter chains of loads
     const int U = (long long)g.T * units >= 8192 ? 3 : 1;
+    const int per = 64 >> g.s.gshift;
+    const auto items = [&](int at_once) { return (g.T + at_once - 1) / std::max(1, at_once); };
+    g.items_q = items(per / g.hq);
+    g.items_k = items(per / g.hkv);
+    const long long all = (long long)g.items_q + g.items_k + (g.v ? items(128 / (g.hkv * g.s.d * (bf16 ? 2 : 4) / 16)) : 0);
+    if (g.hq <= per / 2 && g.hkv <= per / 2 && all < 1 << 26) {     // (a grid holds fewer than 2^32 threads)
+        return with_layout(bf16, V, g.s.interleaved, [&](auto b, auto v, auto il) {
+            const auto go = [&](auto kernel) {
+                launch_kernel(kernel, dim3((unsigned)((all + 3) / 4)), dim3(256), 0, st, g);
+                return launch_status();
+            };
+            return norm ? go(heads_packed_kernel<b.value, v.value, il.value, true>) : go(heads_packed_kernel<b.value, v.value, il.value, false>);
+        });
+    }
     const int waves = std::min(HEADS_WAVES, (units + U - 1) / U + v_pieces);
     return with_layout(bf16, V, g.s.interleaved, [&](auto b, auto v, auto il) {
         const auto go = [&](auto kernel) {

@@ -116,7 +116,8 @@ def test_heads(dtype, il, d, rot):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("T,hq,hkv,d,rot,cache", [(1, 32, 8, 128, 128, True), (300, 28, 4, 112, 28, True), (1100, 64, 8, 128, 64, False), (2049, 5, 5, 64, 64, False),
-                                                  (700, 40, 40, 256, 28, False), (9001, 1, 1, 32, 32, True), (16, 71, 1, 64, 32, False)])
+                                                  (700, 40, 40, 256, 28, False), (9001, 1, 1, 32, 32, True), (16, 71, 1, 64, 32, False),
+                                                  (3001, 4, 1, 64, 64, False), (777, 4, 2, 80, 20, False)])
 def test_heads_of_larger_calls(dtype, T, hq, hkv, d, rot, cache):
     """Calls whose wavefronts take several units of heads, shapes of one K/V head, more units than wavefronts."""
     for il in (False, True):
@@ -164,22 +165,23 @@ def test_infinities_and_nan_stay_in_their_heads():
     assert (to_f64(h.q_out)[0, :32] == 0).all() and np.isfinite(to_f64(h.q_out)).all()
 
 
-def test_many_rows():
-    """More rows than one dimension of a grid takes."""
+@pytest.mark.parametrize("hq", [1, 33])
+def test_many_rows(hq):
+    """More rows than one dimension of a grid takes; rows of few heads share wavefronts."""
     T = (1 << 20) + 777
-    q = torch.randn((T, 8), device="cuda").to(torch.bfloat16)
+    q = torch.randn((T, 8 * hq), device="cuda").to(torch.bfloat16)
     kc = torch.randn((T, 8), device="cuda").to(torch.bfloat16)
     rope = rope_of(np.random.default_rng(0), 64, 8)
     pos = (torch.arange(T, device="cuda") % 64).int()
     slot = torch.arange(T, device="cuda").flip(0).contiguous()
     at = torch.cat((torch.arange(5), torch.arange((1 << 20) - 3, (1 << 20) + 3), torch.arange(T - 5, T))).cuda()
     q0, k0 = to_f64(q[at]), to_f64(kc[slot[at]])
-    dims = ab.make_heads_dims(q, q, None, kc, 1, 1, 8, rope=rope, norm=False)
+    dims = ab.make_heads_dims(q, q, None, kc, hq, 1, 8, rope=rope, norm=False)
     ab.alora_qk_norm_rope(q, q, None, kc, None, None, None, None, rope, pos, slot, dims)
     c, s = angles(rope, pos[at].cpu().numpy())
     for got, x in ((q[at], q0), (kc[slot[at]], k0)):
-        want, size = oh.heads(x.reshape(len(at), 1, 8), None, 0, c, s, False)
-        close(got, want.reshape(len(at), 8), size.reshape(len(at), 8), torch.bfloat16, 32, "rows")
+        want, size = oh.heads(x.reshape(len(at), -1, 8), None, 0, c, s, False)
+        close(got, want.reshape(len(at), -1), size.reshape(len(at), -1), torch.bfloat16, 32, "rows")
 
 
 def test_slots_behind_four_gibibytes():
