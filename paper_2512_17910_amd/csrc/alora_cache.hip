@@ -20,32 +20,20 @@ struct PairList {
 constexpr int PAIRS_FEW = 16, PAIRS_MANY = 352;
 static_assert(sizeof(CacheTable) + sizeof(PairList<PAIRS_MANY>) + 16 <= 4096, "kernel arguments");
 
-// One workgroup per piece of 4 KiB * K of a block, pair and cache; all pairs of a cache before the next cache.  Bound by memory: each byte is
-// read and written once, past the caches, since nothing reads it soon.  1000 blocks of 32 KiB in 16 caches, us: 204 (5.1 TB/s; a
-// large copy reaches 5.2), with ordinary loads and stores 221, with the caches of a pair behind each other 211; pieces of
-// 8, 16, 64 KiB are within 1 %.
-template <int PAIRS, int K>
+// One workgroup per piece of 4 KiB of a block, pair and cache; all pairs of a cache before the next cache.  Bound by memory: each byte is
+// read and written once, past the caches, since nothing reads it soon.  1000 blocks of 32 KiB in 16 caches, us: 200 (5.2 TB/s, what a
+// large copy reaches), with ordinary loads and stores 4 to 8 % more, with the caches of a pair behind each other 3 % more; 724 blocks of 8 KiB in 16
+// caches 39.5.  Pieces of 8, 16, 32 KiB: 204, 205, 204 and 41.5, 45.3, 45.3.  One block in 64 caches takes 2.6 us: a launch.
+template <int PAIRS>
 __global__ __launch_bounds__(256) void copy_blocks_kernel(CacheTable caches, PairList<PAIRS> pairs, long long block_bytes)
 {
     char *cache = caches.p[blockIdx.z];
     const int src = pairs.src[blockIdx.y], dst = pairs.dst[blockIdx.y];
-    const long long piece = (long long)blockIdx.x * (K * 4096);
-    const int left = (int)min(block_bytes - piece, (long long)K * 4096), o = threadIdx.x * 16;
-    const char *from = cache + src * block_bytes + piece;    // (not read where src is -1)
-    char *to = cache + dst * block_bytes + piece;
-    u32x4 x[K];
-    if (left == K * 4096) {
-#pragma unroll
-        for (int i = 0; i < K; ++i) x[i] = u32x4{0u, 0u, 0u, 0u};
-        if (src >= 0) {
-#pragma unroll
-            for (int i = 0; i < K; ++i) x[i] = __builtin_nontemporal_load((const u32x4 *)(from + o + i * 4096));
-        }
-#pragma unroll
-        for (int i = 0; i < K; ++i) __builtin_nontemporal_store(x[i], (u32x4 *)(to + o + i * 4096));
-        return;
-    }
-    for (int i = o; i < left; i += 4096) *(u32x4 *)(to + i) = src >= 0 ? *(const u32x4 *)(from + i) : u32x4{0u, 0u, 0u, 0u};
+    const long long at = (long long)blockIdx.x * 4096 + threadIdx.x * 16;
+    if (at >= block_bytes) return;
+    u32x4 x = {0u, 0u, 0u, 0u};
+    if (src >= 0) x = __builtin_nontemporal_load((const u32x4 *)(cache + src * block_bytes + at));
+    __builtin_nontemporal_store(x, (u32x4 *)(cache + dst * block_bytes + at));
 }
 
 // How rows lie on wavefronts: `rows` of them on one where they leave room, else one on `units`.  Bound by memory; what costs next is the number of
@@ -240,12 +228,7 @@ static void launch_copies(const CacheTable &caches, int n_caches, const int32_t 
         PairList<PAIRS> list;
         std::copy(src + i, src + i + m, list.src);
         std::copy(dst + i, dst + i + m, list.dst);
-        // pieces of 32 KiB where that gives the chip two workgroups for every compute unit, else of 4 (one block in 64 caches: 2.6 us)
-        const long long large = (block_bytes + 32767) / 32768;
-        if (large * n_caches * m >= 512)
-            launch_kernel(copy_blocks_kernel<PAIRS, 8>, dim3((unsigned)large, m, n_caches), dim3(256), 0, st, caches, list, block_bytes);
-        else
-            launch_kernel(copy_blocks_kernel<PAIRS, 1>, dim3((unsigned)((block_bytes + 4095) / 4096), m, n_caches), dim3(256), 0, st, caches, list, block_bytes);
+        launch_kernel(copy_blocks_kernel<PAIRS>, dim3((unsigned)((block_bytes + 4095) / 4096), m, n_caches), dim3(256), 0, st, caches, list, block_bytes);
     }
 }
 
