@@ -214,6 +214,7 @@ struct HeadsBackArgs {
     float *dwq, *dwk;        // where one workgroup does it all, it writes these
     HeadShape s;
     int T, hq, hkv, n_pos;
+    int rows_q, rows_k;      // rows of a unit: several where their heads are at most half of it
     int uq, uk, wq_waves;    // the first wq_waves wavefronts of a workgroup take the queries
     float eps, inv_d;
 };
@@ -225,7 +226,8 @@ constexpr int BACK_WAVES = 16;   // wavefronts of a workgroup, at most
 // The units of heads of all rows, those of queries dealt to the wavefronts of all workgroups that take queries, those of keys to
 // the others, so that a lane's sums for the weights are of one of the two.  Bound by memory: 4096 rows of 32 / 8 heads of 128 take 24.3 us (5.2 TB/s),
 // the second kernel 4.4.  256 workgroups of up to 16 wavefronts (fewer partial sums to add): the pass 27.6 us; with 512 29.9, 1024 of five
-// wavefronts that kept to rows 42.  dx goes past the caches: 27.6, ordinary stores 29.2.
+// wavefronts that kept to rows 42.  dx goes past the caches: 27.6, ordinary stores 29.2.  Rows of few heads share a wavefront: 2869 rows of 8 / 1
+// heads of 32 take 6.5 us, with a row for each 9.3 (11.0 with the sums over the heads through LDS).
 template <bool BF16, int V, bool INTERLEAVED, bool NORM>
 __global__ __launch_bounds__(64 * BACK_WAVES) void heads_back_kernel(HeadsBackArgs g)
 {
@@ -235,13 +237,17 @@ __global__ __launch_bounds__(64 * BACK_WAVES) void heads_back_kernel(HeadsBackAr
     const int gs = g.s.gshift, per = 64 >> gs;
     const LanePlace p = lane_place<V, INTERLEAVED>(g.s, lane & ((1 << gs) - 1));
     const bool is_k = wave >= g.wq_waves;
-    const int heads = is_k ? g.hkv : g.hq, units = is_k ? g.uk : g.uq;
+    const int heads = is_k ? g.hkv : g.hq, units = is_k ? g.uk : g.uq, rows = is_k ? g.rows_k : g.rows_q, T = (g.T + rows - 1) / rows;
     const int mine = is_k ? waves - g.wq_waves : g.wq_waves, step = gridDim.x * mine;
     const int first = blockIdx.x * mine + (is_k ? wave - g.wq_waves : wave);
     const int row_step = step / units, unit_step = step % units;
     const char *xs = is_k ? g.k : g.q, *gs_in = is_k ? g.gk : g.gq;
     char *outs = is_k ? g.dk : g.dq;
     const long long x_row = is_k ? g.k_row : g.q_row, g_row = is_k ? g.gk_row : g.gq_row, d_row = is_k ? g.dk_row : g.dq_row;
+
+    // (several rows of few heads on a wavefront: the lane's row among them, and what that adds to addresses)
+    const int sub = rows > 1 ? (lane >> gs) / heads : 0, lane_head = (lane >> gs) - sub * heads;
+    const long long x_sub = sub * x_row, g_sub = sub * g_row, d_sub = sub * d_row;
 
     float w0[V], w1[V], dw0[V], dw1[V];
     if (NORM) {
@@ -256,29 +262,30 @@ __global__ __launch_bounds__(64 * BACK_WAVES) void heads_back_kernel(HeadsBackAr
 #pragma unroll
         for (int e = 0; e < V; ++e) dw0[e] = dw1[e] = 0.f;
     }
-    for (int row = first / units, unit = first % units; row < g.T; row += row_step, unit += unit_step) {
+    for (int row = first / units, unit = first % units; row < T; row += row_step, unit += unit_step) {
         if (unit >= units) {
             unit -= units;
-            if (++row >= g.T) break;
+            if (++row >= T) break;
         }
         {
+            const bool on = unit * per + lane_head < heads && sub < rows && (rows == 1 || row * rows + sub < g.T);
             float c[V], s[V];
             if (g.s.rot) {
-                const int at = min(max(g.pos[row], 0), g.n_pos - 1);
+                const int pos = rows == 1 ? g.pos[row] : g.pos[min(row * rows + sub, g.T - 1)], at = min(max(pos, 0), g.n_pos - 1);
                 load_angles<V, INTERLEAVED>(g.cos, g.sin, (size_t)at * g.s.half, p, c, s);
             }
-            const int head = unit * per + (lane >> gs);
-            const bool on = head < heads;
-            const long long offset = (long long)head * (g.s.d * E);
+            const long long offset = (long long)(unit * per + lane_head) * (g.s.d * E);
+            const char *x_at = xs + (long long)row * rows * x_row + x_sub + offset, *g_at = gs_in + (long long)row * rows * g_row + g_sub + offset;
+            char *d_at = outs + (long long)row * rows * d_row + d_sub + offset;
             C xa, xb, ga, gb;
             xa.zero(); xb.zero(); ga.zero(); gb.zero();
             if (on && p.has_a) {
-                ga.load(gs_in + row * g_row + offset + p.a * E);
-                if (NORM) xa.load(xs + row * x_row + offset + p.a * E);
+                ga.load(g_at + p.a * E);
+                if (NORM) xa.load(x_at + p.a * E);
             }
             if (on && p.has_b) {
-                gb.load(gs_in + row * g_row + offset + p.b * E);
-                if (NORM) xb.load(xs + row * x_row + offset + p.b * E);
+                gb.load(g_at + p.b * E);
+                if (NORM) xb.load(x_at + p.b * E);
             }
             float u[V], v[V];
             ga.widen(u);
@@ -308,19 +315,14 @@ __global__ __launch_bounds__(64 * BACK_WAVES) void heads_back_kernel(HeadsBackAr
             }
             ga.narrow(u);
             gb.narrow(v);
-            if (on && p.has_a) ga.template store<true>(outs + row * d_row + offset + p.a * E);
-            if (on && p.has_b) gb.template store<true>(outs + row * d_row + offset + p.b * E);
+            if (on && p.has_a) ga.template store<true>(d_at + p.a * E);
+            if (on && p.has_b) gb.template store<true>(d_at + p.b * E);
         }
     }
     if (NORM) {
         __shared__ float red[BACK_WAVES][256];
-        for (int m = 1 << gs; m < 64; m <<= 1) {
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                dw0[e] += __shfl_xor(dw0[e], m);
-                dw1[e] += __shfl_xor(dw1[e], m);
-            }
-        }
+        sum_over_heads<V>(dw0, gs);
+        sum_over_heads<V>(dw1, gs);
         if (lane < (1 << gs)) {
 #pragma unroll
             for (int e = 0; e < V; ++e) {
@@ -474,22 +476,27 @@ struct BackPlan {
 // Units that one workgroup takes alone, without the second kernel; the pass in us with it and without: 5 units 11.2 and 8.4, 40 units 11.1 and
 // 9.5, 80 units 11.1 and 13.9.
 constexpr int ONE_WORKGROUP = 48;
-static BackPlan plan_back(int T, int uq, int uk)
+// rows of `heads` heads that share a unit
+static int rows_of(int heads, const HeadShape &s) { return std::max(1, (64 >> s.gshift) / heads); }
+
+static BackPlan plan_back(int T, int hq, int hkv, const HeadShape &s)
 {
-    const long long all = (long long)T * (uq + uk);
+    const auto units = [&](int heads) { return (T + rows_of(heads, s) - 1) / rows_of(heads, s) * (long long)units_of(heads, s); };
+    const long long uq = units(hq), uk = units(hkv), all = uq + uk;
     const int most = all <= ONE_WORKGROUP ? BACK_WAVES : (int)std::min<long long>(BACK_WAVES, std::max<long long>(2, all / 256));
     BackPlan p = {0, 0, 0};
+    if (T == 0) return p;
     double best = 0.0;
     for (int w = 2; w <= most; ++w) {
         const int q = std::max(1, std::min(w - 1, (int)((double)w * uq / (uq + uk) + 0.5)));
-        const double cost = std::max((double)uq / q, (double)uk / (w - q)) * w;    // wavefronts' time for a row
+        const double cost = std::max((double)uq / q, (double)uk / (w - q)) * w;    // wavefronts' time
         if (w == 2 || cost <= best * 1.02) {
             best = w == 2 ? cost : std::min(best, cost);
             p.waves = w;
             p.q_waves = q;
         }
     }
-    p.groups = T == 0 ? 0 : all <= ONE_WORKGROUP ? 1 : (int)std::min<long long>(256, (all + p.waves - 1) / p.waves);
+    p.groups = all <= ONE_WORKGROUP ? 1 : (int)std::min<long long>(256, (all + p.waves - 1) / p.waves);
     return p;
 }
 
@@ -498,7 +505,7 @@ static HeadShape shape_of(const alora_heads_dims *d) { return head_shape(d->head
 static size_t back_workspace(const alora_heads_dims *d)
 {
     const HeadShape s = shape_of(d);
-    const int groups = plan_back(d->n_tokens, units_of(d->n_q_heads, s), units_of(d->n_kv_heads, s)).groups;
+    const int groups = plan_back(d->n_tokens, d->n_q_heads, d->n_kv_heads, s).groups;
     return d->norm && groups > 1 ? (size_t)groups * 2 * d->head_dim * sizeof(float) : 0;
 }
 
@@ -592,7 +599,8 @@ int alora_qk_norm_rope_backward(const void *q, const void *dq_out, void *dq, con
     g.T = d.n_tokens; g.hq = d.n_q_heads; g.hkv = d.n_kv_heads; g.n_pos = d.rope_positions;
     g.uq = units_of(g.hq, g.s); g.uk = units_of(g.hkv, g.s);
     g.eps = d.eps; g.inv_d = 1.0f / (float)d.head_dim;
-    const BackPlan plan = plan_back(d.n_tokens, g.uq, g.uk);
+    g.rows_q = rows_of(g.hq, g.s); g.rows_k = rows_of(g.hkv, g.s);
+    const BackPlan plan = plan_back(d.n_tokens, g.hq, g.hkv, g.s);
     g.wq_waves = plan.q_waves;
     g.dwq = dwq; g.dwk = dwk;
     const hipStream_t stream = (hipStream_t)hip_stream;

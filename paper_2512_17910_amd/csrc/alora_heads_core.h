@@ -203,6 +203,19 @@ __device__ __forceinline__ float dpp_plus(float v)
     return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
 }
 
+// v and the value 16, or 32, lanes away added: the swap exchanges the odd rows of 16 lanes (the upper half) of one copy with the even ones (the lower
+// half) of the other, which leaves every lane its own value in one of them and its partner's in the other.
+__device__ __forceinline__ float plus_16_away(float v)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float plus_32_away(float v)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 // sums over the 2^gshift lanes of a head, N of them side by side; every lane receives them (all 64 lanes take part)
 template <int N>
 __device__ __forceinline__ void head_sum(float (&v)[N], int gshift)
@@ -215,8 +228,25 @@ __device__ __forceinline__ void head_sum(float (&v)[N], int gshift)
     ALORA_STEP(2, dpp_plus<0x4E>(v[i]))    // quad_perm [2,3,0,1]
     ALORA_STEP(3, dpp_plus<0x141>(v[i]))   // row_half_mirror: the other quad of the 8 lanes
     ALORA_STEP(4, dpp_plus<0x140>(v[i]))   // row_mirror: the other half of the 16 lanes
-    ALORA_STEP(5, v[i] + __shfl_xor(v[i], 16))
-    ALORA_STEP(6, v[i] + __shfl_xor(v[i], 32))
+    ALORA_STEP(5, plus_16_away(v[i]))
+    ALORA_STEP(6, plus_32_away(v[i]))
+#undef ALORA_STEP
+}
+
+// sums over the lanes that are multiples of 2^gshift apart: of what the heads of a wavefront have in the same place
+template <int N>
+__device__ __forceinline__ void sum_over_heads(float (&v)[N], int gshift)
+{
+#define ALORA_STEP(below, value)                    \
+    if (gshift < below) {                           \
+        _Pragma("unroll") for (int i = 0; i < N; ++i) v[i] = value; \
+    }
+    ALORA_STEP(6, plus_32_away(v[i]))
+    ALORA_STEP(5, plus_16_away(v[i]))
+    ALORA_STEP(4, dpp_plus<0x128>(v[i]))   // row_ror:8
+    ALORA_STEP(3, dpp_plus<0x124>(v[i]))   // row_ror:4, of values that repeat every 8 lanes
+    ALORA_STEP(2, dpp_plus<0x122>(v[i]))   // row_ror:2
+    ALORA_STEP(1, dpp_plus<0x121>(v[i]))   // row_ror:1
 #undef ALORA_STEP
 }
 

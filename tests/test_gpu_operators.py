@@ -281,7 +281,8 @@ def test_gradients(dtype, il, d, rot):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("T,hq,hkv,d,rot", [(1100, 32, 8, 128, 128), (2500, 4, 2, 64, 64), (1025, 71, 1, 64, 32), (600, 40, 40, 256, 28)])
+@pytest.mark.parametrize("T,hq,hkv,d,rot", [(1100, 32, 8, 128, 128), (2500, 4, 2, 64, 64), (1025, 71, 1, 64, 32), (600, 40, 40, 256, 28),
+                                            (1533, 8, 1, 32, 32), (300, 4, 2, 80, 20), (30, 1, 1, 8, 8)])
 def test_gradients_of_larger_calls(dtype, T, hq, hkv, d, rot):
     b = Back(dtype, T, hq, hkv, d, rot, False, True, seed=T)
     b.call()
