@@ -117,7 +117,8 @@ def test_heads(dtype, il, d, rot):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("T,hq,hkv,d,rot,cache", [(1, 32, 8, 128, 128, True), (300, 28, 4, 112, 28, True), (1100, 64, 8, 128, 64, False), (2049, 5, 5, 64, 64, False),
                                                   (700, 40, 40, 256, 28, False), (9001, 1, 1, 32, 32, True), (16, 71, 1, 64, 32, False),
-                                                  (3001, 4, 1, 64, 64, False), (777, 4, 2, 80, 20, False)])
+                                                  (3001, 4, 1, 64, 64, False), (777, 4, 2, 80, 20, False), (300, 3, 1, 80, 20, True),
+                                                  (111, 2, 2, 112, 28, True)])
 def test_heads_of_larger_calls(dtype, T, hq, hkv, d, rot, cache):
     """Calls whose wavefronts take several units of heads, shapes of one K/V head, more units than wavefronts."""
     for il in (False, True):
