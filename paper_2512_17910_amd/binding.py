@@ -480,6 +480,8 @@ def alora_qk_norm_rope(q, q_out, k, k_cache, v, v_cache, wq, wk, rope, token_pos
     """Enqueue norm and rotary embedding of the rows' heads (include/alora_heads.h): q to q_out, k (None: in place) to its slots of k_cache,
     v, where given, to v_cache.  The tensors are those that dims was made from, or of the same shapes and strides; wq and wk are None
     without norm, rope without rotation."""
+    if slot_mapping.element_size() != 8 or (token_positions is not None and token_positions.element_size() != 4):
+        raise TypeError("token_positions: int32, slot_mapping: int64 expected")
     cos, sin = (None, None) if rope is None else rope
     s = (_lib or lib()).alora_qk_norm_rope(q.data_ptr(), q_out.data_ptr(), None if k is None else k.data_ptr(), k_cache.data_ptr(),
                                            None if v is None else v.data_ptr(), None if v_cache is None else v_cache.data_ptr(),
@@ -505,6 +507,8 @@ def alora_qk_norm_rope_backward(q, dq_out, dq, k, dk_out, dk, wq, wk, dwq, dwk, 
     """Enqueue the backward pass of alora_qk_norm_rope: dq, dk and, with norm, the fp32 dwq, dwk from the gradients of its outputs."""
     if dims.n_tokens > 1 and (dq.stride(0) != (dims.dq_stride or dims.q_stride) or dk.stride(0) != (dims.dk_stride or dims.k_stride)):
         raise ValueError("dq, dk: strides other than those of dims (make_heads_dims takes dq and dk)")
+    if (token_positions is not None and token_positions.element_size() != 4) or (dwq is not None and (dwq.element_size() != 4 or dwk.element_size() != 4)):
+        raise TypeError("token_positions: int32, dwq and dwk: fp32 expected")
     cos, sin = (None, None) if rope is None else rope
     s = (_lib or lib()).alora_qk_norm_rope_backward(
         q.data_ptr(), dq_out.data_ptr(), dq.data_ptr(), k.data_ptr(), dk_out.data_ptr(), dk.data_ptr(), None if wq is None else wq.data_ptr(),
@@ -578,6 +582,8 @@ def alora_cache_move_rows(src, dst, shift, rope, dims: AloraCacheDims, interleav
     n = src.shape[0]
     if dst.shape[0] != n or (shift is not None and shift.shape[0] != n):
         raise ValueError("src, dst, shift: one length expected")
+    if src.element_size() != 8 or dst.element_size() != 8 or (shift is not None and shift.element_size() != 4) or not (src.is_contiguous() and dst.is_contiguous()):
+        raise TypeError("src, dst: contiguous int64, shift: int32 expected")
     cos, sin, positions, rot = (None, None, 0, 0) if rope is None else (rope[0].data_ptr(), rope[1].data_ptr(), rope[0].shape[0], 2 * rope[0].shape[1])
     s = (_lib or lib()).alora_cache_move_rows(src.data_ptr(), dst.data_ptr(), None if shift is None else shift.data_ptr(), n, cos, sin, positions, rot,
                                     1 if interleaved else 0, ctypes.byref(dims), _stream_handle(stream))

@@ -205,6 +205,14 @@ static int check_pairs(const int32_t *src, const int32_t *dst, int n, long long 
         return ALORA_OK;
     }
     try {
+        if (blocks / 64 > 32ll * n) {      // (a short list of a large pool: sorting it takes less than clearing a bit for every block)
+            std::vector<int32_t> sorted(dst, dst + n);
+            std::sort(sorted.begin(), sorted.end());
+            if (std::adjacent_find(sorted.begin(), sorted.end()) != sorted.end()) return ALORA_EDATA;
+            for (int i = 0; i < n; ++i)
+                if (src[i] >= 0 && std::binary_search(sorted.begin(), sorted.end(), src[i])) return ALORA_EDATA;
+            return ALORA_OK;
+        }
         std::vector<uint64_t> written((size_t)(blocks + 63) / 64, 0);
         for (int i = 0; i < n; ++i) {
             uint64_t &w = written[(size_t)dst[i] / 64];

@@ -128,6 +128,29 @@ def test_heads_of_larger_calls(dtype, T, hq, hkv, d, rot, cache):
         h.check()
 
 
+@pytest.mark.parametrize("il", [False, True], ids=["halves", "neighbours"])
+@pytest.mark.parametrize("dtype,d,rot", [("f32", 4, 4), ("f32", 12, 4), ("f32", 20, 20), ("f32", 36, 12), ("f32", 252, 248), ("f32", 252, 200), ("bf16", 24, 24),
+                                         ("bf16", 40, 36), ("bf16", 248, 124), ("bf16", 248, 244)])
+def test_heads_of_odd_sizes(dtype, d, rot, il):
+    for T, hq, hkv, norm, cache, inplace in ((6, 3, 2, True, False, False), (5, 9, 1, True, True, True), (40, 1, 1, False, False, True), (7, 2, 2, True, True, False)):
+        print(f"[case] {dtype} d={d} rot={rot} il={il} T={T} {hq}/{hkv} norm={norm} cache={cache}", flush=True)
+        h = Heads(dtype, T, hq, hkv, d, rot, il, norm, cache, seed=d + T)
+        h.run()
+        h.check()
+        b = Back(dtype, T, hq, hkv, d, rot, il, norm, seed=d + T, inplace=inplace)
+        b.call()
+        b.check()
+
+
+def test_values_stored_beside_keys_that_lie_in_the_cache():
+    h = Heads("bf16", 20, 8, 2, 64, 64, cache=True, seed=4)
+    v = values(h.rng, (20, 128), h.dt)
+    h.v = v
+    h.dims = ab.make_heads_dims(h.q, h.q_out, None, h.kc, 8, 2, 64, rope=h.rope, eps=h.eps, v=v, v_out=h.vc)
+    h.run()
+    h.check()
+
+
 def test_rows_that_are_left_alone_and_positions_outside():
     h = Heads("bf16", 12, 4, 2, 64, 64, seed=3)
     h.pos[:] = [-1, 50, 1 << 30, -(1 << 31), 0, 49, 7, 8, 9, 10, 11, 12]

@@ -149,11 +149,11 @@ def test_caches_are_refused(kw, status):
         assert ab.lib().alora_cache_move_rows_validate(P, P, P, 3, 10, ctypes.byref(d)) == status
 
 
-@pytest.mark.parametrize("n", [0, 30])      # (short and long lists are checked in different ways)
-def test_lists_of_blocks_are_refused(n):
+@pytest.mark.parametrize("n,blocks", [(0, 200), (30, 200), (30, 1 << 20)])      # (short and long lists, of small and large pools, are checked in different ways)
+def test_lists_of_blocks_are_refused(n, blocks):
     fill = lambda a, first: a + list(range(first, first + n))
-    d = cache_dims(n_slots=16 * 200)
-    for src, dst in (([0, 200], [1, 2]), ([0, -2], [1, 2]), ([0, 1], [3, 200]), ([0, 1], [3, -1]), ([0, 1], [3, 3]), ([0, 1], [1, 2]), ([5, 1], [5, 2]),
+    d = cache_dims(n_slots=16 * blocks)
+    for src, dst in (([0, blocks], [1, 2]), ([0, -2], [1, 2]), ([0, 1], [3, blocks]), ([0, 1], [3, -1]), ([0, 1], [3, 3]), ([0, 1], [1, 2]), ([5, 1], [5, 2]),
                      ([-1, -1], [4, 4]), ([-1, 4], [4, 6])):
         assert copy(fill(src, 40), fill(dst, 100), d) == EDATA, (src, dst)
     assert copy(None, [1], d, 1) == copy([1], None, d, 1) == copy([1], [2], d, -1) == EINVAL
@@ -195,5 +195,14 @@ def test_binding_refuses_what_it_would_misread():
     with pytest.raises(ValueError):
         ab.alora_cache_copy_blocks(some[::2], some[:2], dims)
     ab._host_int32(some[:0], "src"), ab._host_int32(np.zeros(0, np.int32), "src")      # (an empty array's strides say nothing)
+    for bad in (lambda: ab.alora_qk_norm_rope(q, q, None, k, None, None, None, None, rope, torch.zeros(4).long(), torch.zeros(4).long(), ok),
+                lambda: ab.alora_qk_norm_rope(q, q, None, k, None, None, None, None, rope, torch.zeros(4).int(), torch.zeros(4).int(), ok),
+                lambda: ab.alora_qk_norm_rope_backward(q, q, q, k[:4], k[:4], k[:4], None, None, None, None, rope, torch.zeros(4).long(),
+                                                       ab.make_heads_dims(q, q, k[:4], k[:4], 4, 2, 32, rope=rope, norm=False)),
+                lambda: ab.alora_cache_move_rows(torch.zeros(2).int(), torch.zeros(2).int(), None, None, dims),
+                lambda: ab.alora_cache_move_rows(torch.zeros(4).long()[::2], torch.zeros(2).long(), None, None, dims),
+                lambda: ab.alora_cache_move_rows(torch.zeros(2).long(), torch.zeros(2).long(), torch.zeros(2).long(), rope, dims)):
+        with pytest.raises(TypeError):
+            bad()
     one = ab.make_heads_dims(q[:1], q[:1], None, k, 4, 2, 32)
     assert one.q_stride >= 128
