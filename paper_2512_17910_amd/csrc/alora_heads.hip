@@ -222,7 +222,7 @@ struct HeadsBackArgs {
 constexpr int BACK_WAVES = 16;   // wavefronts of a workgroup, at most
 
 // With g = the outputs' gradient turned back, u = g w, r = 1 / sqrt(mean x^2 + eps): both means (of x x and x u) come out of one pass over x and g, then
-// dx = r u - x (r^3 mean(x u)) from registers, and each lane adds g x r to sums for the weights of its features.
+// dx = r (u - x r (r mean(x u))) from registers (r^3 would leave fp32's range for heads of 1e-13), and each lane adds g x r to sums for the weights of its features.
 // The units of heads of all rows, those of queries dealt to the wavefronts of all workgroups that take queries, those of keys to
 // the others, so that a lane's sums for the weights are of one of the two.  Bound by memory: 4096 rows of 32 / 8 heads of 128 take 24.3 us (5.2 TB/s),
 // the second kernel 4.4.  256 workgroups of up to 16 wavefronts (fewer partial sums to add): the pass 27.6 us; with 512 29.9, 1024 of five
@@ -267,57 +267,57 @@ __global__ __launch_bounds__(64 * BACK_WAVES) void heads_back_kernel(HeadsBackAr
             unit -= units;
             if (++row >= T) break;
         }
-        {
-            const bool on = unit * per + lane_head < heads && sub < rows && (rows == 1 || row * rows + sub < g.T);
-            float c[V], s[V];
-            if (g.s.rot) {
-                const int pos = rows == 1 ? g.pos[row] : g.pos[min(row * rows + sub, g.T - 1)], at = min(max(pos, 0), g.n_pos - 1);
-                load_angles<V, INTERLEAVED>(g.cos, g.sin, (size_t)at * g.s.half, p, c, s);
-            }
-            const long long offset = (long long)(unit * per + lane_head) * (g.s.d * E);
-            const char *x_at = xs + (long long)row * rows * x_row + x_sub + offset, *g_at = gs_in + (long long)row * rows * g_row + g_sub + offset;
-            char *d_at = outs + (long long)row * rows * d_row + d_sub + offset;
-            C xa, xb, ga, gb;
-            xa.zero(); xb.zero(); ga.zero(); gb.zero();
-            if (on && p.has_a) {
-                ga.load(g_at + p.a * E);
-                if (NORM) xa.load(x_at + p.a * E);
-            }
-            if (on && p.has_b) {
-                gb.load(g_at + p.b * E);
-                if (NORM) xb.load(x_at + p.b * E);
-            }
-            float u[V], v[V];
-            ga.widen(u);
-            gb.widen(v);
-            turn<V, INTERLEAVED, true>(u, v, c, s, p);
-            if (NORM) {
-                float x[V], y[V], sums[2] = {0.f, 0.f};    // of x x, of x u
-                xa.widen(x);
-                xb.widen(y);
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const float xe = e < p.again_a ? 0.f : x[e], ye = e < p.again_b ? 0.f : y[e];
-                    sums[0] = fmaf(xe, xe, sums[0]);
-                    sums[0] = fmaf(ye, ye, sums[0]);
-                    sums[1] = fmaf(u[e] * w0[e], xe, sums[1]);
-                    sums[1] = fmaf(v[e] * w1[e], ye, sums[1]);
-                }
-                head_sum<2>(sums, gs);
-                const float r = rsqrtf(fmaf(sums[0], g.inv_d, g.eps)), m = r * r * r * (sums[1] * g.inv_d);
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    dw0[e] = fmaf(u[e] * x[e], r, dw0[e]);
-                    dw1[e] = fmaf(v[e] * y[e], r, dw1[e]);
-                    u[e] = r * (u[e] * w0[e]) - x[e] * m;
-                    v[e] = r * (v[e] * w1[e]) - y[e] * m;
-                }
-            }
-            ga.narrow(u);
-            gb.narrow(v);
-            if (on && p.has_a) ga.template store<true>(d_at + p.a * E);
-            if (on && p.has_b) gb.template store<true>(d_at + p.b * E);
+        const bool on = unit * per + lane_head < heads && sub < rows && (rows == 1 || row * rows + sub < g.T);
+        float c[V], s[V];
+        if (g.s.rot) {
+            const int pos = rows == 1 ? g.pos[row] : g.pos[min(row * rows + sub, g.T - 1)], at = min(max(pos, 0), g.n_pos - 1);
+            load_angles<V, INTERLEAVED>(g.cos, g.sin, (size_t)at * g.s.half, p, c, s);
         }
+        const long long offset = (long long)(unit * per + lane_head) * (g.s.d * E);
+        const char *x_at = xs + (long long)row * rows * x_row + x_sub + offset, *g_at = gs_in + (long long)row * rows * g_row + g_sub + offset;
+        char *d_at = outs + (long long)row * rows * d_row + d_sub + offset;
+        C xa, xb, ga, gb;
+        xa.zero(); xb.zero(); ga.zero(); gb.zero();
+        if (on && p.has_a) {
+            ga.load(g_at + p.a * E);
+            if (NORM) xa.load(x_at + p.a * E);
+        }
+        if (on && p.has_b) {
+            gb.load(g_at + p.b * E);
+            if (NORM) xb.load(x_at + p.b * E);
+        }
+        float u[V], v[V];
+        ga.widen(u);
+        gb.widen(v);
+        turn<V, INTERLEAVED, true>(u, v, c, s, p);
+        if (NORM) {
+            float x[V], y[V], sums[2] = {0.f, 0.f};    // of x x, of x u
+            xa.widen(x);
+            xb.widen(y);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float xe = e < p.again_a ? 0.f : x[e], ye = e < p.again_b ? 0.f : y[e];
+                sums[0] = fmaf(xe, xe, sums[0]);
+                sums[0] = fmaf(ye, ye, sums[0]);
+                sums[1] = fmaf(u[e] * w0[e], xe, sums[1]);
+                sums[1] = fmaf(v[e] * w1[e], ye, sums[1]);
+            }
+            head_sum<2>(sums, gs);
+            // (lanes without a head would add 0 times infinity to the weights' sums where eps is 0)
+            const float r = on ? rsqrtf(fmaf(sums[0], g.inv_d, g.eps)) : 0.f, m = r * (sums[1] * g.inv_d);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const float xr = x[e] * r, yr = y[e] * r;
+                dw0[e] = fmaf(u[e], xr, dw0[e]);
+                dw1[e] = fmaf(v[e], yr, dw1[e]);
+                u[e] = r * (u[e] * w0[e] - xr * m);
+                v[e] = r * (v[e] * w1[e] - yr * m);
+            }
+        }
+        ga.narrow(u);
+        gb.narrow(v);
+        if (on && p.has_a) ga.template store<true>(d_at + p.a * E);
+        if (on && p.has_b) gb.template store<true>(d_at + p.b * E);
     }
     if (NORM) {
         __shared__ float red[BACK_WAVES][256];

@@ -257,14 +257,14 @@ def test_calls_on_another_stream_and_in_a_graph():
 
 
 class Back:
-    def __init__(self, dtype, T, hq, hkv, d, rot, il, norm, pad=0, seed=0, inplace=False):
+    def __init__(self, dtype, T, hq, hkv, d, rot, il, norm, pad=0, seed=0, inplace=False, eps=1e-5, std=2.0):
         rng = np.random.default_rng(seed)
         dt = self.dt = DT[dtype]
         self.T, self.hq, self.hkv, self.d, self.il, self.norm = T, hq, hkv, d, il, norm
         self.rope = rope_of(rng, 50, rot)
         self.pos_host = rng.integers(-2, 53, T).astype(np.int32)
         self.pos = dev(self.pos_host)
-        y = values(rng, (T, (hq + 2 * hkv) * d + pad), dt, 2.0)
+        y = values(rng, (T, (hq + 2 * hkv) * d + pad), dt, std)
         self.q, self.k = y[:, : hq * d], y[:, hq * d: (hq + hkv) * d]
         self.gq, self.gk = values(rng, (T, hq * d), dt), values(rng, (T, hkv * d), dt)
         self.wq, self.wk = (values(rng, (d,), dt, 0.3, 1.0) for _ in range(2)) if norm else (None, None)
@@ -275,12 +275,12 @@ class Back:
             dy = torch.full((T, (hq + hkv) * d + pad), float("nan"), dtype=dt, device="cuda")
             self.dq, self.dk = dy[:, : hq * d], dy[:, hq * d: (hq + hkv) * d]
         self.dwq, self.dwk = (torch.full((d,), float("nan"), device="cuda") for _ in range(2)) if norm else (None, None)
-        self.dims = ab.make_heads_dims(self.q, gq, self.k, gk, hq, hkv, d, rope=self.rope, interleaved=il, norm=norm, eps=1e-5, dq=self.dq, dk=self.dk)
+        self.dims = ab.make_heads_dims(self.q, gq, self.k, gk, hq, hkv, d, rope=self.rope, interleaved=il, norm=norm, eps=eps, dq=self.dq, dk=self.dk)
         self.ws = torch.full((max(16, ab.alora_qk_norm_rope_workspace_bytes(self.dims)),), 0xff, dtype=torch.uint8, device="cuda")
         c, s = angles(self.rope, self.pos_host)
         f = lambda t: to_f64(t).reshape(T, -1, d)
         w = lambda t: None if t is None else to_f64(t)
-        self.want = [oh.heads_back(f(x), f(g), w(ww), 1e-5, c, s, il) for x, g, ww in ((self.q, gq, self.wq), (self.k, gk, self.wk))]
+        self.want = [oh.heads_back(f(x), f(g), w(ww), eps, c, s, il) for x, g, ww in ((self.q, gq, self.wq), (self.k, gk, self.wk))]
 
     def call(self):
         ab.alora_qk_norm_rope_backward(self.q, self.gq, self.dq, self.k, self.gk, self.dk, self.wq, self.wk, self.dwq, self.dwk, self.rope, self.pos,
@@ -314,6 +314,16 @@ def test_gradients_of_larger_calls(dtype, T, hq, hkv, d, rot):
     first = [x.clone() for x in (b.dq, b.dk, b.dwq, b.dwk)]
     b.call()
     assert all(torch.equal(x, y) for x, y in zip(first, (b.dq, b.dk, b.dwq, b.dwk))), "equal calls give equal bits"
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("std", [1.0, 1e-15])
+def test_gradients_without_eps(dtype, std):
+    """eps = 0: lanes without a head, of which there are some here, divide by zero; so may heads as small as 1e-15, whose r^3 no fp32 holds."""
+    for T, hq, hkv, d, rot in ((3, 5, 3, 128, 64), (2, 1, 1, 80, 20), (70, 3, 1, 96, 96)):
+        b = Back(dtype, T, hq, hkv, d, rot, False, True, seed=T, eps=0.0, std=std)
+        b.call()
+        b.check()
 
 
 def test_gradients_of_no_rows():
