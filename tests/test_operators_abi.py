@@ -206,3 +206,82 @@ def test_binding_refuses_what_it_would_misread():
             bad()
     one = ab.make_heads_dims(q[:1], q[:1], None, k, 4, 2, 32)
     assert one.q_stride >= 128
+
+
+# ---- launches, recorded without a GPU (see launch_recorder.c) -------------------------------------
+RECORD = """
+import ctypes, json, re, sys, types
+sys.modules["torch"] = types.ModuleType("torch")         # (the real one would register kernels of its own)
+rec = ctypes.CDLL(sys.argv[1], ctypes.RTLD_GLOBAL)      # ahead of the library: its HIP calls bind here
+sys.path[:0] = sys.argv[2:4]
+import test_operators_abi as t
+from launches import _Launch
+t.ab._lib = t.ab.lib()
+rec.rec_get.restype = ctypes.POINTER(_Launch)
+out = []
+for name, args in json.load(sys.stdin):
+    rec.rec_reset()
+    status = getattr(t, name)(*args)
+    launches = []
+    for i in range(rec.rec_count()):
+        r = rec.rec_get(i).contents
+        m = re.search(r"N5alora(\\d+)", r.name.decode())
+        launches.append([r.name.decode()[m.end():m.end() + int(m.group(1))], list(r.grid), list(r.block)])
+    out.append([status, launches])
+print(json.dumps(out))
+"""
+
+
+def record_forward(kw, has_v):
+    d = heads_dims(**kw)
+    return forward(d, **({} if has_v else dict(v=None, vc=None, k=None)))
+
+
+def record_backward(kw):
+    return backward(heads_dims(**kw))
+
+
+def record_copy(n, layers, blocks):
+    return copy(list(range(n)), list(range(n, 2 * n)), cache_dims(layers, n_slots=16 * blocks))
+
+
+def record_move(n, layers, rot, heads):
+    d = cache_dims(layers, n_kv_heads=heads)
+    return move(d, n=n, rot=rot, **({} if rot else dict(shift=None, cos=None, sin=None)))
+
+
+def test_launches_of_calls(tmp_path):
+    import json
+    import os
+    import subprocess
+    import sys
+    here = os.path.dirname(os.path.abspath(__file__))
+    rec = str(tmp_path / "librec.so")
+    subprocess.run(["gcc", "-O1", "-w", "-shared", "-fPIC", "-o", rec, os.path.join(here, "launch_recorder.c")], check=True)
+
+    def run(*calls):
+        r = subprocess.run([sys.executable, "-c", RECORD, rec, here, os.path.dirname(here)], input=json.dumps(calls), capture_output=True, text=True, timeout=120)
+        assert r.returncode == 0, r.stderr[-3000:]
+        out = json.loads(r.stdout)
+        assert all(s == OK for s, _ in out), out
+        return [launches for _, launches in out]
+
+    wide = dict(n_q_heads=32, n_kv_heads=8, head_dim=128, rotary_dim=128, q_stride=4096, q_out_stride=4096, k_stride=1024, k_out_stride=1024,
+                v_stride=1024, v_out_stride=1024)
+    one, small, many, full = run(["record_forward", [dict(wide, n_tokens=1), False]], ["record_forward", [dict(n_tokens=100), True]],
+                                 ["record_forward", [dict(wide, n_tokens=(1 << 20) + 5), True]], ["record_forward", [dict(wide, n_tokens=2000), True]])
+    assert one == [["heads_kernel", [1, 1, 1], [5 * 64, 1, 1]]]                 # four units of queries, one of keys
+    # rows of 4 / 2 heads of 64 (16 heads a wavefront): 4 and 8 rows on one, 8 rows of values
+    assert small == [["heads_packed_kernel", [-(-(25 + 13 + 13) // 4), 1, 1], [256, 1, 1]]]
+    assert many == [["heads_kernel", [1 << 20, 2, 1], [3 * 64, 1, 1]]] and full == [["heads_kernel", [2000, 1, 1], [3 * 64, 1, 1]]]
+    few, back, plain = run(["record_backward", [dict(wide, n_tokens=9)]], ["record_backward", [dict(wide, n_tokens=4096)]], ["record_backward", [dict(n_tokens=0)]])
+    assert [l[0] for l in few] == ["heads_back_kernel"] and few[0][1] == [1, 1, 1]
+    assert [l[:2] for l in back] == [["heads_back_kernel", [256, 1, 1]], ["heads_weights_kernel", [16, 1, 1]]] and back[0][2] == [15 * 64, 1, 1]
+    assert [l[0] for l in plain] == ["heads_weights_kernel"]
+    short, pairs, layers = run(["record_copy", [3, 2, 20]], ["record_copy", [353, 2, 1000]], ["record_copy", [1, 65, 20]])
+    assert short == [["copy_blocks_kernel", [1, 3, 4], [256, 1, 1]]]            # 16 rows of 2 heads of 64: 4 KiB
+    assert [l[1] for l in pairs] == [[1, 352, 4], [1, 1, 4]] and [l[1] for l in layers] == [[1, 1, 128], [1, 1, 2]]
+    turned, copied, wide_rows = run(["record_move", [100, 65, 64, 2]], ["record_move", [100, 1, 0, 2]], ["record_move", [100, 1, 64, 80]])
+    # two heads of 64: 8 rows of a wavefront either way; 80 heads: 5 wavefronts of turned keys a row
+    assert [l[1] for l in turned] == [[4, 128, 1], [4, 2, 1]] and copied == [["move_rows_kernel", [4, 2, 1], [256, 1, 1]]]
+    assert wide_rows[0][1] == [125, 2, 1]
