@@ -361,30 +361,34 @@ __global__ __launch_bounds__(1024) void heads_weights_kernel(const float *__rest
     if ((threadIdx.x & 63) == 0 && o < 2 * d) (o < d ? dwq[o] : dwk[o - d]) = v[0];
 }
 
+struct TableSpec {
+    double exponent;        // theta_i = 2^(i exponent)
+    double shrink;          // 1 / factor; 1 where nothing is scaled
+    double slope, start;    // what is kept of theta_i: turns of a position * slope + start, between 0 and 1
+    double magnitude;
+    int mix;                // scaled by parts
+};
+
 // Cosines and sines.  A thread keeps to one pair and steps through the rows: angles are added by multiplying exp(i angle) by exp(i step) in 64
 // bits, so that sines themselves are computed twice a thread.
 __global__ __launch_bounds__(256) void rope_tables_kernel(float *__restrict__ cos, float *__restrict__ sin, long long first, long long rows,
-                                                          int half, int steps, int scaling, double log2_base, double factor, double original,
-                                                          double low, double high, double magnitude)
+                                                          int half, int steps, TableSpec spec)
 {
     const int at_once = 256 / half;      // rows of a pass
     const int i = threadIdx.x % half, sub = threadIdx.x / half;
     if (sub >= at_once) return;
-    constexpr double TWO_PI = 6.283185307179586476925;
-    double theta = exp2(-(double)i / half * log2_base);
-    if (scaling == ALORA_ROPE_LINEAR) theta /= factor;
-    if (scaling == ALORA_ROPE_BY_PARTS) {
-        const double keep = fmin(fmax((original * theta / TWO_PI - low) / (high - low), 0.0), 1.0);
-        theta *= keep + (1.0 - keep) / factor;
-    }
-    const double turns = theta / TWO_PI;
+    double turns = exp2(i * spec.exponent) * 0.159154943091895335768884;     // of a position: theta_i / 2 pi
+    const double keep = spec.mix ? fmin(fmax(turns * spec.slope + spec.start, 0.0), 1.0) : 0.0;
+    turns *= keep + (1.0 - keep) * spec.shrink;
     long long row = (long long)blockIdx.x * at_once * steps + sub;
-    double t = (double)(first + row) * turns, c, s, dc, ds;
+    double t = (double)(first + row) * turns, c, s, dc = 1.0, ds = 0.0;
     sincospi(2.0 * (t - rint(t)), &s, &c);
-    t = at_once * turns;
-    sincospi(2.0 * (t - rint(t)), &ds, &dc);
-    c *= magnitude;
-    s *= magnitude;
+    if (steps > 1) {
+        t = at_once * turns;
+        sincospi(2.0 * (t - rint(t)), &ds, &dc);
+    }
+    c *= spec.magnitude;
+    s *= spec.magnitude;
     for (int k = 0; k < steps && row < rows; ++k, row += at_once) {
         cos[row * half + i] = (float)c;
         sin[row * half + i] = (float)s;
@@ -479,11 +483,13 @@ constexpr int ONE_WORKGROUP = 48;
 // rows of `heads` heads that share a unit
 static int rows_of(int heads, const HeadShape &s) { return std::max(1, (64 >> s.gshift) / heads); }
 
+// Eight wavefronts a workgroup where the units are few, so that fewer partial sums are left; the first kernel in us with 2 | 4 | 8 | 16: 613 fp32 rows of 4 / 2
+// heads of 64 5.4 | 4.8 | 4.9 | 6.0, 128 rows of 32 / 8 heads of 128 6.6 | 6.6 | 6.0 | 7.3.
 static BackPlan plan_back(int T, int hq, int hkv, const HeadShape &s)
 {
     const auto units = [&](int heads) { return (T + rows_of(heads, s) - 1) / rows_of(heads, s) * (long long)units_of(heads, s); };
     const long long uq = units(hq), uk = units(hkv), all = uq + uk;
-    const int most = all <= ONE_WORKGROUP ? BACK_WAVES : (int)std::min<long long>(BACK_WAVES, std::max<long long>(2, all / 256));
+    const int most = all <= ONE_WORKGROUP ? BACK_WAVES : (int)std::min<long long>(BACK_WAVES, std::max<long long>(8, all / 256));
     BackPlan p = {0, 0, 0};
     if (T == 0) return p;
     double best = 0.0;
@@ -661,8 +667,12 @@ int alora_rope_tables(float *cos, float *sin, int64_t first, int64_t rows, const
     // 65536 rows 8.8 | 9.1 | 10.8, 131072 rows 13.3 | 13.2 | 13.2; two or four pairs a thread with wider stores: 6.4 to 22
     const int steps = (int)std::max<int64_t>(1, std::min<int64_t>(64, rows / ((int64_t)at_once * 512)));
     const int64_t groups = (rows + (int64_t)at_once * steps - 1) / ((int64_t)at_once * steps);
-    launch_kernel(rope_tables_kernel, dim3((unsigned)groups), dim3(256), 0, (hipStream_t)hip_stream, cos, sin, (long long)first, (long long)rows, half, steps,
-                  (int)s.scaling, std::log2(s.base), s.factor, s.original, s.low, s.high, s.magnitude);
+    TableSpec t = {-std::log2(s.base) / half, s.scaling == ALORA_ROPE_PLAIN ? 1.0 : 1.0 / s.factor, 0.0, 0.0, s.magnitude, s.scaling == ALORA_ROPE_BY_PARTS};
+    if (t.mix) {
+        t.slope = s.original / (s.high - s.low);
+        t.start = -s.low / (s.high - s.low);
+    }
+    launch_kernel(rope_tables_kernel, dim3((unsigned)groups), dim3(256), 0, (hipStream_t)hip_stream, cos, sin, (long long)first, (long long)rows, half, steps, t);
     const int e = launch_status();
     if (e) { note_hip_error(e); return ALORA_EHIP; }
     return ALORA_OK;
