@@ -77,7 +77,7 @@ __device__ __forceinline__ void norm_turn_store(const HeadsArgs &g, const LanePl
 // One workgroup per row: its slot and position are scalars, a lane's angles serve all its heads.  A wavefront takes U units at a time (their
 // loads are requested together), the units of queries and keys first, then the row of v in pieces of 2 KiB.  One pass: the mean
 // square is a sum over a lane's chunks and over the lanes of the head (DPP), after which the head is still in registers.  Bound by memory: 8192 rows of
-// 64 / 8 heads of 128 take 62 us (5.4 TB/s; a large copy reaches 5.2), with U = 2 74, 1 75, 4 74.  One row takes 3 us: launch and three dependent loads.
+// 64 / 8 heads of 128 take 60 us a pass (5.6 TB/s; a large copy reaches 5.2), with U = 2 76, 1 75, 4 74 (all measured before chunks were neighbours: 66 with 3).  One row takes 3 us: launch and three dependent loads.
 template <bool BF16, int V, bool INTERLEAVED, bool NORM, int U>
 __global__ __launch_bounds__(64 * HEADS_WAVES) void heads_kernel(HeadsArgs g)
 {
