@@ -107,8 +107,10 @@ typedef struct alora_rope_spec {
 
 /*
  * cos[p - first, i] = magnitude cos(p theta_i), sin likewise, for p = first .. first + rows - 1 and every pair i.
- * Angles are held in 64 bits: far positions are as exact as near ones (the fp32 result is within 0.55 units in the last
- * place of `magnitude`).  0 <= first, first + rows <= 2^24 (ALORA_ESHAPE).  cos, sin: fp32 [rows, rotary_dim / 2], 16-byte aligned.
+ * Angles are held in 64 bits: far positions are as exact as near ones.  A result is off by half a unit in its last place, and by what the angle
+ * loses in 64 bits, at most magnitude * position * 2^-50.  0 <= first, first + rows <= 2^24 (ALORA_ESHAPE).  cos, sin: fp32
+ * [rows, rotary_dim / 2], 16-byte aligned; with magnitude 1 they are tables for alora_cache_move_rows too, with rotary_dim = head_dim for
+ * alora_extras.rope_cos and rope_sin.
  */
 int alora_rope_tables(float *cos, float *sin, int64_t first, int64_t rows, const alora_rope_spec *spec, void *hip_stream);
 

@@ -77,7 +77,7 @@ __device__ __forceinline__ void norm_turn_store(const HeadsArgs &g, const LanePl
 // One workgroup per row: its slot and position are scalars, a lane's angles serve all its heads.  A wavefront takes U units at a time (their
 // loads are requested together), the units of queries and keys first, then the row of v in pieces of 2 KiB.  One pass: the mean
 // square is a sum over a lane's chunks and over the lanes of the head (DPP), after which the head is still in registers.  Bound by memory: 8192 rows of
-// 64 / 8 heads of 128 take 60 us a pass (5.6 TB/s; a large copy reaches 5.2), with U = 2 76, 1 75, 4 74 (all measured before chunks were neighbours: 66 with 3).  One row takes 3 us: launch and three dependent loads.
+// 64 / 8 heads of 128 take 60 us a pass (5.6 TB/s; a large copy reaches 5.2).  Weights loaded behind the sum instead of in front of it, which frees registers: 67.  One row takes 3 us: launch and three dependent loads.
 template <bool BF16, int V, bool INTERLEAVED, bool NORM, int U>
 __global__ __launch_bounds__(64 * HEADS_WAVES) void heads_kernel(HeadsArgs g)
 {
@@ -446,8 +446,10 @@ static int units_of(int heads, const HeadShape &s)
 static int launch_heads(HeadsArgs &g, bool bf16, int V, bool norm, hipStream_t st)
 {
     const int units = g.uq + g.uk, v_pieces = g.v ? (g.hkv * g.s.d * (bf16 ? 2 : 4) + 2047) / 2048 : 0;
-    // three units of a wavefront where the chip is full many times over, else one: more wavefronts have shorter chains of loads
-    const int U = (long long)g.T * units >= 8192 ? 3 : 1;
+    // Units of a wavefront: one where the chip is not full many times over (more wavefronts have shorter chains of loads), else three where
+    // that comes out even, else two.  us with two | three: 9 units, 8192 rows 71.8 | 61.6, 6 units, 4096 rows 27.2 | 25.4; 8 units, 4096 rows
+    // 40.3 | 43.6, 10 units 39.5 | 40.9, 5 units 18.9 | 19.1, 2048 rows 11.4 | 12.1.  Four: 67.4, 28.4, 49.6, 42.5, 20.7, 13.4.
+    const int U = (long long)g.T * units < 8192 ? 1 : units % 3 ? 2 : 3;
     const int per = 64 >> g.s.gshift;
     const auto items = [&](int at_once) { return (g.T + at_once - 1) / std::max(1, at_once); };
     g.items_q = items(per / g.hq);
@@ -468,8 +470,11 @@ static int launch_heads(HeadsArgs &g, bool bf16, int V, bool norm, hipStream_t s
             launch_kernel(kernel, dim3(std::min(g.T, ROWS_AT_ONCE), (g.T - 1) / ROWS_AT_ONCE + 1), dim3(64 * waves), 0, st, g);
             return launch_status();
         };
-        if (norm) return U == 3 ? go(heads_kernel<b.value, v.value, il.value, true, 3>) : go(heads_kernel<b.value, v.value, il.value, true, 1>);
-        return U == 3 ? go(heads_kernel<b.value, v.value, il.value, false, 3>) : go(heads_kernel<b.value, v.value, il.value, false, 1>);
+        const auto with = [&](auto n) {
+            return U == 3 ? go(heads_kernel<b.value, v.value, il.value, n.value, 3>)
+                          : U == 2 ? go(heads_kernel<b.value, v.value, il.value, n.value, 2>) : go(heads_kernel<b.value, v.value, il.value, n.value, 1>);
+        };
+        return norm ? with(std::true_type()) : with(std::false_type());
     });
 }
 

@@ -273,7 +273,8 @@ def test_launches_of_calls(tmp_path):
     assert one == [["heads_kernel", [1, 1, 1], [5 * 64, 1, 1]]]                 # four units of queries, one of keys
     # rows of 4 / 2 heads of 64 (16 heads a wavefront): 4 and 8 rows on one, 8 rows of values
     assert small == [["heads_packed_kernel", [-(-(25 + 13 + 13) // 4), 1, 1], [256, 1, 1]]]
-    assert many == [["heads_kernel", [1 << 20, 2, 1], [3 * 64, 1, 1]]] and full == [["heads_kernel", [2000, 1, 1], [3 * 64, 1, 1]]]
+    # three wavefronts of two units (the last of one) and one of values
+    assert many == [["heads_kernel", [1 << 20, 2, 1], [4 * 64, 1, 1]]] and full == [["heads_kernel", [2000, 1, 1], [4 * 64, 1, 1]]]
     few, back, plain = run(["record_backward", [dict(wide, n_tokens=9)]], ["record_backward", [dict(wide, n_tokens=4096)]], ["record_backward", [dict(n_tokens=0)]])
     assert [l[0] for l in few] == ["heads_back_kernel"] and few[0][1] == [1, 1, 1]
     assert [l[:2] for l in back] == [["heads_back_kernel", [256, 1, 1]], ["heads_weights_kernel", [16, 1, 1]]] and back[0][2] == [15 * 64, 1, 1]
