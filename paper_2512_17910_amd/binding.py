@@ -564,7 +564,10 @@ def make_cache_dims(k_caches: Sequence, v_caches: Sequence, n_kv_heads: int, hea
 def _host_int32(a, name: str) -> int:
     if a.dtype.char != "i" or a.ndim != 1 or (a.strides != (4,) and a.size > 1):
         raise ValueError(f"{name}: a contiguous int32 array on the host expected")
-    return a.__array_interface__["data"][0]
+    try:
+        return ctypes.addressof(ctypes.c_char.from_buffer(a))      # (a third of the time of asking numpy)
+    except (TypeError, ValueError):                                # read-only, or empty
+        return a.__array_interface__["data"][0]
 
 
 def alora_cache_copy_blocks(src, dst, dims: AloraCacheDims, stream=None) -> None:

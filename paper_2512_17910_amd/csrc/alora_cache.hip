@@ -10,22 +10,23 @@ namespace alora {
 // Addresses and block pairs go to the kernel with its arguments (at most 4 KiB of them): a copy needs no memory of its own on the device, and
 // the lists may be read before the call returns.
 constexpr int LAYERS_AT_ONCE = 64;
+template <int LAYERS>
 struct CacheTable {
-    char *p[2 * LAYERS_AT_ONCE];    // K and V of layer 0, K and V of layer 1, ...
+    char *p[2 * LAYERS];    // K and V of layer 0, K and V of layer 1, ...
 };
 template <int PAIRS>
 struct PairList {
     int32_t src[PAIRS], dst[PAIRS];
 };
 constexpr int PAIRS_FEW = 16, PAIRS_MANY = 352;
-static_assert(sizeof(CacheTable) + sizeof(PairList<PAIRS_MANY>) + 16 <= 4096, "kernel arguments");
+static_assert(sizeof(CacheTable<LAYERS_AT_ONCE>) + sizeof(PairList<PAIRS_MANY>) + 16 <= 4096, "kernel arguments");
 
 // One workgroup per piece of 4 KiB of a block, pair and cache; all pairs of a cache before the next cache.  Bound by memory: each byte is
 // read and written once, past the caches, since nothing reads it soon.  1000 blocks of 32 KiB in 16 caches, us: 200 (5.2 TB/s, what a
 // large copy reaches), with ordinary loads and stores 4 to 8 % more, with the caches of a pair behind each other 3 % more; 724 blocks of 8 KiB in 16
 // caches 39.5.  Pieces of 8, 16, 32 KiB: 204, 205, 204 and 41.5, 45.3, 45.3.  One block in 64 caches takes 2.6 us: a launch.
-template <int PAIRS>
-__global__ __launch_bounds__(256) void copy_blocks_kernel(CacheTable caches, PairList<PAIRS> pairs, long long block_bytes)
+template <int LAYERS, int PAIRS>
+__global__ __launch_bounds__(256) void copy_blocks_kernel(CacheTable<LAYERS> caches, PairList<PAIRS> pairs, long long block_bytes)
 {
     char *cache = caches.p[blockIdx.z];
     const int src = pairs.src[blockIdx.y], dst = pairs.dst[blockIdx.y];
@@ -44,7 +45,6 @@ struct RowSplit {
 };
 
 struct MoveArgs {
-    CacheTable caches;
     const int64_t *src, *dst;
     const int32_t *shift;       // or null
     const float *cos, *sin;
@@ -151,11 +151,11 @@ __device__ __forceinline__ void move_copies(const MoveArgs &g, char *cache, int 
 }
 
 // One wavefront per item of a layer's K or V cache; gridDim.y counts the caches.
-template <bool BF16, int V, bool INTERLEAVED>
-__global__ __launch_bounds__(64 * MOVE_WAVES) void move_rows_kernel(MoveArgs g)
+template <int LAYERS, bool BF16, int V, bool INTERLEAVED>
+__global__ __launch_bounds__(64 * MOVE_WAVES) void move_rows_kernel(CacheTable<LAYERS> caches, MoveArgs g)
 {
     const int item = blockIdx.x * MOVE_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    char *cache = g.caches.p[blockIdx.y];
+    char *cache = caches.p[blockIdx.y];
     if (g.shift && !(blockIdx.y & 1)) move_keys<BF16, V, INTERLEAVED>(g, cache, item, lane);
     else move_copies(g, cache, item, lane);
 }
@@ -181,14 +181,24 @@ static int check_pointers(const alora_cache_dims *d)
     return ALORA_OK;
 }
 
-static CacheTable table_of(const alora_cache_dims *d, int first, int n)
+// f(table, number of its layers) for every LAYERS_AT_ONCE layers, with a table of 8, 32 or 64: arguments are written across the bus, and cost
+// 0.3 us for every 512 bytes (one block in 64 caches, the pass: 5.6 us with a table of 64 layers, 5.3 with one of 32).
+template <typename F>
+static void for_layers(const alora_cache_dims *d, F f)
 {
-    CacheTable t;
-    for (int l = 0; l < LAYERS_AT_ONCE; ++l) {
-        t.p[2 * l] = (char *)(l < n ? d->k_caches[first + l] : nullptr);
-        t.p[2 * l + 1] = (char *)(l < n ? d->v_caches[first + l] : nullptr);
+    const auto with = [&](auto table, int first, int n) {
+        for (int l = 0; l < n; ++l) {
+            table.p[2 * l] = (char *)d->k_caches[first + l];
+            table.p[2 * l + 1] = (char *)d->v_caches[first + l];
+        }
+        f(table, n);
+    };
+    for (int first = 0; first < d->n_layers; first += LAYERS_AT_ONCE) {
+        const int n = std::min(LAYERS_AT_ONCE, d->n_layers - first);
+        if (n <= 8) with(CacheTable<8>(), first, n);
+        else if (n <= 32) with(CacheTable<32>(), first, n);
+        else with(CacheTable<LAYERS_AT_ONCE>(), first, n);
     }
-    return t;
 }
 
 static long long row_bytes_of(const alora_cache_dims *d) { return (long long)d->n_kv_heads * d->head_dim * (d->dtype == ALORA_BF16 ? 2 : 4); }
@@ -228,15 +238,15 @@ static int check_pairs(const int32_t *src, const int32_t *dst, int n, long long 
     return ALORA_OK;
 }
 
-template <int PAIRS>
-static void launch_copies(const CacheTable &caches, int n_caches, const int32_t *src, const int32_t *dst, int n, long long block_bytes, hipStream_t st)
+template <int PAIRS, int LAYERS>
+static void launch_copies(const CacheTable<LAYERS> &caches, int n_caches, const int32_t *src, const int32_t *dst, int n, long long block_bytes, hipStream_t st)
 {
     for (int i = 0; i < n; i += PAIRS) {
         const int m = std::min(PAIRS, n - i);
         PairList<PAIRS> list;
         std::copy(src + i, src + i + m, list.src);
         std::copy(dst + i, dst + i + m, list.dst);
-        launch_kernel(copy_blocks_kernel<PAIRS>, dim3((unsigned)((block_bytes + 4095) / 4096), m, n_caches), dim3(256), 0, st, caches, list, block_bytes);
+        launch_kernel(copy_blocks_kernel<LAYERS, PAIRS>, dim3((unsigned)((block_bytes + 4095) / 4096), m, n_caches), dim3(256), 0, st, caches, list, block_bytes);
     }
 }
 
@@ -256,12 +266,10 @@ int alora_cache_copy_blocks(const int32_t *src, const int32_t *dst, int32_t n, c
     if (!st) st = check_pairs(src, dst, n, dims->n_slots / dims->block_size);
     if (st) return st;
     const long long block_bytes = row_bytes_of(dims) * dims->block_size;
-    for (int l = 0; l < dims->n_layers; l += LAYERS_AT_ONCE) {
-        const int layers = std::min(LAYERS_AT_ONCE, dims->n_layers - l);
-        const CacheTable caches = table_of(dims, l, layers);
+    for_layers(dims, [&](const auto &caches, int layers) {
         if (n <= PAIRS_FEW) launch_copies<PAIRS_FEW>(caches, 2 * layers, src, dst, n, block_bytes, (hipStream_t)hip_stream);
         else launch_copies<PAIRS_MANY>(caches, 2 * layers, src, dst, n, block_bytes, (hipStream_t)hip_stream);
-    }
+    });
     const int e = launch_status();
     if (e) { note_hip_error(e); return ALORA_EHIP; }
     return ALORA_OK;
@@ -296,16 +304,15 @@ int alora_cache_move_rows(const int64_t *src, const int64_t *dst, const int32_t 
     g.v = split(g.pieces, 128);
     const auto items = [&](const RowSplit &x) { return ((long long)n_rows + x.rows - 1) / x.rows * x.units; };
     const long long groups = (std::max(items(g.v), shift ? items(g.k) : 0) + MOVE_WAVES - 1) / MOVE_WAVES;
-    for (int l = 0; l < dims->n_layers; l += LAYERS_AT_ONCE) {
-        const int layers = std::min(LAYERS_AT_ONCE, dims->n_layers - l);
-        g.caches = table_of(dims, l, layers);
-        const auto go = [&](auto kernel) { launch_kernel(kernel, dim3((unsigned)groups, 2 * layers), dim3(64 * MOVE_WAVES), 0, (hipStream_t)hip_stream, g); };
-        if (bf16 && V == 8) interleaved ? go(move_rows_kernel<true, 8, true>) : go(move_rows_kernel<true, 8, false>);
-        else if (bf16 && V == 4) interleaved ? go(move_rows_kernel<true, 4, true>) : go(move_rows_kernel<true, 4, false>);
-        else if (bf16) go(move_rows_kernel<true, 2, false>);
-        else if (V == 4) interleaved ? go(move_rows_kernel<false, 4, true>) : go(move_rows_kernel<false, 4, false>);
-        else go(move_rows_kernel<false, 2, false>);
-    }
+    for_layers(dims, [&](const auto &caches, int layers) {
+        constexpr int L = sizeof(caches) / (2 * sizeof(char *));
+        const auto go = [&](auto kernel) { launch_kernel(kernel, dim3((unsigned)groups, 2 * layers), dim3(64 * MOVE_WAVES), 0, (hipStream_t)hip_stream, caches, g); };
+        if (bf16 && V == 8) interleaved ? go(move_rows_kernel<L, true, 8, true>) : go(move_rows_kernel<L, true, 8, false>);
+        else if (bf16 && V == 4) interleaved ? go(move_rows_kernel<L, true, 4, true>) : go(move_rows_kernel<L, true, 4, false>);
+        else if (bf16) go(move_rows_kernel<L, true, 2, false>);
+        else if (V == 4) interleaved ? go(move_rows_kernel<L, false, 4, true>) : go(move_rows_kernel<L, false, 4, false>);
+        else go(move_rows_kernel<L, false, 2, false>);
+    });
     const int e = launch_status();
     if (e) { note_hip_error(e); return ALORA_EHIP; }
     return ALORA_OK;

@@ -195,6 +195,8 @@ def test_binding_refuses_what_it_would_misread():
     with pytest.raises(ValueError):
         ab.alora_cache_copy_blocks(some[::2], some[:2], dims)
     ab._host_int32(some[:0], "src"), ab._host_int32(np.zeros(0, np.int32), "src")      # (an empty array's strides say nothing)
+    some.flags.writeable = False
+    assert ab._host_int32(some, "src") == some.ctypes.data and ab._host_int32(some[1:].copy(), "src") != some.ctypes.data
     for bad in (lambda: ab.alora_qk_norm_rope(q, q, None, k, None, None, None, None, rope, torch.zeros(4).long(), torch.zeros(4).long(), ok),
                 lambda: ab.alora_qk_norm_rope(q, q, None, k, None, None, None, None, rope, torch.zeros(4).int(), torch.zeros(4).int(), ok),
                 lambda: ab.alora_qk_norm_rope_backward(q, q, q, k[:4], k[:4], k[:4], None, None, None, None, rope, torch.zeros(4).long(),
