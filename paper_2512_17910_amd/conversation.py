@@ -135,6 +135,7 @@ def run(layers=4, prompt=1000, dtype="bf16", block_size=16, rotary_dim=128, inte
             p.commit(r)
         return y
 
+    admit(9, tok(5 * block_size + 1))         # another request, over before the pool is made smaller
     admit(1, tok(prompt))
     for _ in range(3):
         answer([1], [tok(1)])
@@ -163,6 +164,7 @@ def run(layers=4, prompt=1000, dtype="bf16", block_size=16, rotary_dim=128, inte
     res["drop_key_off"], res["drop_value_off"] = _off(k, k_new), _off(v, v_new)
     answer([1], [tok(2)])
     # -- the pool is made smaller
+    p.finish(9)
     probe = tok(1)
 
     def look():
