@@ -19,6 +19,9 @@
  *   - block b (positions [b*bs, (b+1)*bs)) carries the adapter id iff adapter_id >= 0 and
  *     (b+1)*bs > activation_start.  Base request: adapter_id = -1.  Standard LoRA:
  *     activation_start = 0.  An aLoRA that is never activated: activation_start >= n_tokens.
+ *   - with the id goes the place in the block from which the adapter is active, max(0, activation_start - b*bs):
+ *     requests with the same tokens and adapter whose activation points differ share the blocks in front of the
+ *     earlier one only (their K/V differ from there on), while requests with one activation point share them all;
  *   - at least one token of an admitted request is always projected: at most
  *     floor((n_tokens-1)/bs) leading blocks are taken from the cache;
  *   - a block becomes reusable at alora_planner_commit (its K/V have been computed), not when it

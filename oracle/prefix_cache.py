@@ -24,6 +24,11 @@ Readings where the paper is silent:
   - a block "holds tokens processed with the adapter" iff it contains a position >= activation_start,
     i.e. (b+1)*block_size > activation_start; a standard LoRA is activation_start = 0, a base request
     has adapter -1 (no block ever carries an id);
+  - beside the adapter id stands the place in the block from which the adapter is active (0: the whole
+    block).  The paper names the id alone, which is enough where the tokens say where the adapter is invoked; but
+    nothing makes the caller's activation points follow from the tokens, and two requests of the same tokens and
+    adapter that are activated at different places of a block have different contents there.  `place = False`
+    is the letter of the paper, for the pin of that reading;
   - at least one token of every admitted request is projected: the reusable prefix is capped at
     floor((n-1)/block_size) blocks;
   - blocks become reusable when the caller says their contents have been computed (commit), not
@@ -60,6 +65,8 @@ class _Req:
 
 
 class PrefixCacheOracle:
+    place = True        # identities hold the place of activation
+
     def __init__(self, block_size: int, n_blocks: int):
         assert block_size > 0 and n_blocks >= 0
         self.bs = block_size
@@ -73,8 +80,8 @@ class PrefixCacheOracle:
     # -- identities ---------------------------------------------------------------------
     def _extra(self, adapter: int, start: int, b: int):
         """Sec. 3 item (3) with the Fig. 1 rule: the adapter id only for blocks that hold a position
-        at or after the activation point."""
-        return adapter if (adapter >= 0 and (b + 1) * self.bs > start) else None
+        at or after the activation point, and with it the place from which it is active."""
+        return (adapter, max(0, start - b * self.bs) if self.place else 0) if (adapter >= 0 and (b + 1) * self.bs > start) else None
 
     def keys(self, tokens: Sequence[int], adapter: int, start: int) -> List[tuple]:
         out, parent = [], None

@@ -4,6 +4,8 @@
 // the hash of the block before it, and an extra identifier (the adapter id, or nothing for the
 // base model).  Fig. 1 caption: for a request that invokes an aLoRA the adapter id is hashed only
 // into blocks holding tokens at or after the activation point, and partial blocks are not cached.
+// With the id goes the place in the block from which the adapter is active: the same tokens projected
+// with the adapter from another place on are other contents.
 // The planner finds the longest cached prefix of a request, allocates blocks for the remainder and
 // emits the rows the projection still has to compute (positions, segment ids, adapter ids, slots).
 //
@@ -32,12 +34,13 @@ inline uint64_t mix64(uint64_t z)
 constexpr uint64_t ROOT_HASH = 0x9e3779b97f4a7c15ull;   // "hash of the block before block 0"
 constexpr uint64_t NO_EXTRA = 0x5851f42d4c957f2dull;    // extra identifier of a base-model block
 
-// Sec. 3 items (1)-(3): tokens of the block, hash of the previous block, extra identifier.
-uint64_t block_hash(uint64_t parent, const int32_t *tok, int bs, bool with_adapter, int32_t adapter)
+// Sec. 3 items (1)-(3): tokens of the block, hash of the previous block, extra identifier (of a block with an adapter: its id, and from which
+// place in the block on it is active, 0 for all of it).
+uint64_t block_hash(uint64_t parent, const int32_t *tok, int bs, bool with_adapter, int32_t adapter, uint32_t place)
 {
     uint64_t h = mix64(parent ^ 0xd6e8feb86659fd93ull);
     for (int i = 0; i < bs; ++i) h = mix64(h ^ (uint64_t)(uint32_t)tok[i] ^ ((uint64_t)(i + 1) << 32));
-    const uint64_t extra = with_adapter ? mix64(0xa24baed4963ee407ull + (uint64_t)(uint32_t)adapter) : NO_EXTRA;
+    const uint64_t extra = with_adapter ? mix64(0xa24baed4963ee407ull + ((uint64_t)place << 32 | (uint32_t)adapter)) : NO_EXTRA;
     return mix64(h ^ extra);
 }
 
@@ -106,7 +109,8 @@ struct alora_planner {
         const int64_t nfull = std::min<int64_t>((int64_t)r.tokens.size() / bs, r.exact);
         for (int64_t b = (int64_t)r.hashes.size(); b < nfull; ++b) {
             const uint64_t parent = b ? r.hashes[b - 1] : ROOT_HASH;
-            r.hashes.push_back(block_hash(parent, r.tokens.data() + b * bs, bs, with_adapter(r, b), r.adapter));
+            const uint32_t place = (uint32_t)std::max<int64_t>(0, r.start - b * bs);     // (below bs where the adapter enters)
+            r.hashes.push_back(block_hash(parent, r.tokens.data() + b * bs, bs, with_adapter(r, b), r.adapter, place));
         }
     }
 };

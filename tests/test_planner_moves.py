@@ -306,6 +306,24 @@ def test_random_conversations(seed):
     s.close()
 
 
+@pytest.mark.parametrize("seed", [59, 272, 402, 419])
+def test_random_conversations_whose_activation_points_share_a_block(seed):
+    test_random_conversations(seed)
+
+
+def test_a_fork_is_not_found_by_a_request_activated_elsewhere():
+    s = Sim(4, 20)
+    s.admit(1, list(range(10)), -1, NEVER)
+    s.fork(1, 2, 0, 10)
+    s.append(2, [10, 11, 12])
+    s.commit(2)
+    assert s.admit(3, list(range(13)), 0, 9) == 8        # position 9 of request 2 was projected by the base model
+    s.check()
+    assert s.admit(4, list(range(13)), 0, 10) == 12
+    s.check()
+    s.close()
+
+
 def test_under_address_and_undefined_behaviour_sanitizers(tmp_path):
     """The tests above on a build of the planner's host code with CPU sanitizers."""
     so = str(tmp_path / "planner_san.so")

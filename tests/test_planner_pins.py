@@ -296,6 +296,54 @@ def test_oracle_reuse_length_equals_the_flat_definition():
             committed.append((t, ad, st))
 
 
+@face
+def test_activation_points_inside_a_block_are_told_apart(Face):
+    """The same tokens and adapter, active from another place of a block on, have other K/V in that block and behind it."""
+    bs, t = 4, list(range(50, 66))
+    c = Face(bs, 64)
+    c.admit(1, t, 0, 10)
+    c.commit(1)
+    assert c.admit(2, t + [1], 0, 10)[0] == 16
+    for rid, start in ((3, 9), (4, 11), (5, 8), (6, 12)):
+        assert c.admit(rid, t + [1], 0, start)[0] == 8, start
+    c.commit(5)                                  # active from the border on: the whole block, as from inside the block before
+    assert c.admit(7, t + [1], 0, 8)[0] == 16 and c.admit(8, t + [1], 0, 7)[0] == 4
+    assert c.admit(9, t + [1], -1, NEVER)[0] == 8
+
+
+def _brute_cached_with_places(committed, tokens, adapter, start, bs):
+    """A block is interchangeable iff the tokens up to its end agree and the adapter was active at the same positions of them."""
+    active = lambda ad, st, n: [ad if (ad >= 0 and p >= st) else None for p in range(n)]
+    best = 0
+    for ct, ca, cs in committed:
+        k = 0
+        while (k + 1) * bs <= min(len(ct), len(tokens)) and ct[: (k + 1) * bs] == tokens[: (k + 1) * bs] and \
+                active(ca, cs, (k + 1) * bs) == active(adapter, start, (k + 1) * bs):
+            k += 1
+        best = max(best, k)
+    return min(best, (len(tokens) - 1) // bs) * bs
+
+
+@pytest.mark.parametrize("bs", [1, 3, 4])
+@face
+def test_reuse_length_equals_the_flat_definition_with_places(Face, bs):
+    rng = np.random.default_rng(70 + bs)
+    for trial in range(60):
+        c = Face(bs, 1000)                      # never evicts
+        committed = []
+        base = _toks(rng, 30, vocab=3)
+        for rid in range(12):
+            n = int(rng.integers(1, 30))
+            t = list(base[:n])
+            if rng.random() < 0.3:              # perturb one token
+                t[int(rng.integers(0, n))] = int(rng.integers(0, 3))
+            ad = int(rng.integers(-1, 2))
+            st = int(rng.integers(0, 32))
+            assert c.admit(rid, t, ad, st)[0] == _brute_cached_with_places(committed, t, ad, st, bs), (trial, rid)
+            c.commit(rid)
+            committed.append((t, ad, st))
+
+
 def _check_invariants(o: PrefixCacheOracle):
     n = len(o.ref)
     assert sorted(o.free) == [b for b in range(n) if o.ref[b] == 0]
