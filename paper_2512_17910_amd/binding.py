@@ -452,6 +452,32 @@ def _check_rope(rope) -> None:
         raise ValueError("rope: two contiguous fp32 tensors [positions, rotary_dim / 2] expected")
 
 
+_types = None
+
+
+def _torch_types():
+    """(types by the library's codes, int32, int64)"""
+    global _types
+    import torch
+    _types = ((torch.float32, torch.bfloat16), torch.int32, torch.int64)
+    return _types
+
+
+# What a call takes beside the tensors that its dims describe is looked at in every call: a type, size or stride that the kernels do not
+# expect would be misread in silence, or read behind its end.
+def _refuse(name: str, t, dtype, n: int) -> None:
+    if t.dtype is not dtype:
+        raise TypeError(f"{name}: {dtype} expected, got {t.dtype}")
+    raise ValueError(f"{name}: {n} contiguous elements expected, got {tuple(t.shape)} with strides {t.stride()}")
+
+
+def _check_weights(name_q: str, wq, name_k: str, wk, dtype, d: int) -> None:
+    if wq.dtype is not dtype or wq.numel() != d or not wq.is_contiguous():
+        _refuse(name_q, wq, dtype, d)
+    if wk.dtype is not dtype or wk.numel() != d or not wk.is_contiguous():
+        _refuse(name_k, wk, dtype, d)
+
+
 def make_heads_dims(q, q_out, k, k_out, n_q_heads: int, n_kv_heads: int, head_dim: int, rope=None, interleaved: bool = False,
                     norm: bool = True, eps: float = 1e-6, v=None, v_out=None, dq=None, dk=None) -> AloraHeadsDims:
     """Description of alora_qk_norm_rope calls on these tensors, or on others of the same shapes and strides: q, q_out, k, v
@@ -478,10 +504,12 @@ def make_heads_dims(q, q_out, k, k_out, n_q_heads: int, n_kv_heads: int, head_di
 def alora_qk_norm_rope(q, q_out, k, k_cache, v, v_cache, wq, wk, rope, token_positions, slot_mapping, dims: AloraHeadsDims,
                        stream=None) -> None:
     """Enqueue norm and rotary embedding of the rows' heads (include/alora_heads.h): q to q_out, k (None: in place) to its slots of k_cache,
-    v, where given, to v_cache.  The tensors are those that dims was made from, or of the same shapes and strides; wq and wk are None
-    without norm, rope without rotation."""
+    v, where given, to v_cache.  The tensors are those that dims was made from, or of the same shapes and strides; wq and wk, of their
+    type, are None without norm, rope without rotation."""
     if slot_mapping.element_size() != 8 or (token_positions is not None and token_positions.element_size() != 4):
         raise TypeError("token_positions: int32, slot_mapping: int64 expected")
+    if wq is not None and wk is not None:
+        _check_weights("wq", wq, "wk", wk, (_types or _torch_types())[0][dims.dtype], dims.head_dim)
     cos, sin = (None, None) if rope is None else rope
     s = (_lib or lib()).alora_qk_norm_rope(q.data_ptr(), q_out.data_ptr(), None if k is None else k.data_ptr(), k_cache.data_ptr(),
                                            None if v is None else v.data_ptr(), None if v_cache is None else v_cache.data_ptr(),
@@ -507,8 +535,13 @@ def alora_qk_norm_rope_backward(q, dq_out, dq, k, dk_out, dk, wq, wk, dwq, dwk, 
     """Enqueue the backward pass of alora_qk_norm_rope: dq, dk and, with norm, the fp32 dwq, dwk from the gradients of its outputs."""
     if dims.n_tokens > 1 and (dq.stride(0) != (dims.dq_stride or dims.q_stride) or dk.stride(0) != (dims.dk_stride or dims.k_stride)):
         raise ValueError("dq, dk: strides other than those of dims (make_heads_dims takes dq and dk)")
-    if (token_positions is not None and token_positions.element_size() != 4) or (dwq is not None and (dwq.element_size() != 4 or dwk.element_size() != 4)):
-        raise TypeError("token_positions: int32, dwq and dwk: fp32 expected")
+    if token_positions is not None and token_positions.element_size() != 4:
+        raise TypeError("token_positions: int32 expected")
+    by_code = (_types or _torch_types())[0]
+    if wq is not None and wk is not None:
+        _check_weights("wq", wq, "wk", wk, by_code[dims.dtype], dims.head_dim)
+    if dwq is not None and dwk is not None:
+        _check_weights("dwq", dwq, "dwk", dwk, by_code[ALORA_F32], dims.head_dim)
     cos, sin = (None, None) if rope is None else rope
     s = (_lib or lib()).alora_qk_norm_rope_backward(
         q.data_ptr(), dq_out.data_ptr(), dq.data_ptr(), k.data_ptr(), dk_out.data_ptr(), dk.data_ptr(), None if wq is None else wq.data_ptr(),

@@ -210,6 +210,46 @@ def test_binding_refuses_what_it_would_misread():
     assert one.q_stride >= 128
 
 
+# ---- tensors of a call that its description does not know: refused in the binding, where they would be misread ---------------------------
+def heads_call(dtype=None, back=False, **kw):
+    """A call of 4 rows, 4 / 2 heads of 32, all right but for what kw says (on the CPU: what is right is refused last, as no device tensor)."""
+    dtype = dtype or torch.bfloat16
+    q, k = torch.zeros(4, 128, dtype=dtype), torch.zeros(32, 64, dtype=dtype)
+    rope = (torch.zeros(10, 16), torch.zeros(10, 16))
+    a = dict(wq=torch.ones(32, dtype=dtype), wk=torch.ones(32, dtype=dtype), rope=rope, pos=torch.zeros(4, dtype=torch.int32), slot=torch.arange(4),
+             dwq=torch.zeros(32), dwk=torch.zeros(32))
+    a.update(kw)
+    if back:
+        dims = ab.make_heads_dims(q, q, k[:4], k[:4], 4, 2, 32, rope=rope)
+        ab.alora_qk_norm_rope_backward(q, q, q, k[:4], k[:4], k[:4], a["wq"], a["wk"], a["dwq"], a["dwk"], a["rope"], a["pos"], dims)
+    else:
+        ab.alora_qk_norm_rope(q, q, None, k, None, None, a["wq"], a["wk"], a["rope"], a["pos"], a["slot"], ab.make_heads_dims(q, q, None, k, 4, 2, 32, rope=rope))
+
+
+@pytest.mark.parametrize("back", [False, True])
+def test_norm_weights_of_another_type_or_size_are_refused(back):
+    bf, f = torch.bfloat16, torch.float32
+    for dtype, w in ((bf, torch.ones(32)), (f, torch.ones(32, dtype=bf)), (bf, torch.ones(32, dtype=torch.float16)), (f, torch.ones(32).double()),
+                     (bf, torch.ones(16))):
+        for name in ("wq", "wk"):
+            with pytest.raises(TypeError, match=name):
+                heads_call(dtype, back, **{name: w})
+    for dtype, w in ((bf, torch.ones(16, dtype=bf)), (f, torch.ones(31)), (f, torch.ones(64)[::2]), (f, torch.ones(1).expand(32)), (f, torch.ones(128))):
+        for name in ("wq", "wk"):
+            with pytest.raises(ValueError, match=name):
+                heads_call(dtype, back, **{name: w})
+
+
+def test_gradients_of_norm_weights_of_another_type_or_size_are_refused():
+    for name in ("dwq", "dwk"):
+        for w in (torch.zeros(32, dtype=torch.int32), torch.zeros(32, dtype=torch.bfloat16), torch.zeros(32).double()):
+            with pytest.raises(TypeError, match=name):
+                heads_call(back=True, **{name: w})
+        for w in (torch.zeros(31), torch.zeros(64)[::2], torch.zeros(8)):
+            with pytest.raises(ValueError, match=name):
+                heads_call(back=True, **{name: w})
+
+
 # ---- launches, recorded without a GPU (see launch_recorder.c) -------------------------------------
 RECORD = """
 import ctypes, json, re, sys, types
