@@ -471,6 +471,12 @@ def _refuse(name: str, t, dtype, n: int) -> None:
     raise ValueError(f"{name}: {n} contiguous elements expected, got {tuple(t.shape)} with strides {t.stride()}")
 
 
+def _check_rows(name: str, t, dtype, n: int) -> None:
+    """One dense number a row; more than the call has rows are not read."""
+    if t.dtype is not dtype or t.numel() < n or not t.is_contiguous():
+        _refuse(name, t, dtype, n)
+
+
 def _check_weights(name_q: str, wq, name_k: str, wk, dtype, d: int) -> None:
     if wq.dtype is not dtype or wq.numel() != d or not wq.is_contiguous():
         _refuse(name_q, wq, dtype, d)
@@ -506,10 +512,13 @@ def alora_qk_norm_rope(q, q_out, k, k_cache, v, v_cache, wq, wk, rope, token_pos
     """Enqueue norm and rotary embedding of the rows' heads (include/alora_heads.h): q to q_out, k (None: in place) to its slots of k_cache,
     v, where given, to v_cache.  The tensors are those that dims was made from, or of the same shapes and strides; wq and wk, of their
     type, are None without norm, rope without rotation."""
-    if slot_mapping.element_size() != 8 or (token_positions is not None and token_positions.element_size() != 4):
-        raise TypeError("token_positions: int32, slot_mapping: int64 expected")
+    by_code, i32, i64 = _types or _torch_types()
+    n = dims.n_tokens
+    _check_rows("slot_mapping", slot_mapping, i64, n)
+    if token_positions is not None:
+        _check_rows("token_positions", token_positions, i32, n)
     if wq is not None and wk is not None:
-        _check_weights("wq", wq, "wk", wk, (_types or _torch_types())[0][dims.dtype], dims.head_dim)
+        _check_weights("wq", wq, "wk", wk, by_code[dims.dtype], dims.head_dim)
     cos, sin = (None, None) if rope is None else rope
     s = (_lib or lib()).alora_qk_norm_rope(q.data_ptr(), q_out.data_ptr(), None if k is None else k.data_ptr(), k_cache.data_ptr(),
                                            None if v is None else v.data_ptr(), None if v_cache is None else v_cache.data_ptr(),
@@ -535,9 +544,9 @@ def alora_qk_norm_rope_backward(q, dq_out, dq, k, dk_out, dk, wq, wk, dwq, dwk, 
     """Enqueue the backward pass of alora_qk_norm_rope: dq, dk and, with norm, the fp32 dwq, dwk from the gradients of its outputs."""
     if dims.n_tokens > 1 and (dq.stride(0) != (dims.dq_stride or dims.q_stride) or dk.stride(0) != (dims.dk_stride or dims.k_stride)):
         raise ValueError("dq, dk: strides other than those of dims (make_heads_dims takes dq and dk)")
-    if token_positions is not None and token_positions.element_size() != 4:
-        raise TypeError("token_positions: int32 expected")
-    by_code = (_types or _torch_types())[0]
+    by_code, i32, _ = _types or _torch_types()
+    if token_positions is not None:
+        _check_rows("token_positions", token_positions, i32, dims.n_tokens)
     if wq is not None and wk is not None:
         _check_weights("wq", wq, "wk", wk, by_code[dims.dtype], dims.head_dim)
     if dwq is not None and dwk is not None:
@@ -554,6 +563,10 @@ def alora_qk_norm_rope_backward(q, dq_out, dq, k, dk_out, dk, wq, wk, dwq, dwk, 
 
 
 def alora_qk_norm_rope_validate(token_positions, slot_mapping, dims: AloraHeadsDims) -> int:
+    _, i32, i64 = _types or _torch_types()
+    for name, t, dtype in (("token_positions", token_positions, i32), ("slot_mapping", slot_mapping, i64)):
+        if t is not None:
+            _check_rows(name, t, dtype, dims.n_tokens)
     return int(lib().alora_qk_norm_rope_validate(_ptr(token_positions), _ptr(slot_mapping), ctypes.byref(dims)))
 
 

@@ -250,6 +250,22 @@ def test_gradients_of_norm_weights_of_another_type_or_size_are_refused():
                 heads_call(back=True, **{name: w})
 
 
+@pytest.mark.parametrize("back", [False, True])
+def test_positions_and_slots_that_are_not_dense_integers_of_every_row_are_refused(back):
+    i32, i64 = torch.int32, torch.int64
+    for name, kinds in (("token_positions", (torch.float32, torch.uint8, i64)), ("slot_mapping", (torch.float64, i32))):
+        key = dict(token_positions="pos", slot_mapping="slot")[name]
+        if back and key == "slot":
+            continue
+        for kind in kinds:
+            with pytest.raises(TypeError, match=name):
+                heads_call(back=back, **{key: torch.zeros(4, dtype=kind)})
+        right = i32 if key == "pos" else i64
+        for t in (torch.zeros(8, dtype=right)[::2], torch.zeros(3, dtype=right), torch.zeros(1, dtype=right).expand(4)):
+            with pytest.raises(ValueError, match=name):
+                heads_call(back=back, **{key: t})
+
+
 # ---- launches, recorded without a GPU (see launch_recorder.c) -------------------------------------
 RECORD = """
 import ctypes, json, re, sys, types
