@@ -445,11 +445,20 @@ def _rows_stride(t, name: str, width: int) -> int:
     return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), width)
 
 
-def _check_rope(rope) -> None:
-    import torch
+def _check_rope(rope):
+    """(positions, pairs) of tables."""
     cos, sin = rope
-    if cos.dim() != 2 or cos.shape != sin.shape or cos.dtype != torch.float32 or sin.dtype != torch.float32 or not (cos.is_contiguous() and sin.is_contiguous()):
+    f32, shape = (_types or _torch_types())[0][ALORA_F32], cos.shape
+    if cos.dtype is not f32 or sin.dtype is not f32 or len(shape) != 2 or sin.shape != shape or not (cos.is_contiguous() and sin.is_contiguous()):
         raise ValueError("rope: two contiguous fp32 tensors [positions, rotary_dim / 2] expected")
+    return shape
+
+
+def _check_rope_of(rope, dims):
+    """The tables that dims was made for, or longer ones."""
+    positions, pairs = _check_rope(rope)
+    if positions < dims.rope_positions or 2 * pairs != dims.rotary_dim:
+        raise ValueError(f"rope: tables of {dims.rope_positions} positions and {dims.rotary_dim // 2} pairs expected, got {positions} and {pairs}")
 
 
 _types = None
@@ -519,6 +528,8 @@ def alora_qk_norm_rope(q, q_out, k, k_cache, v, v_cache, wq, wk, rope, token_pos
         _check_rows("token_positions", token_positions, i32, n)
     if wq is not None and wk is not None:
         _check_weights("wq", wq, "wk", wk, by_code[dims.dtype], dims.head_dim)
+    if rope is not None:
+        _check_rope_of(rope, dims)
     cos, sin = (None, None) if rope is None else rope
     s = (_lib or lib()).alora_qk_norm_rope(q.data_ptr(), q_out.data_ptr(), None if k is None else k.data_ptr(), k_cache.data_ptr(),
                                            None if v is None else v.data_ptr(), None if v_cache is None else v_cache.data_ptr(),
@@ -551,6 +562,8 @@ def alora_qk_norm_rope_backward(q, dq_out, dq, k, dk_out, dk, wq, wk, dwq, dwk, 
         _check_weights("wq", wq, "wk", wk, by_code[dims.dtype], dims.head_dim)
     if dwq is not None and dwk is not None:
         _check_weights("dwq", dwq, "dwk", dwk, by_code[ALORA_F32], dims.head_dim)
+    if rope is not None:
+        _check_rope_of(rope, dims)
     cos, sin = (None, None) if rope is None else rope
     s = (_lib or lib()).alora_qk_norm_rope_backward(
         q.data_ptr(), dq_out.data_ptr(), dq.data_ptr(), k.data_ptr(), dk_out.data_ptr(), dk.data_ptr(), None if wq is None else wq.data_ptr(),
@@ -633,8 +646,13 @@ def alora_cache_move_rows(src, dst, shift, rope, dims: AloraCacheDims, interleav
         raise ValueError("src, dst, shift: one length expected")
     if src.element_size() != 8 or dst.element_size() != 8 or (shift is not None and shift.element_size() != 4) or not (src.is_contiguous() and dst.is_contiguous()):
         raise TypeError("src, dst: contiguous int64, shift: int32 expected")
-    cos, sin, positions, rot = (None, None, 0, 0) if rope is None else (rope[0].data_ptr(), rope[1].data_ptr(), rope[0].shape[0], 2 * rope[0].shape[1])
-    s = (_lib or lib()).alora_cache_move_rows(src.data_ptr(), dst.data_ptr(), None if shift is None else shift.data_ptr(), n, cos, sin, positions, rot,
+    if rope is None:
+        cos = sin = None
+        positions = pairs = 0
+    else:
+        positions, pairs = _check_rope(rope)
+        cos, sin = rope[0].data_ptr(), rope[1].data_ptr()
+    s = (_lib or lib()).alora_cache_move_rows(src.data_ptr(), dst.data_ptr(), None if shift is None else shift.data_ptr(), n, cos, sin, positions, 2 * pairs,
                                     1 if interleaved else 0, ctypes.byref(dims), _stream_handle(stream))
     if s:
         raise AloraError(s, "alora_cache_move_rows")

@@ -266,6 +266,25 @@ def test_positions_and_slots_that_are_not_dense_integers_of_every_row_are_refuse
                 heads_call(back=back, **{key: t})
 
 
+@pytest.mark.parametrize("back", [False, True])
+def test_tables_that_are_not_those_of_the_call_are_refused(back):
+    z = torch.zeros
+    for rope in ((z(10, 16).bfloat16(), z(10, 16)), (z(10, 16), z(10, 16).double()), (z(10, 32)[:, ::2], z(10, 16)), (z(10, 16), z(9, 16)), (z(9, 16), z(9, 16)),
+                 (z(10, 8), z(10, 8)), (z(160), z(160)), (z(16, 10).t(), z(16, 10).t())):
+        with pytest.raises(ValueError, match="rope"):
+            heads_call(back=back, rope=rope)
+
+
+def test_tables_of_moved_rows_are_checked():
+    z, k = torch.zeros, torch.zeros(32, 64)
+    dims = ab.make_cache_dims([k], [k], 2, 32, 16)
+    src, dst, shift = torch.arange(3), torch.arange(8, 11), torch.ones(3, dtype=torch.int32)
+    for rope in ((z(10, 16).half(), z(10, 16)), (z(10, 16).bfloat16(), z(10, 16).bfloat16()), (z(10, 16), z(3, 32)[:, ::2]), (z(10, 16), z(10, 8)), (z(10, 16), z(9, 16)),
+                 (z(160), z(160))):
+        with pytest.raises(ValueError, match="rope"):
+            ab.alora_cache_move_rows(src, dst, shift, rope, dims)
+
+
 # ---- launches, recorded without a GPU (see launch_recorder.c) -------------------------------------
 RECORD = """
 import ctypes, json, re, sys, types
