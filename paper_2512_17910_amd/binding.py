@@ -638,14 +638,22 @@ def alora_cache_copy_blocks(src, dst, dims: AloraCacheDims, stream=None) -> None
         raise AloraError(s, "alora_cache_copy_blocks")
 
 
-def alora_cache_move_rows(src, dst, shift, rope, dims: AloraCacheDims, interleaved: bool = False, stream=None) -> None:
-    """Enqueue moves of rows src[i] to dst[i] (int64 device tensors) in every layer, keys turned by shift[i] positions (int32, with the
-    tables rope; both None: rows are only copied)."""
+def _check_lists(src, dst, shift) -> int:
+    """Rows of a move's lists."""
     n = src.shape[0]
     if dst.shape[0] != n or (shift is not None and shift.shape[0] != n):
         raise ValueError("src, dst, shift: one length expected")
-    if src.element_size() != 8 or dst.element_size() != 8 or (shift is not None and shift.element_size() != 4) or not (src.is_contiguous() and dst.is_contiguous()):
-        raise TypeError("src, dst: contiguous int64, shift: int32 expected")
+    _, i32, i64 = _types or _torch_types()
+    if src.dtype is not i64 or dst.dtype is not i64 or (shift is not None and (shift.dtype is not i32 or not shift.is_contiguous())) or not (
+            src.is_contiguous() and dst.is_contiguous()):
+        raise TypeError("src, dst: contiguous int64, shift: contiguous int32 expected")
+    return n
+
+
+def alora_cache_move_rows(src, dst, shift, rope, dims: AloraCacheDims, interleaved: bool = False, stream=None) -> None:
+    """Enqueue moves of rows src[i] to dst[i] (int64 device tensors) in every layer, keys turned by shift[i] positions (int32, with the
+    tables rope; both None: rows are only copied)."""
+    n = _check_lists(src, dst, shift)
     if rope is None:
         cos = sin = None
         positions = pairs = 0
@@ -659,4 +667,5 @@ def alora_cache_move_rows(src, dst, shift, rope, dims: AloraCacheDims, interleav
 
 
 def alora_cache_move_rows_validate(src, dst, shift, rope, dims: AloraCacheDims) -> int:
-    return int(lib().alora_cache_move_rows_validate(_ptr(src), _ptr(dst), _ptr(shift), src.shape[0], 0 if rope is None else rope[0].shape[0], ctypes.byref(dims)))
+    n = _check_lists(src, dst, shift)
+    return int(lib().alora_cache_move_rows_validate(_ptr(src), _ptr(dst), _ptr(shift), n, 0 if rope is None else rope[0].shape[0], ctypes.byref(dims)))

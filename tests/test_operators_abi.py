@@ -285,6 +285,21 @@ def test_tables_of_moved_rows_are_checked():
             ab.alora_cache_move_rows(src, dst, shift, rope, dims)
 
 
+def test_lists_of_rows_that_are_not_dense_integers_are_refused():
+    z, k = torch.zeros, torch.zeros(32, 64)
+    dims, rope = ab.make_cache_dims([k], [k], 2, 32, 16), (z(10, 16), z(10, 16))
+    src, dst, shift = torch.arange(3), torch.arange(8, 11), torch.ones(3, dtype=torch.int32)
+    for call in (lambda s, d, h: ab.alora_cache_move_rows(s, d, h, rope, dims), lambda s, d, h: ab.alora_cache_move_rows_validate(s, d, h, rope, dims)):
+        for name, lists in (("src", (src.double(), dst, shift)), ("dst", (src, dst.double(), shift)), ("shift", (src, dst, shift.float()))):
+            with pytest.raises(TypeError, match=name):
+                call(*lists)
+        with pytest.raises(TypeError, match="shift"):
+            call(src, dst, torch.ones(6, dtype=torch.int32)[::2])
+        for lists in ((src, dst[:2], shift), (src, dst, shift[:2])):
+            with pytest.raises(ValueError):
+                call(*lists)
+
+
 # ---- launches, recorded without a GPU (see launch_recorder.c) -------------------------------------
 RECORD = """
 import ctypes, json, re, sys, types
