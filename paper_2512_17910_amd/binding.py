@@ -65,6 +65,7 @@ class AloraCacheDims(ctypes.Structure):
     _fields_ = [("dtype", ctypes.c_int32), ("n_layers", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("block_size", ctypes.c_int32), ("n_slots", ctypes.c_int64),
                 ("k_caches", ctypes.c_void_p), ("v_caches", ctypes.c_void_p)]
+    on_host = None          # a cache that is no device tensor
 
 
 class AloraError(RuntimeError):
@@ -454,13 +455,6 @@ def _check_rope(rope):
     return shape
 
 
-def _check_rope_of(rope, dims):
-    """The tables that dims was made for, or longer ones."""
-    positions, pairs = _check_rope(rope)
-    if positions < dims.rope_positions or 2 * pairs != dims.rotary_dim:
-        raise ValueError(f"rope: tables of {dims.rope_positions} positions and {dims.rotary_dim // 2} pairs expected, got {positions} and {pairs}")
-
-
 _types = None
 
 
@@ -473,11 +467,18 @@ def _torch_types():
 
 
 # What a call takes beside the tensors that its dims describe is looked at in every call: a type, size or stride that the kernels do not
-# expect would be misread in silence, or read behind its end.
+# expect would be misread in silence, or read behind its end, and a host address would go to a kernel.  That is 25 attributes of tensors for
+# a call with norm and rotation, 1 us of its host time, which is why they stand in few conditions.
 def _refuse(name: str, t, dtype, n: int) -> None:
     if t.dtype is not dtype:
         raise TypeError(f"{name}: {dtype} expected, got {t.dtype}")
     raise ValueError(f"{name}: {n} contiguous elements expected, got {tuple(t.shape)} with strides {t.stride()}")
+
+
+def _refuse_host(**tensors) -> None:
+    for name, t in tensors.items():
+        if t is not None and not t.is_cuda:
+            raise TypeError(f"{name}: a tensor on the GPU expected, got one on {t.device}")
 
 
 def _check_rows(name: str, t, dtype, n: int) -> None:
@@ -491,6 +492,23 @@ def _check_weights(name_q: str, wq, name_k: str, wk, dtype, d: int) -> None:
         _refuse(name_q, wq, dtype, d)
     if wk.dtype is not dtype or wk.numel() != d or not wk.is_contiguous():
         _refuse(name_k, wk, dtype, d)
+
+
+def _check_heads(wq, wk, rope, token_positions, dims):
+    """What both calls of the heads take; the tables' addresses.  Tables are those that dims was made for, or longer ones."""
+    by_code, i32, _ = _types or _torch_types()
+    if token_positions is not None and (token_positions.dtype is not i32 or token_positions.numel() < dims.n_tokens or not token_positions.is_contiguous()):
+        _refuse("token_positions", token_positions, i32, dims.n_tokens)
+    if wq is not None and wk is not None:
+        dtype, d = by_code[dims.dtype], dims.head_dim
+        if wq.dtype is not dtype or wk.dtype is not dtype or wq.numel() != d or wk.numel() != d or not (wq.is_contiguous() and wk.is_contiguous()):
+            _check_weights("wq", wq, "wk", wk, dtype, d)
+    if rope is None:
+        return None, None
+    positions, pairs = _check_rope(rope)
+    if positions < dims.rope_positions or 2 * pairs != dims.rotary_dim:
+        raise ValueError(f"rope: tables of {dims.rope_positions} positions and {dims.rotary_dim // 2} pairs expected, got {positions} and {pairs}")
+    return rope[0].data_ptr(), rope[1].data_ptr()
 
 
 def make_heads_dims(q, q_out, k, k_out, n_q_heads: int, n_kv_heads: int, head_dim: int, rope=None, interleaved: bool = False,
@@ -521,21 +539,19 @@ def alora_qk_norm_rope(q, q_out, k, k_cache, v, v_cache, wq, wk, rope, token_pos
     """Enqueue norm and rotary embedding of the rows' heads (include/alora_heads.h): q to q_out, k (None: in place) to its slots of k_cache,
     v, where given, to v_cache.  The tensors are those that dims was made from, or of the same shapes and strides; wq and wk, of their
     type, are None without norm, rope without rotation."""
-    by_code, i32, i64 = _types or _torch_types()
-    n = dims.n_tokens
-    _check_rows("slot_mapping", slot_mapping, i64, n)
-    if token_positions is not None:
-        _check_rows("token_positions", token_positions, i32, n)
-    if wq is not None and wk is not None:
-        _check_weights("wq", wq, "wk", wk, by_code[dims.dtype], dims.head_dim)
-    if rope is not None:
-        _check_rope_of(rope, dims)
-    cos, sin = (None, None) if rope is None else rope
+    i64 = (_types or _torch_types())[2]
+    if slot_mapping.dtype is not i64 or slot_mapping.numel() < dims.n_tokens or not slot_mapping.is_contiguous():
+        _refuse("slot_mapping", slot_mapping, i64, dims.n_tokens)
+    cos, sin = _check_heads(wq, wk, rope, token_positions, dims)
+    if not (q.is_cuda and q_out.is_cuda and k_cache.is_cuda and slot_mapping.is_cuda and (k is None or k.is_cuda) and (v is None or v.is_cuda) and (
+            v_cache is None or v_cache.is_cuda) and (wq is None or wq.is_cuda) and (wk is None or wk.is_cuda) and (
+            rope is None or rope[0].is_cuda and rope[1].is_cuda) and (token_positions is None or token_positions.is_cuda)):
+        _refuse_host(q=q, q_out=q_out, k=k, k_cache=k_cache, v=v, v_cache=v_cache, wq=wq, wk=wk, cos=rope and rope[0], sin=rope and rope[1],
+                     token_positions=token_positions, slot_mapping=slot_mapping)
     s = (_lib or lib()).alora_qk_norm_rope(q.data_ptr(), q_out.data_ptr(), None if k is None else k.data_ptr(), k_cache.data_ptr(),
                                            None if v is None else v.data_ptr(), None if v_cache is None else v_cache.data_ptr(),
                                            None if wq is None else wq.data_ptr(), None if wk is None else wk.data_ptr(),
-                                           None if cos is None else cos.data_ptr(), None if sin is None else sin.data_ptr(),
-                                           None if token_positions is None else token_positions.data_ptr(), slot_mapping.data_ptr(),
+                                           cos, sin, None if token_positions is None else token_positions.data_ptr(), slot_mapping.data_ptr(),
                                            ctypes.byref(dims), _stream_handle(stream))
     if s:
         raise AloraError(s, "alora_qk_norm_rope")
@@ -555,21 +571,18 @@ def alora_qk_norm_rope_backward(q, dq_out, dq, k, dk_out, dk, wq, wk, dwq, dwk, 
     """Enqueue the backward pass of alora_qk_norm_rope: dq, dk and, with norm, the fp32 dwq, dwk from the gradients of its outputs."""
     if dims.n_tokens > 1 and (dq.stride(0) != (dims.dq_stride or dims.q_stride) or dk.stride(0) != (dims.dk_stride or dims.k_stride)):
         raise ValueError("dq, dk: strides other than those of dims (make_heads_dims takes dq and dk)")
-    by_code, i32, _ = _types or _torch_types()
-    if token_positions is not None:
-        _check_rows("token_positions", token_positions, i32, dims.n_tokens)
-    if wq is not None and wk is not None:
-        _check_weights("wq", wq, "wk", wk, by_code[dims.dtype], dims.head_dim)
+    cos, sin = _check_heads(wq, wk, rope, token_positions, dims)
     if dwq is not None and dwk is not None:
-        _check_weights("dwq", dwq, "dwk", dwk, by_code[ALORA_F32], dims.head_dim)
-    if rope is not None:
-        _check_rope_of(rope, dims)
-    cos, sin = (None, None) if rope is None else rope
+        _check_weights("dwq", dwq, "dwk", dwk, _types[0][ALORA_F32], dims.head_dim)
+    if not (q.is_cuda and dq_out.is_cuda and dq.is_cuda and k.is_cuda and dk_out.is_cuda and dk.is_cuda and (wq is None or wq.is_cuda) and (
+            wk is None or wk.is_cuda) and (dwq is None or dwq.is_cuda) and (dwk is None or dwk.is_cuda) and (
+            rope is None or rope[0].is_cuda and rope[1].is_cuda) and (token_positions is None or token_positions.is_cuda) and (workspace is None or workspace.is_cuda)):
+        _refuse_host(q=q, dq_out=dq_out, dq=dq, k=k, dk_out=dk_out, dk=dk, wq=wq, wk=wk, dwq=dwq, dwk=dwk, cos=rope and rope[0], sin=rope and rope[1],
+                     token_positions=token_positions, workspace=workspace)
     s = (_lib or lib()).alora_qk_norm_rope_backward(
         q.data_ptr(), dq_out.data_ptr(), dq.data_ptr(), k.data_ptr(), dk_out.data_ptr(), dk.data_ptr(), None if wq is None else wq.data_ptr(),
         None if wk is None else wk.data_ptr(), None if dwq is None else dwq.data_ptr(), None if dwk is None else dwk.data_ptr(),
-        None if cos is None else cos.data_ptr(), None if sin is None else sin.data_ptr(),
-        None if token_positions is None else token_positions.data_ptr(), ctypes.byref(dims), None if workspace is None else workspace.data_ptr(),
+        cos, sin, None if token_positions is None else token_positions.data_ptr(), ctypes.byref(dims), None if workspace is None else workspace.data_ptr(),
         0 if workspace is None else workspace.nbytes, _stream_handle(stream))
     if s:
         raise AloraError(s, "alora_qk_norm_rope_backward")
@@ -599,6 +612,7 @@ def alora_rope_tables(cos, sin, spec: AloraRopeSpec, first: int = 0, stream=None
     rows, pairs = cos.shape
     if 2 * pairs != spec.rotary_dim or sin.shape != cos.shape or not (cos.is_contiguous() and sin.is_contiguous()) or _dtype_code(cos) or _dtype_code(sin):
         raise ValueError(f"cos, sin: contiguous fp32 tensors [rows, {spec.rotary_dim // 2}] expected")
+    _refuse_host(cos=cos, sin=sin)
     s = (_lib or lib()).alora_rope_tables(cos.data_ptr(), sin.data_ptr(), first, rows, ctypes.byref(spec), _stream_handle(stream))
     if s:
         raise AloraError(s, "alora_rope_tables")
@@ -617,6 +631,7 @@ def make_cache_dims(k_caches: Sequence, v_caches: Sequence, n_kv_heads: int, hea
     at = _table(ptrs)
     d = AloraCacheDims(_dtype_code(tensors[0]), n, n_kv_heads, head_dim, block_size, shape[0], at, at + 8 * n)
     d.keep = (ptrs, tensors)
+    d.on_host = next((t for t in tensors if not t.is_cuda), None)
     return d
 
 
@@ -633,7 +648,10 @@ def alora_cache_copy_blocks(src, dst, dims: AloraCacheDims, stream=None) -> None
     """Enqueue copies of blocks src[i] to dst[i] (src[i] = -1: cleared) in every layer; src, dst: int32 numpy arrays."""
     if len(src) != len(dst):
         raise ValueError(f"{len(src)} sources and {len(dst)} destinations")
-    s = (_lib or lib()).alora_cache_copy_blocks(_host_int32(src, "src"), _host_int32(dst, "dst"), len(src), ctypes.byref(dims), _stream_handle(stream))
+    src_at, dst_at = _host_int32(src, "src"), _host_int32(dst, "dst")
+    if dims.on_host is not None:
+        _refuse_host(caches=dims.on_host)
+    s = (_lib or lib()).alora_cache_copy_blocks(src_at, dst_at, len(src), ctypes.byref(dims), _stream_handle(stream))
     if s:
         raise AloraError(s, "alora_cache_copy_blocks")
 
@@ -659,7 +677,11 @@ def alora_cache_move_rows(src, dst, shift, rope, dims: AloraCacheDims, interleav
         positions = pairs = 0
     else:
         positions, pairs = _check_rope(rope)
+        if not (rope[0].is_cuda and rope[1].is_cuda):
+            _refuse_host(cos=rope[0], sin=rope[1])
         cos, sin = rope[0].data_ptr(), rope[1].data_ptr()
+    if not (src.is_cuda and dst.is_cuda and (shift is None or shift.is_cuda)) or dims.on_host is not None:
+        _refuse_host(src=src, dst=dst, shift=shift, caches=dims.on_host)
     s = (_lib or lib()).alora_cache_move_rows(src.data_ptr(), dst.data_ptr(), None if shift is None else shift.data_ptr(), n, cos, sin, positions, 2 * pairs,
                                     1 if interleaved else 0, ctypes.byref(dims), _stream_handle(stream))
     if s:

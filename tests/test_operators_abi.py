@@ -300,6 +300,24 @@ def test_lists_of_rows_that_are_not_dense_integers_are_refused():
                 call(*lists)
 
 
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+def test_host_tensors_are_refused(dtype):
+    """Their addresses would go to a kernel.  (All else about these calls is right.)"""
+    dtype = getattr(torch, dtype)
+    for back in (False, True):
+        with pytest.raises(TypeError, match="on the GPU"):
+            heads_call(dtype, back)
+    k = torch.zeros(32, 64, dtype=dtype)
+    dims, src, dst = ab.make_cache_dims([k], [k], 2, 32, 16), torch.arange(3), torch.arange(8, 11)
+    for shift, rope in ((None, None), (torch.ones(3, dtype=torch.int32), (torch.zeros(10, 16), torch.zeros(10, 16)))):
+        with pytest.raises(TypeError, match="on the GPU"):
+            ab.alora_cache_move_rows(src, dst, shift, rope, dims)
+    with pytest.raises(TypeError, match="on the GPU"):
+        ab.alora_cache_copy_blocks(np.zeros(1, np.int32), np.ones(1, np.int32), dims)
+    with pytest.raises(TypeError, match="on the GPU"):
+        ab.alora_rope_tables(torch.zeros(4, 16), torch.zeros(4, 16), ab.make_rope_spec(32))
+
+
 # ---- launches, recorded without a GPU (see launch_recorder.c) -------------------------------------
 RECORD = """
 import ctypes, json, re, sys, types
