@@ -209,7 +209,8 @@ def _stream_handle(stream) -> Optional[int]:
         return stream.cuda_stream or None
     if _current_raw_stream is None:
         import torch
-        _current_device = torch.cuda.current_device
+        torch.cuda.current_device()         # (initialises the device where nothing has yet, which the plain call does not)
+        _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
         _current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda d: torch.cuda.current_stream(d).cuda_stream)
     return _current_raw_stream(_current_device()) or None
 
@@ -552,7 +553,7 @@ def alora_qk_norm_rope(q, q_out, k, k_cache, v, v_cache, wq, wk, rope, token_pos
                                            None if v is None else v.data_ptr(), None if v_cache is None else v_cache.data_ptr(),
                                            None if wq is None else wq.data_ptr(), None if wk is None else wk.data_ptr(),
                                            cos, sin, None if token_positions is None else token_positions.data_ptr(), slot_mapping.data_ptr(),
-                                           ctypes.byref(dims), _stream_handle(stream))
+                                           dims, _stream_handle(stream))
     if s:
         raise AloraError(s, "alora_qk_norm_rope")
 
@@ -582,7 +583,7 @@ def alora_qk_norm_rope_backward(q, dq_out, dq, k, dk_out, dk, wq, wk, dwq, dwk, 
     s = (_lib or lib()).alora_qk_norm_rope_backward(
         q.data_ptr(), dq_out.data_ptr(), dq.data_ptr(), k.data_ptr(), dk_out.data_ptr(), dk.data_ptr(), None if wq is None else wq.data_ptr(),
         None if wk is None else wk.data_ptr(), None if dwq is None else dwq.data_ptr(), None if dwk is None else dwk.data_ptr(),
-        cos, sin, None if token_positions is None else token_positions.data_ptr(), ctypes.byref(dims), None if workspace is None else workspace.data_ptr(),
+        cos, sin, None if token_positions is None else token_positions.data_ptr(), dims, None if workspace is None else workspace.data_ptr(),
         0 if workspace is None else workspace.nbytes, _stream_handle(stream))
     if s:
         raise AloraError(s, "alora_qk_norm_rope_backward")
@@ -613,7 +614,7 @@ def alora_rope_tables(cos, sin, spec: AloraRopeSpec, first: int = 0, stream=None
     if 2 * pairs != spec.rotary_dim or sin.shape != cos.shape or not (cos.is_contiguous() and sin.is_contiguous()) or _dtype_code(cos) or _dtype_code(sin):
         raise ValueError(f"cos, sin: contiguous fp32 tensors [rows, {spec.rotary_dim // 2}] expected")
     _refuse_host(cos=cos, sin=sin)
-    s = (_lib or lib()).alora_rope_tables(cos.data_ptr(), sin.data_ptr(), first, rows, ctypes.byref(spec), _stream_handle(stream))
+    s = (_lib or lib()).alora_rope_tables(cos.data_ptr(), sin.data_ptr(), first, rows, spec, _stream_handle(stream))
     if s:
         raise AloraError(s, "alora_rope_tables")
 
@@ -651,7 +652,7 @@ def alora_cache_copy_blocks(src, dst, dims: AloraCacheDims, stream=None) -> None
     src_at, dst_at = _host_int32(src, "src"), _host_int32(dst, "dst")
     if dims.on_host is not None:
         _refuse_host(caches=dims.on_host)
-    s = (_lib or lib()).alora_cache_copy_blocks(src_at, dst_at, len(src), ctypes.byref(dims), _stream_handle(stream))
+    s = (_lib or lib()).alora_cache_copy_blocks(src_at, dst_at, len(src), dims, _stream_handle(stream))
     if s:
         raise AloraError(s, "alora_cache_copy_blocks")
 
@@ -683,7 +684,7 @@ def alora_cache_move_rows(src, dst, shift, rope, dims: AloraCacheDims, interleav
     if not (src.is_cuda and dst.is_cuda and (shift is None or shift.is_cuda)) or dims.on_host is not None:
         _refuse_host(src=src, dst=dst, shift=shift, caches=dims.on_host)
     s = (_lib or lib()).alora_cache_move_rows(src.data_ptr(), dst.data_ptr(), None if shift is None else shift.data_ptr(), n, cos, sin, positions, 2 * pairs,
-                                    1 if interleaved else 0, ctypes.byref(dims), _stream_handle(stream))
+                                    1 if interleaved else 0, dims, _stream_handle(stream))
     if s:
         raise AloraError(s, "alora_cache_move_rows")
 
