@@ -455,7 +455,7 @@ static int launch_heads(HeadsArgs &g, bool bf16, int V, bool norm, hipStream_t s
     g.items_q = items(per / g.hq);
     g.items_k = items(per / g.hkv);
     const long long all = (long long)g.items_q + g.items_k + (g.v ? items(128 / (g.hkv * g.s.d * (bf16 ? 2 : 4) / 16)) : 0);
-    if (g.hq <= per / 2 && g.hkv <= per / 2 && all < 1 << 26) {     // (a grid holds fewer than 2^32 threads)
+    if (g.hq <= per / 2 && g.hkv <= per / 2 && all <= (1 << 26) - 4) {     // (a grid holds fewer than 2^32 threads: 2^24 - 1 workgroups of 256)
         return with_layout(bf16, V, g.s.interleaved, [&](auto b, auto v, auto il) {
             const auto go = [&](auto kernel) {
                 launch_kernel(kernel, dim3((unsigned)((all + 3) / 4)), dim3(256), 0, st, g);

@@ -396,3 +396,34 @@ def test_launches_of_calls(tmp_path):
     # two heads of 64: 8 rows of a wavefront either way; 80 heads: 5 wavefronts of turned keys a row
     assert [l[1] for l in turned] == [[4, 128, 1], [4, 2, 1]] and copied == [["move_rows_kernel", [4, 2, 1], [256, 1, 1]]]
     assert wide_rows[0][1] == [125, 2, 1]
+
+
+def record_calls(tmp_path, *calls):
+    """(status, launches) of calls of the record_ functions above, in a process without a GPU."""
+    import json
+    import os
+    import subprocess
+    import sys
+    here = os.path.dirname(os.path.abspath(__file__))
+    rec = str(tmp_path / "librec.so")
+    subprocess.run(["gcc", "-O1", "-w", "-shared", "-fPIC", "-o", rec, os.path.join(here, "launch_recorder.c")], check=True)
+    r = subprocess.run([sys.executable, "-c", RECORD, rec, here, os.path.dirname(here)], input=json.dumps(calls), capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0, r.stderr[-3000:]
+    return json.loads(r.stdout)
+
+
+def test_rows_of_few_heads_fill_a_grid_of_fewer_than_2_to_32_threads(tmp_path):
+    """Heads of 256 on 16 lanes: four rows of one query head, two of two K/V heads and two of their values to a wavefront, 1.25 of them a row.  A dimension of a
+    grid holds fewer than 2^32 threads: 2^26 wavefronts are one too many, whatever the last workgroup leaves empty."""
+    few = dict(n_q_heads=1, n_kv_heads=2, head_dim=256, rotary_dim=256, q_stride=256, q_out_stride=256, k_stride=512, k_out_stride=512, v_stride=512, v_out_stride=512)
+    items = lambda T: -(-T // 4) + 2 * -(-T // 2)
+    most = max(T for T in range(53687080, 53687100) if items(T) <= (1 << 26) - 4)
+    rows = [1000, most - 1, most, most + 1, most + 2, most + 3, most + 4, most + 5, most + 30]
+    assert any((1 << 26) - 4 < items(T) < 1 << 26 for T in rows)
+    for T, (status, launches) in zip(rows, record_calls(tmp_path, *[["record_forward", [dict(few, n_tokens=T), True]] for T in rows])):
+        assert status == OK and len(launches) == 1
+        (name, grid, block), = launches
+        assert all(g * b < 1 << 32 for g, b in zip(grid, block)), (T, launches)
+        assert name == ("heads_packed_kernel" if T <= most else "heads_kernel"), (T, launches)
+        if T <= most:
+            assert grid[0] == -(-items(T) // 4)
