@@ -26,6 +26,9 @@ struct HeadsArgs {
 
 constexpr int HEADS_WAVES = 8;   // wavefronts of a workgroup, at most
 
+// Pieces of 2 KiB of a row of values: a wavefront's work
+__host__ __device__ __forceinline__ int pieces_of(uint32_t bytes) { return (int)(bytes / 2048 + (bytes % 2048 != 0)); }
+
 // U loaded heads of every lane group, normalised, turned and stored where `on`; all 64 lanes take part.
 template <bool BF16, int V, bool INTERLEAVED, bool NORM, int U>
 __device__ __forceinline__ void norm_turn_store(const HeadsArgs &g, const LanePlace &p, Chunk<BF16, V> (&a)[U], Chunk<BF16, V> (&b)[U],
@@ -91,7 +94,8 @@ __global__ __launch_bounds__(64 * HEADS_WAVES) void heads_kernel(HeadsArgs g)
     const long long slot = g.slot[row];
     const bool store = slot >= 0 && slot < g.n_slots;
     const int units = g.uq + g.uk, batches = (units + U - 1) / U;
-    const int v_bytes = g.v ? g.hkv * g.s.d * E : 0, all = batches + (v_bytes + 2047) / 2048;
+    const uint32_t v_bytes = g.v ? (uint32_t)g.hkv * g.s.d * E : 0u;      // (rows have at most 2^32 - 16 bytes: a lane's pieces behind them stay below 2^32)
+    const int all = batches + pieces_of(v_bytes);
 
     float c[V], s[V];
     if (g.s.rot && wave < batches) {
@@ -103,7 +107,7 @@ __global__ __launch_bounds__(64 * HEADS_WAVES) void heads_kernel(HeadsArgs g)
             if (!store) break;
             const char *from = g.v + row * g.v_row;
             char *to = g.vc + slot * g.vo_row;
-            const int o = (i0 - batches) * 2048 + lane * 16;
+            const uint32_t o = (uint32_t)(i0 - batches) * 2048u + lane * 16;
             u32x4 x, y;
             if (o < v_bytes) x = *(const u32x4 *)(from + o);
             if (o + 1024 < v_bytes) y = *(const u32x4 *)(from + o + 1024);
@@ -445,7 +449,8 @@ static int units_of(int heads, const HeadShape &s)
 
 static int launch_heads(HeadsArgs &g, bool bf16, int V, bool norm, hipStream_t st)
 {
-    const int units = g.uq + g.uk, v_pieces = g.v ? (g.hkv * g.s.d * (bf16 ? 2 : 4) + 2047) / 2048 : 0;
+    const uint32_t v_bytes = g.v ? (uint32_t)g.hkv * g.s.d * (bf16 ? 2 : 4) : 0u;
+    const int units = g.uq + g.uk, v_pieces = pieces_of(v_bytes);
     // Units of a wavefront: one where the chip is not full many times over (more wavefronts have shorter chains of loads), else three where
     // that comes out even, else two.  us with two | three: 9 units, 8192 rows 71.8 | 61.6, 6 units, 4096 rows 27.2 | 25.4; 8 units, 4096 rows
     // 40.3 | 43.6, 10 units 39.5 | 40.9, 5 units 18.9 | 19.1, 2048 rows 11.4 | 12.1.  Four: 67.4, 28.4, 49.6, 42.5, 20.7, 13.4.
@@ -454,7 +459,7 @@ static int launch_heads(HeadsArgs &g, bool bf16, int V, bool norm, hipStream_t s
     const auto items = [&](int at_once) { return (g.T + at_once - 1) / std::max(1, at_once); };
     g.items_q = items(per / g.hq);
     g.items_k = items(per / g.hkv);
-    const long long all = (long long)g.items_q + g.items_k + (g.v ? items(128 / (g.hkv * g.s.d * (bf16 ? 2 : 4) / 16)) : 0);
+    const long long all = (long long)g.items_q + g.items_k + (g.v ? items(128 / (int)(v_bytes / 16)) : 0);
     if (g.hq <= per / 2 && g.hkv <= per / 2 && all <= (1 << 26) - 4) {     // (a grid holds fewer than 2^32 threads: 2^24 - 1 workgroups of 256)
         return with_layout(bf16, V, g.s.interleaved, [&](auto b, auto v, auto il) {
             const auto go = [&](auto kernel) {

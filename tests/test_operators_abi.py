@@ -427,3 +427,25 @@ def test_rows_of_few_heads_fill_a_grid_of_fewer_than_2_to_32_threads(tmp_path):
         assert name == ("heads_packed_kernel" if T <= most else "heads_kernel"), (T, launches)
         if T <= most:
             assert grid[0] == -(-items(T) // 4)
+
+
+def test_rows_of_two_gibibytes_and_more(tmp_path):
+    """Values are copied in pieces of 2 KiB; their bytes leave 31 bits behind in fp32 rows of 2^29 features and more, the widest there are."""
+    wide = lambda hkv, d: dict(dtype=0, n_tokens=1, n_q_heads=1, n_kv_heads=hkv, head_dim=d, rotary_dim=4, q_stride=d, q_out_stride=d, k_stride=hkv * d,
+                               k_out_stride=hkv * d, v_stride=hkv * d, v_out_stride=hkv * d)
+    sizes = [(1 << 21, 256), ((1 << 21) - 1, 256), ((1 << 22) - 1, 256), ((1 << 28) - 1, 4), ((1 << 27) + 5, 4)]
+    for size, (status, launches) in zip(sizes, record_calls(tmp_path, *[["record_forward", [wide(*size), True]] for size in sizes])):
+        assert status == OK and launches == [["heads_kernel", [1, 1, 1], [8 * 64, 1, 1]]], (size, launches)
+
+
+def test_pieces_of_values_cover_the_widest_rows_in_32_bits():
+    """What heads_kernel computes of a lane's piece of the values' row, in unsigned 32 bits, for rows of up to 2^32 - 16 bytes."""
+    u = lambda x: x & 0xffffffff
+    for v_bytes in (16, 2048, 2064, (1 << 31) - 16, 1 << 31, (1 << 32) - 4096, (1 << 32) - 2048, (1 << 32) - 1040, (1 << 32) - 16):
+        pieces = u(v_bytes - 1) // 2048 + 1
+        for piece in {0, 1, pieces // 2, pieces - 2, pieces - 1} & set(range(pieces)):
+            covered = set()
+            for lane in range(64):
+                o = u(piece * 2048 + lane * 16)
+                covered |= {x for x in (o, u(o + 1024)) if x < v_bytes}
+            assert covered == set(range(2048 * piece, min(v_bytes, 2048 * piece + 2048), 16)), (v_bytes, piece)
