@@ -108,7 +108,10 @@ typedef struct alora_rope_spec {
 /*
  * cos[p - first, i] = magnitude cos(p theta_i), sin likewise, for p = first .. first + rows - 1 and every pair i.
  * Angles are held in 64 bits: far positions are as exact as near ones.  A result is off by half a unit in its last place, and by what the angle
- * loses in 64 bits, at most magnitude * position * 2^-50.  0 <= first, first + rows <= 2^24 (ALORA_ESHAPE).  cos, sin: fp32
+ * loses in 64 bits, at most magnitude * position * t * 2^-49: t = 1 where base and factor are at least 1, else
+ * max(1, theta) (1 + max(0, -log2 base) / 4) with theta the largest angle of a position; by parts 1 + high / (high - low) times that.  (A position's
+ * angle is off by up to 10 half units of itself, a power of two another 2 for every bit of its exponent; every step of the kernel's products
+ * adds 4, and there are at most as many as positions.)  0 <= first, first + rows <= 2^24 (ALORA_ESHAPE).  cos, sin: fp32
  * [rows, rotary_dim / 2], 16-byte aligned; with magnitude 1 they are tables for alora_cache_move_rows too, with rotary_dim = head_dim for
  * alora_extras.rope_cos and rope_sin.
  */

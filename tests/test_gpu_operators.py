@@ -383,6 +383,31 @@ def test_tables(rot, base, first, rows, kw):
     assert (wide[:, rows * (rot // 2):] == 7.0).all(), "written behind the tables"
 
 
+@pytest.mark.parametrize("rot,base,first,rows,kw", [
+    (128, 1e4, 0, 4097, {}), (512, 1e4, 0, 40000, {}), (2, 1e4, 3, 200000, {}), (64, 1e30, 0, 5000, {}), (6, 1.0, 0, 50, {}), (8, 0.5, 0, 100, {}),
+    (8, 0.001, 0, 3000, {}), (64, 1e-10, 0, 5000, {}), (64, 1e4, 0, 5000, dict(scaling="linear", factor=0.01)),
+    (64, 1e-10, 70000, 500, dict(scaling="linear", factor=1e-3)), (128, 5e5, 0, 70001, dict(scaling="by_parts", factor=16.0, original=8192, low=1, high=32, magnitude=1.27)),
+    (96, 1e4, 0, 60000, dict(scaling="by_parts", factor=0.02, original=4096, low=1, high=4, magnitude=0.5)),
+    (96, 1e4, 5, 600, dict(scaling="by_parts", factor=40.0, original=4096, low=1, high=1.0001))])
+def test_tables_within_the_bound_of_each_position(rot, base, first, rows, kw):
+    """Half a step of the result, and of each row's own position what the header states: 2^-49 of it, more where angles of a position are large."""
+    cos, sin = (torch.empty((rows, rot // 2), device="cuda") for _ in range(2))
+    ab.alora_rope_tables(cos, sin, ab.make_rope_spec(rot, base, **kw), first)
+    c, s = oh.tables(rot, base, first, rows, **kw)
+    largest = max(1.0, base ** (2 / rot - 1))            # of a position, before scaling
+    factor, t = kw.get("factor", 1.0), 1.0
+    if base < 1 or factor < 1:
+        t = max(1.0, largest * max(1.0, 1 / factor)) * (1 + max(0.0, -np.log2(base)) / 4)
+    if kw.get("scaling") == "by_parts":
+        t *= 1 + kw["high"] / (kw["high"] - kw["low"])
+    slack = kw.get("magnitude", 1.0) * t * 2.0 ** -49 * np.arange(first, first + rows)[:, None].astype(np.longdouble)
+    for got, want in ((cos, c), (sin, s)):
+        err = np.abs(got.cpu().numpy().astype(np.longdouble) - want)
+        step = np.spacing(np.abs(want).astype(np.float32)).astype(np.longdouble)
+        over = err - (step / 2 * (1 + 2.0 ** -20) + slack)
+        assert (over <= 0).all(), (float(over.max()), np.unravel_index(int(np.argmax(over)), over.shape))
+
+
 # ---- the cache ----------------------------------------------------------------------------------
 class Cache:
     def __init__(self, dtype, layers, blocks, hkv, d, bs, seed=0):
