@@ -12,6 +12,7 @@ import torch
 from oracle import heads as oh
 from paper_2512_17910_amd import binding as ab
 from gpu_util import raw_bits, to_f64
+from test_operators_abi import LAYOUTS, UNITS, heads_of_a_layout
 
 pytestmark = pytest.mark.gpu
 
@@ -359,6 +360,76 @@ def test_gradient_against_differences_of_the_forward_call():
         e = torch.zeros_like(b.wq)
         e[c] = h
         assert abs((loss(b.q, b.wq + e) - loss(b.q, b.wq - e)) / (2 * h) - float(b.dwq[c])) <= bound(sizes.sum())
+
+
+@pytest.mark.parametrize("norm", [True, False], ids=["norm", "plain"])
+@pytest.mark.parametrize("layout", LAYOUTS, ids=str)
+def test_heads_of_every_instantiation(layout, norm):
+    """One, two and three units of a wavefront, and rows that share wavefronts; test_operators_abi.py finds the kernels that these sizes take."""
+    dtype, d, rot, il = layout
+    cases = [(T, *heads_of_a_layout(dtype, d, rot, il, uq, uk)) for T, uq, uk in UNITS.values()] + [(333, 2, 1)]
+    for i, (T, hq, hkv) in enumerate(cases):
+        print(f"[case] {dtype} T={T} {hq}/{hkv} d={d} rot={rot} il={il} norm={norm}", flush=True)
+        h = Heads(dtype, T, hq, hkv, d, rot, il, norm, cache=bool(i % 2), seed=T + d)
+        h.run()
+        h.check()
+
+
+@pytest.mark.parametrize("norm", [True, False], ids=["norm", "plain"])
+@pytest.mark.parametrize("layout", LAYOUTS, ids=str)
+def test_gradients_of_every_instantiation(layout, norm):
+    dtype, d, rot, il = layout
+    for T, (hq, hkv) in ((333, heads_of_a_layout(dtype, d, rot, il, 4, 2)), (1111, (2, 1))):
+        print(f"[case] {dtype} T={T} {hq}/{hkv} d={d} rot={rot} il={il} norm={norm}", flush=True)
+        b = Back(dtype, T, hq, hkv, d, rot, il, norm, seed=T + d)
+        b.call()
+        b.check()
+
+
+def test_a_head_of_zeros_without_eps():
+    """0 / 0: the head is NaN, and so is its gradient; its neighbours are what they would be."""
+    for dtype, d, rot, il in (("f32", 32, 32, False), ("bf16", 128, 64, True), ("f32", 80, 20, False), ("bf16", 256, 28, False)):
+        h = Heads(dtype, 3, 5, 2, d, rot, il, seed=11, eps=0.0)
+        h.q[1, 2 * d: 3 * d] = 0
+        h.run()
+        got, (want, size) = to_f64(h.q_out).reshape(3, 5, d), (x.reshape(3, 5, d) for x in h.want_q)
+        assert np.isnan(got[1, 2]).all()
+        got[1, 2] = want[1, 2]
+        close(got, want, size, h.dt, 32, "q")
+        close(to_f64(h.kc)[h.slot[h.kept]], *h.want_k, h.dt, 32, "k")
+        b = Back(dtype, 3, 5, 2, d, rot, il, True, seed=11, eps=0.0)
+        b.q[1, 2 * d: 3 * d] = 0
+        b.call()
+        got, (want, size) = to_f64(b.dq).reshape(3, 5, d), (x for x in b.want[0][:2])
+        assert np.isnan(got[1, 2]).all()
+        got[1, 2] = want[1, 2]
+        close(got, want, size, b.dt, 96, "dq")
+        close(b.dk, *[x.reshape(3, -1) for x in b.want[1][:2]], b.dt, 96, "dk")
+        close(b.dwk, *b.want[1][2:], torch.float32, 256, "dwk")
+
+
+def test_gradients_of_infinities_and_nan_stay_in_their_heads():
+    """A NaN among a head's features makes its gradient NaN, an infinite gradient of an output makes its head's not finite (without norm: its pair's); other
+    heads' gradients, and the other norm's weights', are what they would be."""
+    for dtype, d, rot, il in (("bf16", 128, 64, False), ("bf16", 64, 24, True), ("f32", 80, 20, True), ("f32", 32, 32, False), ("f32", 80, 20, False)):
+        for norm in (True, False):
+            for where, value in (("x", float("nan")), ("x", float("inf")), ("g", float("inf")), ("g", float("nan"))):
+                if where == "x" and not norm:
+                    continue              # (features are not looked at)
+                b = Back(dtype, 70, 6, 2, d, rot, il, norm, seed=9)
+                (b.q if where == "x" else b.gq)[41, 2 * d + d - 1] = value
+                b.call()
+                got, (want, size) = to_f64(b.dq).reshape(70, 6, d), b.want[0][:2]
+                bad = np.argwhere(~np.isfinite(got))
+                assert len(bad) and (bad[:, :2] == [41, 2]).all(), (dtype, d, norm, where, bad[:4])
+                assert len(bad) == d if norm else len(bad) <= 2 and bad[-1, 2] == d - 1, (dtype, d, norm, where, bad)
+                keep = np.isfinite(got)
+                got[~keep] = want[~keep]
+                close(got, want, size, b.dt, 96, "dq")
+                close(b.dk, *[x.reshape(70, -1) for x in b.want[1][:2]], b.dt, 96, "dk")
+                if norm:
+                    close(b.dwk, *b.want[1][2:], torch.float32, 256, "dwk")
+                    assert not np.isfinite(to_f64(b.dwq)).all()
 
 
 @pytest.mark.parametrize("rot,base,first,rows,kw", [

@@ -449,3 +449,60 @@ def test_pieces_of_values_cover_the_widest_rows_in_32_bits():
                 o = u(piece * 2048 + lane * 16)
                 covered |= {x for x in (o, u(o + 1024)) if x < v_bytes}
             assert covered == set(range(2048 * piece, min(v_bytes, 2048 * piece + 2048), 16)), (v_bytes, piece)
+
+
+# ---- every instantiation of the kernels of heads: sizes that test_gpu_operators.py runs -----------------------------------------------
+# (type, head_dim, rotary_dim, neighbours): one for each layout of a head on lanes
+LAYOUTS = [("bf16", 32, 32, False), ("bf16", 80, 8, False), ("bf16", 64, 4, False), ("bf16", 96, 24, True), ("bf16", 64, 20, True),
+           ("f32", 80, 20, False), ("f32", 48, 4, False), ("f32", 64, 64, True)]
+
+
+def heads_of_a_layout(dtype, d, rot, il, units_q, units_k):
+    """(query heads, K/V heads) that fill so many units of 64 lanes, the last of each in part."""
+    bf16 = dtype == "bf16"
+    if il:
+        V = 8 if bf16 and rot % 8 == 0 else 4
+        lanes = (d // V + 1) // 2
+    else:
+        V = 8 if bf16 else 4
+        while V > 2 and (0 < rot // 2 < V or 0 < d - rot < V):
+            V //= 2
+        lanes = -(-rot // 2 // V) + (-(-(d - rot) // V) + 1) // 2
+    per = 64 >> (lanes - 1).bit_length()
+    return units_q * per - (per > 1), units_k * per - (per > 2)
+
+
+# (rows, units of queries, units of keys): one, two (one left over) and three units of a wavefront
+UNITS = {1: (70, 4, 2), 2: (1700, 3, 2), 3: (1400, 4, 2)}
+
+
+def record_layout(back, dtype, d, rot, il, norm, T, hq, hkv):
+    w, e = hq * d, hkv * d
+    dims = heads_dims(dtype=1 if dtype == "bf16" else 0, n_tokens=T, n_q_heads=hq, n_kv_heads=hkv, head_dim=d, rotary_dim=rot, interleaved=int(il), norm=int(norm),
+                      q_stride=w, q_out_stride=w, k_stride=e, k_out_stride=e, v_stride=e, v_out_stride=e, n_slots=T)
+    none = {} if norm else dict(wq=None, wk=None)
+    return backward(dims, **none, **({} if norm else dict(dwq=None, dwk=None))) if back else forward(dims, **none)
+
+
+RECORD_INTS = RECORD.replace("list(r.block)]", "[int(v) for v in re.findall(r'L[ib](\\d+)E', r.name.decode())]]")
+
+
+def test_the_cases_run_on_the_gpu_reach_every_instantiation(tmp_path, monkeypatch):
+    monkeypatch.setitem(globals(), "RECORD", RECORD_INTS)
+    calls, want = [], []
+    for dtype, d, rot, il in LAYOUTS:
+        for norm in (True, False):
+            for units, (T, uq, uk) in UNITS.items():
+                calls.append(["record_layout", [False, dtype, d, rot, il, norm, T, *heads_of_a_layout(dtype, d, rot, il, uq, uk)]])
+            calls.append(["record_layout", [False, dtype, d, rot, il, norm, 333, 2, 1]])
+            calls.append(["record_layout", [True, dtype, d, rot, il, norm, 333, *heads_of_a_layout(dtype, d, rot, il, 4, 2)]])
+    got = {"heads_kernel": set(), "heads_packed_kernel": set(), "heads_back_kernel": set()}
+    for call, (status, launches) in zip(calls, record_calls(tmp_path, *calls)):
+        assert status == OK
+        name, grid, ints = launches[0]
+        assert ints[0] == (call[1][1] == "bf16") and ints[2] == call[1][4] and ints[3] == call[1][5], (call, launches)
+        got[name].add(tuple(ints))
+    layouts = {(1, 8, 0), (1, 4, 0), (1, 2, 0), (1, 8, 1), (1, 4, 1), (0, 4, 0), (0, 2, 0), (0, 4, 1)}
+    normed = {(*l, n) for l in layouts for n in (0, 1)}
+    assert got["heads_kernel"] == {(*l, u) for l in normed for u in (1, 2, 3)}
+    assert got["heads_packed_kernel"] == got["heads_back_kernel"] == normed
