@@ -506,3 +506,13 @@ def test_the_cases_run_on_the_gpu_reach_every_instantiation(tmp_path, monkeypatc
     normed = {(*l, n) for l in layouts for n in (0, 1)}
     assert got["heads_kernel"] == {(*l, u) for l in normed for u in (1, 2, 3)}
     assert got["heads_packed_kernel"] == got["heads_back_kernel"] == normed
+
+
+def test_lists_of_blocks_are_checked_on_both_sides_of_the_rule():
+    """30 blocks: up to 128 words of bits for each the pool's bits, from there on the sorted list."""
+    for blocks in (30 * 64 * 128, 30 * 64 * 129):
+        d = cache_dims(n_slots=16 * blocks)
+        src, dst = list(range(30)), [blocks - 1 - i for i in range(30)]
+        for i, value in ((3, dst[4]), (29, dst[0])):
+            assert copy(src, dst[:i] + [value] + dst[i + 1:], d) == EDATA       # named twice
+            assert copy(src[:i] + [value] + src[i + 1:], dst, d) == EDATA       # source and destination
