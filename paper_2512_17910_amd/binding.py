@@ -637,7 +637,7 @@ def make_cache_dims(k_caches: Sequence, v_caches: Sequence, n_kv_heads: int, hea
 
 
 def _host_int32(a, name: str) -> int:
-    if a.dtype.char != "i" or a.ndim != 1 or (a.strides != (4,) and a.size > 1):
+    if a.dtype.char != "i" or not a.dtype.isnative or a.ndim != 1 or (a.strides != (4,) and a.size > 1):
         raise ValueError(f"{name}: a contiguous int32 array on the host expected")
     try:
         return ctypes.addressof(ctypes.c_char.from_buffer(a))      # (a third of the time of asking numpy)

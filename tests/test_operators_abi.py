@@ -516,3 +516,11 @@ def test_lists_of_blocks_are_checked_on_both_sides_of_the_rule():
         for i, value in ((3, dst[4]), (29, dst[0])):
             assert copy(src, dst[:i] + [value] + dst[i + 1:], d) == EDATA       # named twice
             assert copy(src[:i] + [value] + src[i + 1:], dst, d) == EDATA       # source and destination
+
+
+def test_host_lists_in_another_byte_order_are_refused():
+    k = torch.zeros(32, 64)
+    dims, one = ab.make_cache_dims([k], [k], 2, 32, 16), np.ones(1, np.int32)
+    for src, dst in ((one.astype(">i4"), one), (one, one.astype(">i4"))):
+        with pytest.raises(ValueError, match="int32"):
+            ab.alora_cache_copy_blocks(src, dst, dims)
