@@ -228,9 +228,10 @@ constexpr int BACK_WAVES = 16;   // wavefronts of a workgroup, at most
 // With g = the outputs' gradient turned back, u = g w, r = 1 / sqrt(mean x^2 + eps): both means (of x x and x u) come out of one pass over x and g, then
 // dx = r (u - x r (r mean(x u))) from registers (r^3 would leave fp32's range for heads of 1e-13), and each lane adds g x r to sums for the weights of its features.
 // The units of heads of all rows, those of queries dealt to the wavefronts of all workgroups that take queries, those of keys to
-// the others, so that a lane's sums for the weights are of one of the two.  Bound by memory: 4096 rows of 32 / 8 heads of 128 take 24.3 us (5.2 TB/s),
-// the second kernel 4.4.  256 workgroups of up to 16 wavefronts (fewer partial sums to add): the pass 27.6 us; with 512 29.9, 1024 of five
-// wavefronts that kept to rows 42.  dx goes past the caches: 27.6, ordinary stores 29.2.  Rows of few heads share a wavefront: 2869 rows of 8 / 1
+// the others, so that a lane's sums for the weights are of one of the two.  Bound by memory: 4096 rows of 32 / 8 heads of 128 take 24.5 us (5.2 TB/s),
+// the second kernel 4.5, both under the profiler, and the pass of both 28.3.  What was compared when this was chosen, passes of that time: 256 workgroups
+// of up to 16 wavefronts (fewer partial sums to add) 27.6, with 512 29.9, 1024 of five wavefronts that kept to rows 42; ordinary stores in place of dx
+// past the caches 29.2.  Rows of few heads share a wavefront: 2869 rows of 8 / 1
 // heads of 32 take 6.5 us, with a row for each 9.3 (11.0 with the sums over the heads through LDS).
 template <bool BF16, int V, bool INTERLEAVED, bool NORM>
 __global__ __launch_bounds__(64 * BACK_WAVES) void heads_back_kernel(HeadsBackArgs g)
