@@ -68,6 +68,16 @@ class AloraCacheDims(ctypes.Structure):
     on_host = None          # a cache that is no device tensor
 
 
+class AloraStepDims(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int32), ("max_blocks", ctypes.c_int32), ("block_size", ctypes.c_int32),
+                ("row_cap", ctypes.c_int32), ("pool_cap", ctypes.c_int32), ("n_slots", ctypes.c_int64)]
+
+
+class AloraBoundsDims(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("n_rows", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("block_size", ctypes.c_int32), ("n_slots", ctypes.c_int64)]
+
+
 class AloraError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -139,6 +149,16 @@ def lib() -> ctypes.CDLL:
         L.alora_cache_copy_blocks.argtypes = [vp, vp, i32, cache, vp]
         L.alora_cache_move_rows.argtypes = [vp, vp, vp, i32, vp, vp, i32, i32, i32, cache, vp]
         L.alora_cache_move_rows_validate.argtypes = [vp, vp, vp, i32, i32, cache]
+        attn = ctypes.POINTER(AloraAttnDims)
+        L.alora_step_rows.argtypes = [vp] * 14 + [ctypes.POINTER(AloraStepDims), vp]
+        L.alora_tree_rows.argtypes = [vp, vp, vp, vp, vp, i32, i32, i32, vp]
+        L.alora_tree_attention_workspace_bytes.argtypes = [attn, i32, ctypes.POINTER(sz)]
+        L.alora_tree_attention.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, vp, attn, vp, sz, vp]
+        L.alora_block_bounds.argtypes = [vp, vp, vp, vp, ctypes.POINTER(AloraBoundsDims), vp]
+        L.alora_block_select_workspace_bytes.argtypes = [attn, ctypes.POINTER(sz)]
+        L.alora_block_select.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, attn, vp, sz, vp]
+        L.alora_selected_attention_workspace_bytes.argtypes = [attn, i32, ctypes.POINTER(sz)]
+        L.alora_selected_attention.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, vp, attn, vp, sz, vp]
         L.alora_status_string.argtypes = [ctypes.c_int]
         L.alora_status_string.restype = ctypes.c_char_p
         L.alora_qkv_set_tuning.argtypes = [ctypes.c_int, ctypes.c_int]
@@ -154,7 +174,9 @@ def lib() -> ctypes.CDLL:
                      "alora_paged_attention_workspace_bytes", "alora_paged_attention_suffix_split",
                      "alora_paged_attention_suffix_workspace_bytes", "alora_qk_norm_rope", "alora_qk_norm_rope_backward",
                      "alora_qk_norm_rope_workspace_bytes", "alora_qk_norm_rope_validate", "alora_rope_tables", "alora_cache_copy_blocks",
-                     "alora_cache_move_rows", "alora_cache_move_rows_validate"):
+                     "alora_cache_move_rows", "alora_cache_move_rows_validate", "alora_step_rows", "alora_tree_rows", "alora_tree_attention",
+                     "alora_tree_attention_workspace_bytes", "alora_block_bounds", "alora_block_select", "alora_block_select_workspace_bytes",
+                     "alora_selected_attention", "alora_selected_attention_workspace_bytes"):
             getattr(L, name).restype = ctypes.c_int
         _lib = L
     return _lib
@@ -692,3 +714,179 @@ def alora_cache_move_rows(src, dst, shift, rope, dims: AloraCacheDims, interleav
 def alora_cache_move_rows_validate(src, dst, shift, rope, dims: AloraCacheDims) -> int:
     n = _check_lists(src, dst, shift)
     return int(lib().alora_cache_move_rows_validate(_ptr(src), _ptr(dst), _ptr(shift), n, 0 if rope is None else rope[0].shape[0], ctypes.byref(dims)))
+
+
+# ---- steps from lengths on the device, drafted trees, selected blocks ------------------------------
+# (include/alora_steps.h, alora_tree.h, alora_select.h).  Every tensor of a call is looked at: its type, that it is dense and holds what the call's sizes
+# say, and that it lies on the device the call goes to, the current one.
+def _check_tensors(tensors) -> None:
+    """tensors: (name, tensor, dtype, elements; a negative number: at least as many) each."""
+    device = _current_device() if _current_device is not None else _device_now()
+    for name, t, dtype, n in tensors:
+        if t.get_device() != device or t.dtype is not dtype or not t.is_contiguous() or (t.numel() != n if n >= 0 else t.numel() < -n):
+            if device >= 0 and not t.is_cuda:
+                _refuse_host(**{name: t})
+            if t.get_device() != device:
+                raise ValueError(f"{name}: a tensor on the current device, cuda:{device}, expected, got one on {t.device}")
+            _refuse(name, t, dtype, abs(n))
+    if device < 0:
+        _refuse_host(**{tensors[0][0]: tensors[0][1]})
+
+
+def _device_now() -> int:
+    """The current device, -1 without any."""
+    import torch
+    if not torch.cuda.is_available():
+        return -1
+    _stream_handle(None)
+    return _current_device()
+
+
+def _check_reader(q, k_cache, v_cache, block_tables, out, dims: AloraAttnDims):
+    """What the readers share, as _check_tensors takes it."""
+    dtype = (_types or _torch_types())[0][dims.dtype]
+    rows, slots = dims.n_tokens * dims.n_q_heads * dims.head_dim, dims.n_slots * dims.n_kv_heads * dims.head_dim
+    return (("q", q, dtype, rows), ("k_cache", k_cache, dtype, slots), ("v_cache", v_cache, dtype, slots),
+            ("block_tables", block_tables, _types[1], dims.n_seqs * dims.max_blocks), ("out", out, dtype, rows))
+
+
+def _bytes(t) -> int:
+    return 0 if t is None else t.nbytes
+
+
+def make_step_dims(block_tables, block_size: int, row_cap: int, pool, n_slots: int) -> AloraStepDims:
+    """Description of alora_step_rows calls: block_tables [n_seqs, max_blocks], pool a ring of block ids, row_cap rows of the token arrays."""
+    return AloraStepDims(block_tables.shape[0], block_tables.shape[1], block_size, row_cap, pool.shape[0], n_slots)
+
+
+def alora_step_rows(lengths, change, kept_blocks, seq_adapters, block_tables, pool, state, lengths_out, state_out, row_offsets, token_seq_ids,
+                    token_positions, token_adapter_ids, slot_mapping, dims: AloraStepDims, stream=None) -> None:
+    """Enqueue the step's rows, slots and block tables from the requests' lengths and changes (include/alora_steps.h); kept_blocks and seq_adapters may
+    be None."""
+    _, i32, i64 = _types or _torch_types()
+    n, rows = dims.n_seqs, dims.row_cap
+    _check_tensors((("lengths", lengths, i32, n), ("change", change, i32, n), ("block_tables", block_tables, i32, n * dims.max_blocks),
+                    ("pool", pool, i32, dims.pool_cap), ("state", state, i32, 6), ("lengths_out", lengths_out, i32, n), ("state_out", state_out, i32, 6),
+                    ("row_offsets", row_offsets, i32, n + 1), ("token_seq_ids", token_seq_ids, i32, rows), ("token_positions", token_positions, i32, rows),
+                    ("token_adapter_ids", token_adapter_ids, i32, rows), ("slot_mapping", slot_mapping, i64, rows)))
+    if kept_blocks is not None or seq_adapters is not None:
+        _check_tensors([(name, t, i32, n) for name, t in (("kept_blocks", kept_blocks), ("seq_adapters", seq_adapters)) if t is not None])
+    s = (_lib or lib()).alora_step_rows(lengths.data_ptr(), change.data_ptr(), _ptr(kept_blocks), _ptr(seq_adapters), block_tables.data_ptr(), pool.data_ptr(),
+                                        state.data_ptr(), lengths_out.data_ptr(), state_out.data_ptr(), row_offsets.data_ptr(), token_seq_ids.data_ptr(),
+                                        token_positions.data_ptr(), token_adapter_ids.data_ptr(), slot_mapping.data_ptr(), dims, _stream_handle(stream))
+    if s:
+        raise AloraError(s, "alora_step_rows")
+
+
+def alora_tree_rows(tree_parents, row_offsets, context_lens, tree_mask, token_positions, stream=None) -> None:
+    """Enqueue the masks (int64 [rows, words], bit j: the sequence's draft j is seen) and positions of drafted trees (include/alora_tree.h)."""
+    _, i32, i64 = _types or _torch_types()
+    (rows, words), seqs = tree_mask.shape, context_lens.shape[0]
+    _check_tensors((("tree_parents", tree_parents, i32, rows), ("row_offsets", row_offsets, i32, seqs + 1), ("context_lens", context_lens, i32, seqs),
+                    ("tree_mask", tree_mask, i64, rows * words), ("token_positions", token_positions, i32, rows)))
+    s = (_lib or lib()).alora_tree_rows(tree_parents.data_ptr(), row_offsets.data_ptr(), context_lens.data_ptr(), tree_mask.data_ptr(), token_positions.data_ptr(),
+                                        rows, seqs, words, _stream_handle(stream))
+    if s:
+        raise AloraError(s, "alora_tree_rows")
+
+
+def alora_tree_attention_workspace_bytes(dims: AloraAttnDims, mask_words: int) -> int:
+    out = ctypes.c_size_t(0)
+    s = lib().alora_tree_attention_workspace_bytes(ctypes.byref(dims), mask_words, ctypes.byref(out))
+    if s:
+        raise AloraError(s, "alora_tree_attention_workspace_bytes")
+    return int(out.value)
+
+
+def alora_tree_attention(q, k_cache, v_cache, block_tables, row_offsets, context_lens, tree_mask, out, dims: AloraAttnDims, workspace,
+                         stream=None) -> None:
+    """Enqueue attention of drafted trees over the paged cache (include/alora_tree.h); dims from make_attn_dims."""
+    shared = _check_reader(q, k_cache, v_cache, block_tables, out, dims)
+    _, i32, i64 = _types
+    words = tree_mask.shape[-1]
+    _check_tensors((*shared, ("row_offsets", row_offsets, i32, dims.n_seqs + 1), ("context_lens", context_lens, i32, dims.n_seqs),
+                    ("tree_mask", tree_mask, i64, dims.n_tokens * words)))
+    if workspace is not None and not workspace.is_cuda:
+        _refuse_host(workspace=workspace)
+    s = (_lib or lib()).alora_tree_attention(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_tables.data_ptr(), row_offsets.data_ptr(),
+                                             context_lens.data_ptr(), tree_mask.data_ptr(), words, out.data_ptr(), dims, _ptr(workspace), _bytes(workspace),
+                                             _stream_handle(stream))
+    if s:
+        raise AloraError(s, "alora_tree_attention")
+
+
+def make_bounds_dims(k_cache, slot_mapping, n_kv_heads: int, head_dim: int, block_size: int) -> AloraBoundsDims:
+    return AloraBoundsDims(_dtype_code(k_cache), slot_mapping.shape[0], n_kv_heads, head_dim, block_size, k_cache.shape[0])
+
+
+def alora_block_bounds(k_cache, slot_mapping, bounds, scales, dims: AloraBoundsDims, stream=None) -> None:
+    """Enqueue the bounds (int8 [blocks, n_kv_heads, 2, head_dim], fp32 scales [blocks, n_kv_heads]) of the blocks that the rows of slot_mapping lie
+    in (include/alora_select.h)."""
+    by_code, _, i64 = _types or _torch_types()
+    global _int8
+    if _int8 is None:
+        import torch
+        _int8 = torch.int8
+    heads = dims.n_slots // dims.block_size * dims.n_kv_heads
+    _check_tensors((("k_cache", k_cache, by_code[dims.dtype], dims.n_slots * dims.n_kv_heads * dims.head_dim), ("slot_mapping", slot_mapping, i64, -dims.n_rows),
+                    ("bounds", bounds, _int8, heads * 2 * dims.head_dim), ("scales", scales, by_code[ALORA_F32], heads)))
+    s = (_lib or lib()).alora_block_bounds(k_cache.data_ptr(), slot_mapping.data_ptr(), bounds.data_ptr(), scales.data_ptr(), dims, _stream_handle(stream))
+    if s:
+        raise AloraError(s, "alora_block_bounds")
+
+
+_int8 = None
+
+
+def alora_block_select_workspace_bytes(dims: AloraAttnDims) -> int:
+    out = ctypes.c_size_t(0)
+    s = lib().alora_block_select_workspace_bytes(ctypes.byref(dims), ctypes.byref(out))
+    if s:
+        raise AloraError(s, "alora_block_select_workspace_bytes")
+    return int(out.value)
+
+
+def alora_block_select(q, bounds, scales, block_tables, token_seq_ids, token_positions, selected, n_first: int, n_recent: int, dims: AloraAttnDims, workspace,
+                       stream=None) -> None:
+    """Enqueue the choice of the blocks that every row and K/V head reads: selected, int32 [rows, n_kv_heads, budget] (include/alora_select.h)."""
+    by_code, i32, _ = _types or _torch_types()
+    global _int8
+    if _int8 is None:
+        import torch
+        _int8 = torch.int8
+    t, budget, heads = dims.n_tokens, selected.shape[-1], dims.n_slots // dims.block_size * dims.n_kv_heads
+    _check_tensors((("q", q, by_code[dims.dtype], t * dims.n_q_heads * dims.head_dim), ("bounds", bounds, _int8, heads * 2 * dims.head_dim),
+                    ("scales", scales, by_code[ALORA_F32], heads), ("block_tables", block_tables, i32, dims.n_seqs * dims.max_blocks),
+                    ("token_seq_ids", token_seq_ids, i32, -t), ("token_positions", token_positions, i32, -t),
+                    ("selected", selected, i32, t * dims.n_kv_heads * budget)))
+    if workspace is not None and not workspace.is_cuda:
+        _refuse_host(workspace=workspace)
+    s = (_lib or lib()).alora_block_select(q.data_ptr(), bounds.data_ptr(), scales.data_ptr(), block_tables.data_ptr(), token_seq_ids.data_ptr(),
+                                           token_positions.data_ptr(), selected.data_ptr(), budget, n_first, n_recent, dims, _ptr(workspace), _bytes(workspace),
+                                           _stream_handle(stream))
+    if s:
+        raise AloraError(s, "alora_block_select")
+
+
+def alora_selected_attention_workspace_bytes(dims: AloraAttnDims, budget: int) -> int:
+    out = ctypes.c_size_t(0)
+    s = lib().alora_selected_attention_workspace_bytes(ctypes.byref(dims), budget, ctypes.byref(out))
+    if s:
+        raise AloraError(s, "alora_selected_attention_workspace_bytes")
+    return int(out.value)
+
+
+def alora_selected_attention(q, k_cache, v_cache, block_tables, token_seq_ids, token_positions, selected, out, dims: AloraAttnDims, workspace=None,
+                             stream=None) -> None:
+    """Enqueue attention over the selected blocks alone (include/alora_select.h); selected as alora_block_select leaves it."""
+    shared = _check_reader(q, k_cache, v_cache, block_tables, out, dims)
+    i32, t, budget = _types[1], dims.n_tokens, selected.shape[-1]
+    _check_tensors((*shared, ("token_seq_ids", token_seq_ids, i32, -t), ("token_positions", token_positions, i32, -t),
+                    ("selected", selected, i32, t * dims.n_kv_heads * budget)))
+    if workspace is not None and not workspace.is_cuda:
+        _refuse_host(workspace=workspace)
+    s = (_lib or lib()).alora_selected_attention(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_tables.data_ptr(), token_seq_ids.data_ptr(),
+                                                 token_positions.data_ptr(), selected.data_ptr(), budget, out.data_ptr(), dims, _ptr(workspace),
+                                                 _bytes(workspace), _stream_handle(stream))
+    if s:
+        raise AloraError(s, "alora_selected_attention")

@@ -19,96 +19,12 @@
 #include "alora_internal.h"
 #include "alora_attention.h"
 #include <type_traits>
-#include "alora_attention_internal.h"
+#include "alora_attention_core.h"
 #include <new>
 #include <algorithm>
 #include <vector>
 
 namespace alora {
-
-
-template <int CTRL>
-__device__ __forceinline__ float dpp_add(float v)
-{
-    const int o = __builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true);
-    return v + __int_as_float(o);
-}
-
-// sum over the LPP lanes that share a position; all of them receive it
-template <int LPP>
-__device__ __forceinline__ float group_sum(float v)
-{
-    v = dpp_add<0xB1>(v);    // quad_perm [1,0,3,2]
-    v = dpp_add<0x4E>(v);    // quad_perm [2,3,0,1]
-    v = dpp_add<0x141>(v);   // row_half_mirror: the other quad of the 8 lanes
-    if (LPP == 16) v = dpp_add<0x140>(v);   // row_mirror: the other half of the 16 lanes
-    return v;
-}
-
-// 8 consecutive elements of a cache or query row, as loaded
-template <bool BF16> struct Raw8;
-template <> struct Raw8<true> {
-    u32x4 v;
-    __device__ __forceinline__ void zero() { v = u32x4{0u, 0u, 0u, 0u}; }
-    template <bool STREAM = false>
-    __device__ __forceinline__ void load(const void *base, size_t elem)
-    {
-        const u32x4 *p = (const u32x4 *)((const bf16_t *)base + elem);
-        v = STREAM ? __builtin_nontemporal_load(p) : *p;
-    }
-    __device__ __forceinline__ void widen(float f[8]) const
-    {
-        f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xffff0000u);
-        f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xffff0000u);
-        f[4] = __uint_as_float(v.z << 16); f[5] = __uint_as_float(v.z & 0xffff0000u);
-        f[6] = __uint_as_float(v.w << 16); f[7] = __uint_as_float(v.w & 0xffff0000u);
-    }
-};
-template <> struct Raw8<false> {
-    f32x4 a, b;
-    __device__ __forceinline__ void zero() { a = f32x4{0.f, 0.f, 0.f, 0.f}; b = a; }
-    template <bool = false>    // (always ordinary loads)
-    __device__ __forceinline__ void load(const void *base, size_t elem)
-    {
-        a = *(const f32x4 *)((const float *)base + elem);
-        b = *(const f32x4 *)((const float *)base + elem + 4);
-    }
-    __device__ __forceinline__ void widen(float f[8]) const
-    {
-        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
-        f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-    }
-};
-
-constexpr float NEG_INF = -__builtin_inff();
-
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-typedef __attribute__((ext_vector_type(2))) float f32x2;
-
-// <q chunk, k chunk> over 8 elements.  bf16: four packed two-element dot products on the stored bits
-// (fp32 accumulate); fp32: eight FMAs.  The pairs are taken with shufflevector on the 8-element vector:
-// bit casts of the single 32-bit words were compiled into four uses of the first word by this toolchain.
-__device__ __forceinline__ float dot8(const Raw8<true> &q, const Raw8<true> &k)
-{
-    const bf16x8 qv = __builtin_bit_cast(bf16x8, q.v), kv = __builtin_bit_cast(bf16x8, k.v);
-    float d = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(qv, qv, 0, 1), __builtin_shufflevector(kv, kv, 0, 1), 0.f, false);
-    d = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(qv, qv, 2, 3), __builtin_shufflevector(kv, kv, 2, 3), d, false);
-    d = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(qv, qv, 4, 5), __builtin_shufflevector(kv, kv, 4, 5), d, false);
-    d = __builtin_amdgcn_fdot2_f32_bf16(__builtin_shufflevector(qv, qv, 6, 7), __builtin_shufflevector(kv, kv, 6, 7), d, false);
-    return d;
-}
-__device__ __forceinline__ float dot8(const Raw8<false> &q, const Raw8<false> &k)
-{
-    float d = q.a.x * k.a.x;
-    d = fmaf(q.a.y, k.a.y, d); d = fmaf(q.a.z, k.a.z, d); d = fmaf(q.a.w, k.a.w, d);
-    d = fmaf(q.b.x, k.b.x, d); d = fmaf(q.b.y, k.b.y, d); d = fmaf(q.b.z, k.b.z, d); d = fmaf(q.b.w, k.b.w, d);
-    return d;
-}
-
-// The running maximum starts at a large negative FINITE number: differences with it stay finite, so the
-// softmax needs no "nothing seen yet" cases (a position that is left out scores -inf and weighs
-// exp2(-inf) = 0).  Scores below it are treated like -inf.
-constexpr float M_FLOOR = -1.0e30f;
 
 // What is known of a call's contexts: nothing, that there are no more rows than sequences (see contexts_read_once), or that there are several turns
 // of workgroups of them besides, which take the longest first: whole contexts (in runs of `sorted` batch rows), or some in more parts than others.
@@ -599,7 +515,7 @@ static bool launch_d(const AttnArgs &a, int G, bool bf16, hipStream_t st)
     return false;
 }
 
-static int check_dims(const alora_attn_dims *d)
+int check_attention(const alora_attn_dims *d)
 {
     if (!d) return ALORA_EINVAL;
     if (d->dtype != ALORA_F32 && d->dtype != ALORA_BF16) return ALORA_EINVAL;
@@ -668,7 +584,7 @@ int alora_paged_attention_workspace_bytes(const alora_attn_dims *dims, size_t *o
 {
     using namespace alora;
     if (!out_bytes) return ALORA_EINVAL;
-    const int st = check_dims(dims);
+    const int st = check_attention(dims);
     if (st) return st;
     *out_bytes = split_bytes(dims, plan_splits(dims));
     return ALORA_OK;
@@ -694,7 +610,7 @@ int alora_paged_attention_suffix_workspace_bytes(const alora_attn_dims *dims, si
 {
     using namespace alora;
     if (!out_bytes) return ALORA_EINVAL;
-    const int st = check_dims(dims);
+    const int st = check_attention(dims);
     if (st) return st;
     if (dims->dtype != ALORA_BF16 || dims->head_dim != 128) return ALORA_ESHAPE;
     *out_bytes = block_split_bytes(dims);
@@ -725,7 +641,7 @@ static int run(const void *q, const void *k_cache, const void *v_cache, const in
                const int32_t *token_seq_ids, const int32_t *token_positions, void *out, const alora_attn_dims *dims,
                void *workspace, size_t workspace_bytes, Reader mode, void *hip_stream)
 {
-    const int st = check_dims(dims);
+    const int st = check_attention(dims);
     if (st) return st;
     const bool blocks_asked = mode == ROW_BLOCKS || mode == ROW_BLOCKS_SPLIT;
     if (blocks_asked && (dims->dtype != ALORA_BF16 || dims->head_dim != 128)) return ALORA_ESHAPE;
@@ -789,7 +705,7 @@ int alora_paged_attention_validate(const int32_t *block_tables, const int32_t *t
                                    const int32_t *token_positions, const alora_attn_dims *dims)
 {
     using namespace alora;
-    const int st = check_dims(dims);
+    const int st = check_attention(dims);
     if (st) return st;
     if (dims->n_tokens == 0) return ALORA_OK;
     if (!block_tables || !token_seq_ids || !token_positions) return ALORA_EINVAL;

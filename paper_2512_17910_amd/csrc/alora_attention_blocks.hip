@@ -36,56 +36,10 @@
 // scores of the next block and the output of the one before it between the vector instructions of the softmax
 // (three blocks in flight, one matrix product per four vector instructions) was built and measured: 2470 us.
 #include <numeric>
-#include "alora_attention_internal.h"
+#include "alora_attention_core.h"
 
 namespace alora {
 
-typedef __attribute__((ext_vector_type(4))) short s16x4;
-typedef __attribute__((ext_vector_type(8))) short s16x8;
-typedef __attribute__((ext_vector_type(2))) float f32x2;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-typedef __attribute__((address_space(3))) unsigned char lds_byte;
-
-constexpr float AB_NEG_INF = -__builtin_inff();
-constexpr float AB_M_FLOOR = -1.0e30f;   // finite floor of the running maximum (scores below it weigh nothing)
-
-// four k of this lane's column, then the four that lie eight rows further on
-__device__ __forceinline__ bf16x8 read_tr_frag(const lds_byte *p, int pitch)
-{
-    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)p);
-    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(p + 8 * pitch));
-    const s16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    return __builtin_bit_cast(bf16x8, v);
-}
-
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
-{
-    const f32x2 v = {lo, hi};
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
-}
-
-// 16 bytes straight from global memory into LDS at lds_addr + 16 * lane.  An assembly statement: the
-// kernel orders these copies against its LDS reads itself (wait counts and barriers in the main loop).
-__device__ __forceinline__ void load_lds16(uint32_t lds_addr, const void *p)
-{
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds_addr), "v"(p) : "memory");
-}
-// the same with a scalar base address and a 32-bit byte offset per lane; ONCE: no other workgroup will read these bytes
-template <bool ONCE>
-__device__ __forceinline__ void load_lds16(uint32_t lds_addr, const void *base, uint32_t voffset)
-{
-    if constexpr (ONCE) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" : : "s"(lds_addr), "v"(voffset), "s"(base) : "memory");
-    else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds_addr), "v"(voffset), "s"(base) : "memory");
-}
-// Exchange between the two lanes of a column (lanes c, c+32), as an assembly statement (the builtin returned its
-// first result twice) with wait states on both sides, which the compiler cannot place for an instruction it does
-// not see.  Checked with an in-bounds probe:
-//   v_permlane32_swap on two copies of x: lo <- x of the lower 32 lanes, hi <- the upper 32 lanes'
-__device__ __forceinline__ void both_halves(float x, float &lo, float &hi)
-{
-    lo = x, hi = x;
-    asm("s_nop 3\n\tv_permlane32_swap_b32 %0, %1\n\ts_nop 3" : "+v"(lo), "+v"(hi));
-}
 // sums of floats, and largest from 0 on, over lanes 0 .. lane
 __device__ __forceinline__ float sum_upto64(float x)
 {
@@ -105,9 +59,6 @@ __device__ __forceinline__ int max_upto64(int x)
     x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));
     return max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
 }
-// what a lane loads for a position that is not part of the context (the weighted sum multiplies it by 0)
-__device__ const uint32_t ab_zero_chunk[4] = {0u, 0u, 0u, 0u};
-
 // whether the kernel settles the number of parts (a kernel of its own: what the counting adds costs 2 x 2 rows at 2000 positions 1.3 of 13 us)
 struct AsPlanned { static constexpr bool count = false, once = false; };
 struct Counted { static constexpr bool count = true, once = false; };

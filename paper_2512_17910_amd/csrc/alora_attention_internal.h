@@ -18,6 +18,9 @@ struct AttnArgs {
     float *part;         // [T][Hq][splits][D + 2]: running maximum, sum of weights, unnormalised weighted V
 };
 
+// What the readers' entry points check of dims; a status.
+int check_attention(const alora_attn_dims *d);
+
 constexpr int MAX_PARTS = 32;   // of a row's context
 
 // A layer's K and V that the memory-side cache (256 MB) would not keep until they are read again.

@@ -1,0 +1,263 @@
+// Attention of drafted tokens that form a tree over the paged cache (include/alora_tree.h).
+//
+// The rows of a sequence read the same context, so a workgroup takes a tile of them and loads every cached row once for all; what a row
+// sees of the drafts, which lie behind the context, a mask says.  The contexts are cut into parts of one length, found on the device
+// from all lengths of the call (their sum is not known on the host), so that workgroups have equal work however ragged the lengths are.
+#include <algorithm>
+#include <new>
+#include "alora_tree.h"
+#include "alora_listed.h"
+
+namespace alora {
+
+// A tile of a sequence's rows, for the kernel that combines its parts.
+struct TreeTile {
+    int row0, rows, parts, first, step, pad[3];
+};
+
+struct TreeArgs {
+    ListArgs list;
+    const int32_t *offsets, *context;
+    const uint32_t *mask;       // [T][2 * words]
+    int words, tile_rows;       // rows of a tile
+    int target;                 // workgroups per K/V head the parts are cut for
+    int max_tiles, max_items;   // the workspace has room for (offsets that do not ascend may give more)
+    int *n_tiles;
+    TreeTile *tiles;
+};
+
+constexpr int UNIT = 32;        // positions that parts are counted in
+constexpr int LEAST_UNITS = 8;  // of a part
+
+struct TreeItem {
+    int row0, rows;             // the tile's rows
+    int seq, ctx, drafts;       // drafts: those that lie in the table
+    int lo, hi, parts, part_at; // places of the sequence this workgroup reads; number of its part's sums
+};
+
+struct TreeScratch {
+    float total[4];
+    int sums[4][2], found[8];
+};
+
+// Which tile and part workgroup `item` (of one K/V head) is for; false: none.  The same sums in every workgroup of the call.
+__device__ __forceinline__ bool find_item(const TreeArgs &a, int item, int hk, TreeScratch &scr, TreeItem &it)
+{
+    const ListArgs &g = a.list;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, n_seqs = g.n_seqs;
+    const long long cap = min((long long)g.max_blocks * g.bs, 0x7fffffffll);
+    struct Seq { int r0, n, ctx, places, tiles, units; };
+    auto seq_of = [&](int s) {
+        Seq q = {0, 0, 0, 0, 0, 0};
+        if (s < n_seqs) {
+            q.r0 = min(max(a.offsets[s], 0), g.T);
+            q.n = min(max(a.offsets[s + 1], q.r0), g.T) - q.r0;
+            q.ctx = (int)min((long long)max(a.context[s], 0), cap);
+            q.places = (int)min((long long)q.ctx + min(q.n, 64 * a.words), cap);
+            q.tiles = (q.n + a.tile_rows - 1) / a.tile_rows;
+            q.units = (q.places + UNIT - 1) / UNIT;
+        }
+        return q;
+    };
+    // all units of all tiles, in a fixed order
+    Seq q = seq_of(tid);
+    float mine = 0.f;
+    for (int s = tid;; s += 256) {
+        const Seq x = s == tid ? q : seq_of(s);
+        mine += (float)x.tiles * (float)x.units;
+        if (s + 256 >= n_seqs) break;
+    }
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) mine += __shfl_xor(mine, off);
+    if (lane == 0) scr.total[w] = mine;
+    if (tid == 0) scr.found[0] = -1;
+    __syncthreads();
+    const float total = scr.total[0] + scr.total[1] + scr.total[2] + scr.total[3];
+    const int per = max(LEAST_UNITS, (int)fminf(ceilf(total / (float)a.target), 1.0e9f));
+    int items0 = 0, tiles0 = 0;
+    for (int s0 = 0; s0 < n_seqs; s0 += 256) {
+        if (s0) q = seq_of(s0 + tid);
+        const int parts = max(1, (q.units + per - 1) / per), items = q.tiles * parts;
+        const int u = sum_upto64(items), v = sum_upto64(q.tiles);
+        if (lane == 63) scr.sums[w][0] = u, scr.sums[w][1] = v;
+        __syncthreads();
+        int at = items0 + u - items, tile_at = tiles0 + v - q.tiles;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (i < w) at += scr.sums[i][0], tile_at += scr.sums[i][1];
+            items0 += scr.sums[i][0], tiles0 += scr.sums[i][1];
+        }
+        if (item >= at && item < at + items) {
+            const int i = item - at, part = i / q.tiles, tile = i - part * q.tiles;      // (tiles of one part next to each other: they read the same rows)
+            const int row0 = q.r0 + tile * a.tile_rows, rows = min(a.tile_rows, q.n - tile * a.tile_rows);
+            scr.found[0] = s0 + tid;
+            scr.found[1] = row0;
+            scr.found[2] = rows;
+            scr.found[3] = q.ctx;
+            scr.found[4] = q.places - q.ctx;
+            scr.found[5] = part;
+            scr.found[6] = parts;
+            if (hk == 0 && part == 0 && tile_at + tile < a.max_tiles) a.tiles[tile_at + tile] = {row0, rows, parts, at + tile, q.tiles, {}};
+        }
+        __syncthreads();
+        if (scr.found[0] >= 0 && item != 0) break;       // (workgroup 0 counts all tiles)
+    }
+    if (item == 0 && hk == 0 && tid == 0) *a.n_tiles = min(tiles0, a.max_tiles);
+    if (scr.found[0] < 0) return false;
+    it.seq = scr.found[0], it.row0 = scr.found[1], it.rows = scr.found[2], it.ctx = scr.found[3], it.drafts = scr.found[4], it.parts = scr.found[6];
+    const int part = scr.found[5], places = it.ctx + it.drafts;
+    it.lo = (int)min((long long)part * per * UNIT, (long long)places);
+    it.hi = (int)min((long long)it.lo + (long long)per * UNIT, (long long)places);
+    it.part_at = item;
+    return true;
+}
+
+// Rows of no sequence: zeros.  The last workgroup of a K/V head.
+template <int D, bool BF16>
+__device__ __forceinline__ void clear_rows(const TreeArgs &a, int hk)
+{
+    const ListArgs &g = a.list;
+    const int begin = g.n_seqs ? min(max(a.offsets[0], 0), g.T) : 0, end = g.n_seqs ? min(max(a.offsets[g.n_seqs], begin), g.T) : 0;
+    const int chunks = (D << g.lg_g) * (BF16 ? 2 : 4) / 16;
+    const size_t width = (size_t)g.Hq * D * (BF16 ? 2 : 4);
+    auto clear = [&](int t0, int t1) {
+        for (long long i = threadIdx.x; i < (long long)(t1 - t0) * chunks; i += 256)
+            *(u32x4 *)((char *)g.out + (t0 + i / chunks) * width + ((size_t)hk * chunks + i % chunks) * 16) = (u32x4){0u, 0u, 0u, 0u};
+    };
+    clear(0, begin);
+    clear(end, g.T);
+}
+
+// C columns: C >> lg_g rows of a sequence.
+template <int D, int C, bool BF16>
+__global__ __launch_bounds__(256) void tree_vector_kernel(TreeArgs a)
+{
+    __shared__ VectorScratch<C, D> scr;
+    __shared__ TreeScratch find;
+    __shared__ uint32_t bits[C][2 * ALORA_MAX_TREE_WORDS];
+    const ListArgs &g = a.list;
+    const int hk = (int)blockIdx.x % g.Hkv, item = (int)blockIdx.x / g.Hkv, tid = threadIdx.x;
+    if (item == (int)(gridDim.x / g.Hkv) - 1) return clear_rows<D, BF16>(a, hk);
+    TreeItem it;
+    if (!find_item(a, item, hk, find, it)) return;
+    const int G = 1 << g.lg_g;
+    if (tid < 2 * a.words * it.rows) bits[tid / (2 * a.words)][tid % (2 * a.words)] = a.mask[(size_t)it.row0 * 2 * a.words + tid];
+    __syncthreads();
+    const int32_t *bt = g.bt + (size_t)it.seq * g.max_blocks;
+    const auto column_at = [&](int c) { return (((long long)it.row0 + (c >> g.lg_g)) * g.Hq + hk * G + (c & (G - 1))) * D; };
+    read_list_vector<D, C, BF16>(
+        g, hk, scr, it.lo, it.hi, it.ctx,
+        [&](int v) { return slot_at(g, bt, v / g.bs, v % g.bs); },
+        [&](int c, int v) { return v < it.ctx || (bits[c >> g.lg_g][(v - it.ctx) >> 5] >> ((v - it.ctx) & 31) & 1u); },
+        [&](int c) { return c >> g.lg_g < it.rows ? column_at(c) : -1ll; },
+        [&](int c, int d, float M, float L, float o) {
+            if (c >> g.lg_g >= it.rows) return;
+            if (it.parts > 1) {
+                const size_t at = ((size_t)it.part_at * g.Hkv + hk) * C + c;
+                if (d == 0) *(f32x2 *)(g.ml + 2 * at) = (f32x2){M, L};
+                g.o[at * D + d] = o;
+                return;
+            }
+            const float y = L == 0.f ? 0.f : o / L;
+            if (BF16) ((bf16_t *)g.out)[column_at(c) + d] = (bf16_t)f32_to_bf16_bits(y);
+            else ((float *)g.out)[column_at(c) + d] = y;
+        });
+}
+
+// One wavefront per column of a tile that has parts.
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int columns)
+{
+    const ListArgs &g = a.list;
+    const int c = (int)blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hk = (int)blockIdx.x % g.Hkv, tile = (int)blockIdx.x / g.Hkv;
+    if (tile >= *a.n_tiles) return;
+    const TreeTile t = a.tiles[tile];
+    if (t.parts <= 1 || c >> g.lg_g >= t.rows || (long long)t.first + (long long)(t.parts - 1) * t.step >= a.max_items) return;
+    combine_parts<D, BF16>(g, (size_t)t.first * g.Hkv + hk, (size_t)t.step * g.Hkv, t.parts, columns, c,
+                           ((size_t)(t.row0 + (c >> g.lg_g)) * g.Hq + ((size_t)hk << g.lg_g) + (c & ((1 << g.lg_g) - 1))) * D);
+}
+
+// ---- host ---------------------------------------------------------------------------------------
+// How a call is cut: columns of a tile, the most tiles and items (tile, part) of a K/V head there can be, and where the workspace's arrays lie.
+struct TreePlan {
+    int columns, tile_rows, target;
+    long long tiles, items;
+    size_t tiles_at, ml_at, o_at, bytes;
+};
+static TreePlan plan_tree(const alora_attn_dims *d)
+{
+    TreePlan p;
+    const int G = d->n_q_heads / d->n_kv_heads;
+    p.columns = 8;
+    p.tile_rows = p.columns / G;
+    p.target = std::max(1, 1024 / d->n_kv_heads);
+    p.tiles = d->n_tokens / p.tile_rows + std::min(d->n_seqs, d->n_tokens);      // (a sequence's last tile may not be full)
+    p.items = p.tiles + p.target + 1;                                            // sum of ceil(units / per) over tiles, per >= all units / target
+    const auto up = [](size_t n) { return (n + 255) / 256 * 256; };
+    p.tiles_at = 256;
+    p.ml_at = p.tiles_at + up((size_t)p.tiles * sizeof(TreeTile));
+    p.o_at = p.ml_at + up((size_t)p.items * d->n_kv_heads * p.columns * 8);
+    p.bytes = p.o_at + (size_t)p.items * d->n_kv_heads * p.columns * d->head_dim * 4;
+    return p;
+}
+
+static int check_tree(const alora_attn_dims *d, int words)
+{
+    const int st = check_attention(d);
+    if (st) return st;
+    if (words < 1 || words > ALORA_MAX_TREE_WORDS || d->n_seqs > 1 << 20) return ALORA_ESHAPE;
+    if (plan_tree(d).items * d->n_kv_heads > 0x3fffffffll) return ALORA_ESHAPE;
+    return ALORA_OK;
+}
+
+}  // namespace alora
+
+using namespace alora;
+
+extern "C" {
+
+int alora_tree_attention_workspace_bytes(const alora_attn_dims *dims, int32_t mask_words, size_t *out_bytes)
+{
+    if (!out_bytes) return ALORA_EINVAL;
+    const int st = check_tree(dims, mask_words);
+    if (st) return st;
+    *out_bytes = dims->n_tokens ? plan_tree(dims).bytes : 0;
+    return ALORA_OK;
+}
+
+int alora_tree_attention(const void *q, const void *k_cache, const void *v_cache, const int32_t *block_tables, const int32_t *row_offsets,
+                         const int32_t *context_lens, const uint64_t *tree_mask, int32_t mask_words, void *out, const alora_attn_dims *dims,
+                         void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    const int st = check_tree(dims, mask_words);
+    if (st) return st;
+    if (dims->n_tokens == 0) return ALORA_OK;
+    const TreePlan p = plan_tree(dims);
+    if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < p.bytes) return ALORA_EWORKSPACE;
+    if (!q || !k_cache || !v_cache || !block_tables || !row_offsets || !context_lens || !tree_mask || !out) return ALORA_EINVAL;
+    if (((uintptr_t)q | (uintptr_t)k_cache | (uintptr_t)v_cache | (uintptr_t)out) & 15 || (uintptr_t)tree_mask & 7) return ALORA_EINVAL;
+    if (((uintptr_t)block_tables | (uintptr_t)row_offsets | (uintptr_t)context_lens) & 3) return ALORA_EINVAL;
+    TreeArgs a;
+    a.list = list_args(dims, q, k_cache, v_cache, block_tables, out);
+    a.list.ml = (float *)((char *)workspace + p.ml_at);
+    a.list.o = (float *)((char *)workspace + p.o_at);
+    a.offsets = row_offsets; a.context = context_lens;
+    a.mask = (const uint32_t *)tree_mask; a.words = mask_words;
+    a.tile_rows = p.tile_rows; a.target = p.target;
+    a.max_tiles = (int)p.tiles; a.max_items = (int)p.items;
+    a.n_tiles = (int *)workspace;
+    a.tiles = (TreeTile *)((char *)workspace + p.tiles_at);
+    const bool bf16 = dims->dtype == ALORA_BF16;
+    const dim3 grid((unsigned)((p.items + 1) * dims->n_kv_heads)), merge((unsigned)(p.tiles * dims->n_kv_heads), (unsigned)p.columns / 4);
+    const auto go = [&](auto kernel, auto combine) {
+        launch_kernel(kernel, grid, dim3(256), 0, (hipStream_t)hip_stream, a);
+        launch_kernel(combine, merge, dim3(256), 0, (hipStream_t)hip_stream, a, p.columns);
+    };
+    if (dims->head_dim == 128) bf16 ? go(tree_vector_kernel<128, 8, true>, tree_merge_kernel<128, true>) : go(tree_vector_kernel<128, 8, false>, tree_merge_kernel<128, false>);
+    else bf16 ? go(tree_vector_kernel<64, 8, true>, tree_merge_kernel<64, true>) : go(tree_vector_kernel<64, 8, false>, tree_merge_kernel<64, false>);
+    const int e = launch_status();
+    if (e) { note_hip_error(e); return ALORA_EHIP; }
+    return ALORA_OK;
+}
+
+}  // extern "C"
