@@ -177,6 +177,296 @@ __device__ __forceinline__ void read_list_vector(const ListArgs &a, int hk, Vect
     }
 }
 
+// ---- matrix instructions: 32 columns a wavefront, bf16 ---------------------------------------------
+// The wavefronts of a workgroup share tiles of 32 places in LDS, which all of them copy and each multiplies with its own 32 columns
+// (32x32x16 products): scores^T = K Q^T leaves a column in two lanes, down which the softmax runs, and out^T += V^T P takes the weights from the
+// score registers.  Rows of K and V go from global memory straight into LDS, two tiles of each per barrier, NB in flight or in use.
+// A lane copies 16 bytes of a row; which of the row's 16-byte chunks is rotated by the row (XOR), so that neither the reads of K fragments (one
+// chunk of 32 rows) nor the transposing reads of V (four chunks of four rows) meet in a bank.
+template <int D, int NW>
+struct MatrixTiles {
+    static constexpr int PITCH = 2 * D, TILE = 32 * PITCH;      // bytes of a row, of 32
+    static constexpr int NB = (NW == 8 ? 98304 : 65536) / (2 * TILE);
+    static constexpr int LPR = D / 8, R = 64 / LPR;             // lanes per row, rows per copy
+    static constexpr int GROUPS = 32 / R;                       // copies of a tile
+    static constexpr int IPW = 2 * GROUPS / NW;                 // copies a wavefront makes of 32 places: K and V
+    static constexpr int GPW = GROUPS < NW ? 1 : GROUPS / NW;   // groups of rows it copies (of eight wavefronts and heads of 64, half copy K, half V)
+    static constexpr int SP = PITCH + 16;                       // bytes per column where results are turned around
+    static_assert(NB % 2 == 0 && NB >= 4 && IPW >= 1 && 32 * SP * NW <= NB * 2 * TILE, "tiles");
+    __attribute__((aligned(1024))) unsigned char tiles[NB * 2 * TILE];
+    int slots[LIST_WINDOW];
+    uint32_t ok[LIST_WINDOW / 32], tile_ok[NB];
+};
+
+// Whether either bf16 of x is not finite.
+__device__ __forceinline__ bool not_finite2(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
+
+//   columns        of the workgroup that exist; a wavefront beyond them only copies
+//   masked_from    places from here on are seen by some columns only: seen(place) = 32 bits of this lane's column, place a multiple of 32 from lo on
+//   q_at, out_at   element of q and out where this lane's column begins (column `col`)
+//   part           < 0: rows of out; else number of the part whose sums are left, of room for part_columns columns
+// WHOLE: the weights go into the product with V as two bf16 numbers (their rounding then adds nothing to that of the result), for twice
+// the products.  ONCE: rows are not read again soon (non-temporal copies).
+template <int D, int NW, bool WHOLE, bool ONCE, class SlotOf, class Seen>
+__device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, MatrixTiles<D, NW> &lds, int lo, int hi, int masked_from, int columns, SlotOf slot_of,
+                                                 Seen seen, size_t q_at, size_t out_at, long long part, int part_columns)
+{
+    typedef MatrixTiles<D, NW> L;
+    constexpr int NB = L::NB, TILE = L::TILE, PITCH = L::PITCH, WIN = LIST_WINDOW / 32, KS = D / 16, DT = D / 32;
+    typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
+    typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+    const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c16 = lane & 15, li = lane & 31, lh = lane >> 5;
+    const int col = 32 * w + li;
+    const bool col_ok = col < columns, work = 32 * w < columns;
+    const uint32_t tiles_at = (uint32_t)(uintptr_t)(lds_byte *)lds.tiles, row_bytes = (uint32_t)a.Hkv * (uint32_t)PITCH, head = (uint32_t)hk * (uint32_t)PITCH;
+    const int c_hi = (hi - lo + 31) >> 5;                       // tiles of this part
+
+    bf16x8 qf[KS];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+        u32x4 v = {0u, 0u, 0u, 0u};
+        if (col_ok) v = *(const u32x4 *)((const bf16_t *)a.q + q_at + 16 * s + 8 * lh);
+        qf[s] = __builtin_bit_cast(bf16x8, v);
+    }
+    f32x16 acc[DT];
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[t][e] = 0.f;
+    float m = M_FLOOR, l = 0.f;
+
+    // ---- the window: slots of WIN tiles, and which of their places there are -----------------------
+    int win = 0;                                                // first tile of the window
+    auto refill = [&](int c) {
+        win = c;
+        __syncthreads();
+        const int end = min(32 * WIN, hi - lo - 32 * c);
+        for (int i = tid; i - lane < end; i += 64 * NW) {
+            const int s = i < end ? slot_of(lo + 32 * c + i) : -1;
+            lds.slots[i] = s;
+            const unsigned long long have = __builtin_amdgcn_ballot_w64(s >= 0);
+            if (li == 0) lds.ok[i >> 5] = (uint32_t)(lh ? have >> 32 : have);
+        }
+        __syncthreads();
+    };
+    // ---- copies -------------------------------------------------------------------------------------
+    struct Entry {
+        int slot[L::GPW];
+        uint32_t ok;
+    };
+    const int first_group = L::GROUPS < NW ? w % L::GROUPS : w;
+    auto lookup = [&](int c) {
+        Entry e;
+#pragma unroll
+        for (int g = 0; g < L::GPW; ++g) e.slot[g] = -1;
+        e.ok = 0;
+        if (c < c_hi) {
+#pragma unroll
+            for (int g = 0; g < L::GPW; ++g) e.slot[g] = lds.slots[32 * (c - win) + (first_group + g * NW) * L::R + lane / L::LPR];
+            e.ok = lds.ok[c - win];
+        }
+        return e;
+    };
+    const uint32_t chunk = (uint32_t)(lane % L::LPR);
+    auto issue = [&](int pair, const Entry &e) {
+#pragma unroll
+        for (int i = 0; i < L::IPW; ++i) {
+            const int g = i % L::GPW, group = first_group + g * NW;
+            const bool v = L::GROUPS < NW ? w >= L::GROUPS : i >= L::GPW;       // K first, then V
+            const int row = group * L::R + lane / L::LPR;
+            const uint32_t turn = v ? (D == 128 ? (uint32_t)(row & 3) << 2 : (uint32_t)(row >> 1 & 1) << 2) : D == 128 ? (uint32_t)(row & 15) : (uint32_t)(row >> 1 & 7);
+            const char *at = (const char *)(v ? a.vc : a.kc) + (unsigned long long)(uint32_t)e.slot[g] * row_bytes + (head + ((chunk ^ turn) << 4));
+            const void *from = e.slot[g] >= 0 ? (const void *)at : (const void *)ab_zero_chunk;
+            const uint32_t to = tiles_at + (uint32_t)pair * (2 * TILE) + (v ? TILE : 0) + ((uint32_t)group << 10);
+            if constexpr (ONCE) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" : : "s"(to), "v"(from) : "memory");
+            else load_lds16(to, from);
+        }
+        lds.tile_ok[pair] = e.ok;                               // (the same value from every lane)
+    };
+    // ---- products -----------------------------------------------------------------------------------
+    const uint32_t k_base = (uint32_t)li * PITCH + (uint32_t)((lh ^ (D == 128 ? li & 15 : li >> 1 & 7)) << 4);
+    uint32_t v_base;
+    {
+        const int j = c16 >> 2, row = 4 * lh + j;
+        const uint32_t turn = D == 128 ? (uint32_t)j << 2 : (uint32_t)(j >> 1) << 2;
+        v_base = (uint32_t)row * PITCH + (((uint32_t)(2 * (lane >> 4 & 1) + ((c16 & 3) >> 1)) ^ turn) << 4) + (uint32_t)((c16 & 1) << 3);
+    }
+    auto consume = [&](int c, int pair) {
+        const lds_byte *kb = (const lds_byte *)lds.tiles + pair * (2 * TILE), *vb = kb + TILE;
+        f32x16 sc;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) sc[v] = 0.f;
+        bf16x8 kf[KS];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) kf[ks] = *(const __attribute__((address_space(3))) bf16x8 *)(kb + (k_base ^ (uint32_t)(ks << 5)));
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[ks], sc, 0, 0, 0);
+        const uint32_t ok = __builtin_amdgcn_readfirstlane(lds.tile_ok[pair]);
+        bf16x8 vf[2][DT];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int t = 0; t < DT; ++t) vf[s][t] = read_tr_frag(vb + (v_base ^ (uint32_t)(t << 6)) + s * 16 * PITCH, PITCH);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(2);
+        const int place = lo + 32 * c;
+        const bool some = place + 31 >= masked_from;
+        if (some || ok != 0xffffffffu) {
+            const uint32_t on = some ? ok & seen(place) : ok;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) sc[v] = on >> (8 * (v >> 2) + 4 * lh + (v & 3)) & 1u ? sc[v] : NEG_INF;
+        }
+        float mx = fmaxf(sc[0], sc[1]);
+#pragma unroll
+        for (int v = 2; v < 16; v += 2) mx = fmaxf(fmaxf(mx, sc[v]), sc[v + 1]);
+        if (__builtin_amdgcn_ballot_w64(mx * a.scale_log2e > m)) {       // (most tiles of a long list bring no new maximum)
+            float x, y;
+            both_halves(mx, x, y);
+            const float mn = fmaxf(m, fmaxf(x, y) * a.scale_log2e);
+            const float corr = __builtin_amdgcn_exp2f(m - mn);
+            m = mn;
+            l *= corr;
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[t][e] *= corr;
+        }
+        float ps = 0.f;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            sc[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[v], a.scale_log2e, -m));
+            ps += sc[v];
+        }
+        l += ps;
+        u32x4 pv[2], pr[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float x = sc[8 * s + 2 * i], y = sc[8 * s + 2 * i + 1];
+                pv[s][i] = pack_bf16(x, y);
+                if (WHOLE) pr[s][i] = pack_bf16(x - __uint_as_float(pv[s][i] << 16), y - __uint_as_float(pv[s][i] & 0xffff0000u));
+            }
+        __builtin_amdgcn_s_setprio(0);
+        if (some) {
+            // A value that some columns do not see may be anything: what is not finite leaves the product (where it would be multiplied by their zeros)
+            // and is added for the columns that do see it.
+            bool any = false;
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int t = 0; t < DT; ++t) {
+                    u32x4 x = __builtin_bit_cast(u32x4, vf[s][t]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) any |= not_finite2(x[i]);
+                }
+            if (__builtin_amdgcn_ballot_w64(any)) {
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int t = 0; t < DT; ++t) {
+                        u32x4 x = __builtin_bit_cast(u32x4, vf[s][t]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if ((x[i] & 0x7f80u) == 0x7f80u) x[i] &= 0xffff0000u;
+                            if ((x[i] & 0x7f800000u) == 0x7f800000u) x[i] &= 0xffffu;
+                        }
+                        vf[s][t] = __builtin_bit_cast(bf16x8, x);
+                    }
+#pragma unroll 1
+                for (int i = 0; i < 32; ++i) {
+                    // the weight of place i: in register (i / 8) * 4 + i % 4 of the lane with lh = i / 4 % 2
+                    float mine = 0.f;
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) mine = (i >> 3) * 4 + (i & 3) == v ? sc[v] : mine;
+                    float x, y;
+                    both_halves(mine, x, y);
+                    const float p = i >> 2 & 1 ? y : x;
+                    const uint32_t turn = D == 128 ? (uint32_t)(i & 3) << 2 : (uint32_t)(i >> 1 & 1) << 2;
+#pragma unroll
+                    for (int t = 0; t < DT; ++t)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) {
+                            const int d = 32 * t + 8 * (v >> 2) + 4 * lh + (v & 3);
+                            const float z = bf16_bits_to_f32(*(const __attribute__((address_space(3))) bf16_t *)(vb + i * PITCH + ((((uint32_t)d >> 3) ^ turn) << 4) + (d & 7) * 2));
+                            if (!(fabsf(z) <= 3.402823466e38f) && !(p == 0.f)) acc[t][v] += p * z;
+                        }
+                }
+            }
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int t = 0; t < DT; ++t) {
+                acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[s][t], __builtin_bit_cast(bf16x8, pv[s]), acc[t], 0, 0, 0);
+                if (WHOLE) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[s][t], __builtin_bit_cast(bf16x8, pr[s]), acc[t], 0, 0, 0);
+            }
+    };
+    // ---- the list, two tiles at a time --------------------------------------------------------------
+    // Tile c lives in pair c % NB.  A step waits for its own copies of tiles c and c + 1 (those of the NB - 4 behind them stay in flight); the barrier
+    // makes that hold for all wavefronts and tells that c - 2 and c - 1 have been multiplied by everyone: their pairs take the next two, whose
+    // slots were looked up a step earlier.  Tiles past the list are copied too (zeros), which keeps the count in flight the same.
+    if (c_hi > 0) {
+        refill(0);
+#pragma unroll
+        for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qf[s]));      // (waited for here, not in the loop, where the copies would be waited for too)
+#pragma unroll
+        for (int k = 0; k < NB - 2; ++k) issue(k, lookup(k));
+        Entry b0 = lookup(NB - 2), b1 = lookup(NB - 1);
+        int cur = 0, nxt = NB - 2;
+        for (int c = 0; c < c_hi; c += 2) {
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(L::IPW * (NB - 4)) : "memory");
+            issue(nxt, b0);
+            issue(nxt + 1, b1);
+            const int cn = c + NB;
+            if (cn == win + WIN && cn < c_hi) refill(cn);
+            b0 = lookup(cn), b1 = lookup(cn + 1);
+            if (work) {
+                consume(c, cur);
+                if (c + 1 < c_hi) consume(c + 1, cur + 1);
+            }
+            cur = cur + 2 == NB ? 0 : cur + 2;
+            nxt = nxt + 2 == NB ? 0 : nxt + 2;
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // nothing may be on its way into LDS when the workgroup gives it back
+    }
+    {
+        float x, y;
+        both_halves(l, x, y);
+        l = x + y;
+    }
+    if (part >= 0) {
+        if (col_ok) {
+            const size_t at = (size_t)part * part_columns + col;
+            if (lh == 0) *(f32x2 *)(a.ml + 2 * at) = (f32x2){m, l};
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int v = 0; v < 16; v += 4) *(f32x4 *)(a.o + at * D + 32 * t + 2 * v + 4 * lh) = (f32x4){acc[t][v], acc[t][v + 1], acc[t][v + 2], acc[t][v + 3]};
+        }
+        return;
+    }
+    // columns are rows of the result: a wavefront turns its 32 around in the tiles, which nobody reads any more
+    __syncthreads();
+    if (!work) return;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    lds_byte *strip = (lds_byte *)lds.tiles + w * (32 * L::SP);
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int v = 0; v < 16; v += 4)
+            *(lds_u32x2 *)(strip + li * L::SP + (32 * t + 2 * v + 4 * lh) * 2) =
+                (u32x2){pack_bf16(acc[t][v] * inv, acc[t][v + 1] * inv), pack_bf16(acc[t][v + 2] * inv, acc[t][v + 3] * inv)};
+#pragma unroll
+    for (int i = 0; i < L::GROUPS; ++i) {
+        const int c = L::R * i + lane / L::LPR;                 // (a column of this wavefront)
+        const u32x4 o = *(const lds_u32x4 *)(strip + c * L::SP + 16 * (lane % L::LPR));
+        const size_t at = (size_t)__shfl((unsigned long long)out_at, c);
+        if (32 * w + c < columns) *(u32x4 *)((bf16_t *)a.out + at + 8 * (lane % L::LPR)) = o;
+    }
+}
+
 // ---- parts of a list, combined --------------------------------------------------------------------
 // One wavefront per column: parts first, first + step, ... of `columns` columns each.  head_dim / 4 lanes take a part (four elements each), the others of
 // the wavefront the next ones.

@@ -304,6 +304,23 @@ __global__ __launch_bounds__(256) void selected_vector_kernel(SelectedArgs a)
         });
 }
 
+// The heads of a group are columns of one wavefront; the others of the workgroup copy.
+template <int D, bool ONCE>
+__global__ __launch_bounds__(256, 2) void selected_matrix_kernel(SelectedArgs a)
+{
+    __shared__ MatrixTiles<D, 4> lds;
+    __shared__ int scratch[4];
+    const ListArgs &g = a.list;
+    const SelectedItem it = selected_item(a, scratch);
+    const int columns = 1 << g.lg_g, col = min((int)threadIdx.x & 31, columns - 1);
+    const size_t at = ((size_t)it.t * g.Hq + ((size_t)it.hk << g.lg_g) + col) * D;
+    read_list_matrix<D, 4, true, ONCE>(
+        g, it.hk, lds, it.lo, it.hi, 0x7fffffff, columns,
+        [&](int v) { return selected_slot(g, it, v); },
+        [&](int) { return 0xffffffffu; },
+        at, at, a.parts > 1 ? (long long)blockIdx.x : -1ll, columns);
+}
+
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void selected_merge_kernel(SelectedArgs a)
 {
@@ -448,7 +465,9 @@ int alora_selected_attention(const void *q, const void *k_cache, const void *v_c
     const auto choose = [&](auto head_dim, auto is_bf16) {
         constexpr int D = decltype(head_dim)::value;
         constexpr bool B = decltype(is_bf16)::value;
-        switch (a.list.lg_g) {
+        if constexpr (B) {
+            go(selected_matrix_kernel<D, false>);
+        } else switch (a.list.lg_g) {
         case 0: go(selected_vector_kernel<D, 1, B>); break;
         case 1: go(selected_vector_kernel<D, 2, B>); break;
         case 2: go(selected_vector_kernel<D, 4, B>); break;

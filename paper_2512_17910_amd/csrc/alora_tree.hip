@@ -36,11 +36,12 @@ struct TreeItem {
 };
 
 struct TreeScratch {
-    float total[4];
-    int sums[4][2], found[8];
+    float total[8];
+    int sums[8][2], found[8];
 };
 
-// Which tile and part workgroup `item` (of one K/V head) is for; false: none.  The same sums in every workgroup of the call.
+// Which tile and part workgroup `item` (of one K/V head, NW wavefronts) is for; false: none.  The same sums in every workgroup of the call.
+template <int NW>
 __device__ __forceinline__ bool find_item(const TreeArgs &a, int item, int hk, TreeScratch &scr, TreeItem &it)
 {
     const ListArgs &g = a.list;
@@ -62,20 +63,22 @@ __device__ __forceinline__ bool find_item(const TreeArgs &a, int item, int hk, T
     // all units of all tiles, in a fixed order
     Seq q = seq_of(tid);
     float mine = 0.f;
-    for (int s = tid;; s += 256) {
+    for (int s = tid;; s += 64 * NW) {
         const Seq x = s == tid ? q : seq_of(s);
         mine += (float)x.tiles * (float)x.units;
-        if (s + 256 >= n_seqs) break;
+        if (s + 64 * NW >= n_seqs) break;
     }
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) mine += __shfl_xor(mine, off);
     if (lane == 0) scr.total[w] = mine;
     if (tid == 0) scr.found[0] = -1;
     __syncthreads();
-    const float total = scr.total[0] + scr.total[1] + scr.total[2] + scr.total[3];
+    float total = 0.f;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) total += scr.total[i];
     const int per = max(LEAST_UNITS, (int)fminf(ceilf(total / (float)a.target), 1.0e9f));
     int items0 = 0, tiles0 = 0;
-    for (int s0 = 0; s0 < n_seqs; s0 += 256) {
+    for (int s0 = 0; s0 < n_seqs; s0 += 64 * NW) {
         if (s0) q = seq_of(s0 + tid);
         const int parts = max(1, (q.units + per - 1) / per), items = q.tiles * parts;
         const int u = sum_upto64(items), v = sum_upto64(q.tiles);
@@ -83,7 +86,7 @@ __device__ __forceinline__ bool find_item(const TreeArgs &a, int item, int hk, T
         __syncthreads();
         int at = items0 + u - items, tile_at = tiles0 + v - q.tiles;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < NW; ++i) {
             if (i < w) at += scr.sums[i][0], tile_at += scr.sums[i][1];
             items0 += scr.sums[i][0], tiles0 += scr.sums[i][1];
         }
@@ -113,7 +116,7 @@ __device__ __forceinline__ bool find_item(const TreeArgs &a, int item, int hk, T
 }
 
 // Rows of no sequence: zeros.  The last workgroup of a K/V head.
-template <int D, bool BF16>
+template <int D, bool BF16, int NW>
 __device__ __forceinline__ void clear_rows(const TreeArgs &a, int hk)
 {
     const ListArgs &g = a.list;
@@ -121,7 +124,7 @@ __device__ __forceinline__ void clear_rows(const TreeArgs &a, int hk)
     const int chunks = (D << g.lg_g) * (BF16 ? 2 : 4) / 16;
     const size_t width = (size_t)g.Hq * D * (BF16 ? 2 : 4);
     auto clear = [&](int t0, int t1) {
-        for (long long i = threadIdx.x; i < (long long)(t1 - t0) * chunks; i += 256)
+        for (long long i = threadIdx.x; i < (long long)(t1 - t0) * chunks; i += 64 * NW)
             *(u32x4 *)((char *)g.out + (t0 + i / chunks) * width + ((size_t)hk * chunks + i % chunks) * 16) = (u32x4){0u, 0u, 0u, 0u};
     };
     clear(0, begin);
@@ -137,9 +140,9 @@ __global__ __launch_bounds__(256) void tree_vector_kernel(TreeArgs a)
     __shared__ uint32_t bits[C][2 * ALORA_MAX_TREE_WORDS];
     const ListArgs &g = a.list;
     const int hk = (int)blockIdx.x % g.Hkv, item = (int)blockIdx.x / g.Hkv, tid = threadIdx.x;
-    if (item == (int)(gridDim.x / g.Hkv) - 1) return clear_rows<D, BF16>(a, hk);
+    if (item == (int)(gridDim.x / g.Hkv) - 1) return clear_rows<D, BF16, 4>(a, hk);
     TreeItem it;
-    if (!find_item(a, item, hk, find, it)) return;
+    if (!find_item<4>(a, item, hk, find, it)) return;
     const int G = 1 << g.lg_g;
     if (tid < 2 * a.words * it.rows) bits[tid / (2 * a.words)][tid % (2 * a.words)] = a.mask[(size_t)it.row0 * 2 * a.words + tid];
     __syncthreads();
@@ -164,6 +167,32 @@ __global__ __launch_bounds__(256) void tree_vector_kernel(TreeArgs a)
         });
 }
 
+// 32 NW columns: 32 NW >> lg_g rows of a sequence.
+template <int D, int NW, bool WHOLE, bool ONCE>
+__global__ __launch_bounds__(64 * NW, 2) void tree_matrix_kernel(TreeArgs a)
+{
+    __shared__ MatrixTiles<D, NW> lds;
+    __shared__ TreeScratch find;
+    const ListArgs &g = a.list;
+    const int hk = (int)blockIdx.x % g.Hkv, item = (int)blockIdx.x / g.Hkv;
+    if (item == (int)(gridDim.x / g.Hkv) - 1) return clear_rows<D, true, NW>(a, hk);
+    TreeItem it;
+    if (!find_item<NW>(a, item, hk, find, it)) return;
+    const int32_t *bt = g.bt + (size_t)it.seq * g.max_blocks;
+    const int col = 32 * ((int)threadIdx.x >> 6) + ((int)threadIdx.x & 31), columns = it.rows << g.lg_g, row = it.row0 + (min(col, columns - 1) >> g.lg_g);
+    const uint32_t *bits = a.mask + (size_t)row * 2 * a.words;
+    const size_t at = ((size_t)row * g.Hq + ((size_t)hk << g.lg_g) + (col & ((1 << g.lg_g) - 1))) * D;
+    read_list_matrix<D, NW, WHOLE, ONCE>(
+        g, hk, lds, it.lo, it.hi, it.ctx, columns,
+        [&](int v) { return slot_at(g, bt, v / g.bs, v % g.bs); },
+        [&](int place) {               // the row's bits of drafts place - ctx .. + 31; what lies in front of them is seen
+            const int from = place - it.ctx, i = from >> 5, s = from & 31;
+            const uint32_t x = i < 0 ? 0xffffffffu : i < 2 * a.words ? bits[i] : 0u, y = i + 1 < 2 * a.words ? bits[i + 1] : 0u;
+            return s ? x >> s | y << (32 - s) : x;
+        },
+        at, at, it.parts > 1 ? (long long)it.part_at * g.Hkv + hk : -1ll, 32 * NW);
+}
+
 // One wavefront per column of a tile that has parts.
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int columns)
@@ -180,6 +209,7 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int columns
 // ---- host ---------------------------------------------------------------------------------------
 // How a call is cut: columns of a tile, the most tiles and items (tile, part) of a K/V head there can be, and where the workspace's arrays lie.
 struct TreePlan {
+    int waves;                  // wavefronts of a workgroup on matrix instructions; 0: vector arithmetic
     int columns, tile_rows, target;
     long long tiles, items;
     size_t tiles_at, ml_at, o_at, bytes;
@@ -188,7 +218,8 @@ static TreePlan plan_tree(const alora_attn_dims *d)
 {
     TreePlan p;
     const int G = d->n_q_heads / d->n_kv_heads;
-    p.columns = 8;
+    p.waves = d->dtype != ALORA_BF16 ? 0 : (long long)d->n_tokens * G > 160ll * d->n_seqs ? 8 : 4;
+    p.columns = p.waves ? 32 * p.waves : 8;
     p.tile_rows = p.columns / G;
     p.target = std::max(1, 1024 / d->n_kv_heads);
     p.tiles = d->n_tokens / p.tile_rows + std::min(d->n_seqs, d->n_tokens);      // (a sequence's last tile may not be full)
@@ -250,11 +281,17 @@ int alora_tree_attention(const void *q, const void *k_cache, const void *v_cache
     const bool bf16 = dims->dtype == ALORA_BF16;
     const dim3 grid((unsigned)((p.items + 1) * dims->n_kv_heads)), merge((unsigned)(p.tiles * dims->n_kv_heads), (unsigned)p.columns / 4);
     const auto go = [&](auto kernel, auto combine) {
-        launch_kernel(kernel, grid, dim3(256), 0, (hipStream_t)hip_stream, a);
+        launch_kernel(kernel, grid, dim3(p.waves ? 64 * (unsigned)p.waves : 256), 0, (hipStream_t)hip_stream, a);
         launch_kernel(combine, merge, dim3(256), 0, (hipStream_t)hip_stream, a, p.columns);
     };
-    if (dims->head_dim == 128) bf16 ? go(tree_vector_kernel<128, 8, true>, tree_merge_kernel<128, true>) : go(tree_vector_kernel<128, 8, false>, tree_merge_kernel<128, false>);
-    else bf16 ? go(tree_vector_kernel<64, 8, true>, tree_merge_kernel<64, true>) : go(tree_vector_kernel<64, 8, false>, tree_merge_kernel<64, false>);
+    const auto choose = [&](auto head_dim) {
+        constexpr int D = decltype(head_dim)::value;
+        if (!bf16) go(tree_vector_kernel<D, 8, false>, tree_merge_kernel<D, false>);
+        else if (p.waves == 8) go(tree_matrix_kernel<D, 8, false, false>, tree_merge_kernel<D, true>);
+        else go(tree_matrix_kernel<D, 4, true, false>, tree_merge_kernel<D, true>);
+    };
+    if (dims->head_dim == 128) choose(std::integral_constant<int, 128>{});
+    else choose(std::integral_constant<int, 64>{});
     const int e = launch_status();
     if (e) { note_hip_error(e); return ALORA_EHIP; }
     return ALORA_OK;
