@@ -109,8 +109,7 @@ struct SelectArgs {
     int T, Hkv, lg_g, n_seqs, max_blocks, bs, n_blocks, budget, n_first, n_recent;
 };
 
-// Scores as whole numbers of the same order (a zero has no sign).
-constexpr uint32_t KEY_ALWAYS = 0xffffffffu;
+// Scores as whole numbers of the same order (a zero has no sign); 0 is no score's.
 __device__ __forceinline__ uint32_t key_of(float x)
 {
     const uint32_t u = __float_as_uint(x + 0.f);
@@ -124,112 +123,255 @@ __device__ __forceinline__ int context_blocks(int seq, int pos, int n_seqs, int 
     return (int)min((long long)pos / bs + 1, (long long)max_blocks);
 }
 
-// The 8-bit query of a K/V head, 2 D bytes in LDS: up, then down.  The sums over the heads are made in 64 bits, so that they round the same way in any order.
+// The 8-bit query of a K/V head, 2 D bytes in LDS: up, then down.  One wavefront.  The sums over the heads are made in 64 bits, so that they round the
+// same way in any order.
 template <int D, bool BF16>
-__device__ __forceinline__ void quantize_query(const SelectArgs &a, int t, int hk, int8_t *to, float *scratch)
+__device__ __forceinline__ void quantize_query(const SelectArgs &a, int t, int hk, int8_t *to)
 {
-    const int tid = threadIdx.x, G = 1 << a.lg_g;
-    double up = 0., down = 0.;
-    if (tid < D) {
-        for (int g = 0; g < G; ++g) {
-            const size_t at = (((size_t)t * a.Hkv + hk) * G + g) * D + tid;
-            const float x = BF16 ? bf16_bits_to_f32(((const bf16_t *)a.q)[at]) : ((const float *)a.q)[at];
-            up += x > 0.f ? x : 0.f;
-            down += x < 0.f ? x : 0.f;
+    constexpr int E = D / 64;        // components a lane
+    const int lane = threadIdx.x & 63, G = 1 << a.lg_g;
+    double up[E] = {}, down[E] = {};
+    for (int g = 0; g < G; ++g) {
+        const size_t at = (((size_t)t * a.Hkv + hk) * G + g) * D + lane * E;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float x = BF16 ? bf16_bits_to_f32(((const bf16_t *)a.q)[at + e]) : ((const float *)a.q)[at + e];
+            up[e] += x > 0.f ? x : 0.f;
+            down[e] += x < 0.f ? x : 0.f;
         }
     }
-    const float u = (float)up, v = (float)down;
-    float m = fmaxf(u, -v);
+    float m = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) m = fmaxf(m, fmaxf((float)up[e], -(float)down[e]));
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
-    if ((tid & 63) == 0 && tid < D) scratch[tid >> 6] = m;
-    __syncthreads();
-    m = scratch[0];
-    if (D > 64) m = fmaxf(m, scratch[1]);
     const float f = m >= TINY && m <= LARGEST ? 127.f / m : 0.f;
-    if (tid < D) {
-        const float x = rintf(u * f), y = rintf(v * f);
-        to[tid] = (int8_t)(fabsf(x) <= 127.f ? (int)x : 0);      // (a sum that is not finite counts as zero)
-        to[D + tid] = (int8_t)(fabsf(y) <= 127.f ? (int)y : 0);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const float x = rintf((float)up[e] * f), y = rintf((float)down[e] * f);
+        to[lane * E + e] = (int8_t)(fabsf(x) <= 127.f ? (int)x : 0);      // (a sum that is not finite counts as zero)
+        to[D + lane * E + e] = (int8_t)(fabsf(y) <= 127.f ? (int)y : 0);
     }
-    __syncthreads();
 }
 
-// One workgroup per (row, K/V head): scores of all blocks, then the budget-th largest key by its digits of 8 bits from the top, then the list.
+// N sums over the lanes that share a block's bounds (N lanes of a row), half of them left to a lane after every step: lane i ends with sum i.  The mirrored
+// lanes come first, when every lane still has a share of every sum.
+template <int CTRL, int BIT, int N>
+__device__ __forceinline__ void meet(int (&sum)[16], int lane)
+{
+    const bool up = lane & BIT;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int keep = up ? sum[i + N] : sum[i], give = up ? sum[i] : sum[i + N];
+        sum[i] = keep + __builtin_amdgcn_update_dpp(0, give, CTRL, 0xf, 0xf, true);
+    }
+}
+
+// The scores of as many blocks as lanes share one, with one head's query: 2 D / 16 lanes hold a block's bounds, 16 bytes each (`mine`: those of the query), lane i of them gets the key of
+// block i.  All loads are requested before the first is looked at.
+template <int D>
+__device__ __forceinline__ uint32_t block_keys(const SelectArgs &a, int head, u32x4 mine, const int (&block)[2 * D / 16])
+{
+    constexpr int LPB = 2 * D / 16;
+    const int lane = threadIdx.x & 63, part = lane % LPB;
+    u32x4 x[LPB];
+#pragma unroll
+    for (int i = 0; i < LPB; ++i) {
+        x[i] = (u32x4){0u, 0u, 0u, 0u};
+        if ((unsigned)block[i] < (unsigned)a.n_blocks) x[i] = *(const u32x4 *)(a.bounds + ((size_t)block[i] * a.Hkv + head) * 2 * D + part * 16);
+    }
+    int b = block[0];
+#pragma unroll
+    for (int i = 1; i < LPB; ++i) b = part == i ? block[i] : b;
+    const bool in = (unsigned)b < (unsigned)a.n_blocks;
+    const float scale = in ? a.scales[(size_t)b * a.Hkv + head] : 0.f;
+    int sum[16];
+#pragma unroll
+    for (int i = 0; i < LPB; ++i) {
+        sum[i] = __builtin_amdgcn_sdot4((int)x[i].x, (int)mine.x, 0, false);
+        sum[i] = __builtin_amdgcn_sdot4((int)x[i].y, (int)mine.y, sum[i], false);
+        sum[i] = __builtin_amdgcn_sdot4((int)x[i].z, (int)mine.z, sum[i], false);
+        sum[i] = __builtin_amdgcn_sdot4((int)x[i].w, (int)mine.w, sum[i], false);
+    }
+    if constexpr (LPB == 16) meet<0x140, 8, 8>(sum, lane);      // row_mirror
+    meet<0x141, 4, 4>(sum, lane);                               // row_half_mirror
+    meet<0x4E, 2, 2>(sum, lane);                                // quad_perm [2,3,0,1]
+    meet<0xB1, 1, 1>(sum, lane);                                // quad_perm [1,0,3,2]
+    const float score = scale <= LARGEST ? fminf(fmaxf((float)sum[0] * scale, -LARGEST), LARGEST) : LARGEST;
+    return key_of(in ? score : NEG_INF);
+}
+
+// ---- the list from the keys ----
+// n keys, of which the first n_first and the last n_recent blocks' do not count (those are always chosen); n > budget.  The threshold is found by counting: keys
+// between the smallest and the largest fall into 2048 bins, the bin it lies in is cut again, until a bin is taken whole or holds one value.
+constexpr int BINS = 2048;
+struct ListScratch {
+    int bins[BINS], sums[16][2];
+    uint32_t ends[16][2], bin, left, inside;
+};
+template <int NT, class Key>
+__device__ __forceinline__ void list_of_keys(const SelectArgs &a, int n, Key key, int32_t *out, ListScratch &scr)
+{
+    constexpr int NW = NT / 64, PER = BINS / NT;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, c0 = a.n_first, c1 = n - a.n_recent;
+    int want = a.budget - a.n_first - a.n_recent;
+    uint32_t above = 0xffffffffu, equal = 0;        // chosen: keys above `above`, and `want` of those equal to `equal`
+    if (want > 0) {
+        uint32_t low = 0xffffffffu, high = 0;
+        for (int i = c0 + tid; i < c1; i += NT) {
+            const uint32_t k = key(i);
+            low = min(low, k), high = max(high, k);
+        }
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) low = min(low, (uint32_t)__shfl_xor((int)low, o)), high = max(high, (uint32_t)__shfl_xor((int)high, o));
+        if (lane == 0) scr.ends[w][0] = low, scr.ends[w][1] = high;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < NW; ++i) low = min(low, scr.ends[i][0]), high = max(high, scr.ends[i][1]);
+        uint32_t span = high - low;                 // keys low .. low + span are looked at
+        for (;;) {
+            const int shift = max(0, 32 - (int)__builtin_clz(span | 1u) - 11);
+            for (int i = tid; i < BINS; i += NT) scr.bins[i] = 0;
+            __syncthreads();
+            for (int i = c0 + tid; i < c1; i += NT) {
+                const uint32_t k = key(i) - low;
+                if (k <= span) atomicAdd(&scr.bins[k >> shift], 1);      // (counts: the same in any order)
+            }
+            __syncthreads();
+            int mine = 0, h[PER];
+#pragma unroll
+            for (int j = 0; j < PER; ++j) h[j] = scr.bins[BINS - 1 - (tid * PER + j)], mine += h[j];      // from the largest down
+            int upto = sum_upto64(mine);
+            if (lane == 63) scr.sums[w][0] = upto;
+            __syncthreads();
+            for (int i = 0; i < w; ++i) upto += scr.sums[i][0];
+            int before = upto - mine;
+            if (before < want && want <= upto) {
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+                    if (before < want && want <= before + h[j]) scr.bin = (uint32_t)(BINS - 1 - (tid * PER + j)), scr.left = (uint32_t)(want - before), scr.inside = (uint32_t)h[j];
+                    before += h[j];
+                }
+            }
+            __syncthreads();
+            want = (int)scr.left;
+            low += scr.bin << shift;
+            if ((int)scr.inside == want) {          // the whole bin
+                above = low - 1, want = 0;          // (keys are above 0)
+                break;
+            }
+            if (shift == 0) {
+                above = equal = low;
+                break;
+            }
+            span = (1u << shift) - 1;
+            __syncthreads();
+        }
+    }
+    // a thread looks through blocks that follow each other, so that ranks are in their order (an odd number of them: LDS banks)
+    const int per = ((n + NT - 1) / NT) | 1, begin = min(n, tid * per), end = min(n, begin + per);
+    int more = 0, same = 0;
+    for (int i = begin; i < end; ++i) {
+        const bool always = i < c0 || i >= c1;
+        const uint32_t k = key(i);
+        more += always || k > above;
+        same += !always && want > 0 && k == equal;
+    }
+    int um = sum_upto64(more), us = sum_upto64(same);
+    __syncthreads();
+    if (lane == 63) scr.sums[w][0] = um, scr.sums[w][1] = us;
+    __syncthreads();
+    for (int i = 0; i < w; ++i) um += scr.sums[i][0], us += scr.sums[i][1];
+    um -= more, us -= same;
+    for (int i = begin; i < end; ++i) {
+        const bool always = i < c0 || i >= c1;
+        const uint32_t k = key(i);
+        const bool m = always || k > above, e = !always && want > 0 && k == equal;
+        if (m || (e && us < want)) out[um + min(us, want)] = i;
+        um += m, us += e;
+    }
+}
+
+// All blocks of a context that fits the budget, or of a row that is out of range: true.
+template <int NT>
+__device__ __forceinline__ bool whole_context(const SelectArgs &a, int n, int32_t *out)
+{
+    if (n > a.budget) return false;
+    for (int i = threadIdx.x; i < a.budget; i += NT) out[i] = i < n ? i : -1;
+    return true;
+}
+
+// One workgroup per (row, K/V head): block ids to LDS, keys in their place, the list.
+constexpr int MOST_IN_LDS = 8192;
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void block_select_kernel(SelectArgs a)
 {
+    constexpr int LPB = 2 * D / 16, UNITS = 64 / LPB;
+    extern __shared__ __attribute__((aligned(16))) int ids[];      // max_blocks, rounded up to LPB
     __shared__ __attribute__((aligned(16))) int8_t query[2 * D];
-    __shared__ float scratch[2];
-    __shared__ int histogram[256], wave_sums[4][2], digit, left;
+    __shared__ ListScratch scr;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, t = (int)blockIdx.x / a.Hkv, hk = (int)blockIdx.x % a.Hkv;
-    const int seq = a.seq[t], pos = a.pos[t], n = context_blocks(seq, pos, a.n_seqs, a.max_blocks, a.bs);
+    const int seq = a.seq[t], n = context_blocks(seq, a.pos[t], a.n_seqs, a.max_blocks, a.bs);
     int32_t *out = a.selected + (size_t)blockIdx.x * a.budget;
-    if (n <= a.budget) {
-        for (int i = tid; i < a.budget; i += 256) out[i] = i < n ? i : -1;
-        return;
-    }
-    quantize_query<D, BF16>(a, t, hk, query, scratch);
-    uint32_t *keys = a.keys + (size_t)blockIdx.x * a.max_blocks;
+    if (whole_context<256>(a, n, out)) return;
     const int32_t *bt = a.bt + (size_t)seq * a.max_blocks;
-    constexpr int LPB = 2 * D / 16;      // lanes per block, 16 bytes each
+    const int padded = (n + LPB - 1) / LPB * LPB;
+    for (int i = tid; i < padded; i += 256) ids[i] = i < n ? bt[i] : -1;
+    if (w == 0) quantize_query<D, BF16>(a, t, hk, query);
+    __syncthreads();
     const u32x4 mine = *(const u32x4 *)(query + lane % LPB * 16);
-    for (int b0 = w * (64 / LPB); b0 < n; b0 += 256 / LPB) {
-        const int b = b0 + lane / LPB, block = b < n ? bt[b] : -1;
-        const bool in = (unsigned)block < (unsigned)a.n_blocks;
-        int sum = 0;
-        float scale = 0.f;
-        if (in) {
-            const u32x4 x = *(const u32x4 *)(a.bounds + ((size_t)block * a.Hkv + hk) * 2 * D + lane % LPB * 16);
-            scale = a.scales[(size_t)block * a.Hkv + hk];
-            sum = __builtin_amdgcn_sdot4((int)x.x, (int)mine.x, sum, false);
-            sum = __builtin_amdgcn_sdot4((int)x.y, (int)mine.y, sum, false);
-            sum = __builtin_amdgcn_sdot4((int)x.z, (int)mine.z, sum, false);
-            sum = __builtin_amdgcn_sdot4((int)x.w, (int)mine.w, sum, false);
-        }
+    for (int b0 = (w * UNITS + lane / LPB) * LPB; b0 < padded; b0 += 4 * UNITS * LPB) {      // (whole heads of lanes leave the loop together)
+        int block[LPB];
 #pragma unroll
-        for (int o = 1; o < LPB; o <<= 1) sum += __shfl_xor(sum, o);
-        if (lane % LPB == 0 && b < n) {
-            const float score = scale <= LARGEST ? fminf(fmaxf((float)sum * scale, -LARGEST), LARGEST) : LARGEST;
-            keys[b] = b < a.n_first || b >= n - a.n_recent ? KEY_ALWAYS : key_of(in ? score : NEG_INF);
-        }
+        for (int i = 0; i < LPB; ++i) block[i] = ids[b0 + i];
+        ids[b0 + lane % LPB] = (int)block_keys<D>(a, hk, mine, block);
     }
     __syncthreads();
-    // the budget-th largest key, digit by digit; `left` of those equal to it are taken
-    uint32_t prefix = 0;
-    int want = a.budget;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        histogram[tid] = 0;
-        __syncthreads();
-        for (int i = tid; i < n; i += 256) {
-            const uint32_t k = keys[i];
-            if (shift == 24 || k >> (shift + 8) == prefix) atomicAdd(&histogram[k >> shift & 255u], 1);      // (counts: the same in any order)
-        }
-        __syncthreads();
-        const int h = histogram[255 - tid];      // from the largest digit down
-        int upto = sum_upto64(h);
-        if (lane == 63) wave_sums[w][0] = upto;
-        __syncthreads();
-        for (int i = 0; i < w; ++i) upto += wave_sums[i][0];
-        if (upto >= want && upto - h < want) digit = 255 - tid, left = want - (upto - h);
-        __syncthreads();
-        prefix = prefix << 8 | (uint32_t)digit;
-        want = left;
-        __syncthreads();
-    }
-    // a thread looks through blocks that follow each other, so that ranks are in their order
-    const int per = (n + 255) / 256, begin = min(n, tid * per), end = min(n, begin + per);
-    int above = 0, equal = 0;
-    for (int i = begin; i < end; ++i) above += keys[i] > prefix, equal += keys[i] == prefix;
-    int ua = sum_upto64(above), ue = sum_upto64(equal);
-    if (lane == 63) wave_sums[w][0] = ua, wave_sums[w][1] = ue;
+    list_of_keys<256>(a, n, [&](int i) { return (uint32_t)ids[i]; }, out, scr);
+}
+
+// The same in two kernels.  Keys of CHUNK blocks of a row, all heads (whose bounds of a block lie next to each other); then a workgroup per
+// (row, head) makes the list.
+constexpr int CHUNK = 64;
+template <int D, bool BF16>
+__global__ __launch_bounds__(256) void block_keys_kernel(SelectArgs a)
+{
+    constexpr int LPB = 2 * D / 16, HEADS = 64 / LPB;
+    __shared__ __attribute__((aligned(16))) int8_t query[HEADS][2 * D];
+    __shared__ __attribute__((aligned(16))) int ids[CHUNK];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, t = blockIdx.y, h0 = (int)blockIdx.z * HEADS, b0 = (int)blockIdx.x * CHUNK;
+    const int seq = a.seq[t], n = context_blocks(seq, a.pos[t], a.n_seqs, a.max_blocks, a.bs);
+    if (n <= a.budget || b0 >= n) return;
+    if (tid < CHUNK) ids[tid] = b0 + tid < n ? a.bt[(size_t)seq * a.max_blocks + b0 + tid] : -1;
+    for (int h = w; h < HEADS; h += 4)
+        if (h0 + h < a.Hkv) quantize_query<D, BF16>(a, t, h0 + h, query[h]);
     __syncthreads();
-    for (int i = 0; i < w; ++i) ua += wave_sums[i][0], ue += wave_sums[i][1];
-    ua -= above, ue -= equal;
-    for (int i = begin; i < end; ++i) {
-        const uint32_t k = keys[i];
-        if (k > prefix || (k == prefix && ue < want)) out[ua + min(ue, want)] = i;
-        ua += k > prefix, ue += k == prefix;
+    const int head = lane / LPB;
+    const u32x4 mine = *(const u32x4 *)(query[head] + lane % LPB * 16);
+    for (int g = w * LPB; g < CHUNK; g += 4 * LPB) {
+        int block[LPB];
+#pragma unroll
+        for (int i = 0; i < LPB; ++i) block[i] = h0 + head < a.Hkv ? ids[g + i] : -1;
+        const uint32_t k = block_keys<D>(a, h0 + head, mine, block);
+        const int b = b0 + g + lane % LPB;
+        if (h0 + head < a.Hkv && b < n) a.keys[((size_t)t * a.Hkv + h0 + head) * a.max_blocks + b] = k;
+    }
+}
+template <int NT>
+__global__ __launch_bounds__(NT) void block_list_kernel(SelectArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) int ids[];      // keys, where max_blocks of them have room
+    __shared__ ListScratch scr;
+    const int t = (int)blockIdx.x / a.Hkv, n = context_blocks(a.seq[t], a.pos[t], a.n_seqs, a.max_blocks, a.bs);
+    int32_t *out = a.selected + (size_t)blockIdx.x * a.budget;
+    if (whole_context<NT>(a, n, out)) return;
+    const uint32_t *keys = a.keys + (size_t)blockIdx.x * a.max_blocks;
+    if (a.max_blocks <= MOST_IN_LDS) {
+        for (int i = threadIdx.x; i < n; i += NT) ids[i] = (int)keys[i];
+        __syncthreads();
+        list_of_keys<NT>(a, n, [&](int i) { return (uint32_t)ids[i]; }, out, scr);
+    } else {
+        list_of_keys<NT>(a, n, [&](int i) { return keys[i]; }, out, scr);
     }
 }
 
@@ -338,7 +480,9 @@ static int check_select(const alora_attn_dims *d)
     if (st) return st;
     return (long long)d->n_tokens * d->n_q_heads > 0x3fffffffll ? ALORA_ESHAPE : ALORA_OK;
 }
-static size_t select_bytes(const alora_attn_dims *d) { return (size_t)d->n_tokens * d->n_kv_heads * d->max_blocks * sizeof(uint32_t); }
+// Whether keys and lists are made by kernels of their own.
+static bool two_kernels(const alora_attn_dims *d) { return d->max_blocks > MOST_IN_LDS || ((long long)d->n_tokens * d->n_kv_heads < 256 && d->max_blocks > 512); }
+static size_t select_bytes(const alora_attn_dims *d) { return two_kernels(d) ? (size_t)d->n_tokens * d->n_kv_heads * d->max_blocks * sizeof(uint32_t) : 0; }
 
 constexpr int MOST_BUDGET = 1 << 20;
 
@@ -419,10 +563,28 @@ int alora_block_select(const void *q, const int8_t *bounds, const float *scales,
     const ListArgs g = list_args(dims, q, nullptr, nullptr, block_tables, nullptr);
     a.T = g.T; a.Hkv = g.Hkv; a.lg_g = g.lg_g; a.n_seqs = g.n_seqs; a.max_blocks = g.max_blocks; a.bs = g.bs; a.n_blocks = g.n_blocks;
     a.budget = budget; a.n_first = n_first; a.n_recent = n_recent;
-    const auto go = [&](auto kernel) { launch_kernel(kernel, dim3((unsigned)a.T * (unsigned)a.Hkv), dim3(256), 0, (hipStream_t)hip_stream, a); };
     const bool bf16 = dims->dtype == ALORA_BF16;
-    if (dims->head_dim == 128) bf16 ? go(block_select_kernel<128, true>) : go(block_select_kernel<128, false>);
-    else bf16 ? go(block_select_kernel<64, true>) : go(block_select_kernel<64, false>);
+    const dim3 lists((unsigned)a.T * (unsigned)a.Hkv);
+    const auto go = [&](auto head_dim, auto is_bf16) {
+        constexpr int D = decltype(head_dim)::value, LPB = D / 8, HEADS = 64 / LPB;
+        constexpr bool B = decltype(is_bf16)::value;
+        if (!two_kernels(dims)) {
+            launch_kernel(block_select_kernel<D, B>, lists, dim3(256), (unsigned)((a.max_blocks + LPB - 1) / LPB * LPB) * 4, (hipStream_t)hip_stream, a);
+            return;
+        }
+        for (int t0 = 0; t0 < dims->n_tokens; t0 += 65535) {      // (a grid's second dimension)
+            SelectArgs part = a;
+            part.T = std::min(65535, dims->n_tokens - t0);
+            part.q = (const char *)a.q + (size_t)t0 * dims->n_q_heads * D * (B ? 2 : 4);
+            part.seq = a.seq + t0, part.pos = a.pos + t0, part.keys = a.keys + (size_t)t0 * a.Hkv * a.max_blocks;
+            launch_kernel(block_keys_kernel<D, B>, dim3((unsigned)(a.max_blocks + CHUNK - 1) / CHUNK, (unsigned)part.T, (unsigned)(a.Hkv + HEADS - 1) / HEADS), dim3(256), 0, (hipStream_t)hip_stream, part);
+        }
+        launch_kernel(block_list_kernel<1024>, lists, dim3(1024), a.max_blocks <= MOST_IN_LDS ? (unsigned)a.max_blocks * 4 : 0, (hipStream_t)hip_stream, a);
+    };
+    typedef std::integral_constant<int, 128> D128;
+    typedef std::integral_constant<int, 64> D64;
+    if (bf16) dims->head_dim == 128 ? go(D128{}, std::true_type{}) : go(D64{}, std::true_type{});
+    else dims->head_dim == 128 ? go(D128{}, std::false_type{}) : go(D64{}, std::false_type{});
     const int e = launch_status();
     if (e) { note_hip_error(e); return ALORA_EHIP; }
     return ALORA_OK;
