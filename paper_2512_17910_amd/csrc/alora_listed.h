@@ -11,8 +11,6 @@
 
 namespace alora {
 
-constexpr int LIST_WINDOW = 2048;      // places of the list whose slots are in LDS
-
 // What every reader of a list knows.
 struct ListArgs {
     const void *q, *kc, *vc;
@@ -40,7 +38,8 @@ __device__ __forceinline__ int slot_at(const ListArgs &a, const int32_t *bt, int
 //   store(c, d, M, L, o) takes column c's maximum, sum of weights and, for element d, unnormalised output
 template <int C, int D>
 struct VectorScratch {
-    int slots[LIST_WINDOW];
+    static constexpr int WINDOW = 2048;      // places of the list whose slots are in LDS
+    int slots[WINDOW];
     float m[4][C], l[4][C], acc[4][C][D];
 };
 
@@ -48,8 +47,8 @@ template <int D, int C, bool BF16, class SlotOf, class Seen, class QAt, class St
 __device__ __forceinline__ void read_list_vector(const ListArgs &a, int hk, VectorScratch<C, D> &scr, int lo, int hi, int masked_from, SlotOf slot_of, Seen seen,
                                                  QAt q_at, Store store)
 {
-    constexpr int LPP = D / 8, PPW = 64 / LPP, PPI = 4 * PPW, U = BF16 ? 4 : 2, BLK = PPI * U;
-    static_assert(LIST_WINDOW % (2 * BLK) == 0, "whole blocks in a window");
+    constexpr int LPP = D / 8, PPW = 64 / LPP, PPI = 4 * PPW, U = BF16 ? 4 : 2, BLK = PPI * U, WINDOW = VectorScratch<C, D>::WINDOW;
+    static_assert(WINDOW % (2 * BLK) == 0, "whole blocks in a window");
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, grp = lane / LPP, ch = lane % LPP, jl = wave * PPW + grp;
     const size_t width = (size_t)a.Hkv * D, col = (size_t)hk * D + 8 * ch;
     Raw8<BF16> qr[C];
@@ -68,7 +67,7 @@ __device__ __forceinline__ void read_list_vector(const ListArgs &a, int hk, Vect
         unsigned ok = 0;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int j = j0 + u * PPI + jl, s = j < hi && j - w0 < LIST_WINDOW ? scr.slots[j - w0] : -1;
+            const int j = j0 + u * PPI + jl, s = j < hi && j - w0 < WINDOW ? scr.slots[j - w0] : -1;
             kr[u].zero(), vr[u].zero();
             if (s >= 0) {
                 ok |= 1u << u;
@@ -125,11 +124,11 @@ __device__ __forceinline__ void read_list_vector(const ListArgs &a, int hk, Vect
             }
         }
     };
-    for (; w0 < hi; w0 += LIST_WINDOW) {
+    for (; w0 < hi; w0 += WINDOW) {
         __syncthreads();
-        for (int i = tid; i < LIST_WINDOW && w0 + i < hi; i += 256) scr.slots[i] = slot_of(w0 + i);
+        for (int i = tid; i < WINDOW && w0 + i < hi; i += 256) scr.slots[i] = slot_of(w0 + i);
         __syncthreads();
-        const int end = min(hi, w0 + LIST_WINDOW);
+        const int end = min(hi, w0 + WINDOW);
         Raw8<BF16> kA[U], vA[U], kB[U], vB[U];
         unsigned okA = fetch(w0, kA, vA), okB;
         for (int j0 = w0; j0 < end; j0 += 2 * BLK) {
@@ -177,47 +176,56 @@ __device__ __forceinline__ void read_list_vector(const ListArgs &a, int hk, Vect
     }
 }
 
-// ---- matrix instructions: 32 columns a wavefront, bf16 ---------------------------------------------
-// The wavefronts of a workgroup share tiles of 32 places in LDS, which all of them copy and each multiplies with its own 32 columns
-// (32x32x16 products): scores^T = K Q^T leaves a column in two lanes, down which the softmax runs, and out^T += V^T P takes the weights from the
-// score registers.  Rows of K and V go from global memory straight into LDS, two tiles of each per barrier, NB in flight or in use.
-// A lane copies 16 bytes of a row; which of the row's 16-byte chunks is rotated by the row (XOR), so that neither the reads of K fragments (one
-// chunk of 32 rows) nor the transposing reads of V (four chunks of four rows) meet in a bank.
-template <int D, int NW>
+// ---- matrix instructions: 32 or 16 columns a wavefront, bf16 ----------------------------------------
+// The wavefronts of a workgroup share tiles of 32 places in LDS, which all of them copy and each multiplies with its own columns (32x32x16 or 16x16x32
+// products): scores^T = K Q^T leaves a column in two or four lanes, down which the softmax runs, and out^T += V^T P takes the weights from the
+// score registers.  Rows of K and V go from global memory straight into LDS, STEP tiles of each per barrier, NB in flight or in use.
+// A lane copies 16 bytes of a row; which of the row's 16-byte chunks is turned by the row (XOR), so that neither the reads of K fragments (one
+// chunk of 32 or 16 rows) nor the transposing reads of V (chunks of four or eight rows) meet in a bank.
+template <int D_, int NW_, int COLS_, int NB_, int STEP_, int WINDOW_>
 struct MatrixTiles {
+    static constexpr int D = D_, NW = NW_, COLS = COLS_, NB = NB_, STEP = STEP_, WINDOW = WINDOW_;
     static constexpr int PITCH = 2 * D, TILE = 32 * PITCH;      // bytes of a row, of 32
-    static constexpr int NB = (NW == 8 ? 98304 : 65536) / (2 * TILE);
     static constexpr int LPR = D / 8, R = 64 / LPR;             // lanes per row, rows per copy
     static constexpr int GROUPS = 32 / R;                       // copies of a tile
-    static constexpr int IPW = 2 * GROUPS / NW;                 // copies a wavefront makes of 32 places: K and V
-    static constexpr int GPW = GROUPS < NW ? 1 : GROUPS / NW;   // groups of rows it copies (of eight wavefronts and heads of 64, half copy K, half V)
+    static constexpr int GPW = GROUPS / NW, IPW = 2 * GPW;      // of which a wavefront makes so many, of K and of V
     static constexpr int SP = PITCH + 16;                       // bytes per column where results are turned around
-    static_assert(NB % 2 == 0 && NB >= 4 && IPW >= 1 && 32 * SP * NW <= NB * 2 * TILE, "tiles");
+    static_assert(NB % STEP == 0 && NB > STEP && GPW >= 1 && COLS * SP * NW <= NB * 2 * TILE && WINDOW / 32 % STEP == 0 && NB <= WINDOW / 32, "tiles");
     __attribute__((aligned(1024))) unsigned char tiles[NB * 2 * TILE];
-    int slots[LIST_WINDOW];
-    uint32_t ok[LIST_WINDOW / 32], tile_ok[NB];
+    int slots[WINDOW];
+    uint32_t ok[WINDOW / 32], tile_ok[NB];
+    __device__ static __forceinline__ uint32_t k_turn(int row) { return D == 128 ? (uint32_t)(row & 15) : (uint32_t)(row >> 1 & 7); }
+    __device__ static __forceinline__ uint32_t v_turn(int row) { return (D == 128 ? (uint32_t)(row & 3) << 2 : (uint32_t)(row >> 1 & 1) << 2) ^ (uint32_t)(row >> 2 & 1) << 1; }
 };
 
-// Whether either bf16 of x is not finite.
-__device__ __forceinline__ bool not_finite2(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
+template <int N> struct FloatsOf;
+template <> struct FloatsOf<16> { typedef f32x16 type; };
+template <> struct FloatsOf<4> { typedef f32x4 type; };
+__device__ __forceinline__ f32x16 multiply(bf16x8 x, bf16x8 y, f32x16 z) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, z, 0, 0, 0); }
+__device__ __forceinline__ f32x4 multiply(bf16x8 x, bf16x8 y, f32x4 z) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, z, 0, 0, 0); }
 
 //   columns        of the workgroup that exist; a wavefront beyond them only copies
 //   masked_from    places from here on are seen by some columns only: seen(place) = 32 bits of this lane's column, place a multiple of 32 from lo on
-//   q_at, out_at   element of q and out where this lane's column begins (column `col`)
+//   q_at, out_at   element of q and out where this lane's column begins (column COLS * wavefront + lane % COLS)
 //   part           < 0: rows of out; else number of the part whose sums are left, of room for part_columns columns
 // WHOLE: the weights go into the product with V as two bf16 numbers (their rounding then adds nothing to that of the result), for twice
 // the products.  ONCE: rows are not read again soon (non-temporal copies).
-template <int D, int NW, bool WHOLE, bool ONCE, class SlotOf, class Seen>
-__device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, MatrixTiles<D, NW> &lds, int lo, int hi, int masked_from, int columns, SlotOf slot_of,
+template <bool WHOLE, bool ONCE, class L, class SlotOf, class Seen>
+__device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, L &lds, int lo, int hi, int masked_from, int columns, SlotOf slot_of,
                                                  Seen seen, size_t q_at, size_t out_at, long long part, int part_columns)
 {
-    typedef MatrixTiles<D, NW> L;
-    constexpr int NB = L::NB, TILE = L::TILE, PITCH = L::PITCH, WIN = LIST_WINDOW / 32, KS = D / 16, DT = D / 32;
+    constexpr int D = L::D, NW = L::NW, COLS = L::COLS, NB = L::NB, STEP = L::STEP, TILE = L::TILE, PITCH = L::PITCH, WIN = L::WINDOW / 32;
+    constexpr int LG = 64 / COLS;                               // lanes of a column
+    constexpr int KD = 8 * LG, KS = D / KD;                     // components a product of scores takes, products
+    constexpr int ST = 32 / COLS, NV = 32 / LG;                 // score tiles of 32 places, scores a lane holds: places 4 LG (v / 4) + 4 g + v % 4
+    constexpr int PS = 32 / KD;                                 // products per 32 places of V
+    constexpr int DT = D / COLS, NA = COLS / LG;                // tiles of the result, components a lane holds of one: COLS t + 4 LG (v / 4) + 4 g + v % 4
+    typedef typename FloatsOf<NA>::type Floats;
     typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
     typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
-    const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c16 = lane & 15, li = lane & 31, lh = lane >> 5;
-    const int col = 32 * w + li;
-    const bool col_ok = col < columns, work = 32 * w < columns;
+    const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c16 = lane & 15, li = lane % COLS, g = lane / COLS;
+    const int col = COLS * w + li;
+    const bool col_ok = col < columns, work = COLS * w < columns;
     const uint32_t tiles_at = (uint32_t)(uintptr_t)(lds_byte *)lds.tiles, row_bytes = (uint32_t)a.Hkv * (uint32_t)PITCH, head = (uint32_t)hk * (uint32_t)PITCH;
     const int c_hi = (hi - lo + 31) >> 5;                       // tiles of this part
 
@@ -225,15 +233,22 @@ __device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, Matr
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
         u32x4 v = {0u, 0u, 0u, 0u};
-        if (col_ok) v = *(const u32x4 *)((const bf16_t *)a.q + q_at + 16 * s + 8 * lh);
+        if (col_ok) v = *(const u32x4 *)((const bf16_t *)a.q + q_at + KD * s + 8 * g);
         qf[s] = __builtin_bit_cast(bf16x8, v);
     }
-    f32x16 acc[DT];
+    Floats acc[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[t][e] = 0.f;
+        for (int e = 0; e < NA; ++e) acc[t][e] = 0.f;
     float m = M_FLOOR, l = 0.f;
+    // over the lanes of a column
+    auto column_max = [&](float x) {
+        float y, z;
+        if (LG == 4) x = fmaxf(x, __shfl_xor(x, 16));
+        both_halves(x, y, z);
+        return fmaxf(y, z);
+    };
 
     // ---- the window: slots of WIN tiles, and which of their places there are -----------------------
     int win = 0;                                                // first tile of the window
@@ -245,24 +260,25 @@ __device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, Matr
             const int s = i < end ? slot_of(lo + 32 * c + i) : -1;
             lds.slots[i] = s;
             const unsigned long long have = __builtin_amdgcn_ballot_w64(s >= 0);
-            if (li == 0) lds.ok[i >> 5] = (uint32_t)(lh ? have >> 32 : have);
+            if ((lane & 31) == 0) lds.ok[i >> 5] = (uint32_t)(lane ? have >> 32 : have);
         }
         __syncthreads();
     };
     // ---- copies -------------------------------------------------------------------------------------
+    // (Scalar addresses where a copy's rows lie in one cache block, as block sizes of 4 and more allow, gained nothing: 505 us | 501 where products
+    // bound the call, 230 | 243 where memory does.)
     struct Entry {
         int slot[L::GPW];
         uint32_t ok;
     };
-    const int first_group = L::GROUPS < NW ? w % L::GROUPS : w;
     auto lookup = [&](int c) {
         Entry e;
 #pragma unroll
-        for (int g = 0; g < L::GPW; ++g) e.slot[g] = -1;
+        for (int i = 0; i < L::GPW; ++i) e.slot[i] = -1;
         e.ok = 0;
         if (c < c_hi) {
 #pragma unroll
-            for (int g = 0; g < L::GPW; ++g) e.slot[g] = lds.slots[32 * (c - win) + (first_group + g * NW) * L::R + lane / L::LPR];
+            for (int i = 0; i < L::GPW; ++i) e.slot[i] = lds.slots[32 * (c - win) + (w + i * NW) * L::R + lane / L::LPR];
             e.ok = lds.ok[c - win];
         }
         return e;
@@ -271,12 +287,11 @@ __device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, Matr
     auto issue = [&](int pair, const Entry &e) {
 #pragma unroll
         for (int i = 0; i < L::IPW; ++i) {
-            const int g = i % L::GPW, group = first_group + g * NW;
-            const bool v = L::GROUPS < NW ? w >= L::GROUPS : i >= L::GPW;       // K first, then V
-            const int row = group * L::R + lane / L::LPR;
-            const uint32_t turn = v ? (D == 128 ? (uint32_t)(row & 3) << 2 : (uint32_t)(row >> 1 & 1) << 2) : D == 128 ? (uint32_t)(row & 15) : (uint32_t)(row >> 1 & 7);
-            const char *at = (const char *)(v ? a.vc : a.kc) + (unsigned long long)(uint32_t)e.slot[g] * row_bytes + (head + ((chunk ^ turn) << 4));
-            const void *from = e.slot[g] >= 0 ? (const void *)at : (const void *)ab_zero_chunk;
+            const bool v = i >= L::GPW;                         // K first, then V
+            const int group = w + i % L::GPW * NW, row = group * L::R + lane / L::LPR, slot = e.slot[i % L::GPW];
+            const uint32_t at = head + ((chunk ^ (v ? L::v_turn(row) : L::k_turn(row))) << 4);
+            const void *from = (const char *)(v ? a.vc : a.kc) + (unsigned long long)(uint32_t)slot * row_bytes + at;
+            if (slot < 0) from = ab_zero_chunk;
             const uint32_t to = tiles_at + (uint32_t)pair * (2 * TILE) + (v ? TILE : 0) + ((uint32_t)group << 10);
             if constexpr (ONCE) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off nt" : : "s"(to), "v"(from) : "memory");
             else load_lds16(to, from);
@@ -284,64 +299,68 @@ __device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, Matr
         lds.tile_ok[pair] = e.ok;                               // (the same value from every lane)
     };
     // ---- products -----------------------------------------------------------------------------------
-    const uint32_t k_base = (uint32_t)li * PITCH + (uint32_t)((lh ^ (D == 128 ? li & 15 : li >> 1 & 7)) << 4);
-    uint32_t v_base;
-    {
-        const int j = c16 >> 2, row = 4 * lh + j;
-        const uint32_t turn = D == 128 ? (uint32_t)j << 2 : (uint32_t)(j >> 1) << 2;
-        v_base = (uint32_t)row * PITCH + (((uint32_t)(2 * (lane >> 4 & 1) + ((c16 & 3) >> 1)) ^ turn) << 4) + (uint32_t)((c16 & 1) << 3);
-    }
+    const uint32_t k_base = (uint32_t)li * PITCH + (((uint32_t)g ^ L::k_turn(li)) << 4);      // row li, chunk LG ks + g (of 16 columns: and row 16 + li)
+    const int v_row = 4 * g + (c16 >> 2);
+    // 8 bytes of components 4 (c16 % 4) .. of a tile (32 columns: of its half lane / 16 % 2); rows 4 g .. + 3, and 4 LG further on, are the places of a lane's scores
+    const uint32_t v_base = (uint32_t)v_row * PITCH + (((uint32_t)((c16 & 3) >> 1) + (LG == 2 ? (uint32_t)(2 * (lane >> 4 & 1)) : 0u)) ^ L::v_turn(v_row)) * 16u + (uint32_t)((c16 & 1) << 3);
     auto consume = [&](int c, int pair) {
         const lds_byte *kb = (const lds_byte *)lds.tiles + pair * (2 * TILE), *vb = kb + TILE;
-        f32x16 sc;
+        Floats st[ST];
 #pragma unroll
-        for (int v = 0; v < 16; ++v) sc[v] = 0.f;
-        bf16x8 kf[KS];
+        for (int t = 0; t < ST; ++t)
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) kf[ks] = *(const __attribute__((address_space(3))) bf16x8 *)(kb + (k_base ^ (uint32_t)(ks << 5)));
+            for (int e = 0; e < NA; ++e) st[t][e] = 0.f;
+        bf16x8 kf[KS][ST];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int t = 0; t < ST; ++t) kf[ks][t] = *(const __attribute__((address_space(3))) bf16x8 *)(kb + (k_base ^ (uint32_t)(ks * LG << 4)) + t * 16 * PITCH);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[ks], sc, 0, 0, 0);
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int t = 0; t < ST; ++t) st[t] = multiply(kf[ks][t], qf[ks], st[t]);
         const uint32_t ok = __builtin_amdgcn_readfirstlane(lds.tile_ok[pair]);
-        bf16x8 vf[2][DT];
+        bf16x8 vf[PS][DT];
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+        for (int s = 0; s < PS; ++s)
 #pragma unroll
-            for (int t = 0; t < DT; ++t) vf[s][t] = read_tr_frag(vb + (v_base ^ (uint32_t)(t << 6)) + s * 16 * PITCH, PITCH);
+            for (int t = 0; t < DT; ++t) vf[s][t] = read_tr_frag(vb + (v_base ^ (uint32_t)(t * COLS * 2)) + s * 16 * PITCH, PITCH * LG / 2);
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(2);
+        float sc[NV];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) sc[v] = st[v / NA][v % NA];
         const int place = lo + 32 * c;
         const bool some = place + 31 >= masked_from;
         if (some || ok != 0xffffffffu) {
             const uint32_t on = some ? ok & seen(place) : ok;
 #pragma unroll
-            for (int v = 0; v < 16; ++v) sc[v] = on >> (8 * (v >> 2) + 4 * lh + (v & 3)) & 1u ? sc[v] : NEG_INF;
+            for (int v = 0; v < NV; ++v) sc[v] = on >> (4 * LG * (v >> 2) + 4 * g + (v & 3)) & 1u ? sc[v] : NEG_INF;
         }
         float mx = fmaxf(sc[0], sc[1]);
 #pragma unroll
-        for (int v = 2; v < 16; v += 2) mx = fmaxf(fmaxf(mx, sc[v]), sc[v + 1]);
+        for (int v = 2; v < NV; v += 2) mx = fmaxf(fmaxf(mx, sc[v]), sc[v + 1]);
         if (__builtin_amdgcn_ballot_w64(mx * a.scale_log2e > m)) {       // (most tiles of a long list bring no new maximum)
-            float x, y;
-            both_halves(mx, x, y);
-            const float mn = fmaxf(m, fmaxf(x, y) * a.scale_log2e);
+            const float mn = fmaxf(m, column_max(mx) * a.scale_log2e);
             const float corr = __builtin_amdgcn_exp2f(m - mn);
             m = mn;
             l *= corr;
 #pragma unroll
             for (int t = 0; t < DT; ++t)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) acc[t][e] *= corr;
+                for (int e = 0; e < NA; ++e) acc[t][e] *= corr;
         }
         float ps = 0.f;
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
+        for (int v = 0; v < NV; ++v) {
             sc[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[v], a.scale_log2e, -m));
             ps += sc[v];
         }
         l += ps;
-        u32x4 pv[2], pr[2];
+        u32x4 pv[PS], pr[PS];
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+        for (int s = 0; s < PS; ++s)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float x = sc[8 * s + 2 * i], y = sc[8 * s + 2 * i + 1];
@@ -354,16 +373,16 @@ __device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, Matr
             // and is added for the columns that do see it.
             bool any = false;
 #pragma unroll
-            for (int s = 0; s < 2; ++s)
+            for (int s = 0; s < PS; ++s)
 #pragma unroll
                 for (int t = 0; t < DT; ++t) {
-                    u32x4 x = __builtin_bit_cast(u32x4, vf[s][t]);
+                    const u32x4 x = __builtin_bit_cast(u32x4, vf[s][t]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) any |= not_finite2(x[i]);
+                    for (int i = 0; i < 4; ++i) any |= (x[i] & 0x7f80u) == 0x7f80u || (x[i] & 0x7f800000u) == 0x7f800000u;
                 }
             if (__builtin_amdgcn_ballot_w64(any)) {
 #pragma unroll
-                for (int s = 0; s < 2; ++s)
+                for (int s = 0; s < PS; ++s)
 #pragma unroll
                     for (int t = 0; t < DT; ++t) {
                         u32x4 x = __builtin_bit_cast(u32x4, vf[s][t]);
@@ -376,94 +395,96 @@ __device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, Matr
                     }
 #pragma unroll 1
                 for (int i = 0; i < 32; ++i) {
-                    // the weight of place i: in register (i / 8) * 4 + i % 4 of the lane with lh = i / 4 % 2
-                    float mine = 0.f;
+                    float p = 0.f;              // the column's weight of place i
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) mine = (i >> 3) * 4 + (i & 3) == v ? sc[v] : mine;
-                    float x, y;
-                    both_halves(mine, x, y);
-                    const float p = i >> 2 & 1 ? y : x;
-                    const uint32_t turn = D == 128 ? (uint32_t)(i & 3) << 2 : (uint32_t)(i >> 1 & 1) << 2;
+                    for (int v = 0; v < NV; ++v) p = i / (4 * LG) * 4 + (i & 3) == v ? sc[v] : p;
+                    p = __shfl(p, li + COLS * (i >> 2 & (LG - 1)));
 #pragma unroll
                     for (int t = 0; t < DT; ++t)
 #pragma unroll
-                        for (int v = 0; v < 16; ++v) {
-                            const int d = 32 * t + 8 * (v >> 2) + 4 * lh + (v & 3);
-                            const float z = bf16_bits_to_f32(*(const __attribute__((address_space(3))) bf16_t *)(vb + i * PITCH + ((((uint32_t)d >> 3) ^ turn) << 4) + (d & 7) * 2));
+                        for (int v = 0; v < NA; ++v) {
+                            const uint32_t d = (uint32_t)(COLS * t + 4 * LG * (v >> 2) + 4 * g + (v & 3));
+                            const float z = bf16_bits_to_f32(*(const __attribute__((address_space(3))) bf16_t *)(vb + i * PITCH + (((d >> 3) ^ L::v_turn(i)) << 4) + (d & 7) * 2));
                             if (!(fabsf(z) <= 3.402823466e38f) && !(p == 0.f)) acc[t][v] += p * z;
                         }
                 }
             }
         }
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+        for (int s = 0; s < PS; ++s)
 #pragma unroll
             for (int t = 0; t < DT; ++t) {
-                acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[s][t], __builtin_bit_cast(bf16x8, pv[s]), acc[t], 0, 0, 0);
-                if (WHOLE) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[s][t], __builtin_bit_cast(bf16x8, pr[s]), acc[t], 0, 0, 0);
+                acc[t] = multiply(vf[s][t], __builtin_bit_cast(bf16x8, pv[s]), acc[t]);
+                if (WHOLE) acc[t] = multiply(vf[s][t], __builtin_bit_cast(bf16x8, pr[s]), acc[t]);
             }
     };
-    // ---- the list, two tiles at a time --------------------------------------------------------------
-    // Tile c lives in pair c % NB.  A step waits for its own copies of tiles c and c + 1 (those of the NB - 4 behind them stay in flight); the barrier
-    // makes that hold for all wavefronts and tells that c - 2 and c - 1 have been multiplied by everyone: their pairs take the next two, whose
-    // slots were looked up a step earlier.  Tiles past the list are copied too (zeros), which keeps the count in flight the same.
+    // ---- the list, STEP tiles at a time -------------------------------------------------------------
+    // Tile c lives in pair c % NB.  A step waits for its own copies of tiles c .. c + STEP - 1 (those of the NB - 2 STEP behind them stay in flight); the
+    // barrier makes that hold for all wavefronts and tells that the step before has been multiplied by everyone: its pairs take the next tiles,
+    // whose slots were looked up a step earlier.  Tiles past the list are copied too (zeros), which keeps the count in flight the same.
     if (c_hi > 0) {
         refill(0);
 #pragma unroll
         for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qf[s]));      // (waited for here, not in the loop, where the copies would be waited for too)
 #pragma unroll
-        for (int k = 0; k < NB - 2; ++k) issue(k, lookup(k));
-        Entry b0 = lookup(NB - 2), b1 = lookup(NB - 1);
-        int cur = 0, nxt = NB - 2;
-        for (int c = 0; c < c_hi; c += 2) {
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(L::IPW * (NB - 4)) : "memory");
-            issue(nxt, b0);
-            issue(nxt + 1, b1);
+        for (int k = 0; k < NB - STEP; ++k) issue(k, lookup(k));
+        Entry next[STEP];
+#pragma unroll
+        for (int k = 0; k < STEP; ++k) next[k] = lookup(NB - STEP + k);
+        int cur = 0, nxt = NB - STEP;
+        for (int c = 0; c < c_hi; c += STEP) {
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(L::IPW * (NB - 2 * STEP)) : "memory");
+#pragma unroll
+            for (int k = 0; k < STEP; ++k) issue(nxt + k, next[k]);
             const int cn = c + NB;
             if (cn == win + WIN && cn < c_hi) refill(cn);
-            b0 = lookup(cn), b1 = lookup(cn + 1);
+#pragma unroll
+            for (int k = 0; k < STEP; ++k) next[k] = lookup(cn + k);
             if (work) {
-                consume(c, cur);
-                if (c + 1 < c_hi) consume(c + 1, cur + 1);
+#pragma unroll
+                for (int k = 0; k < STEP; ++k)
+                    if (k == 0 || c + k < c_hi) consume(c + k, cur + k);
             }
-            cur = cur + 2 == NB ? 0 : cur + 2;
-            nxt = nxt + 2 == NB ? 0 : nxt + 2;
+            cur = cur + STEP == NB ? 0 : cur + STEP;
+            nxt = nxt + STEP == NB ? 0 : nxt + STEP;
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");         // nothing may be on its way into LDS when the workgroup gives it back
     }
     {
         float x, y;
+        if (LG == 4) l += __shfl_xor(l, 16);
         both_halves(l, x, y);
         l = x + y;
     }
     if (part >= 0) {
         if (col_ok) {
             const size_t at = (size_t)part * part_columns + col;
-            if (lh == 0) *(f32x2 *)(a.ml + 2 * at) = (f32x2){m, l};
+            if (g == 0) *(f32x2 *)(a.ml + 2 * at) = (f32x2){m, l};
 #pragma unroll
             for (int t = 0; t < DT; ++t)
 #pragma unroll
-                for (int v = 0; v < 16; v += 4) *(f32x4 *)(a.o + at * D + 32 * t + 2 * v + 4 * lh) = (f32x4){acc[t][v], acc[t][v + 1], acc[t][v + 2], acc[t][v + 3]};
+                for (int v = 0; v < NA; v += 4)
+                    *(f32x4 *)(a.o + at * D + COLS * t + LG * v + 4 * g) = (f32x4){acc[t][v], acc[t][v + 1], acc[t][v + 2], acc[t][v + 3]};
         }
         return;
     }
-    // columns are rows of the result: a wavefront turns its 32 around in the tiles, which nobody reads any more
+    // columns are rows of the result: a wavefront turns its own around in the tiles, which nobody reads any more
     __syncthreads();
     if (!work) return;
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    lds_byte *strip = (lds_byte *)lds.tiles + w * (32 * L::SP);
+    lds_byte *strip = (lds_byte *)lds.tiles + w * (COLS * L::SP);
 #pragma unroll
     for (int t = 0; t < DT; ++t)
 #pragma unroll
-        for (int v = 0; v < 16; v += 4)
-            *(lds_u32x2 *)(strip + li * L::SP + (32 * t + 2 * v + 4 * lh) * 2) =
+        for (int v = 0; v < NA; v += 4)
+            *(lds_u32x2 *)(strip + li * L::SP + (COLS * t + LG * v + 4 * g) * 2) =
                 (u32x2){pack_bf16(acc[t][v] * inv, acc[t][v + 1] * inv), pack_bf16(acc[t][v + 2] * inv, acc[t][v + 3] * inv)};
 #pragma unroll
-    for (int i = 0; i < L::GROUPS; ++i) {
+    for (int i = 0; i < COLS / L::R; ++i) {
         const int c = L::R * i + lane / L::LPR;                 // (a column of this wavefront)
         const u32x4 o = *(const lds_u32x4 *)(strip + c * L::SP + 16 * (lane % L::LPR));
         const size_t at = (size_t)__shfl((unsigned long long)out_at, c);
-        if (32 * w + c < columns) *(u32x4 *)((bf16_t *)a.out + at + 8 * (lane % L::LPR)) = o;
+        if (COLS * w + c < columns) *(u32x4 *)((bf16_t *)a.out + at + 8 * (lane % L::LPR)) = o;
     }
 }
 
@@ -473,14 +494,9 @@ __device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, Matr
 template <int D, bool BF16>
 __device__ __forceinline__ void combine_parts(const ListArgs &a, size_t first, size_t step, int parts, int columns, int column, size_t out_at)
 {
-    constexpr int LP = D / 4, NS = 64 / LP, AHEAD = 4;
+    constexpr int LP = D / 4, NS = 64 / LP, AHEAD = 8;
     const int lane = threadIdx.x & 63, sub = lane / LP, d = lane % LP * 4;
-    auto ml = [&](int p) { return *(const f32x2 *)(a.ml + 2 * ((first + p * step) * columns + column)); };
-    float M = M_FLOOR;
-    for (int p = lane; p < parts; p += 64) M = fmaxf(M, ml(p).x);
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) M = fmaxf(M, __shfl_xor(M, off));
-    float L = 0.f;
+    float M = M_FLOOR, L = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     for (int p0 = sub; p0 < parts; p0 += NS * AHEAD) {
         f32x2 x[AHEAD];
@@ -488,25 +504,34 @@ __device__ __forceinline__ void combine_parts(const ListArgs &a, size_t first, s
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
             const int p = p0 + NS * i;
-            x[i] = (f32x2){M_FLOOR, 0.f};
-            y[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
-            if (p < parts) {
-                x[i] = ml(p);
-                y[i] = *(const f32x4 *)(a.o + ((first + p * step) * columns + column) * D + d);
-            }
+            const size_t at = (first + (p < parts ? p : 0) * step) * columns + column;      // (loads without branches)
+            x[i] = *(const f32x2 *)(a.ml + 2 * at);
+            y[i] = *(const f32x4 *)(a.o + at * D + d);
         }
+        float mn = M;
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) {
-            const float f = __builtin_amdgcn_exp2f(x[i].x - M);
+            if (p0 + NS * i >= parts) x[i] = (f32x2){NEG_INF, 0.f};
+            mn = fmaxf(mn, x[i].x);
+        }
+        const float was = __builtin_amdgcn_exp2f(M - mn);
+        M = mn;
+        L *= was;
+        o *= was;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const float f = __builtin_amdgcn_exp2f(x[i].x - mn);
             L += x[i].y * f;
-            o += y[i] * f;
+            if (p0 + NS * i < parts) o += y[i] * f;
         }
     }
 #pragma unroll
     for (int off = LP; off < 64; off <<= 1) {
-        L += __shfl_xor(L, off);
+        const float mo = __shfl_xor(M, off), lo = __shfl_xor(L, off), mn = fmaxf(M, mo), f = __builtin_amdgcn_exp2f(M - mn), h = __builtin_amdgcn_exp2f(mo - mn);
+        M = mn;
+        L = L * f + lo * h;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], off);
+        for (int e = 0; e < 4; ++e) o[e] = o[e] * f + __shfl_xor(o[e], off) * h;
     }
     if (sub != 0) return;
     const float inv = L == 0.f ? 0.f : 1.f / L;      // (not a number where a weight is none)

@@ -379,19 +379,21 @@ __global__ __launch_bounds__(NT) void block_list_kernel(SelectArgs a)
 struct SelectedArgs {
     ListArgs list;
     const int32_t *seq, *pos, *selected;
-    int budget, parts;
+    int budget, whole, parts;        // the first `whole` lists, of a (row, K/V head) each, are read by one workgroup, the others in parts
 };
 
 // The part of a row's list that workgroup blockIdx.x reads, counted in cache rows: places budget entry x block_size + offset.
 struct SelectedItem {
     int t, hk, n, pos, lo, hi;
+    long long part;      // number of the part whose sums are left, -1: a whole list
     const int32_t *bt, *entries;
 };
 __device__ __forceinline__ SelectedItem selected_item(const SelectedArgs &a, int *scratch)
 {
     const ListArgs &g = a.list;
-    const int rh = (int)blockIdx.x / a.parts, part = (int)blockIdx.x - rh * a.parts, tid = threadIdx.x;
+    const int tid = threadIdx.x, i = (int)blockIdx.x - a.whole, rh = i < 0 ? (int)blockIdx.x : a.whole + i / a.parts, parts = i < 0 ? 1 : a.parts, part = i < 0 ? 0 : i % a.parts;
     SelectedItem it;
+    it.part = i < 0 ? -1 : i;
     it.t = rh / g.Hkv, it.hk = rh - it.t * g.Hkv;
     const int seq = a.seq[it.t];
     it.pos = a.pos[it.t];
@@ -407,8 +409,9 @@ __device__ __forceinline__ SelectedItem selected_item(const SelectedArgs &a, int
     for (int o = 1; o < 64; o <<= 1) used = max(used, __shfl_xor(used, o));
     if ((tid & 63) == 0) scratch[tid >> 6] = used;
     __syncthreads();
-    used = max(max(scratch[0], scratch[1]), max(scratch[2], scratch[3]));
-    const long long places = (long long)used * g.bs, per = ((places + a.parts - 1) / a.parts + 31) / 32 * 32;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) used = max(used, scratch[i]);
+    const long long places = (long long)used * g.bs, per = ((places + parts - 1) / parts + 31) / 32 * 32;
     it.lo = (int)min(part * per, places);
     it.hi = (int)min(it.lo + per, places);
     return it;
@@ -434,8 +437,8 @@ __global__ __launch_bounds__(256) void selected_vector_kernel(SelectedArgs a)
         [&](int, int) { return true; },
         column_at,
         [&](int c, int d, float M, float L, float o) {
-            if (a.parts > 1) {
-                const size_t at = (size_t)blockIdx.x * G + c;
+            if (it.part >= 0) {
+                const size_t at = (size_t)it.part * G + c;
                 if (d == 0) *(f32x2 *)(g.ml + 2 * at) = (f32x2){M, L};
                 g.o[at * D + d] = o;
                 return;
@@ -450,27 +453,27 @@ __global__ __launch_bounds__(256) void selected_vector_kernel(SelectedArgs a)
 template <int D, bool ONCE>
 __global__ __launch_bounds__(256, 2) void selected_matrix_kernel(SelectedArgs a)
 {
-    __shared__ MatrixTiles<D, 4> lds;
+    __shared__ MatrixTiles<D, 4, 16, 512 / D, 1, 2048> lds;      // 64 KiB of tiles: two workgroups share a CU's LDS
     __shared__ int scratch[4];
     const ListArgs &g = a.list;
     const SelectedItem it = selected_item(a, scratch);
-    const int columns = 1 << g.lg_g, col = min((int)threadIdx.x & 31, columns - 1);
+    const int columns = 1 << g.lg_g, col = min((int)threadIdx.x & 15, columns - 1);
     const size_t at = ((size_t)it.t * g.Hq + ((size_t)it.hk << g.lg_g) + col) * D;
-    read_list_matrix<D, 4, true, ONCE>(
+    read_list_matrix<true, ONCE>(
         g, it.hk, lds, it.lo, it.hi, 0x7fffffff, columns,
         [&](int v) { return selected_slot(g, it, v); },
         [&](int) { return 0xffffffffu; },
-        at, at, a.parts > 1 ? (long long)blockIdx.x : -1ll, columns);
+        at, at, it.part, columns);
 }
 
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void selected_merge_kernel(SelectedArgs a)
 {
     const ListArgs &g = a.list;
-    const int c = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);      // (row, query head)
-    if (c >= g.T * g.Hq) return;
+    const int c = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), list = c >> g.lg_g;      // query head of a list in parts
+    if (list >= g.T * g.Hkv - a.whole) return;
     const int G = 1 << g.lg_g;
-    combine_parts<D, BF16>(g, (size_t)(c >> g.lg_g) * a.parts, 1, a.parts, G, c & (G - 1), (size_t)c * D);
+    combine_parts<D, BF16>(g, (size_t)list * a.parts, 1, a.parts, G, c & (G - 1), (((size_t)a.whole << g.lg_g) + c) * D);
 }
 
 // ---- host -----------------------------------------------------------------------------------------
@@ -486,18 +489,27 @@ static size_t select_bytes(const alora_attn_dims *d) { return two_kernels(d) ? (
 
 constexpr int MOST_BUDGET = 1 << 20;
 
-// Parts of every list: workgroups for the whole chip, of at least 256 places.
-static int selected_parts(const alora_attn_dims *d, int budget)
+// Lists are read whole while they fill the chip (512 workgroups: two to a compute unit), the others, behind them, in parts: as many as are done first, by what
+// was measured: a turn of workgroups takes 4 us and 0.03 for every place, the second kernel 3, each part 0.1 more.  us, 4, 8, 16, 32 parts of 8 lists of 2048
+// places: 18.8, 13.4, 11.5, 11.4.
+struct ListPlan {
+    int whole, parts;      // lists that are read whole; parts of the others
+};
+static ListPlan plan_lists(const alora_attn_dims *d, int budget)
 {
-    const long long lists = (long long)d->n_tokens * d->n_kv_heads, places = (long long)budget * d->block_size;
-    if (lists == 0) return 1;
-    return (int)std::max(1ll, std::min({(1024 + lists - 1) / lists, (places + 255) / 256, (long long)MAX_PARTS}));
+    const int lists = d->n_tokens * d->n_kv_heads, rest = lists % 512;
+    const float places = (float)budget * (float)d->block_size;
+    int best = 1;
+    float least = 4.f + 0.03f * places;
+    for (int p = 2; p <= MAX_PARTS; ++p) {
+        const float us = (float)((rest * p + 511) / 512) * (4.f + 0.03f * places / (float)p) + 3.f + 0.1f * (float)p;
+        if (us < least) least = us, best = p;
+    }
+    return best > 1 && rest ? ListPlan{lists - rest, best} : ListPlan{lists, 1};
 }
-static size_t selected_ml_bytes(const alora_attn_dims *d, int parts) { return ((size_t)d->n_tokens * d->n_q_heads * parts * 8 + 255) / 256 * 256; }
-static size_t selected_bytes(const alora_attn_dims *d, int parts)
-{
-    return parts > 1 ? selected_ml_bytes(d, parts) + (size_t)d->n_tokens * d->n_q_heads * parts * d->head_dim * 4 : 0;
-}
+static size_t in_parts(const alora_attn_dims *d, const ListPlan &p) { return ((size_t)d->n_tokens * d->n_kv_heads - p.whole) * p.parts * (d->n_q_heads / d->n_kv_heads); }
+static size_t selected_ml_bytes(const alora_attn_dims *d, const ListPlan &p) { return (in_parts(d, p) * 8 + 255) / 256 * 256; }
+static size_t selected_bytes(const alora_attn_dims *d, const ListPlan &p) { return p.parts > 1 ? selected_ml_bytes(d, p) + in_parts(d, p) * d->head_dim * 4 : 0; }
 
 }  // namespace alora
 
@@ -595,7 +607,7 @@ int alora_selected_attention_workspace_bytes(const alora_attn_dims *dims, int32_
     if (!out_bytes || budget < 1 || budget > MOST_BUDGET) return ALORA_EINVAL;
     const int st = check_select(dims);
     if (st) return st;
-    *out_bytes = selected_bytes(dims, selected_parts(dims, budget));
+    *out_bytes = selected_bytes(dims, plan_lists(dims, budget));
     return ALORA_OK;
 }
 
@@ -608,35 +620,36 @@ int alora_selected_attention(const void *q, const void *k_cache, const void *v_c
     if (budget < 1 || budget > MOST_BUDGET) return ALORA_EINVAL;
     if ((long long)budget * dims->block_size > 0x3fffffffll) return ALORA_ESHAPE;
     if (dims->n_tokens == 0) return ALORA_OK;
-    const int parts = selected_parts(dims, budget);
-    const size_t need = selected_bytes(dims, parts);
+    const ListPlan plan = plan_lists(dims, budget);
+    const size_t need = selected_bytes(dims, plan);
     if (need && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < need)) return ALORA_EWORKSPACE;
     if (!q || !k_cache || !v_cache || !block_tables || !token_seq_ids || !token_positions || !selected || !out) return ALORA_EINVAL;
     if (((uintptr_t)q | (uintptr_t)k_cache | (uintptr_t)v_cache | (uintptr_t)out) & 15) return ALORA_EINVAL;
     if (((uintptr_t)block_tables | (uintptr_t)token_seq_ids | (uintptr_t)token_positions | (uintptr_t)selected) & 3) return ALORA_EINVAL;
     SelectedArgs a;
     a.list = list_args(dims, q, k_cache, v_cache, block_tables, out);
-    a.seq = token_seq_ids; a.pos = token_positions; a.selected = selected; a.budget = budget; a.parts = parts;
-    if (parts > 1) {
+    a.seq = token_seq_ids; a.pos = token_positions; a.selected = selected; a.budget = budget; a.whole = plan.whole; a.parts = plan.parts;
+    const int lists = dims->n_tokens * dims->n_kv_heads, rest = lists - plan.whole;
+    if (rest) {
         a.list.ml = (float *)workspace;
-        a.list.o = (float *)((char *)workspace + selected_ml_bytes(dims, parts));
+        a.list.o = (float *)((char *)workspace + selected_ml_bytes(dims, plan));
     }
     const bool bf16 = dims->dtype == ALORA_BF16;
-    const dim3 grid((unsigned)dims->n_tokens * (unsigned)dims->n_kv_heads * (unsigned)parts);
+    const bool once = dims->n_tokens <= dims->n_seqs && outgrows_cache(dims->n_slots, dims->n_kv_heads, dims->head_dim, true);      // (see launch_attention_blocks)
+    const dim3 grid((unsigned)plan.whole + (unsigned)rest * (unsigned)plan.parts);
     const auto go = [&](auto kernel) { launch_kernel(kernel, grid, dim3(256), 0, (hipStream_t)hip_stream, a); };
     const auto choose = [&](auto head_dim, auto is_bf16) {
         constexpr int D = decltype(head_dim)::value;
         constexpr bool B = decltype(is_bf16)::value;
         if constexpr (B) {
-            go(selected_matrix_kernel<D, false>);
+            once ? go(selected_matrix_kernel<D, true>) : go(selected_matrix_kernel<D, false>);
         } else switch (a.list.lg_g) {
         case 0: go(selected_vector_kernel<D, 1, B>); break;
         case 1: go(selected_vector_kernel<D, 2, B>); break;
         case 2: go(selected_vector_kernel<D, 4, B>); break;
         default: go(selected_vector_kernel<D, 8, B>); break;
         }
-        if (parts > 1)
-            launch_kernel(selected_merge_kernel<D, B>, dim3(((unsigned)dims->n_tokens * (unsigned)dims->n_q_heads + 3) / 4), dim3(256), 0, (hipStream_t)hip_stream, a);
+        if (rest) launch_kernel(selected_merge_kernel<D, B>, dim3((((unsigned)rest << a.list.lg_g) + 3) / 4), dim3(256), 0, (hipStream_t)hip_stream, a);
     };
     typedef std::integral_constant<int, 128> D128;
     typedef std::integral_constant<int, 64> D64;

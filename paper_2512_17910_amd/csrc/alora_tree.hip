@@ -20,7 +20,7 @@ struct TreeArgs {
     const int32_t *offsets, *context;
     const uint32_t *mask;       // [T][2 * words]
     int words, tile_rows;       // rows of a tile
-    int target;                 // workgroups per K/V head the parts are cut for
+    int places;                 // workgroups per K/V head that the chip holds at once
     int max_tiles, max_items;   // the workspace has room for (offsets that do not ascend may give more)
     int *n_tiles;
     TreeTile *tiles;
@@ -28,6 +28,7 @@ struct TreeArgs {
 
 constexpr int UNIT = 32;        // positions that parts are counted in
 constexpr int LEAST_UNITS = 8;  // of a part
+constexpr int GOOD_UNITS = 12;
 
 struct TreeItem {
     int row0, rows;             // the tile's rows
@@ -35,16 +36,21 @@ struct TreeItem {
     int lo, hi, parts, part_at; // places of the sequence this workgroup reads; number of its part's sums
 };
 
+constexpr int CLASSES = 4;      // of parts by their length
+
 struct TreeScratch {
-    float total[8];
-    int sums[8][2], found[8];
+    float total[8][2];
+    int sums[8][CLASSES + 1], found[8];
 };
 
 // Which tile and part workgroup `item` (of one K/V head, NW wavefronts) is for; false: none.  The same sums in every workgroup of the call.
+// A sequence's parts are equal, none longer than `per`; the longest start first (in quarters of per): 48 contexts of 1000 to 16000, wide trees, in
+// batch order ORDER_US.
 template <int NW>
 __device__ __forceinline__ bool find_item(const TreeArgs &a, int item, int hk, TreeScratch &scr, TreeItem &it)
 {
     const ListArgs &g = a.list;
+    constexpr int NT = 64 * NW;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, n_seqs = g.n_seqs;
     const long long cap = min((long long)g.max_blocks * g.bs, 0x7fffffffll);
     struct Seq { int r0, n, ctx, places, tiles, units; };
@@ -60,35 +66,83 @@ __device__ __forceinline__ bool find_item(const TreeArgs &a, int item, int hk, T
         }
         return q;
     };
-    // all units of all tiles, in a fixed order
+    // all units of all tiles, and the tiles, in a fixed order
     Seq q = seq_of(tid);
-    float mine = 0.f;
-    for (int s = tid;; s += 64 * NW) {
+    float mine = 0.f, mine_tiles = 0.f;
+    for (int s = tid;; s += NT) {
         const Seq x = s == tid ? q : seq_of(s);
         mine += (float)x.tiles * (float)x.units;
-        if (s + 64 * NW >= n_seqs) break;
+        mine_tiles += (float)x.tiles;
+        if (s + NT >= n_seqs) break;
     }
 #pragma unroll
-    for (int off = 1; off < 64; off <<= 1) mine += __shfl_xor(mine, off);
-    if (lane == 0) scr.total[w] = mine;
+    for (int off = 1; off < 64; off <<= 1) mine += __shfl_xor(mine, off), mine_tiles += __shfl_xor(mine_tiles, off);
+    if (lane == 0) scr.total[w][0] = mine, scr.total[w][1] = mine_tiles;
     if (tid == 0) scr.found[0] = -1;
     __syncthreads();
-    float total = 0.f;
+    float total = 0.f, tiles = 0.f;
 #pragma unroll
-    for (int i = 0; i < NW; ++i) total += scr.total[i];
-    const int per = max(LEAST_UNITS, (int)fminf(ceilf(total / (float)a.target), 1.0e9f));
-    int items0 = 0, tiles0 = 0;
-    for (int s0 = 0; s0 < n_seqs; s0 += 64 * NW) {
-        if (s0) q = seq_of(s0 + tid);
-        const int parts = max(1, (q.units + per - 1) / per), items = q.tiles * parts;
-        const int u = sum_upto64(items), v = sum_upto64(q.tiles);
-        if (lane == 63) scr.sums[w][0] = u, scr.sums[w][1] = v;
+    for (int i = 0; i < NW; ++i) total += scr.total[i][0], tiles += scr.total[i][1];
+    // Units of a part.  Few tiles: as many workgroups as the chip holds at once (a tile's last part may be short: one more for each), of short contexts half as many,
+    // one to a compute unit.  Many: one and a half times as many, the longest first.  us, 32/8 heads, 128, 256, 384, 512, 768 workgroups: 13 rows at 9000
+    // positions 25.2, 21.1, 24.9, 24.8, 24.7, at 32000 59.7, 39.4, 40.4, 37.9, 47.6, 4 x 13 rows at 16000 106, 63.5, 62.5, 53.7, 68.6; 64/8 heads, 64 rows at
+    // 64000 387, 212, 209, 181, 204.
+    const float room = (float)a.places - tiles, half = (float)(a.places / 2) - tiles;
+    float units = ceilf(total / ((float)a.places * 1.5f));
+    if (2.f * tiles <= (float)a.places) units = ceilf(total / room);
+    if (units < (float)GOOD_UNITS && half >= 1.f) units = ceilf(total / half);
+    const int per = max(LEAST_UNITS, (int)fminf(units, 1.0e9f));
+    auto parts_of = [&](const Seq &x) { return max(1, (x.units + per - 1) / per); };
+    auto size_of = [&](const Seq &x, int parts) { return (x.units + parts - 1) / parts; };      // units of a part (the last one's may be fewer)
+    auto class_of = [&](int size) { return min(CLASSES - 1, (int)((float)(per - size) * (float)CLASSES / (float)per)); };
+    // where a class's items begin: one chunk of requests finds it with their own places, more of them ahead
+    int begin[CLASSES + 1] = {};           // (the last: tiles)
+    if (n_seqs > NT) {
+        int count[CLASSES] = {};
+        for (int s = tid; s < n_seqs; s += NT) {
+            const Seq x = s == tid ? q : seq_of(s);
+            const int parts = parts_of(x), c = class_of(size_of(x, parts));
+#pragma unroll
+            for (int i = 0; i < CLASSES; ++i) count[i] += c == i ? x.tiles * parts : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < CLASSES; ++i) {
+            const int u = sum_upto64(count[i]);
+            if (lane == 63) scr.sums[w][i] = u;
+        }
         __syncthreads();
-        int at = items0 + u - items, tile_at = tiles0 + v - q.tiles;
+        int upto = 0;
 #pragma unroll
-        for (int i = 0; i < NW; ++i) {
-            if (i < w) at += scr.sums[i][0], tile_at += scr.sums[i][1];
-            items0 += scr.sums[i][0], tiles0 += scr.sums[i][1];
+        for (int i = 0; i < CLASSES; ++i) {
+            begin[i] = upto;
+#pragma unroll
+            for (int j = 0; j < NW; ++j) upto += scr.sums[j][i];
+        }
+        __syncthreads();
+    }
+    for (int s0 = 0; s0 < n_seqs; s0 += NT) {
+        if (s0) q = seq_of(s0 + tid);
+        const int parts = parts_of(q), size = size_of(q, parts), c = class_of(size), items = q.tiles * parts;
+        int mine[CLASSES + 1], upto[CLASSES + 1];
+#pragma unroll
+        for (int i = 0; i <= CLASSES; ++i) {
+            mine[i] = i == CLASSES ? q.tiles : c == i ? items : 0;
+            upto[i] = sum_upto64(mine[i]);
+            if (lane == 63) scr.sums[w][i] = upto[i];
+        }
+        __syncthreads();
+        int all = 0, at = 0, tile_at = 0;
+#pragma unroll
+        for (int i = 0; i <= CLASSES; ++i) {
+            int here = (n_seqs > NT || i == CLASSES ? begin[i] : all) + upto[i] - mine[i];
+#pragma unroll
+            for (int j = 0; j < NW; ++j) {
+                if (j < w) here += scr.sums[j][i];
+                if (i < CLASSES) all += scr.sums[j][i];
+                begin[i] += scr.sums[j][i];
+            }
+            if (i == CLASSES) tile_at = here;
+            else if (c == i) at = here;
         }
         if (item >= at && item < at + items) {
             const int i = item - at, part = i / q.tiles, tile = i - part * q.tiles;      // (tiles of one part next to each other: they read the same rows)
@@ -100,17 +154,18 @@ __device__ __forceinline__ bool find_item(const TreeArgs &a, int item, int hk, T
             scr.found[4] = q.places - q.ctx;
             scr.found[5] = part;
             scr.found[6] = parts;
+            scr.found[7] = size;
             if (hk == 0 && part == 0 && tile_at + tile < a.max_tiles) a.tiles[tile_at + tile] = {row0, rows, parts, at + tile, q.tiles, {}};
         }
         __syncthreads();
         if (scr.found[0] >= 0 && item != 0) break;       // (workgroup 0 counts all tiles)
     }
-    if (item == 0 && hk == 0 && tid == 0) *a.n_tiles = min(tiles0, a.max_tiles);
+    if (item == 0 && hk == 0 && tid == 0) *a.n_tiles = min(begin[CLASSES], a.max_tiles);
     if (scr.found[0] < 0) return false;
     it.seq = scr.found[0], it.row0 = scr.found[1], it.rows = scr.found[2], it.ctx = scr.found[3], it.drafts = scr.found[4], it.parts = scr.found[6];
-    const int part = scr.found[5], places = it.ctx + it.drafts;
-    it.lo = (int)min((long long)part * per * UNIT, (long long)places);
-    it.hi = (int)min((long long)it.lo + (long long)per * UNIT, (long long)places);
+    const int places = it.ctx + it.drafts;
+    it.lo = (int)min((long long)scr.found[5] * scr.found[7] * UNIT, (long long)places);
+    it.hi = (int)min((long long)it.lo + (long long)scr.found[7] * UNIT, (long long)places);
     it.part_at = item;
     return true;
 }
@@ -171,7 +226,7 @@ __global__ __launch_bounds__(256) void tree_vector_kernel(TreeArgs a)
 template <int D, int NW, bool WHOLE, bool ONCE>
 __global__ __launch_bounds__(64 * NW, 2) void tree_matrix_kernel(TreeArgs a)
 {
-    __shared__ MatrixTiles<D, NW> lds;
+    __shared__ MatrixTiles<D, NW, 32, 512 / D, 2, 2048> lds;      // 64 KiB of tiles: two workgroups share a CU's LDS
     __shared__ TreeScratch find;
     const ListArgs &g = a.list;
     const int hk = (int)blockIdx.x % g.Hkv, item = (int)blockIdx.x / g.Hkv;
@@ -182,7 +237,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_matrix_kernel(TreeArgs a)
     const int col = 32 * ((int)threadIdx.x >> 6) + ((int)threadIdx.x & 31), columns = it.rows << g.lg_g, row = it.row0 + (min(col, columns - 1) >> g.lg_g);
     const uint32_t *bits = a.mask + (size_t)row * 2 * a.words;
     const size_t at = ((size_t)row * g.Hq + ((size_t)hk << g.lg_g) + (col & ((1 << g.lg_g) - 1))) * D;
-    read_list_matrix<D, NW, WHOLE, ONCE>(
+    read_list_matrix<WHOLE, ONCE>(
         g, hk, lds, it.lo, it.hi, it.ctx, columns,
         [&](int v) { return slot_at(g, bt, v / g.bs, v % g.bs); },
         [&](int place) {               // the row's bits of drafts place - ctx .. + 31; what lies in front of them is seen
@@ -208,9 +263,10 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int columns
 
 // ---- host ---------------------------------------------------------------------------------------
 // How a call is cut: columns of a tile, the most tiles and items (tile, part) of a K/V head there can be, and where the workspace's arrays lie.
+constexpr int WAVES = 4;
 struct TreePlan {
-    int waves;                  // wavefronts of a workgroup on matrix instructions; 0: vector arithmetic
-    int columns, tile_rows, target;
+    bool matrix;                // instructions; else vector arithmetic
+    int columns, tile_rows, places;
     long long tiles, items;
     size_t tiles_at, ml_at, o_at, bytes;
 };
@@ -218,12 +274,12 @@ static TreePlan plan_tree(const alora_attn_dims *d)
 {
     TreePlan p;
     const int G = d->n_q_heads / d->n_kv_heads;
-    p.waves = d->dtype != ALORA_BF16 ? 0 : (long long)d->n_tokens * G > 160ll * d->n_seqs ? 8 : 4;
-    p.columns = p.waves ? 32 * p.waves : 8;
+    p.matrix = d->dtype == ALORA_BF16;
+    p.columns = p.matrix ? 32 * WAVES : 8;
     p.tile_rows = p.columns / G;
-    p.target = std::max(1, 1024 / d->n_kv_heads);
+    p.places = std::max(1, 512 / d->n_kv_heads);
     p.tiles = d->n_tokens / p.tile_rows + std::min(d->n_seqs, d->n_tokens);      // (a sequence's last tile may not be full)
-    p.items = p.tiles + p.target + 1;                                            // sum of ceil(units / per) over tiles, per >= all units / target
+    p.items = p.tiles + p.places * 3 / 2 + 1;                                    // sum of ceil(units / per) over tiles, per >= all units / (1.5 places)
     const auto up = [](size_t n) { return (n + 255) / 256 * 256; };
     p.tiles_at = 256;
     p.ml_at = p.tiles_at + up((size_t)p.tiles * sizeof(TreeTile));
@@ -274,21 +330,27 @@ int alora_tree_attention(const void *q, const void *k_cache, const void *v_cache
     a.list.o = (float *)((char *)workspace + p.o_at);
     a.offsets = row_offsets; a.context = context_lens;
     a.mask = (const uint32_t *)tree_mask; a.words = mask_words;
-    a.tile_rows = p.tile_rows; a.target = p.target;
+    a.tile_rows = p.tile_rows; a.places = p.places;
     a.max_tiles = (int)p.tiles; a.max_items = (int)p.items;
     a.n_tiles = (int *)workspace;
     a.tiles = (TreeTile *)((char *)workspace + p.tiles_at);
     const bool bf16 = dims->dtype == ALORA_BF16;
     const dim3 grid((unsigned)((p.items + 1) * dims->n_kv_heads)), merge((unsigned)(p.tiles * dims->n_kv_heads), (unsigned)p.columns / 4);
     const auto go = [&](auto kernel, auto combine) {
-        launch_kernel(kernel, grid, dim3(p.waves ? 64 * (unsigned)p.waves : 256), 0, (hipStream_t)hip_stream, a);
+        launch_kernel(kernel, grid, dim3(64 * WAVES), 0, (hipStream_t)hip_stream, a);
         launch_kernel(combine, merge, dim3(256), 0, (hipStream_t)hip_stream, a, p.columns);
     };
+    // Weights whole where a sequence brings one wavefront's columns on average: then the call waits for memory.  Non-temporal copies where it brings one tile, so
+    // that its context is read once, and the memory-side cache would not keep K and V.  us, ordinary | non-temporal | with whole weights, 32/8 heads, 8192
+    // positions: 64 x 1 rows 376 | | 341, 64 x 8 379 | | 344, 2000 positions: 300 x 4 480 | | 452; 64/8 heads, 64 rows at 64000, four tiles 181 | | 245.
+    const long long columns = (long long)dims->n_tokens * (dims->n_q_heads / dims->n_kv_heads);
+    const bool whole = columns <= 32ll * dims->n_seqs;
+    const bool once = columns <= 32ll * WAVES * dims->n_seqs && outgrows_cache(dims->n_slots, dims->n_kv_heads, dims->head_dim, true);
     const auto choose = [&](auto head_dim) {
         constexpr int D = decltype(head_dim)::value;
         if (!bf16) go(tree_vector_kernel<D, 8, false>, tree_merge_kernel<D, false>);
-        else if (p.waves == 8) go(tree_matrix_kernel<D, 8, false, false>, tree_merge_kernel<D, true>);
-        else go(tree_matrix_kernel<D, 4, true, false>, tree_merge_kernel<D, true>);
+        else if (whole) once ? go(tree_matrix_kernel<D, WAVES, true, true>, tree_merge_kernel<D, true>) : go(tree_matrix_kernel<D, WAVES, true, false>, tree_merge_kernel<D, true>);
+        else once ? go(tree_matrix_kernel<D, WAVES, false, true>, tree_merge_kernel<D, true>) : go(tree_matrix_kernel<D, WAVES, false, false>, tree_merge_kernel<D, true>);
     };
     if (dims->head_dim == 128) choose(std::integral_constant<int, 128>{});
     else choose(std::integral_constant<int, 64>{});
