@@ -28,7 +28,7 @@ struct TreeArgs {
 
 constexpr int UNIT = 32;        // positions that parts are counted in
 constexpr int LEAST_UNITS = 8;  // of a part
-constexpr int GOOD_UNITS = 12;
+constexpr int GOOD_UNITS = 12;  // from which two workgroups to a compute unit are worth their parts
 
 struct TreeItem {
     int row0, rows;             // the tile's rows
@@ -38,20 +38,25 @@ struct TreeItem {
 
 constexpr int CLASSES = 4;      // of parts by their length
 
+constexpr int CUTS = 5;
+// What a call costs in units (32 positions of a tile), by what was measured: a workgroup's start, and a part's sums.
+constexpr float START = 7.f, PART = 7.f;
+
 struct TreeScratch {
-    float total[8][2];
-    int sums[8][CLASSES + 1], found[8];
+    float sums[3 * CUTS][8];
+    int counts[8][CLASSES + 1], found[8];
 };
 
-// Which tile and part workgroup `item` (of one K/V head, NW wavefronts) is for; false: none.  The same sums in every workgroup of the call.
-// A sequence's parts are equal, none longer than `per`; the longest start first (in quarters of per): 48 contexts of 1000 to 16000, wide trees, in
-// batch order ORDER_US.
+// Which tile and part workgroup `item` (of one K/V head, NW wavefronts) is for; false: none.  The same sums, in the same order, in every workgroup of the
+// call.  A sequence's parts are equal, none longer than `per`; the longest start first (in quarters of per).  Up to 64 sequences, every wavefront
+// finds out for itself; of more, each has a share and LDS brings them together.
 template <int NW>
 __device__ __forceinline__ bool find_item(const TreeArgs &a, int item, int hk, TreeScratch &scr, TreeItem &it)
 {
     const ListArgs &g = a.list;
-    constexpr int NT = 64 * NW;
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, n_seqs = g.n_seqs;
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n_seqs = g.n_seqs;
+    const bool alone = n_seqs <= 64;
+    const int first = alone ? lane : (int)threadIdx.x, step = alone ? 64 : 64 * NW;
     const long long cap = min((long long)g.max_blocks * g.bs, 0x7fffffffll);
     struct Seq { int r0, n, ctx, places, tiles, units; };
     auto seq_of = [&](int s) {
@@ -66,49 +71,90 @@ __device__ __forceinline__ bool find_item(const TreeArgs &a, int item, int hk, T
         }
         return q;
     };
-    // all units of all tiles, and the tiles, in a fixed order
-    Seq q = seq_of(tid);
-    float mine = 0.f, mine_tiles = 0.f;
-    for (int s = tid;; s += NT) {
-        const Seq x = s == tid ? q : seq_of(s);
-        mine += (float)x.tiles * (float)x.units;
-        mine_tiles += (float)x.tiles;
-        if (s + NT >= n_seqs) break;
+    auto for_each = [&](const Seq &q, auto f) {
+        f(q);
+        for (int s = first + step; s < n_seqs; s += step) f(seq_of(s));
+    };
+    // a sum over lanes 0 .. lane of every wavefront -> that over all sequences
+    auto over_all = [&](float x, float (&of_wave)[8], bool largest) {
+        x = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+        if (alone) return x;
+        if (lane == 0) of_wave[w] = x;
+        __syncthreads();
+        x = of_wave[0];
+#pragma unroll
+        for (int i = 1; i < NW; ++i) x = largest ? fmaxf(x, of_wave[i]) : x + of_wave[i];
+        return x;
+    };
+    // Units of all tiles, tiles, the longest.
+    Seq q = seq_of(first);
+    float total = 0.f, tiles = 0.f, most = 0.f;
+    for_each(q, [&](const Seq &x) {
+        total += (float)x.tiles * (float)x.units;
+        tiles += (float)x.tiles;
+        most = fmaxf(most, x.tiles ? (float)x.units : 0.f);
+    });
+    total = over_all(sum_upto64(total), scr.sums[0], false);
+    tiles = over_all(sum_upto64(tiles), scr.sums[1], false);
+    most = fmaxf(over_all(__int_as_float(max_upto64(__float_as_int(most))), scr.sums[2], true), 1.f);
+    // Units of a part.  (Reciprocals: an IEEE division is 15 instructions, and every workgroup does this before its first copy.)
+    auto over = [](float x, float y) { return x * __builtin_amdgcn_rcpf(y); };
+    const float places = (float)a.places, share = over(total, places), room = places - tiles, half = .5f * places - tiles;
+    float units = most;
+    if (half >= 1.f) {
+        // Few tiles: as many parts as fit the chip in one turn, or, of short contexts, half of it, a workgroup to each compute unit (a tile's last part may be
+        // short: one more for each).  us, 32/8 heads, 128, 256, 384, 512, 768 workgroups: 13 rows at 9000 positions 25.2, 21.1, 24.9, 24.8, 24.7, at 32000 59.7, 39.4,
+        // 40.4, 37.9, 47.6, 4 x 13 rows at 16000 106, 63.5, 62.5, 53.7, 68.6; 64/8 heads, 64 rows at 64000 387, 212, 209, 181, 204.
+        units = over(total, room);
+        if (units < (float)GOOD_UNITS) units = over(total, half);
+        units = fmaxf(fminf(ceilf(units), most), (float)LEAST_UNITS);
+    } else {
+        // Many: the best of whole tiles, an equal share for every place of the chip or two thirds of it, as many parts as fit in one turn or in two.
+        float cut[CUTS] = {most, share, share * (2.f / 3), over(total, room), over(total, 2.f * places - tiles)};
+        float items_of[CUTS] = {}, parts_at[CUTS] = {}, most_of[CUTS] = {}, one_over[CUTS];
+#pragma unroll
+        for (int i = 0; i < CUTS; ++i) {
+            cut[i] = cut[i] > 0.f ? fmaxf(fminf(ceilf(cut[i]), most), (float)LEAST_UNITS) : most;
+            one_over[i] = __builtin_amdgcn_rcpf(cut[i]);
+        }
+        for_each(q, [&](const Seq &x) {
+#pragma unroll
+            for (int i = 0; i < CUTS; ++i) {
+                const float parts = fmaxf(ceilf((float)x.units * one_over[i] - 1e-3f), 1.f), n = parts * (float)x.tiles;
+                items_of[i] += n;
+                parts_at[i] += parts > 1.f ? n : 0.f;
+                most_of[i] = fmaxf(most_of[i], x.tiles ? over((float)x.units, parts) : 0.f);
+            }
+        });
+        float best = 3.0e38f;
+#pragma unroll
+        for (int i = 0; i < CUTS; ++i) {
+            const float n = over_all(sum_upto64(items_of[i]), scr.sums[3 * i], false), p = over_all(sum_upto64(parts_at[i]), scr.sums[3 * i + 1], false);
+            const float m = over_all(__int_as_float(max_upto64(__float_as_int(most_of[i]))), scr.sums[3 * i + 2], true);
+            // In units: as many turns as the chip takes, or its places filled by the longest first; a start for each turn; what parts leave and are combined from.
+            const float filled = over(n, places), turns = ceilf(filled - 1e-3f);
+            const float span = fminf(turns * m, fmaxf(m, fminf(share, filled * m) + m * (1.f / 3))), cost = span + START * turns + over(PART * p, places);
+            if (cost < best) best = cost, units = cut[i];
+        }
     }
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) mine += __shfl_xor(mine, off), mine_tiles += __shfl_xor(mine_tiles, off);
-    if (lane == 0) scr.total[w][0] = mine, scr.total[w][1] = mine_tiles;
-    if (tid == 0) scr.found[0] = -1;
-    __syncthreads();
-    float total = 0.f, tiles = 0.f;
-#pragma unroll
-    for (int i = 0; i < NW; ++i) total += scr.total[i][0], tiles += scr.total[i][1];
-    // Units of a part.  Few tiles: as many workgroups as the chip holds at once (a tile's last part may be short: one more for each), of short contexts half as many,
-    // one to a compute unit.  Many: one and a half times as many, the longest first.  us, 32/8 heads, 128, 256, 384, 512, 768 workgroups: 13 rows at 9000
-    // positions 25.2, 21.1, 24.9, 24.8, 24.7, at 32000 59.7, 39.4, 40.4, 37.9, 47.6, 4 x 13 rows at 16000 106, 63.5, 62.5, 53.7, 68.6; 64/8 heads, 64 rows at
-    // 64000 387, 212, 209, 181, 204.
-    const float room = (float)a.places - tiles, half = (float)(a.places / 2) - tiles;
-    float units = ceilf(total / ((float)a.places * 1.5f));
-    if (2.f * tiles <= (float)a.places) units = ceilf(total / room);
-    if (units < (float)GOOD_UNITS && half >= 1.f) units = ceilf(total / half);
-    const int per = max(LEAST_UNITS, (int)fminf(units, 1.0e9f));
+    const int per = (int)fminf(units, 1.0e9f);
     auto parts_of = [&](const Seq &x) { return max(1, (x.units + per - 1) / per); };
     auto size_of = [&](const Seq &x, int parts) { return (x.units + parts - 1) / parts; };      // units of a part (the last one's may be fewer)
-    auto class_of = [&](int size) { return min(CLASSES - 1, (int)((float)(per - size) * (float)CLASSES / (float)per)); };
-    // where a class's items begin: one chunk of requests finds it with their own places, more of them ahead
-    int begin[CLASSES + 1] = {};           // (the last: tiles)
-    if (n_seqs > NT) {
+    auto class_of = [&](int size) { return min(CLASSES - 1, (int)((float)(per - size) * (float)CLASSES * __builtin_amdgcn_rcpf((float)per))); };
+    // Where a class's items begin, and behind them the tiles: `begin` of the sequences before, of all classes where there is more than one round.
+    int begin[CLASSES + 1] = {};
+    if (n_seqs > step) {
         int count[CLASSES] = {};
-        for (int s = tid; s < n_seqs; s += NT) {
-            const Seq x = s == tid ? q : seq_of(s);
+        for_each(q, [&](const Seq &x) {
             const int parts = parts_of(x), c = class_of(size_of(x, parts));
 #pragma unroll
             for (int i = 0; i < CLASSES; ++i) count[i] += c == i ? x.tiles * parts : 0;
-        }
+        });
+        __syncthreads();
 #pragma unroll
         for (int i = 0; i < CLASSES; ++i) {
             const int u = sum_upto64(count[i]);
-            if (lane == 63) scr.sums[w][i] = u;
+            if (lane == 63) scr.counts[w][i] = u;
         }
         __syncthreads();
         int upto = 0;
@@ -116,56 +162,76 @@ __device__ __forceinline__ bool find_item(const TreeArgs &a, int item, int hk, T
         for (int i = 0; i < CLASSES; ++i) {
             begin[i] = upto;
 #pragma unroll
-            for (int j = 0; j < NW; ++j) upto += scr.sums[j][i];
+            for (int j = 0; j < NW; ++j) upto += scr.counts[j][i];
         }
-        __syncthreads();
     }
-    for (int s0 = 0; s0 < n_seqs; s0 += NT) {
-        if (s0) q = seq_of(s0 + tid);
+    int found[8] = {-1};
+    if (!alone) {
+        __syncthreads();
+        if (threadIdx.x == 0) scr.found[0] = -1;
+    }
+    for (int s0 = 0; s0 < n_seqs; s0 += step) {
+        if (s0) q = seq_of(s0 + first);
         const int parts = parts_of(q), size = size_of(q, parts), c = class_of(size), items = q.tiles * parts;
         int mine[CLASSES + 1], upto[CLASSES + 1];
 #pragma unroll
         for (int i = 0; i <= CLASSES; ++i) {
             mine[i] = i == CLASSES ? q.tiles : c == i ? items : 0;
             upto[i] = sum_upto64(mine[i]);
-            if (lane == 63) scr.sums[w][i] = upto[i];
+            if (!alone && lane == 63) scr.counts[w][i] = upto[i];
         }
-        __syncthreads();
+        if (!alone) __syncthreads();
         int all = 0, at = 0, tile_at = 0;
 #pragma unroll
         for (int i = 0; i <= CLASSES; ++i) {
-            int here = (n_seqs > NT || i == CLASSES ? begin[i] : all) + upto[i] - mine[i];
+            int here = (n_seqs > step || i == CLASSES ? begin[i] : all) + upto[i] - mine[i];
+            if (alone) {
+                const int sum = __builtin_amdgcn_readlane(upto[i], 63);
+                if (i < CLASSES) all += sum;
+                begin[i] += sum;
+            } else {
 #pragma unroll
-            for (int j = 0; j < NW; ++j) {
-                if (j < w) here += scr.sums[j][i];
-                if (i < CLASSES) all += scr.sums[j][i];
-                begin[i] += scr.sums[j][i];
+                for (int j = 0; j < NW; ++j) {
+                    if (j < w) here += scr.counts[j][i];
+                    if (i < CLASSES) all += scr.counts[j][i];
+                    begin[i] += scr.counts[j][i];
+                }
             }
             if (i == CLASSES) tile_at = here;
             else if (c == i) at = here;
         }
-        if (item >= at && item < at + items) {
+        const bool here = item >= at && item < at + items;
+        int mine_found[8] = {};
+        if (here) {
             const int i = item - at, part = i / q.tiles, tile = i - part * q.tiles;      // (tiles of one part next to each other: they read the same rows)
             const int row0 = q.r0 + tile * a.tile_rows, rows = min(a.tile_rows, q.n - tile * a.tile_rows);
-            scr.found[0] = s0 + tid;
-            scr.found[1] = row0;
-            scr.found[2] = rows;
-            scr.found[3] = q.ctx;
-            scr.found[4] = q.places - q.ctx;
-            scr.found[5] = part;
-            scr.found[6] = parts;
-            scr.found[7] = size;
-            if (hk == 0 && part == 0 && tile_at + tile < a.max_tiles) a.tiles[tile_at + tile] = {row0, rows, parts, at + tile, q.tiles, {}};
+            mine_found[0] = s0 + first, mine_found[1] = row0, mine_found[2] = rows, mine_found[3] = q.ctx, mine_found[4] = q.places - q.ctx, mine_found[5] = part;
+            mine_found[6] = parts, mine_found[7] = size;
+            if (hk == 0 && part == 0 && (!alone || w == 0) && tile_at + tile < a.max_tiles) a.tiles[tile_at + tile] = {row0, rows, parts, at + tile, q.tiles, {}};
         }
-        __syncthreads();
-        if (scr.found[0] >= 0 && item != 0) break;       // (workgroup 0 counts all tiles)
+        const unsigned long long who = __builtin_amdgcn_ballot_w64(here);
+        if (alone) {
+            if (who)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) found[i] = __builtin_amdgcn_readlane(mine_found[i], (int)__builtin_ctzll(who));
+        } else {
+            if (here)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) scr.found[i] = mine_found[i];
+            __syncthreads();
+            if (scr.found[0] >= 0 && item != 0) break;       // (workgroup 0 counts all tiles)
+        }
     }
-    if (item == 0 && hk == 0 && tid == 0) *a.n_tiles = min(begin[CLASSES], a.max_tiles);
-    if (scr.found[0] < 0) return false;
-    it.seq = scr.found[0], it.row0 = scr.found[1], it.rows = scr.found[2], it.ctx = scr.found[3], it.drafts = scr.found[4], it.parts = scr.found[6];
-    const int places = it.ctx + it.drafts;
-    it.lo = (int)min((long long)scr.found[5] * scr.found[7] * UNIT, (long long)places);
-    it.hi = (int)min((long long)it.lo + (long long)scr.found[7] * UNIT, (long long)places);
+    if (item == 0 && hk == 0 && threadIdx.x == 0) *a.n_tiles = min(begin[CLASSES], a.max_tiles);
+    if (!alone) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) found[i] = __builtin_amdgcn_readfirstlane(scr.found[i]);
+    }
+    if (found[0] < 0) return false;
+    it.seq = found[0], it.row0 = found[1], it.rows = found[2], it.ctx = found[3], it.drafts = found[4], it.parts = found[6];
+    const int end = it.ctx + it.drafts;
+    it.lo = (int)min((long long)found[5] * found[7] * UNIT, (long long)end);
+    it.hi = (int)min((long long)it.lo + (long long)found[7] * UNIT, (long long)end);
     it.part_at = item;
     return true;
 }
@@ -279,7 +345,7 @@ static TreePlan plan_tree(const alora_attn_dims *d)
     p.tile_rows = p.columns / G;
     p.places = std::max(1, 512 / d->n_kv_heads);
     p.tiles = d->n_tokens / p.tile_rows + std::min(d->n_seqs, d->n_tokens);      // (a sequence's last tile may not be full)
-    p.items = p.tiles + p.places * 3 / 2 + 1;                                    // sum of ceil(units / per) over tiles, per >= all units / (1.5 places)
+    p.items = p.tiles + 2ll * p.places + 2;                                      // sum of ceil(units / per) over tiles, see find_item
     const auto up = [](size_t n) { return (n + 255) / 256 * 256; };
     p.tiles_at = 256;
     p.ml_at = p.tiles_at + up((size_t)p.tiles * sizeof(TreeTile));
@@ -345,7 +411,7 @@ int alora_tree_attention(const void *q, const void *k_cache, const void *v_cache
     // positions: 64 x 1 rows 376 | | 341, 64 x 8 379 | | 344, 2000 positions: 300 x 4 480 | | 452; 64/8 heads, 64 rows at 64000, four tiles 181 | | 245.
     const long long columns = (long long)dims->n_tokens * (dims->n_q_heads / dims->n_kv_heads);
     const bool whole = columns <= 32ll * dims->n_seqs;
-    const bool once = columns <= 32ll * WAVES * dims->n_seqs && outgrows_cache(dims->n_slots, dims->n_kv_heads, dims->head_dim, true);
+    const bool once = columns <= 64ll * dims->n_seqs && outgrows_cache(dims->n_slots, dims->n_kv_heads, dims->head_dim, true);
     const auto choose = [&](auto head_dim) {
         constexpr int D = decltype(head_dim)::value;
         if (!bf16) go(tree_vector_kernel<D, 8, false>, tree_merge_kernel<D, false>);
