@@ -204,24 +204,28 @@ __device__ __forceinline__ uint32_t block_keys(const SelectArgs &a, int head, u3
 // ---- the list from the keys ----
 // n keys, of which the first n_first and the last n_recent blocks' do not count (those are always chosen); n > budget.  The threshold is found by counting: keys
 // between the smallest and the largest fall into 2048 bins, the bin it lies in is cut again, until a bin is taken whole or holds one value.
+// A thread keeps the keys of PER blocks that follow each other (begin ..), 0 where there is none: ranks are then in the blocks' order.
 constexpr int BINS = 2048;
 struct ListScratch {
-    int bins[BINS], sums[16][2];
+    int bins[2][BINS], sums[16][2];
     uint32_t ends[16][2], bin, left, inside;
 };
-template <int NT, class Key>
-__device__ __forceinline__ void list_of_keys(const SelectArgs &a, int n, Key key, int32_t *out, ListScratch &scr)
+template <int NT, int PER>
+__device__ __forceinline__ void list_of_keys(const SelectArgs &a, int n, const uint32_t (&key)[PER], int begin, int32_t *out, ListScratch &scr)
 {
-    constexpr int NW = NT / 64, PER = BINS / NT;
+    constexpr int NW = NT / 64, BPT = BINS / NT;
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, c0 = a.n_first, c1 = n - a.n_recent;
     int want = a.budget - a.n_first - a.n_recent;
     uint32_t above = 0xffffffffu, equal = 0;        // chosen: keys above `above`, and `want` of those equal to `equal`
+    auto counts = [&](int j) { return begin + j >= c0 && begin + j < c1; };
     if (want > 0) {
         uint32_t low = 0xffffffffu, high = 0;
-        for (int i = c0 + tid; i < c1; i += NT) {
-            const uint32_t k = key(i);
-            low = min(low, k), high = max(high, k);
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            low = min(low, counts(j) ? key[j] : 0xffffffffu);
+            high = max(high, counts(j) ? key[j] : 0u);
         }
+        for (int i = tid; i < BINS; i += NT) scr.bins[0][i] = 0;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) low = min(low, (uint32_t)__shfl_xor((int)low, o)), high = max(high, (uint32_t)__shfl_xor((int)high, o));
         if (lane == 0) scr.ends[w][0] = low, scr.ends[w][1] = high;
@@ -229,27 +233,28 @@ __device__ __forceinline__ void list_of_keys(const SelectArgs &a, int n, Key key
 #pragma unroll
         for (int i = 0; i < NW; ++i) low = min(low, scr.ends[i][0]), high = max(high, scr.ends[i][1]);
         uint32_t span = high - low;                 // keys low .. low + span are looked at
-        for (;;) {
+        for (int turn = 0;; turn ^= 1) {
             const int shift = max(0, 32 - (int)__builtin_clz(span | 1u) - 11);
-            for (int i = tid; i < BINS; i += NT) scr.bins[i] = 0;
-            __syncthreads();
-            for (int i = c0 + tid; i < c1; i += NT) {
-                const uint32_t k = key(i) - low;
-                if (k <= span) atomicAdd(&scr.bins[k >> shift], 1);      // (counts: the same in any order)
-            }
-            __syncthreads();
-            int mine = 0, h[PER];
 #pragma unroll
-            for (int j = 0; j < PER; ++j) h[j] = scr.bins[BINS - 1 - (tid * PER + j)], mine += h[j];      // from the largest down
+            for (int j = 0; j < PER; ++j) {
+                const uint32_t k = key[j] - low;
+                if (counts(j) && k <= span) atomicAdd(&scr.bins[turn][k >> shift], 1);      // (counts: the same in any order)
+            }
+            for (int i = tid; i < BINS; i += NT) scr.bins[turn ^ 1][i] = 0;
+            __syncthreads();
+            int mine = 0, h[BPT];
+#pragma unroll
+            for (int j = 0; j < BPT; ++j) h[j] = scr.bins[turn][BINS - 1 - (tid * BPT + j)], mine += h[j];      // from the largest down
             int upto = sum_upto64(mine);
             if (lane == 63) scr.sums[w][0] = upto;
             __syncthreads();
-            for (int i = 0; i < w; ++i) upto += scr.sums[i][0];
+#pragma unroll
+            for (int i = 0; i < NW; ++i) upto += i < w ? scr.sums[i][0] : 0;
             int before = upto - mine;
             if (before < want && want <= upto) {
 #pragma unroll
-                for (int j = 0; j < PER; ++j) {
-                    if (before < want && want <= before + h[j]) scr.bin = (uint32_t)(BINS - 1 - (tid * PER + j)), scr.left = (uint32_t)(want - before), scr.inside = (uint32_t)h[j];
+                for (int j = 0; j < BPT; ++j) {
+                    if (before < want && want <= before + h[j]) scr.bin = (uint32_t)(BINS - 1 - (tid * BPT + j)), scr.left = (uint32_t)(want - before), scr.inside = (uint32_t)h[j];
                     before += h[j];
                 }
             }
@@ -265,30 +270,95 @@ __device__ __forceinline__ void list_of_keys(const SelectArgs &a, int n, Key key
                 break;
             }
             span = (1u << shift) - 1;
+        }
+    }
+    int more = 0, same = 0;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const bool in = begin + j < n, c = counts(j);
+        more += in && (!c || key[j] > above);
+        same += c && want > 0 && key[j] == equal;
+    }
+    int um = sum_upto64(more), us = sum_upto64(same);
+    if (lane == 63) scr.sums[w][0] = um, scr.sums[w][1] = us;      // (the sums of the bins were read ahead of the last barrier)
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NW; ++i) um += i < w ? scr.sums[i][0] : 0, us += i < w ? scr.sums[i][1] : 0;
+    um -= more, us -= same;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const bool in = begin + j < n, c = counts(j), m = in && (!c || key[j] > above), e = c && want > 0 && key[j] == equal;
+        if (m || (e && us < want)) out[um + min(us, want)] = begin + j;
+        um += m, us += e;
+    }
+}
+
+// The same for more keys than threads keep: they are read again in every step.
+template <int NT>
+__device__ __forceinline__ void list_of_many_keys(const SelectArgs &a, int n, const uint32_t *key, int32_t *out, ListScratch &scr)
+{
+    constexpr int NW = NT / 64, BPT = BINS / NT;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, c0 = a.n_first, c1 = n - a.n_recent;
+    int want = a.budget - a.n_first - a.n_recent;
+    uint32_t above = 0xffffffffu, equal = 0;
+    if (want > 0) {
+        uint32_t low = 0, span = 0xffffffffu;
+        for (;;) {
+            const int shift = max(0, 32 - (int)__builtin_clz(span | 1u) - 11);
+            for (int i = tid; i < BINS; i += NT) scr.bins[0][i] = 0;
+            __syncthreads();
+            for (int i = c0 + tid; i < c1; i += NT) {
+                const uint32_t k = key[i] - low;
+                if (k <= span) atomicAdd(&scr.bins[0][k >> shift], 1);
+            }
+            __syncthreads();
+            int mine = 0, h[BPT];
+#pragma unroll
+            for (int j = 0; j < BPT; ++j) h[j] = scr.bins[0][BINS - 1 - (tid * BPT + j)], mine += h[j];
+            int upto = sum_upto64(mine);
+            if (lane == 63) scr.sums[w][0] = upto;
+            __syncthreads();
+            for (int i = 0; i < w; ++i) upto += scr.sums[i][0];
+            int before = upto - mine;
+            if (before < want && want <= upto) {
+#pragma unroll
+                for (int j = 0; j < BPT; ++j) {
+                    if (before < want && want <= before + h[j]) scr.bin = (uint32_t)(BINS - 1 - (tid * BPT + j)), scr.left = (uint32_t)(want - before), scr.inside = (uint32_t)h[j];
+                    before += h[j];
+                }
+            }
+            __syncthreads();
+            want = (int)scr.left;
+            low += scr.bin << shift;
+            if ((int)scr.inside == want) {
+                above = low - 1, want = 0;
+                break;
+            }
+            if (shift == 0) {
+                above = equal = low;
+                break;
+            }
+            span = (1u << shift) - 1;
             __syncthreads();
         }
     }
-    // a thread looks through blocks that follow each other, so that ranks are in their order (an odd number of them: LDS banks)
-    const int per = ((n + NT - 1) / NT) | 1, begin = min(n, tid * per), end = min(n, begin + per);
-    int more = 0, same = 0;
-    for (int i = begin; i < end; ++i) {
-        const bool always = i < c0 || i >= c1;
-        const uint32_t k = key(i);
-        more += always || k > above;
-        same += !always && want > 0 && k == equal;
-    }
-    int um = sum_upto64(more), us = sum_upto64(same);
-    __syncthreads();
-    if (lane == 63) scr.sums[w][0] = um, scr.sums[w][1] = us;
-    __syncthreads();
-    for (int i = 0; i < w; ++i) um += scr.sums[i][0], us += scr.sums[i][1];
-    um -= more, us -= same;
-    for (int i = begin; i < end; ++i) {
-        const bool always = i < c0 || i >= c1;
-        const uint32_t k = key(i);
-        const bool m = always || k > above, e = !always && want > 0 && k == equal;
+    int chosen = 0, same_before = 0;                // in the chunks before: a chunk is NT blocks that follow each other
+    for (int i0 = 0; i0 < n; i0 += NT) {
+        const int i = i0 + tid;
+        const bool in = i < n, c = i >= c0 && i < c1;
+        const uint32_t k = in ? key[i] : 0u;
+        const bool m = in && (!c || k > above), e = in && c && want > 0 && k == equal;
+        const unsigned long long bm = __builtin_amdgcn_ballot_w64(m), be = __builtin_amdgcn_ballot_w64(e), under = (1ull << lane) - 1;
+        __syncthreads();
+        if (lane == 0) scr.sums[w][0] = (int)__builtin_popcountll(bm), scr.sums[w][1] = (int)__builtin_popcountll(be);
+        __syncthreads();
+        int um = chosen + (int)__builtin_popcountll(bm & under), us = same_before + (int)__builtin_popcountll(be & under);
+#pragma unroll
+        for (int j = 0; j < NW; ++j) {
+            if (j < w) um += scr.sums[j][0], us += scr.sums[j][1];
+            chosen += scr.sums[j][0], same_before += scr.sums[j][1];
+        }
         if (m || (e && us < want)) out[um + min(us, want)] = i;
-        um += m, us += e;
     }
 }
 
@@ -302,7 +372,7 @@ __device__ __forceinline__ bool whole_context(const SelectArgs &a, int n, int32_
 }
 
 // One workgroup per (row, K/V head): block ids to LDS, keys in their place, the list.
-constexpr int MOST_IN_LDS = 8192;
+constexpr int MOST_IN_LDS = 17 * 256;
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void block_select_kernel(SelectArgs a)
 {
@@ -327,7 +397,16 @@ __global__ __launch_bounds__(256) void block_select_kernel(SelectArgs a)
         ids[b0 + lane % LPB] = (int)block_keys<D>(a, hk, mine, block);
     }
     __syncthreads();
-    list_of_keys<256>(a, n, [&](int i) { return (uint32_t)ids[i]; }, out, scr);
+    const auto list = [&](auto per) {
+        constexpr int PER = decltype(per)::value;
+        uint32_t key[PER];
+#pragma unroll
+        for (int j = 0; j < PER; ++j) key[j] = tid * PER + j < n ? (uint32_t)ids[tid * PER + j] : 0u;
+        list_of_keys<256, PER>(a, n, key, tid * PER, out, scr);
+    };
+    if (n <= 3 * 256) list(std::integral_constant<int, 3>{});      // (odd numbers: LDS banks)
+    else if (n <= 7 * 256) list(std::integral_constant<int, 7>{});
+    else list(std::integral_constant<int, 17>{});
 }
 
 // The same in two kernels.  Keys of CHUNK blocks of a row, all heads (whose bounds of a block lie next to each other); then a workgroup per
@@ -360,19 +439,22 @@ __global__ __launch_bounds__(256) void block_keys_kernel(SelectArgs a)
 template <int NT>
 __global__ __launch_bounds__(NT) void block_list_kernel(SelectArgs a)
 {
-    extern __shared__ __attribute__((aligned(16))) int ids[];      // keys, where max_blocks of them have room
     __shared__ ListScratch scr;
-    const int t = (int)blockIdx.x / a.Hkv, n = context_blocks(a.seq[t], a.pos[t], a.n_seqs, a.max_blocks, a.bs);
+    const int tid = threadIdx.x, t = (int)blockIdx.x / a.Hkv, n = context_blocks(a.seq[t], a.pos[t], a.n_seqs, a.max_blocks, a.bs);
     int32_t *out = a.selected + (size_t)blockIdx.x * a.budget;
     if (whole_context<NT>(a, n, out)) return;
     const uint32_t *keys = a.keys + (size_t)blockIdx.x * a.max_blocks;
-    if (a.max_blocks <= MOST_IN_LDS) {
-        for (int i = threadIdx.x; i < n; i += NT) ids[i] = (int)keys[i];
-        __syncthreads();
-        list_of_keys<NT>(a, n, [&](int i) { return (uint32_t)ids[i]; }, out, scr);
-    } else {
-        list_of_keys<NT>(a, n, [&](int i) { return keys[i]; }, out, scr);
-    }
+    const auto list = [&](auto per) {
+        constexpr int PER = decltype(per)::value;
+        uint32_t key[PER];
+#pragma unroll
+        for (int j = 0; j < PER; ++j) key[j] = tid * PER + j < n ? keys[tid * PER + j] : 0u;
+        list_of_keys<NT, PER>(a, n, key, tid * PER, out, scr);
+    };
+    if (n <= 2 * NT) list(std::integral_constant<int, 2>{});
+    else if (n <= 8 * NT) list(std::integral_constant<int, 8>{});
+    else if (n <= 32 * NT) list(std::integral_constant<int, 32>{});
+    else list_of_many_keys<NT>(a, n, keys, out, scr);
 }
 
 // ---- attention over the selected blocks -----------------------------------------------------------
@@ -591,7 +673,7 @@ int alora_block_select(const void *q, const int8_t *bounds, const float *scales,
             part.seq = a.seq + t0, part.pos = a.pos + t0, part.keys = a.keys + (size_t)t0 * a.Hkv * a.max_blocks;
             launch_kernel(block_keys_kernel<D, B>, dim3((unsigned)(a.max_blocks + CHUNK - 1) / CHUNK, (unsigned)part.T, (unsigned)(a.Hkv + HEADS - 1) / HEADS), dim3(256), 0, (hipStream_t)hip_stream, part);
         }
-        launch_kernel(block_list_kernel<1024>, lists, dim3(1024), a.max_blocks <= MOST_IN_LDS ? (unsigned)a.max_blocks * 4 : 0, (hipStream_t)hip_stream, a);
+        launch_kernel(block_list_kernel<1024>, lists, dim3(1024), 0, (hipStream_t)hip_stream, a);
     };
     typedef std::integral_constant<int, 128> D128;
     typedef std::integral_constant<int, 64> D64;
@@ -635,7 +717,7 @@ int alora_selected_attention(const void *q, const void *k_cache, const void *v_c
         a.list.o = (float *)((char *)workspace + selected_ml_bytes(dims, plan));
     }
     const bool bf16 = dims->dtype == ALORA_BF16;
-    const bool once = dims->n_tokens <= dims->n_seqs && outgrows_cache(dims->n_slots, dims->n_kv_heads, dims->head_dim, true);      // (see launch_attention_blocks)
+    const bool once = dims->n_tokens <= dims->n_seqs;      // contexts that are read once: non-temporal copies (200 rows of 1600 places 242 | 221 us, one row the same)
     const dim3 grid((unsigned)plan.whole + (unsigned)rest * (unsigned)plan.parts);
     const auto go = [&](auto kernel) { launch_kernel(kernel, grid, dim3(256), 0, (hipStream_t)hip_stream, a); };
     const auto choose = [&](auto head_dim, auto is_bf16) {

@@ -21,13 +21,13 @@ struct TreeArgs {
     const uint32_t *mask;       // [T][2 * words]
     int words, tile_rows;       // rows of a tile
     int places;                 // workgroups per K/V head that the chip holds at once
+    int least_units;            // of a part
     int max_tiles, max_items;   // the workspace has room for (offsets that do not ascend may give more)
     int *n_tiles;
     TreeTile *tiles;
 };
 
 constexpr int UNIT = 32;        // positions that parts are counted in
-constexpr int LEAST_UNITS = 8;  // of a part
 constexpr int GOOD_UNITS = 12;  // from which two workgroups to a compute unit are worth their parts
 
 struct TreeItem {
@@ -107,14 +107,14 @@ __device__ __forceinline__ bool find_item(const TreeArgs &a, int item, int hk, T
         // 40.4, 37.9, 47.6, 4 x 13 rows at 16000 106, 63.5, 62.5, 53.7, 68.6; 64/8 heads, 64 rows at 64000 387, 212, 209, 181, 204.
         units = over(total, room);
         if (units < (float)GOOD_UNITS) units = over(total, half);
-        units = fmaxf(fminf(ceilf(units), most), (float)LEAST_UNITS);
+        units = fmaxf(fminf(ceilf(units), most), (float)a.least_units);
     } else {
         // Many: the best of whole tiles, an equal share for every place of the chip or two thirds of it, as many parts as fit in one turn or in two.
         float cut[CUTS] = {most, share, share * (2.f / 3), over(total, room), over(total, 2.f * places - tiles)};
         float items_of[CUTS] = {}, parts_at[CUTS] = {}, most_of[CUTS] = {}, one_over[CUTS];
 #pragma unroll
         for (int i = 0; i < CUTS; ++i) {
-            cut[i] = cut[i] > 0.f ? fmaxf(fminf(ceilf(cut[i]), most), (float)LEAST_UNITS) : most;
+            cut[i] = cut[i] > 0.f ? fmaxf(fminf(ceilf(cut[i]), most), (float)a.least_units) : most;
             one_over[i] = __builtin_amdgcn_rcpf(cut[i]);
         }
         for_each(q, [&](const Seq &x) {
@@ -288,22 +288,23 @@ __global__ __launch_bounds__(256) void tree_vector_kernel(TreeArgs a)
         });
 }
 
-// 32 NW columns: 32 NW >> lg_g rows of a sequence.
-template <int D, int NW, bool WHOLE, bool ONCE>
-__global__ __launch_bounds__(64 * NW, 2) void tree_matrix_kernel(TreeArgs a)
+// 32 columns a wavefront: 128 >> lg_g rows of a sequence.
+constexpr int WAVES = 4;
+template <int D, bool ONCE>
+__global__ __launch_bounds__(64 * WAVES, 2) void tree_matrix_kernel(TreeArgs a)
 {
-    __shared__ MatrixTiles<D, NW, 32, 512 / D, 2, 2048> lds;      // 64 KiB of tiles: two workgroups share a CU's LDS
+    __shared__ MatrixTiles<D, WAVES, 32, 512 / D, 2, 2048> lds;      // 64 KiB of tiles: two workgroups share a CU's LDS
     __shared__ TreeScratch find;
     const ListArgs &g = a.list;
     const int hk = (int)blockIdx.x % g.Hkv, item = (int)blockIdx.x / g.Hkv;
-    if (item == (int)(gridDim.x / g.Hkv) - 1) return clear_rows<D, true, NW>(a, hk);
+    if (item == (int)(gridDim.x / g.Hkv) - 1) return clear_rows<D, true, WAVES>(a, hk);
     TreeItem it;
-    if (!find_item<NW>(a, item, hk, find, it)) return;
+    if (!find_item<WAVES>(a, item, hk, find, it)) return;
     const int32_t *bt = g.bt + (size_t)it.seq * g.max_blocks;
     const int col = 32 * ((int)threadIdx.x >> 6) + ((int)threadIdx.x & 31), columns = it.rows << g.lg_g, row = it.row0 + (min(col, columns - 1) >> g.lg_g);
     const uint32_t *bits = a.mask + (size_t)row * 2 * a.words;
     const size_t at = ((size_t)row * g.Hq + ((size_t)hk << g.lg_g) + (col & ((1 << g.lg_g) - 1))) * D;
-    read_list_matrix<WHOLE, ONCE>(
+    read_list_matrix<false, ONCE>(
         g, hk, lds, it.lo, it.hi, it.ctx, columns,
         [&](int v) { return slot_at(g, bt, v / g.bs, v % g.bs); },
         [&](int place) {               // the row's bits of drafts place - ctx .. + 31; what lies in front of them is seen
@@ -311,7 +312,7 @@ __global__ __launch_bounds__(64 * NW, 2) void tree_matrix_kernel(TreeArgs a)
             const uint32_t x = i < 0 ? 0xffffffffu : i < 2 * a.words ? bits[i] : 0u, y = i + 1 < 2 * a.words ? bits[i + 1] : 0u;
             return s ? x >> s | y << (32 - s) : x;
         },
-        at, at, it.parts > 1 ? (long long)it.part_at * g.Hkv + hk : -1ll, 32 * NW);
+        at, at, it.parts > 1 ? (long long)it.part_at * g.Hkv + hk : -1ll, 32 * WAVES);
 }
 
 // One wavefront per column of a tile that has parts.
@@ -329,7 +330,6 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int columns
 
 // ---- host ---------------------------------------------------------------------------------------
 // How a call is cut: columns of a tile, the most tiles and items (tile, part) of a K/V head there can be, and where the workspace's arrays lie.
-constexpr int WAVES = 4;
 struct TreePlan {
     bool matrix;                // instructions; else vector arithmetic
     int columns, tile_rows, places;
@@ -396,7 +396,7 @@ int alora_tree_attention(const void *q, const void *k_cache, const void *v_cache
     a.list.o = (float *)((char *)workspace + p.o_at);
     a.offsets = row_offsets; a.context = context_lens;
     a.mask = (const uint32_t *)tree_mask; a.words = mask_words;
-    a.tile_rows = p.tile_rows; a.places = p.places;
+    a.tile_rows = p.tile_rows; a.places = p.places; a.least_units = p.matrix ? 8 : 4;      // (fp32, 5 trees over up to 700 positions: 2 units 22.2 us, 4 20.7, 8 23.8)
     a.max_tiles = (int)p.tiles; a.max_items = (int)p.items;
     a.n_tiles = (int *)workspace;
     a.tiles = (TreeTile *)((char *)workspace + p.tiles_at);
@@ -406,17 +406,14 @@ int alora_tree_attention(const void *q, const void *k_cache, const void *v_cache
         launch_kernel(kernel, grid, dim3(64 * WAVES), 0, (hipStream_t)hip_stream, a);
         launch_kernel(combine, merge, dim3(256), 0, (hipStream_t)hip_stream, a, p.columns);
     };
-    // Weights whole where a sequence brings one wavefront's columns on average: then the call waits for memory.  Non-temporal copies where it brings one tile, so
-    // that its context is read once, and the memory-side cache would not keep K and V.  us, ordinary | non-temporal | with whole weights, 32/8 heads, 8192
-    // positions: 64 x 1 rows 376 | | 341, 64 x 8 379 | | 344, 2000 positions: 300 x 4 480 | | 452; 64/8 heads, 64 rows at 64000, four tiles 181 | | 245.
-    const long long columns = (long long)dims->n_tokens * (dims->n_q_heads / dims->n_kv_heads);
-    const bool whole = columns <= 32ll * dims->n_seqs;
-    const bool once = columns <= 64ll * dims->n_seqs && outgrows_cache(dims->n_slots, dims->n_kv_heads, dims->head_dim, true);
+    // Non-temporal copies where a sequence brings one tile on average: then its context is read once.  us, ordinary | non-temporal, 32/8 heads: 13 rows at 9000
+    // positions 21.5 | 19.7, at 128000 118 | 102, 64 x 8 rows at 8192 385 | 350, 64 x 24 400 | 385, 64 x 32 430 | 427, 64 x 40 (two tiles) 702 | 739; one context of
+    // 16000 for 12 sequences 101 | 97, of 8000 for 64 222 | 218.
+    const bool once = (long long)dims->n_tokens * (dims->n_q_heads / dims->n_kv_heads) <= 32ll * WAVES * dims->n_seqs;
     const auto choose = [&](auto head_dim) {
         constexpr int D = decltype(head_dim)::value;
         if (!bf16) go(tree_vector_kernel<D, 8, false>, tree_merge_kernel<D, false>);
-        else if (whole) once ? go(tree_matrix_kernel<D, WAVES, true, true>, tree_merge_kernel<D, true>) : go(tree_matrix_kernel<D, WAVES, true, false>, tree_merge_kernel<D, true>);
-        else once ? go(tree_matrix_kernel<D, WAVES, false, true>, tree_merge_kernel<D, true>) : go(tree_matrix_kernel<D, WAVES, false, false>, tree_merge_kernel<D, true>);
+        else once ? go(tree_matrix_kernel<D, true>, tree_merge_kernel<D, true>) : go(tree_matrix_kernel<D, false>, tree_merge_kernel<D, true>);
     };
     if (dims->head_dim == 128) choose(std::integral_constant<int, 128>{});
     else choose(std::integral_constant<int, 64>{});

@@ -451,6 +451,17 @@ def test_long_contexts(dtype):
         t.attend()
 
 
+@pytest.mark.parametrize("coarse", [False, True])
+def test_more_blocks_than_threads_keep(coarse):
+    """Blocks of one position: 40000 of them, and, in one kernel and in two, numbers of blocks around what a thread keeps."""
+    t = Select("bf16", [40000, 200, 33000], 2, 1, 64, 1, seed=5, coarse=coarse)
+    for budget, first, recent in ((300, 1, 2), (1, 0, 1), (33000, 5, 5)):
+        t.select(budget, first, recent)
+    for hkv, ctx in ((1, [1022, 1023, 1024, 1025, 2046, 2047, 2048, 2049, 8191, 8192]), (32, [767, 768, 1791, 1792, 1793, 2000, 4350, 4351])):
+        t = Select("f32", ctx, hkv, hkv, 64, 1, seed=6, coarse=coarse)
+        t.select(64, 1, 1)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_lists_of_any_kind(dtype):
     """Entries twice, out of order, outside the context, with holes, and none at all."""
