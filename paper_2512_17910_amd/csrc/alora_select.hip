@@ -167,9 +167,11 @@ __device__ __forceinline__ void meet(int (&sum)[16], int lane)
     }
 }
 
+// Bound by memory: 223 MB for 200 rows over 94 to 1500 blocks in 60 us, 3.7 TB/s (contexts of one length, one after the other in the pool, 42: what is ragged starts late, and pieces
+// of 2 KiB lie far apart).  Batches of eight blocks, with six workgroups to a compute unit instead of five, 62; keys and lists in two kernels 65.
 // The scores of as many blocks as lanes share one, with one head's query: 2 D / 16 lanes hold a block's bounds, 16 bytes each (`mine`: those of the query), lane i of them gets the key of
 // block i.  All loads are requested before the first is looked at.
-template <int D>
+template <int D, bool ONCE>
 __device__ __forceinline__ uint32_t block_keys(const SelectArgs &a, int head, u32x4 mine, const int (&block)[2 * D / 16])
 {
     constexpr int LPB = 2 * D / 16;
@@ -178,7 +180,10 @@ __device__ __forceinline__ uint32_t block_keys(const SelectArgs &a, int head, u3
 #pragma unroll
     for (int i = 0; i < LPB; ++i) {
         x[i] = (u32x4){0u, 0u, 0u, 0u};
-        if ((unsigned)block[i] < (unsigned)a.n_blocks) x[i] = *(const u32x4 *)(a.bounds + ((size_t)block[i] * a.Hkv + head) * 2 * D + part * 16);
+        if ((unsigned)block[i] < (unsigned)a.n_blocks) {
+            const u32x4 *from = (const u32x4 *)(a.bounds + ((size_t)block[i] * a.Hkv + head) * 2 * D + part * 16);
+            x[i] = ONCE ? __builtin_nontemporal_load(from) : *from;
+        }
     }
     int b = block[0];
 #pragma unroll
@@ -373,7 +378,7 @@ __device__ __forceinline__ bool whole_context(const SelectArgs &a, int n, int32_
 
 // One workgroup per (row, K/V head): block ids to LDS, keys in their place, the list.
 constexpr int MOST_IN_LDS = 17 * 256;
-template <int D, bool BF16>
+template <int D, bool BF16, bool ONCE>
 __global__ __launch_bounds__(256) void block_select_kernel(SelectArgs a)
 {
     constexpr int LPB = 2 * D / 16, UNITS = 64 / LPB;
@@ -394,7 +399,7 @@ __global__ __launch_bounds__(256) void block_select_kernel(SelectArgs a)
         int block[LPB];
 #pragma unroll
         for (int i = 0; i < LPB; ++i) block[i] = ids[b0 + i];
-        ids[b0 + lane % LPB] = (int)block_keys<D>(a, hk, mine, block);
+        ids[b0 + lane % LPB] = (int)block_keys<D, ONCE>(a, hk, mine, block);
     }
     __syncthreads();
     const auto list = [&](auto per) {
@@ -412,7 +417,7 @@ __global__ __launch_bounds__(256) void block_select_kernel(SelectArgs a)
 // The same in two kernels.  Keys of CHUNK blocks of a row, all heads (whose bounds of a block lie next to each other); then a workgroup per
 // (row, head) makes the list.
 constexpr int CHUNK = 64;
-template <int D, bool BF16>
+template <int D, bool BF16, bool ONCE>
 __global__ __launch_bounds__(256) void block_keys_kernel(SelectArgs a)
 {
     constexpr int LPB = 2 * D / 16, HEADS = 64 / LPB;
@@ -431,7 +436,7 @@ __global__ __launch_bounds__(256) void block_keys_kernel(SelectArgs a)
         int block[LPB];
 #pragma unroll
         for (int i = 0; i < LPB; ++i) block[i] = h0 + head < a.Hkv ? ids[g + i] : -1;
-        const uint32_t k = block_keys<D>(a, h0 + head, mine, block);
+        const uint32_t k = block_keys<D, ONCE>(a, h0 + head, mine, block);
         const int b = b0 + g + lane % LPB;
         if (h0 + head < a.Hkv && b < n) a.keys[((size_t)t * a.Hkv + h0 + head) * a.max_blocks + b] = k;
     }
@@ -659,11 +664,12 @@ int alora_block_select(const void *q, const int8_t *bounds, const float *scales,
     a.budget = budget; a.n_first = n_first; a.n_recent = n_recent;
     const bool bf16 = dims->dtype == ALORA_BF16;
     const dim3 lists((unsigned)a.T * (unsigned)a.Hkv);
+    const bool once = dims->n_tokens <= dims->n_seqs;      // bounds that are read once: non-temporal loads (200 rows over 500 blocks 65.7 | 60.0 us, one over 8188 17.3 | 16.4)
     const auto go = [&](auto head_dim, auto is_bf16) {
         constexpr int D = decltype(head_dim)::value, LPB = D / 8, HEADS = 64 / LPB;
         constexpr bool B = decltype(is_bf16)::value;
         if (!two_kernels(dims)) {
-            launch_kernel(block_select_kernel<D, B>, lists, dim3(256), (unsigned)((a.max_blocks + LPB - 1) / LPB * LPB) * 4, (hipStream_t)hip_stream, a);
+            launch_kernel(once ? block_select_kernel<D, B, true> : block_select_kernel<D, B, false>, lists, dim3(256), (unsigned)((a.max_blocks + LPB - 1) / LPB * LPB) * 4, (hipStream_t)hip_stream, a);
             return;
         }
         for (int t0 = 0; t0 < dims->n_tokens; t0 += 65535) {      // (a grid's second dimension)
@@ -671,7 +677,7 @@ int alora_block_select(const void *q, const int8_t *bounds, const float *scales,
             part.T = std::min(65535, dims->n_tokens - t0);
             part.q = (const char *)a.q + (size_t)t0 * dims->n_q_heads * D * (B ? 2 : 4);
             part.seq = a.seq + t0, part.pos = a.pos + t0, part.keys = a.keys + (size_t)t0 * a.Hkv * a.max_blocks;
-            launch_kernel(block_keys_kernel<D, B>, dim3((unsigned)(a.max_blocks + CHUNK - 1) / CHUNK, (unsigned)part.T, (unsigned)(a.Hkv + HEADS - 1) / HEADS), dim3(256), 0, (hipStream_t)hip_stream, part);
+            launch_kernel(once ? block_keys_kernel<D, B, true> : block_keys_kernel<D, B, false>, dim3((unsigned)(a.max_blocks + CHUNK - 1) / CHUNK, (unsigned)part.T, (unsigned)(a.Hkv + HEADS - 1) / HEADS), dim3(256), 0, (hipStream_t)hip_stream, part);
         }
         launch_kernel(block_list_kernel<1024>, lists, dim3(1024), 0, (hipStream_t)hip_stream, a);
     };
