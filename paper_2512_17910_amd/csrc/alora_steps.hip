@@ -157,8 +157,8 @@ __global__ __launch_bounds__(64 * WORDS) void tree_rows_kernel(const int32_t *pa
         }
         return;
     }
-    __shared__ uint64_t bits[N][WORDS];
-    __shared__ int next[N];              // the ancestor to go on from, -1: none; -2: an ancestor is not valid
+    __shared__ uint64_t bits[2][WORDS][N];
+    __shared__ int next[2][N];           // the ancestor to go on from, -1: none; -2: an ancestor is not valid
     const int t0 = min(max(offsets[blockIdx.x], 0), n_tokens), rows = min(max(offsets[blockIdx.x + 1], t0), n_tokens) - t0, ctx = context[blockIdx.x];
     uint64_t m[WORDS];
     int to = -1;
@@ -168,25 +168,17 @@ __global__ __launch_bounds__(64 * WORDS) void tree_rows_kernel(const int32_t *pa
         if (to < -1 || to >= tid) to = -2;
     }
 #pragma unroll
-    for (int i = 0; i < WORDS; ++i) {
-        m[i] = own && tid / 64 == i ? 1ull << (tid & 63) : 0ull;
-        bits[tid][i] = m[i];
-    }
-    next[tid] = to;
-    __syncthreads();
-    while (__syncthreads_or(to >= 0)) {
-        int further = to;
+    for (int i = 0; i < WORDS; ++i) m[i] = own && tid / 64 == i ? 1ull << (tid & 63) : 0ull;
+    for (int round = 0;; round ^= 1) {   // (what a round reads the next but one overwrites: a barrier a round)
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) bits[round][i][tid] = m[i];
+        next[round][tid] = to;
+        if (!__syncthreads_or(to >= 0)) break;
         if (to >= 0) {
-            further = next[to];
 #pragma unroll
-            for (int i = 0; i < WORDS; ++i) m[i] |= bits[to][i];
+            for (int i = 0; i < WORDS; ++i) m[i] |= bits[round][i][to];
+            to = next[round][to];
         }
-        __syncthreads();
-        to = further;
-#pragma unroll
-        for (int i = 0; i < WORDS; ++i) bits[tid][i] = m[i];
-        next[tid] = to;
-        __syncthreads();
     }
     if (own) {
         int depth = -1;

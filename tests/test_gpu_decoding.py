@@ -451,6 +451,19 @@ def test_long_contexts(dtype):
         t.attend()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_of_one_sequence(dtype):
+    """A chunk: 40 rows of two sequences, each with its own choice."""
+    t = Select(dtype, [700, 90], 8, 2, 128, 16, seed=8)
+    rng = np.random.default_rng(9)
+    t.seq, t.pos = np.repeat([0, 1], 20).astype(np.int32), np.concatenate([np.arange(681, 701), np.arange(71, 91)]).astype(np.int32)
+    t.q = values(rng, (40, 8 * 128), t.dt)
+    t.dev, t.dims = [dev(t.seq), dev(t.pos)], ab.make_attn_dims(t.q, t.cache.k, t.bt, 8, 2, 128, 16)
+    for budget in (4, 13):
+        t.select(budget, 1, 2)
+        t.attend()
+
+
 @pytest.mark.parametrize("coarse", [False, True])
 def test_more_blocks_than_threads_keep(coarse):
     """Blocks of one position: 40000 of them, and, in one kernel and in two, numbers of blocks around what a thread keeps."""
