@@ -105,8 +105,8 @@ struct SelectArgs {
     const float *scales;
     const int32_t *bt, *seq, *pos;
     int32_t *selected;
-    uint32_t *keys;                  // [T][Hkv][max_blocks]
-    int T, Hkv, lg_g, n_seqs, max_blocks, bs, n_blocks, budget, n_first, n_recent;
+    uint32_t *keys;                  // [T][Hkv][key_stride]
+    int T, Hkv, lg_g, n_seqs, max_blocks, bs, n_blocks, budget, n_first, n_recent, key_stride;
 };
 
 // Scores as whole numbers of the same order (a zero has no sign); 0 is no score's.
@@ -206,6 +206,17 @@ __device__ __forceinline__ uint32_t block_keys(const SelectArgs &a, int head, u3
     return key_of(in ? score : NEG_INF);
 }
 
+// largest over lanes 0 .. lane
+__device__ __forceinline__ uint32_t largest_upto64(uint32_t x)
+{
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false));
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false));
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false));
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false));
+    x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false));
+    return max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false));
+}
+
 // ---- the list from the keys ----
 // n keys, of which the first n_first and the last n_recent blocks' do not count (those are always chosen); n > budget.  The threshold is found by counting: keys
 // between the smallest and the largest fall into 2048 bins, the bin it lies in is cut again, until a bin is taken whole or holds one value.
@@ -231,10 +242,10 @@ __device__ __forceinline__ void list_of_keys(const SelectArgs &a, int n, const u
             high = max(high, counts(j) ? key[j] : 0u);
         }
         for (int i = tid; i < BINS; i += NT) scr.bins[0][i] = 0;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) low = min(low, (uint32_t)__shfl_xor((int)low, o)), high = max(high, (uint32_t)__shfl_xor((int)high, o));
-        if (lane == 0) scr.ends[w][0] = low, scr.ends[w][1] = high;
+        low = ~largest_upto64(~low), high = largest_upto64(high);
+        if (lane == 63) scr.ends[w][0] = low, scr.ends[w][1] = high;
         __syncthreads();
+        low = 0xffffffffu, high = 0;
 #pragma unroll
         for (int i = 0; i < NW; ++i) low = min(low, scr.ends[i][0]), high = max(high, scr.ends[i][1]);
         uint32_t span = high - low;                 // keys low .. low + span are looked at
@@ -438,7 +449,7 @@ __global__ __launch_bounds__(256) void block_keys_kernel(SelectArgs a)
         for (int i = 0; i < LPB; ++i) block[i] = h0 + head < a.Hkv ? ids[g + i] : -1;
         const uint32_t k = block_keys<D, ONCE>(a, h0 + head, mine, block);
         const int b = b0 + g + lane % LPB;
-        if (h0 + head < a.Hkv && b < n) a.keys[((size_t)t * a.Hkv + h0 + head) * a.max_blocks + b] = k;
+        if (h0 + head < a.Hkv && b < n) a.keys[((size_t)t * a.Hkv + h0 + head) * a.key_stride + b] = k;
     }
 }
 template <int NT>
@@ -448,15 +459,20 @@ __global__ __launch_bounds__(NT) void block_list_kernel(SelectArgs a)
     const int tid = threadIdx.x, t = (int)blockIdx.x / a.Hkv, n = context_blocks(a.seq[t], a.pos[t], a.n_seqs, a.max_blocks, a.bs);
     int32_t *out = a.selected + (size_t)blockIdx.x * a.budget;
     if (whole_context<NT>(a, n, out)) return;
-    const uint32_t *keys = a.keys + (size_t)blockIdx.x * a.max_blocks;
+    const uint32_t *keys = a.keys + (size_t)blockIdx.x * a.key_stride;
     const auto list = [&](auto per) {
         constexpr int PER = decltype(per)::value;
         uint32_t key[PER];
 #pragma unroll
-        for (int j = 0; j < PER; ++j) key[j] = tid * PER + j < n ? keys[tid * PER + j] : 0u;
+        for (int j = 0; j < PER; j += 4) {      // (four at once: single loads of neighbours that lie in different lanes took 2 of 10 us; the last ones read past n, not past the stride)
+            u32x4 x = {0u, 0u, 0u, 0u};
+            if (tid * PER + j < n) x = *(const u32x4 *)(keys + tid * PER + j);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) key[j + i] = tid * PER + j + i < n ? x[i] : 0u;
+        }
         list_of_keys<NT, PER>(a, n, key, tid * PER, out, scr);
     };
-    if (n <= 2 * NT) list(std::integral_constant<int, 2>{});
+    if (n <= 4 * NT) list(std::integral_constant<int, 4>{});
     else if (n <= 8 * NT) list(std::integral_constant<int, 8>{});
     else if (n <= 32 * NT) list(std::integral_constant<int, 32>{});
     else list_of_many_keys<NT>(a, n, keys, out, scr);
@@ -572,7 +588,8 @@ static int check_select(const alora_attn_dims *d)
 }
 // Whether keys and lists are made by kernels of their own.
 static bool two_kernels(const alora_attn_dims *d) { return d->max_blocks > MOST_IN_LDS || ((long long)d->n_tokens * d->n_kv_heads < 256 && d->max_blocks > 512); }
-static size_t select_bytes(const alora_attn_dims *d) { return two_kernels(d) ? (size_t)d->n_tokens * d->n_kv_heads * d->max_blocks * sizeof(uint32_t) : 0; }
+static size_t key_stride(const alora_attn_dims *d) { return ((size_t)d->max_blocks + 3) / 4 * 4; }
+static size_t select_bytes(const alora_attn_dims *d) { return two_kernels(d) ? (size_t)d->n_tokens * d->n_kv_heads * key_stride(d) * sizeof(uint32_t) : 0; }
 
 constexpr int MOST_BUDGET = 1 << 20;
 
@@ -661,7 +678,7 @@ int alora_block_select(const void *q, const int8_t *bounds, const float *scales,
     a.keys = (uint32_t *)workspace;
     const ListArgs g = list_args(dims, q, nullptr, nullptr, block_tables, nullptr);
     a.T = g.T; a.Hkv = g.Hkv; a.lg_g = g.lg_g; a.n_seqs = g.n_seqs; a.max_blocks = g.max_blocks; a.bs = g.bs; a.n_blocks = g.n_blocks;
-    a.budget = budget; a.n_first = n_first; a.n_recent = n_recent;
+    a.budget = budget; a.n_first = n_first; a.n_recent = n_recent; a.key_stride = (int)key_stride(dims);
     const bool bf16 = dims->dtype == ALORA_BF16;
     const dim3 lists((unsigned)a.T * (unsigned)a.Hkv);
     const bool once = dims->n_tokens <= dims->n_seqs;      // bounds that are read once: non-temporal loads (200 rows over 500 blocks 65.7 | 60.0 us, one over 8188 17.3 | 16.4)
@@ -676,7 +693,7 @@ int alora_block_select(const void *q, const int8_t *bounds, const float *scales,
             SelectArgs part = a;
             part.T = std::min(65535, dims->n_tokens - t0);
             part.q = (const char *)a.q + (size_t)t0 * dims->n_q_heads * D * (B ? 2 : 4);
-            part.seq = a.seq + t0, part.pos = a.pos + t0, part.keys = a.keys + (size_t)t0 * a.Hkv * a.max_blocks;
+            part.seq = a.seq + t0, part.pos = a.pos + t0, part.keys = a.keys + (size_t)t0 * a.Hkv * a.key_stride;
             launch_kernel(once ? block_keys_kernel<D, B, true> : block_keys_kernel<D, B, false>, dim3((unsigned)(a.max_blocks + CHUNK - 1) / CHUNK, (unsigned)part.T, (unsigned)(a.Hkv + HEADS - 1) / HEADS), dim3(256), 0, (hipStream_t)hip_stream, part);
         }
         launch_kernel(block_list_kernel<1024>, lists, dim3(1024), 0, (hipStream_t)hip_stream, a);
