@@ -30,94 +30,6 @@ namespace alora {
 // of workgroups of them besides, which take the longest first: whole contexts (in runs of `sorted` batch rows), or some in more parts than others.
 enum Contexts { ANY, READ_ONCE, LONGEST_FIRST, IN_PARTS };
 
-// Which row, K/V head and part of the context workgroup b is for when the longest contexts go first; of 256 threads.  Lengths count in
-// steps of an eighth (128 of them from 16 positions to a million), rows of one step in batch order: every workgroup finds the same
-// order, and each row once.  Where no context is longer than SHORT_CONTEXT, or rows read together (see there), it is the batch's order.  Without parts the order is that
-// of every `sorted` rows (at most 256).  In parts there are no more rows than that; those of a.splits parts (see parts_of) come first, where there are
-// none the batch's order stays, and the last workgroups find nothing to do (t = -1).  scr: ORDER_SCRATCH ints of LDS.  near: this thread's row.
-// GROUPS: look for rows that read together.
-struct Turn { int t, seq, pos, hk, part; };
-struct Near { int t, seq, n_ctx; };   // a row, its sequence and context (0: none)
-constexpr int ORDER_SCRATCH = 128 + 8 + 2;
-constexpr int SHORT_CONTEXT = 512;
-constexpr int LONG_PART = 512;      // positions per part from which a context is cut into the larger number of parts
-__device__ __forceinline__ int parts_of(const AttnArgs &a, int n_ctx) { return n_ctx < a.splits * LONG_PART ? a.short_splits : a.splits; }
-template <bool PARTS, bool GROUPS>
-__device__ __forceinline__ Turn longest_first(const AttnArgs &a, int sorted, int b, int *scr, Near &near, bool &together)
-{
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    unsigned long long *const masks = (unsigned long long *)(scr + 128);
-    const int first = PARTS ? 0 : b / a.Hkv / sorted * sorted, rows = min(sorted, a.T - first);
-    int key = -1, n_ctx = 0, sq = -1, p = -1;
-    bool more = false;
-    if (tid < rows) {
-        sq = a.seq[first + tid], p = a.pos[first + tid];
-        if (sq >= 0 && sq < a.n_seqs && p >= 0) n_ctx = (int)min(p + 1ll, (long long)a.max_blocks * a.bs);
-        key = 127 - min(max((int)(__float_as_uint((float)n_ctx) >> 20) - ((127 + 4) << 3), 0), 127);
-        more = PARTS && parts_of(a, n_ctx) > a.short_splits;
-        if (PARTS) key = (more ? 0 : 64) + (key >> 1);   // (steps of a quarter)
-    }
-    near = {first + tid, sq, n_ctx};
-    if (tid < 128) scr[tid] = 0;
-    b -= first * a.Hkv;
-    int rank, unit, parts = PARTS ? a.short_splits : 1;
-    bool ordered = n_ctx > SHORT_CONTEXT;
-    if (PARTS) {
-        const int n_more = __syncthreads_count(more), in_more = n_more * a.splits * a.Hkv;
-        ordered = n_more > 0;
-        if (b < in_more) parts = a.splits;
-        else b -= in_more;
-        unit = parts * a.Hkv;
-        rank = b / unit;
-        b -= rank * unit;
-        if (parts == a.short_splits) rank += n_more;
-        if (rank >= rows) return {-1, -1, -1, 0, 0};
-    } else {
-        unit = a.Hkv;
-        rank = b / unit;
-        b -= rank * unit;
-    }
-    const int hk = b / parts, part = b - hk * parts;
-    if (tid == rank) scr[136] = sq, scr[137] = p;
-    // Groups of rows that read one context: a row goes with the one before it in the batch if both read the same cache block half way through
-    // the shorter of the two.  Where three quarters of the rows are in groups, of eight on average or fewer, the batch's order stays, in which a group
-    // reads its context together, with ordinary loads.  us, longest first | batch order: 200 rows that share 1024 of 1075 to 1625 positions in pairs, 8/8
-    // heads 184 | 152, 16/8 185 | 155, 32/8 195 | 170 (64/8 265 | 272: not looked for), in fours 8/8 175 | 127, 32/8 186 | 160, in eights 158 | 114 and 171 | 157;
-    // half of the rows in pairs 243 | 257 and 260 | 279; a chunk of 144 rows beside 56 others 308 | 333; one prefix for all 196 | 207.
-    bool same = false;
-    if (GROUPS && tid > 0 && tid < rows) {
-        const int sq1 = a.seq[first + tid - 1], half = min(n_ctx, a.pos[first + tid - 1] + 1) >> 1;
-        if (half > SHORT_CONTEXT / 2 && sq1 >= 0 && sq1 < a.n_seqs) {
-            const int at = a.bs_shift >= 0 ? half >> a.bs_shift : half / a.bs;
-            same = a.bt[(size_t)sq * a.max_blocks + at] == a.bt[(size_t)sq1 * a.max_blocks + at];
-        }
-    }
-    const unsigned long long with_last = __builtin_amdgcn_ballot_w64(same);
-    const int begin = (int)__builtin_popcountll(with_last & ~(with_last << 1)), in_groups = begin + (int)__builtin_popcountll(with_last);
-    if (lane == 0) scr[128 + w] = (__builtin_amdgcn_ballot_w64(ordered) ? 1 << 24 : 0) + (begin << 12) + in_groups;   // (64 and 128 at most)
-    __syncthreads();
-    const int all = scr[128] + scr[129] + scr[130] + scr[131];
-    together = GROUPS && 8 * ((all >> 12) & 0xfff) >= rows && 4 * (all & 0xfff) >= 3 * rows;
-    if (all < 1 << 24 || together) return {first + rank, scr[136], scr[137], hk, part};
-    if (key >= 0) atomicAdd(&scr[key], 1);   // counts only: their values do not depend on the order
-    __syncthreads();
-    const int h0 = scr[2 * lane], h1 = scr[2 * lane + 1], upto = sum_upto64(h0 + h1);
-    const int at = (int)__builtin_ctzll(__builtin_amdgcn_ballot_w64(rank < upto));   // (rank < rows, the last lane's)
-    int n = rank - __builtin_amdgcn_readlane(upto - h0 - h1, at);
-    const int even = __builtin_amdgcn_readlane(h0, at), step = 2 * at + (n >= even ? 1 : 0);
-    if (n >= even) n -= even;
-    const unsigned long long mine = __builtin_amdgcn_ballot_w64(key == step);
-    if (lane == 0) masks[w] = mine;
-    __syncthreads();
-    // the n-th of the step's rows: its thread says which it is
-    int before = 0;
-    for (int i = 0; i < w; ++i) before += (int)__builtin_popcountll(masks[i]);
-    before += __builtin_amdgcn_mbcnt_hi((unsigned)(mine >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mine, 0u));
-    if (key == step && before == n) scr[0] = first + tid, scr[136] = sq, scr[137] = p;
-    __syncthreads();
-    return {scr[0], scr[136], scr[137], hk, part};
-}
-
 template <int D, int G, bool BF16, bool POW2, Contexts CONTEXTS>
 __global__ __launch_bounds__(256, G == 4 ? 3 : 1) void paged_attention_kernel(AttnArgs a, int sorted)
 {

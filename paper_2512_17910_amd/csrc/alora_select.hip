@@ -222,7 +222,7 @@ __device__ __forceinline__ uint32_t largest_upto64(uint32_t x)
 // between the smallest and the largest fall into 2048 bins, the bin it lies in is cut again, until a bin is taken whole or holds one value.
 // A thread keeps the keys of PER blocks that follow each other (begin ..), 0 where there is none: ranks are then in the blocks' order.
 constexpr int BINS = 2048;
-struct ListScratch {
+struct __attribute__((aligned(16))) ListScratch {
     int bins[2][BINS], sums[16][2];
     uint32_t ends[16][2], bin, left, inside;
 };
@@ -390,15 +390,25 @@ __device__ __forceinline__ bool whole_context(const SelectArgs &a, int n, int32_
 // One workgroup per (row, K/V head): block ids to LDS, keys in their place, the list.
 constexpr int MOST_IN_LDS = 17 * 256;
 template <int D, bool BF16, bool ONCE>
-__global__ __launch_bounds__(256) void block_select_kernel(SelectArgs a)
+__global__ __launch_bounds__(256) void block_select_kernel(SelectArgs a, AttnArgs rows, int sorted)
 {
     constexpr int LPB = 2 * D / 16, UNITS = 64 / LPB;
     extern __shared__ __attribute__((aligned(16))) int ids[];      // max_blocks, rounded up to LPB
     __shared__ __attribute__((aligned(16))) int8_t query[2 * D];
     __shared__ ListScratch scr;
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, t = (int)blockIdx.x / a.Hkv, hk = (int)blockIdx.x % a.Hkv;
-    const int seq = a.seq[t], n = context_blocks(seq, a.pos[t], a.n_seqs, a.max_blocks, a.bs);
-    int32_t *out = a.selected + (size_t)blockIdx.x * a.budget;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    int t = (int)blockIdx.x / a.Hkv, hk = (int)blockIdx.x % a.Hkv, seq, pos;
+    if (sorted) {
+        Near near;
+        bool together;
+        const Turn turn = longest_first<false, false>(rows, sorted, (int)blockIdx.x, scr.bins[0], near, together);
+        t = __builtin_amdgcn_readfirstlane(turn.t), hk = turn.hk, seq = __builtin_amdgcn_readfirstlane(turn.seq), pos = __builtin_amdgcn_readfirstlane(turn.pos);
+        __syncthreads();
+    } else {
+        seq = a.seq[t], pos = a.pos[t];
+    }
+    const int n = context_blocks(seq, pos, a.n_seqs, a.max_blocks, a.bs);
+    int32_t *out = a.selected + ((size_t)t * a.Hkv + hk) * a.budget;
     if (whole_context<256>(a, n, out)) return;
     const int32_t *bt = a.bt + (size_t)seq * a.max_blocks;
     const int padded = (n + LPB - 1) / LPB * LPB;
@@ -686,7 +696,11 @@ int alora_block_select(const void *q, const int8_t *bounds, const float *scales,
         constexpr int D = decltype(head_dim)::value, LPB = D / 8, HEADS = 64 / LPB;
         constexpr bool B = decltype(is_bf16)::value;
         if (!two_kernels(dims)) {
-            launch_kernel(once ? block_select_kernel<D, B, true> : block_select_kernel<D, B, false>, lists, dim3(256), (unsigned)((a.max_blocks + LPB - 1) / LPB * LPB) * 4, (hipStream_t)hip_stream, a);
+            AttnArgs rows = {};
+            rows.bt = a.bt; rows.seq = a.seq; rows.pos = a.pos;
+            rows.T = a.T; rows.Hkv = a.Hkv; rows.n_seqs = a.n_seqs; rows.max_blocks = a.max_blocks; rows.bs = a.bs; rows.splits = 1;
+            const int runs = (a.T + 255) / 256, sorted = lists.x > 1280 ? (a.T + runs - 1) / runs : 0;
+            launch_kernel(once ? block_select_kernel<D, B, true> : block_select_kernel<D, B, false>, lists, dim3(256), (unsigned)((a.max_blocks + LPB - 1) / LPB * LPB) * 4, (hipStream_t)hip_stream, a, rows, sorted);
             return;
         }
         for (int t0 = 0; t0 < dims->n_tokens; t0 += 65535) {      // (a grid's second dimension)

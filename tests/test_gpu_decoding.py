@@ -464,6 +464,16 @@ def test_rows_of_one_sequence(dtype):
         t.attend()
 
 
+@pytest.mark.parametrize("rows", [170, 300])
+def test_more_lists_than_the_chip_holds(rows):
+    """The longest contexts are looked through first; some rows are out of range."""
+    rng = np.random.default_rng(rows)
+    t = Select("bf16", rng.integers(0, 1500, rows), 8, 8, 64, 16, seed=10, spoiled=True)
+    t.select(17, 1, 2)
+    out = t.attend()
+    assert not out[1:4].any()
+
+
 @pytest.mark.parametrize("coarse", [False, True])
 def test_more_blocks_than_threads_keep(coarse):
     """Blocks of one position: 40000 of them, and, in one kernel and in two, numbers of blocks around what a thread keeps."""
