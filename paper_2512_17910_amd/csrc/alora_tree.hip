@@ -341,7 +341,7 @@ static TreePlan plan_tree(const alora_attn_dims *d)
     TreePlan p;
     const int G = d->n_q_heads / d->n_kv_heads;
     p.matrix = d->dtype == ALORA_BF16;
-    p.columns = p.matrix ? 32 * WAVES : 8;
+    p.columns = p.matrix ? 32 * WAVES : std::max(4, G);      // (fp32, 2, 4, 8 columns, us: 30 rows at 4000 positions, 4 sequences, 72, 61, 109, 16 at 8000, 8 sequences 258, 204, 425)
     p.tile_rows = p.columns / G;
     p.places = std::max(1, 512 / d->n_kv_heads);
     p.tiles = d->n_tokens / p.tile_rows + std::min(d->n_seqs, d->n_tokens);      // (a sequence's last tile may not be full)
@@ -396,7 +396,7 @@ int alora_tree_attention(const void *q, const void *k_cache, const void *v_cache
     a.list.o = (float *)((char *)workspace + p.o_at);
     a.offsets = row_offsets; a.context = context_lens;
     a.mask = (const uint32_t *)tree_mask; a.words = mask_words;
-    a.tile_rows = p.tile_rows; a.places = p.places; a.least_units = p.matrix ? 8 : 4;      // (fp32, 5 trees over up to 700 positions: 2 units 22.2 us, 4 20.7, 8 23.8)
+    a.tile_rows = p.tile_rows; a.places = p.places; a.least_units = p.matrix ? 8 : 4;      // (fp32, 5 trees over up to 700 positions, eight columns: 2 units 22.2 us, 4 20.7, 8 23.8)
     a.max_tiles = (int)p.tiles; a.max_items = (int)p.items;
     a.n_tiles = (int *)workspace;
     a.tiles = (TreeTile *)((char *)workspace + p.tiles_at);
@@ -412,7 +412,7 @@ int alora_tree_attention(const void *q, const void *k_cache, const void *v_cache
     const bool once = (long long)dims->n_tokens * (dims->n_q_heads / dims->n_kv_heads) <= 32ll * WAVES * dims->n_seqs;
     const auto choose = [&](auto head_dim) {
         constexpr int D = decltype(head_dim)::value;
-        if (!bf16) go(tree_vector_kernel<D, 8, false>, tree_merge_kernel<D, false>);
+        if (!bf16) p.columns == 4 ? go(tree_vector_kernel<D, 4, false>, tree_merge_kernel<D, false>) : go(tree_vector_kernel<D, 8, false>, tree_merge_kernel<D, false>);
         else once ? go(tree_matrix_kernel<D, true>, tree_merge_kernel<D, true>) : go(tree_matrix_kernel<D, false>, tree_merge_kernel<D, true>);
     };
     if (dims->head_dim == 128) choose(std::integral_constant<int, 128>{});
