@@ -34,14 +34,19 @@ __global__ __launch_bounds__(256) void block_bounds_kernel(BoundsArgs a)
     int next = __shfl(block, later ? lane + 1 + (int)__builtin_ctzll(later) : 63);
     if (!later) next = -1;
     if (have && (int)(63 - __builtin_clzll(have)) < ROWS) {      // (the last of these may be followed from further on)
-        for (long long j = row0 + 64ll; j < a.n_rows; j += 64) {
-            const int far = block_of(j + lane < a.n_rows ? a.slot[j + lane] : -1);
-            const unsigned long long any = __builtin_amdgcn_ballot_w64(far >= 0);
-            if (!any) continue;
-            const int found = __builtin_amdgcn_readlane(far, (int)__builtin_ctzll(any));
-            if (!later) next = found;
-            break;
+        // (512 rows at a time: behind the last row of a batch padded to a fixed size there is none up to its end)
+        int found = -1;
+        for (long long j = row0 + 64ll; j < a.n_rows && found < 0; j += 512) {
+            int far[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) far[i] = block_of(j + 64 * i + lane < a.n_rows ? a.slot[j + 64 * i + lane] : -1);
+#pragma unroll
+            for (int i = 7; i >= 0; --i) {
+                const unsigned long long any = __builtin_amdgcn_ballot_w64(far[i] >= 0);
+                if (any) found = __builtin_amdgcn_readlane(far[i], (int)__builtin_ctzll(any));
+            }
         }
+        if (!later) next = found;
     }
     const bool last = lane < ROWS && block >= 0 && next != block;
     unsigned long long todo = __builtin_amdgcn_ballot_w64(last);
@@ -594,7 +599,8 @@ static int check_select(const alora_attn_dims *d)
 {
     const int st = check_attention(d);
     if (st) return st;
-    return (long long)d->n_tokens * d->n_q_heads > 0x3fffffffll ? ALORA_ESHAPE : ALORA_OK;
+    // (a grid holds fewer than 2^32 threads in a dimension, and 65535 workgroups in the third)
+    return (long long)d->n_tokens * d->n_kv_heads >= 1 << 22 || d->max_blocks > 1 << 28 || d->n_kv_heads > 1 << 16 ? ALORA_ESHAPE : ALORA_OK;
 }
 // Whether keys and lists are made by kernels of their own.
 static bool two_kernels(const alora_attn_dims *d) { return d->max_blocks > MOST_IN_LDS || ((long long)d->n_tokens * d->n_kv_heads < 256 && d->max_blocks > 512); }
@@ -637,7 +643,7 @@ int alora_block_bounds(const void *k_cache, const int64_t *slot_mapping, int8_t 
     if (!d) return ALORA_EINVAL;
     if (d->dtype != ALORA_F32 && d->dtype != ALORA_BF16) return ALORA_EINVAL;
     if (d->n_rows < 0 || d->n_kv_heads < 1 || d->block_size < 1 || d->n_slots < 0) return ALORA_EINVAL;
-    if ((d->head_dim != 64 && d->head_dim != 128) || d->n_slots > 0x7fffffffll || d->n_kv_heads > 1 << 16) return ALORA_ESHAPE;
+    if ((d->head_dim != 64 && d->head_dim != 128) || d->n_slots > 0x7fffffffll || d->n_kv_heads > 1 << 16 || d->n_rows > 1 << 27) return ALORA_ESHAPE;
     if (d->n_rows == 0) return ALORA_OK;
     if (!k_cache || !slot_mapping || !bounds || !scales) return ALORA_EINVAL;
     if (((uintptr_t)k_cache | (uintptr_t)bounds) & 15 || (uintptr_t)slot_mapping & 7 || (uintptr_t)scales & 3) return ALORA_EINVAL;

@@ -30,6 +30,9 @@ __device__ __forceinline__ unsigned sum_upto64_capped(unsigned x)
     return x;
 }
 
+// of the lanes before, from sums over lanes 0 .. lane
+__device__ __forceinline__ unsigned sum_before64(unsigned x) { return (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x138, 0xf, 0xf, false); }      // wave_shr:1
+
 constexpr int STEP_SEQS = 256;      // requests looked at together: one a thread
 
 // Largest i with at[i] <= x, of STEP_SEQS ascending entries of which the first is <= x.
@@ -54,6 +57,7 @@ __global__ __launch_bounds__(STEP_SEQS) void step_rows_kernel(StepArgs a)
     const unsigned first_item = blockIdx.x * STEP_SEQS + tid, stride = gridDim.x * STEP_SEQS;
     int first = a.state[0], count = a.state[1];
     if (first < 0 || first >= a.pool_cap || count < 0 || count > a.pool_cap) first = count = 0;
+    auto blocks_of = [&](int n) { return (int)(((unsigned)n + (unsigned)a.bs - 1u) / (unsigned)a.bs); };      // (n + block_size - 1 may pass 31 bits)
     auto ring = [&](unsigned i) {       // (first + i with i < pool_cap)
         const unsigned x = (unsigned)first + i;
         return x < (unsigned)a.pool_cap ? x : x - (unsigned)a.pool_cap;
@@ -70,7 +74,7 @@ __global__ __launch_bounds__(STEP_SEQS) void step_rows_kernel(StepArgs a)
             if (a.adapters) adapter = a.adapters[s];
         }
         const bool valid = n >= 0 && n <= cap && n + c >= 0 && n + c <= cap;
-        const int have = valid ? ((int)n + a.bs - 1) / a.bs : 0, want = valid ? (int)((n + c + a.bs - 1) / a.bs) : 0;
+        const int have = valid ? blocks_of((int)n) : 0, want = valid ? (int)((n + c + a.bs - 1) / a.bs) : 0;
         unsigned take = (unsigned)min(max(want - have, 0), (int)LIMIT), fresh = valid ? (unsigned)min(max(c, 0ll), (long long)LIMIT) : 0u;
         // what is asked for decides who is served
         unsigned u = sum_upto64_capped(take), v = sum_upto64_capped(fresh);
@@ -86,16 +90,17 @@ __global__ __launch_bounds__(STEP_SEQS) void step_rows_kernel(StepArgs a)
         asked_blocks = bu, asked_rows = bv;
         const bool ok = valid && (c <= 0 || (u <= (unsigned)count && v <= (unsigned)a.row_cap));
         if (!ok) take = fresh = 0;
-        const unsigned given = ok ? (unsigned)max(have - max(want, kept), 0) : 0u;
+        const unsigned given = ok ? min((unsigned)max(have - max(want, kept), 0), LIMIT) : 0u;
         // what they get
         const unsigned t1 = sum_upto64_capped(take), f1 = sum_upto64_capped(fresh), g1 = sum_upto64_capped(given);
+        const unsigned g0 = sum_before64(g1);      // (a difference would be wrong once the sums stop)
         const unsigned no = (unsigned)__builtin_popcountll(__builtin_amdgcn_ballot_w64(!ok && s < a.n_seqs));
         if (lane == 63) wave_sums[1][w][0] = t1, wave_sums[1][w][1] = f1, wave_sums[1][w][2] = g1, wave_sums[1][w][3] = no;
         __syncthreads();
         unsigned before[4] = {blocks, rows, back, refused}, mine[3] = {};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            if (i == w) mine[0] = before[0] + t1 - take, mine[1] = before[1] + f1 - fresh, mine[2] = min(before[2] + g1, LIMIT) - given;
+            if (i == w) mine[0] = before[0] + t1 - take, mine[1] = before[1] + f1 - fresh, mine[2] = min(before[2] + g0, LIMIT);
 #pragma unroll
             for (int j = 0; j < 4; ++j) before[j] = min(before[j] + wave_sums[1][i][j], LIMIT);
         }
@@ -107,7 +112,7 @@ __global__ __launch_bounds__(STEP_SEQS) void step_rows_kernel(StepArgs a)
         __syncthreads();
         // rows
         for (unsigned r = rows + first_item; r < before[1]; r += stride) {
-            const int i = find_upto(new_at, r), p = len[i] + (int)(r - new_at[i]), at = p / a.bs, was = (len[i] + a.bs - 1) / a.bs;
+            const int i = find_upto(new_at, r), p = len[i] + (int)(r - new_at[i]), at = p / a.bs, was = blocks_of(len[i]);
             const int block = at < was ? a.tables[(size_t)(s0 + i) * a.max_blocks + at] : a.pool[ring(take_at[i] + (unsigned)(at - was))];
             a.seq[r] = s0 + i;
             a.pos[r] = p;
@@ -116,13 +121,13 @@ __global__ __launch_bounds__(STEP_SEQS) void step_rows_kernel(StepArgs a)
         }
         // blocks taken
         for (unsigned k = blocks + first_item; k < before[0]; k += stride) {
-            const int i = find_upto(take_at, k), was = (len[i] + a.bs - 1) / a.bs;
+            const int i = find_upto(take_at, k), was = blocks_of(len[i]);
             a.tables[(size_t)(s0 + i) * a.max_blocks + was + (k - take_at[i])] = a.pool[ring(k)];
         }
-        // blocks returned, behind those the ring holds
-        for (unsigned k = back + first_item; k < before[2]; k += stride) {
-            const int i = find_upto(back_at, k), was = (len[i] + a.bs - 1) / a.bs;
-            if ((unsigned)count + k < (unsigned)a.pool_cap) a.pool[ring((unsigned)count + k)] = a.tables[(size_t)(s0 + i) * a.max_blocks + was - 1 - (int)(k - back_at[i])];
+        // blocks returned, behind those the ring holds, while it has room
+        for (unsigned k = back + first_item; k < min(before[2], (unsigned)a.pool_cap - (unsigned)count); k += stride) {
+            const int i = find_upto(back_at, k), was = blocks_of(len[i]);
+            a.pool[ring((unsigned)count + k)] = a.tables[(size_t)(s0 + i) * a.max_blocks + was - 1 - (int)(k - back_at[i])];
         }
         blocks = before[0], rows = before[1], back = before[2], refused = before[3];
     }
@@ -140,7 +145,7 @@ __global__ __launch_bounds__(STEP_SEQS) void step_rows_kernel(StepArgs a)
 }
 
 // ---- trees --------------------------------------------------------------------------------------
-// One workgroup per sequence, one draft a thread; the last workgroup clears the rows of no sequence.  Steps to the parent are doubled: after round r a
+// One workgroup per sequence, one draft a thread; those behind them clear the rows of no sequence.  Steps to the parent are doubled: after round r a
 // draft holds the bits of 2^r ancestors and the place of the next one, so a chain of 255 takes eight rounds, an ordinary tree three.
 template <int WORDS>
 __global__ __launch_bounds__(64 * WORDS) void tree_rows_kernel(const int32_t *parents, const int32_t *offsets, const int32_t *context, uint64_t *mask,
@@ -148,9 +153,9 @@ __global__ __launch_bounds__(64 * WORDS) void tree_rows_kernel(const int32_t *pa
 {
     constexpr int N = 64 * WORDS;
     const int tid = threadIdx.x;
-    if ((int)blockIdx.x == n_seqs) {
+    if ((int)blockIdx.x >= n_seqs) {
         const int begin = n_seqs ? min(max(offsets[0], 0), n_tokens) : 0, end = n_seqs ? min(max(offsets[n_seqs], begin), n_tokens) : 0;
-        for (int t = tid; t < n_tokens; t += N) {
+        for (long long t = (long long)((int)blockIdx.x - n_seqs) * N + tid; t < n_tokens; t += (long long)((int)gridDim.x - n_seqs) * N) {
             if (t >= begin && t < end) continue;
             for (int i = 0; i < WORDS; ++i) mask[(size_t)t * WORDS + i] = 0;
             pos[t] = 0;
@@ -231,7 +236,7 @@ int alora_step_rows(const int32_t *lengths, const int32_t *change, const int32_t
     a.seq = token_seq_ids; a.pos = token_positions; a.aid = token_adapter_ids; a.slot = slot_mapping;
     a.n_seqs = dims->n_seqs; a.max_blocks = dims->max_blocks; a.bs = dims->block_size;
     a.row_cap = dims->row_cap; a.pool_cap = dims->pool_cap; a.n_blocks = (int)(dims->n_slots / dims->block_size);
-    const int wgs = std::min(256, std::max(1, dims->row_cap / 512));
+    const int wgs = std::min(256, std::max({1, dims->row_cap / 512, dims->pool_cap / 8192}));
     launch_kernel(step_rows_kernel, dim3((unsigned)wgs), dim3(STEP_SEQS), 0, (hipStream_t)hip_stream, a);
     const int e = launch_status();
     if (e) { note_hip_error(e); return ALORA_EHIP; }
@@ -246,8 +251,9 @@ int alora_tree_rows(const int32_t *tree_parents, const int32_t *row_offsets, con
     if (n_tokens == 0) return ALORA_OK;
     if (!tree_parents || !row_offsets || (n_seqs && !context_lens) || !tree_mask || !token_positions) return ALORA_EINVAL;
     if (((uintptr_t)tree_parents | (uintptr_t)row_offsets | (uintptr_t)context_lens | (uintptr_t)token_positions) & 3 || (uintptr_t)tree_mask & 7) return ALORA_EINVAL;
+    const int clearing = (int)std::min(64ll, 1 + n_tokens / (256ll * mask_words));      // workgroups
     const auto go = [&](auto kernel) {
-        launch_kernel(kernel, dim3((unsigned)n_seqs + 1u), dim3(64 * (unsigned)mask_words), 0, (hipStream_t)hip_stream, tree_parents, row_offsets, context_lens, tree_mask,
+        launch_kernel(kernel, dim3((unsigned)(n_seqs + clearing)), dim3(64 * (unsigned)mask_words), 0, (hipStream_t)hip_stream, tree_parents, row_offsets, context_lens, tree_mask,
                       token_positions, n_tokens, n_seqs);
     };
     mask_words == 1 ? go(tree_rows_kernel<1>) : mask_words == 2 ? go(tree_rows_kernel<2>) : mask_words == 3 ? go(tree_rows_kernel<3>) : go(tree_rows_kernel<4>);

@@ -236,16 +236,18 @@ __device__ __forceinline__ bool find_item(const TreeArgs &a, int item, int hk, T
     return true;
 }
 
-// Rows of no sequence: zeros.  The last workgroup of a K/V head.
+// Rows of no sequence: zeros.  Done by the workgroups of a K/V head behind those for items, 64 rows of the call each (as many as there may be in a batch
+// that is padded to a fixed size), at most MOST_CLEARING.
+constexpr int MOST_CLEARING = 256;
 template <int D, bool BF16, int NW>
-__device__ __forceinline__ void clear_rows(const TreeArgs &a, int hk)
+__device__ __forceinline__ void clear_rows(const TreeArgs &a, int hk, int number, int of)
 {
     const ListArgs &g = a.list;
     const int begin = g.n_seqs ? min(max(a.offsets[0], 0), g.T) : 0, end = g.n_seqs ? min(max(a.offsets[g.n_seqs], begin), g.T) : 0;
     const int chunks = (D << g.lg_g) * (BF16 ? 2 : 4) / 16;
     const size_t width = (size_t)g.Hq * D * (BF16 ? 2 : 4);
     auto clear = [&](int t0, int t1) {
-        for (long long i = threadIdx.x; i < (long long)(t1 - t0) * chunks; i += 64 * NW)
+        for (long long i = (long long)number * (64 * NW) + threadIdx.x; i < (long long)(t1 - t0) * chunks; i += (long long)of * (64 * NW))
             *(u32x4 *)((char *)g.out + (t0 + i / chunks) * width + ((size_t)hk * chunks + i % chunks) * 16) = (u32x4){0u, 0u, 0u, 0u};
     };
     clear(0, begin);
@@ -261,7 +263,7 @@ __global__ __launch_bounds__(256) void tree_vector_kernel(TreeArgs a)
     __shared__ uint32_t bits[C][2 * ALORA_MAX_TREE_WORDS];
     const ListArgs &g = a.list;
     const int hk = (int)blockIdx.x % g.Hkv, item = (int)blockIdx.x / g.Hkv, tid = threadIdx.x;
-    if (item == (int)(gridDim.x / g.Hkv) - 1) return clear_rows<D, BF16, 4>(a, hk);
+    if (item >= a.max_items) return clear_rows<D, BF16, 4>(a, hk, item - a.max_items, (int)(gridDim.x / g.Hkv) - a.max_items);
     TreeItem it;
     if (!find_item<4>(a, item, hk, find, it)) return;
     const int G = 1 << g.lg_g;
@@ -297,7 +299,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_matrix_kernel(TreeArgs a)
     __shared__ TreeScratch find;
     const ListArgs &g = a.list;
     const int hk = (int)blockIdx.x % g.Hkv, item = (int)blockIdx.x / g.Hkv;
-    if (item == (int)(gridDim.x / g.Hkv) - 1) return clear_rows<D, true, WAVES>(a, hk);
+    if (item >= a.max_items) return clear_rows<D, true, WAVES>(a, hk, item - a.max_items, (int)(gridDim.x / g.Hkv) - a.max_items);
     TreeItem it;
     if (!find_item<WAVES>(a, item, hk, find, it)) return;
     const int32_t *bt = g.bt + (size_t)it.seq * g.max_blocks;
@@ -359,7 +361,8 @@ static int check_tree(const alora_attn_dims *d, int words)
     const int st = check_attention(d);
     if (st) return st;
     if (words < 1 || words > ALORA_MAX_TREE_WORDS || d->n_seqs > 1 << 20) return ALORA_ESHAPE;
-    if (plan_tree(d).items * d->n_kv_heads > 0x3fffffffll) return ALORA_ESHAPE;
+    if ((long long)d->max_blocks * d->block_size > 1 << 30) return ALORA_ESHAPE;
+    if ((plan_tree(d).items + MOST_CLEARING) * d->n_kv_heads >= 1 << 24) return ALORA_ESHAPE;      // (workgroups of 256: a grid holds fewer than 2^32 threads)
     return ALORA_OK;
 }
 
@@ -401,7 +404,8 @@ int alora_tree_attention(const void *q, const void *k_cache, const void *v_cache
     a.n_tiles = (int *)workspace;
     a.tiles = (TreeTile *)((char *)workspace + p.tiles_at);
     const bool bf16 = dims->dtype == ALORA_BF16;
-    const dim3 grid((unsigned)((p.items + 1) * dims->n_kv_heads)), merge((unsigned)(p.tiles * dims->n_kv_heads), (unsigned)p.columns / 4);
+    const int clearing = std::min(MOST_CLEARING, 1 + dims->n_tokens / 64);
+    const dim3 grid((unsigned)((p.items + clearing) * dims->n_kv_heads)), merge((unsigned)(p.tiles * dims->n_kv_heads), (unsigned)p.columns / 4);
     const auto go = [&](auto kernel, auto combine) {
         launch_kernel(kernel, grid, dim3(64 * WAVES), 0, (hipStream_t)hip_stream, a);
         launch_kernel(combine, merge, dim3(256), 0, (hipStream_t)hip_stream, a, p.columns);

@@ -96,6 +96,11 @@ def test_readers_refuse_arguments():
         assert call(attn(n_tokens=0), ws=None, size=0, **{n: None for n in names}) == OK
     assert tree(d, words=0) == tree(d, words=5) == tree(attn(n_seqs=(1 << 20) + 1)) == ESHAPE
     assert select(d, budget=2) == select(d, first=-1) == select(d, recent=0) == select(d, budget=(1 << 20) + 1) == select(d, budget=2**31 - 1, recent=2**31 - 1) == EINVAL
+    for big in (dict(n_tokens=(1 << 22) // 2), dict(max_blocks=(1 << 28) + 1), dict(n_kv_heads=(1 << 16) + 1, n_q_heads=(1 << 16) + 1)):
+        assert select(attn(**big)) == selected(attn(**big)) == size_of("alora_block_select", attn(**big))[0] == ESHAPE, big
+    for big in (dict(max_blocks=(1 << 26) + 1), dict(n_tokens=1 << 29), dict(n_tokens=1 << 24, n_q_heads=64, n_kv_heads=64, dtype=0), dict(n_tokens=1 << 24, n_q_heads=8, dtype=0)):
+        assert tree(attn(**big)) == size_of("alora_tree_attention", attn(**big), 1)[0] == ESHAPE, big
+    assert size_of("alora_block_select", attn(n_tokens=(1 << 21) - 1, max_blocks=1 << 28))[0] == size_of("alora_tree_attention", attn(max_blocks=1 << 26, n_tokens=1 << 22), 4)[0] == OK
     assert selected(d, budget=0) == selected(d, budget=(1 << 20) + 1) == EINVAL and selected(attn(block_size=1 << 20), budget=1 << 20) == ESHAPE
     assert size_of("alora_selected_attention", d, 0)[0] == EINVAL
 
@@ -115,7 +120,7 @@ def test_bounds_are_refused():
         a = [kw.get(n, P) for n in ("k", "slot", "bounds", "scales")]
         return ab.lib().alora_block_bounds(*a, ctypes.byref(ab.AloraBoundsDims(**dims)), None)
     for kw, status in ((dict(dtype=2), EINVAL), (dict(n_rows=-1), EINVAL), (dict(n_kv_heads=0), EINVAL), (dict(block_size=0), EINVAL), (dict(n_slots=-1), EINVAL),
-                       (dict(head_dim=80), ESHAPE), (dict(n_slots=1 << 31), ESHAPE), (dict(n_kv_heads=1 << 17), ESHAPE), (dict(k=None), EINVAL), (dict(slot=None), EINVAL),
+                       (dict(head_dim=80), ESHAPE), (dict(n_slots=1 << 31), ESHAPE), (dict(n_kv_heads=1 << 17), ESHAPE), (dict(n_rows=(1 << 27) + 1), ESHAPE), (dict(k=None), EINVAL), (dict(slot=None), EINVAL),
                        (dict(bounds=None), EINVAL), (dict(scales=None), EINVAL), (dict(k=P + 8), EINVAL), (dict(slot=P + 4), EINVAL), (dict(bounds=P + 8), EINVAL),
                        (dict(scales=P + 2), EINVAL), (dict(n_rows=0, k=None), OK)):
         assert bounds(**kw) == status, kw

@@ -109,6 +109,38 @@ def test_steps_with_lengths_and_pools_out_of_range():
         s.check()
 
 
+def test_steps_of_lengths_up_to_the_largest():
+    """A length that, rounded up to blocks, passes 31 bits; the table has room for exactly so many."""
+    n, bs, columns = 2 ** 31 - 5, 16, 1 << 27
+    tables = torch.full((1, columns), -1, dtype=torch.int32, device="cuda")
+    last = (n - 1) // bs
+    tables[0, last - 40: last + 1] = torch.arange(100, 141, dtype=torch.int32, device="cuda")
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    pool = i32(*range(60))
+    for change, length, freed in ((3, n + 3, []), (4, n + 4, []), (5, n, []), (-500, n - 500, [140 - i for i in range(31)])):
+        out = [i32(*[-9] * k) for k in (1, 6, 2, 8, 8, 8)] + [torch.full((8,), -9, dtype=torch.int64, device="cuda")]
+        ab.alora_step_rows(i32(n), i32(change), None, None, tables, pool, i32(7, 2, 0, 0, 0, 0), *out, ab.make_step_dims(tables, bs, 8, pool, 200 * bs))
+        served = length - n if 0 < length - n else 0
+        assert out[0].item() == length and out[1].tolist() == [7, 2 + len(freed), served, 0, len(freed), int(change == 5)]
+        assert out[4].tolist() == [*range(n, n + served), *[0] * (8 - served)]
+        assert out[6].tolist() == [140 * bs + (n + i) % bs for i in range(served)] + [-1] * (8 - served)
+        assert pool[9: 9 + len(freed)].tolist() == freed
+
+
+def test_steps_that_give_back_more_blocks_than_a_pool_holds():
+    """2^30 blocks of one position and more: the sums stop there, the pool much earlier."""
+    columns = (1 << 30) + 100
+    tables = torch.empty((2, columns), dtype=torch.int32, device="cuda")
+    tables[0, :100] = torch.arange(100, dtype=torch.int32, device="cuda")
+    tables[1, -300:] = torch.arange(1000, 1300, dtype=torch.int32, device="cuda")
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    pool = torch.full((300,), -6, dtype=torch.int32, device="cuda")
+    out = [i32(*[-9] * k) for k in (2, 6, 3, 1, 1, 1)] + [torch.full((1,), -9, dtype=torch.int64, device="cuda")]
+    ab.alora_step_rows(i32(100, columns), i32(-100, -columns), None, None, tables, pool, i32(290, 0, 0, 0, 0, 0), *out, ab.make_step_dims(tables, 1, 1, pool, 5000))
+    assert out[0].tolist() == [0, 0] and out[1].tolist() == [290, 300, 0, 0, 300, 0]
+    assert torch.cat([pool[290:], pool[:290]]).tolist() == [*range(99, -1, -1), *range(1299, 1099, -1)]
+
+
 def test_a_loop_of_steps_on_the_device():
     """Lengths, tables and pool stay on the device over 40 steps; the loop exchanges the states."""
     rng = np.random.default_rng(8)
@@ -298,6 +330,16 @@ def test_tree_tables_with_entries_outside_the_cache(dtype):
     t.check()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_trees_in_a_padded_batch(dtype):
+    t = Tree(dtype, [90, 3], [5, 2], 1, 16, 4, 64, 16, seed=11, first=70, behind=5000)
+    t.run()
+    got = to_f64(t.out)
+    assert not got[:70].any() and not got[77:].any()
+    t.off, t.mask, t.q, t.out = t.off - 70, t.mask[70: 77], t.q[70: 77], t.out[70: 77]
+    t.check()
+
+
 def test_tree_contexts_past_the_table_are_cut():
     t = Tree("f32", [50, 30], [4, 3], 1, 2, 1, 64, 16, seed=7)
     t.ctx[1] = 1 << 30
@@ -344,6 +386,19 @@ def test_block_bounds_of_values_at_the_ends_of_their_range(dtype):
     wb, ws = od.block_bounds(to_f64(kt), np.arange(36), np.zeros((9, hkv, 2, d), np.int8), np.zeros((9, hkv), np.float32), bs, hkv, d)
     assert np.array_equal(scales.cpu().numpy(), ws) and np.array_equal(bounds.cpu().numpy(), wb)
     assert np.isinf(ws).sum() == 3 and not wb[3].any()
+
+
+def test_bounds_in_a_padded_batch():
+    """A block's next row may be thousands of rows without a slot further on, or not there."""
+    bs, hkv, d = 16, 2, 64
+    k = np.random.default_rng(2).standard_normal((6 * bs, hkv * d)).astype(np.float32)
+    for gap, tail in ((1500, 0), (511, 4000), (512, 1), (513, 700), (0, 3000)):
+        slots = np.concatenate([np.arange(40), np.full(gap, -1), np.arange(40, 75), np.full(tail, 96)])
+        b0, s0 = np.ones((6, hkv, 2, d), np.int8), np.ones((6, hkv), np.float32)
+        kt, slot, bounds, scales = dev(k), dev(slots), dev(b0), dev(s0)
+        ab.alora_block_bounds(kt, slot, bounds, scales, ab.make_bounds_dims(kt, slot, hkv, d, bs))
+        wb, ws = od.block_bounds(to_f64(kt), slots, b0, s0, bs, hkv, d)
+        assert np.array_equal(scales.cpu().numpy(), ws) and np.array_equal(bounds.cpu().numpy(), wb), (gap, tail)
 
 
 class Select:
@@ -497,6 +552,41 @@ def test_lists_of_any_kind(dtype):
     lists[4, :, 0] = 0
     out = t.attend(lists)
     assert not out[3].any() and not out[2, 4 * 128:].any()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_caches_and_bounds_past_4_gib(dtype):
+    """The same blocks at the end of a pool whose byte offsets pass 32 bits (blocks of one position, so that those of the bounds do too): the same results, bit by bit."""
+    hq, hkv, d = 16, 8, 128
+    s = Select(dtype, [600, 90], hq, hkv, d, 1, seed=12)
+    t = Tree(dtype, [500, 40], [20, 7], 1, hq, hkv, d, 1, seed=12)
+    n = 2_200_000
+
+    def moved(c):
+        k = [torch.empty((n, hkv * d), dtype=s.dt, device="cuda") for _ in range(2)]
+        for x, y in zip(k, (c.k, c.v)):
+            x[-y.shape[0]:] = y
+        return k, dev(np.where(c.tables >= 0, c.tables + n - c.k.shape[0], -1).astype(np.int32))
+
+    def run(k, v, bt, bounds, scales, shift):
+        slots = s.cache.tables[0, :601].astype(np.int64) + shift
+        slot = dev(slots)
+        ab.alora_block_bounds(k, slot, bounds, scales, ab.make_bounds_dims(k, slot, hkv, d, 1))
+        dims, sel, out = ab.make_attn_dims(s.q, k, bt, hq, hkv, d, 1), torch.empty((2, hkv, 50), dtype=torch.int32, device="cuda"), torch.empty_like(s.q)
+        ws = [torch.empty((m + 16,), dtype=torch.uint8, device="cuda") for m in (ab.alora_block_select_workspace_bytes(dims), ab.alora_selected_attention_workspace_bytes(dims, 50))]
+        ab.alora_block_select(s.q, bounds, scales, bt, *s.dev, sel, 1, 2, dims, ws[0])
+        ab.alora_selected_attention(s.q, k, v, bt, *s.dev, sel, out, dims, ws[1])
+        return sel, out, bounds[slot], scales[slot]
+    near = run(s.cache.k, s.cache.v, s.bt, s.b, s.s, 0)
+    (k, v), bt = moved(s.cache)
+    bounds, scales, m = torch.empty((n, hkv, 2, d), dtype=torch.int8, device="cuda"), torch.empty((n, hkv), device="cuda"), s.cache.k.shape[0]
+    bounds[-m:], scales[-m:] = dev(s.bounds), dev(s.scales)
+    far = run(k, v, bt, bounds, scales, n - m)
+    assert all(torch.equal(x, y) for x, y in zip(near, far)) and torch.isfinite(near[1]).all()
+    near = t.run().clone()
+    (k, v), bt = moved(t.cache)
+    ab.alora_tree_attention(t.q, k, v, bt, *t.dev, t.out, ab.make_attn_dims(t.q, k, bt, hq, hkv, d, 1), t.ws)
+    assert torch.equal(t.out, near) and torch.isfinite(near).all()
 
 
 # ---- streams, graphs ------------------------------------------------------------------------------
