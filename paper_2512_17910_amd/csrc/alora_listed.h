@@ -205,13 +205,14 @@ __device__ __forceinline__ f32x16 multiply(bf16x8 x, bf16x8 y, f32x16 z) { retur
 __device__ __forceinline__ f32x4 multiply(bf16x8 x, bf16x8 y, f32x4 z) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, z, 0, 0, 0); }
 
 //   columns        of the workgroup that exist; a wavefront beyond them only copies
+//   share          (SHARE, two tiles a step) true, of columns for half of the wavefronts at most: the second half has the first half's, and takes every other tile
 //   masked_from    places from here on are seen by some columns only: seen(place) = 32 bits of this lane's column, place a multiple of 32 from lo on
 //   q_at, out_at   element of q and out where this lane's column begins (column COLS * wavefront + lane % COLS)
 //   part           < 0: rows of out; else number of the part whose sums are left, of room for part_columns columns
 // WHOLE: the weights go into the product with V as two bf16 numbers (their rounding then adds nothing to that of the result), for twice
 // the products.  ONCE: rows are not read again soon (non-temporal copies).
-template <bool WHOLE, bool ONCE, class L, class SlotOf, class Seen>
-__device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, L &lds, int lo, int hi, int masked_from, int columns, SlotOf slot_of,
+template <bool WHOLE, bool ONCE, bool SHARE, class L, class SlotOf, class Seen>
+__device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, L &lds, int lo, int hi, int masked_from, int columns, bool may_share, SlotOf slot_of,
                                                  Seen seen, size_t q_at, size_t out_at, long long part, int part_columns)
 {
     constexpr int D = L::D, NW = L::NW, COLS = L::COLS, NB = L::NB, STEP = L::STEP, TILE = L::TILE, PITCH = L::PITCH, WIN = L::WINDOW / 32;
@@ -224,8 +225,9 @@ __device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, L &l
     typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
     typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c16 = lane & 15, li = lane % COLS, g = lane / COLS;
-    const int col = COLS * w + li;
-    const bool col_ok = col < columns, work = COLS * w < columns;
+    const bool share = SHARE && may_share;
+    const int wc = share && w >= NW / 2 ? w - NW / 2 : w, col = COLS * wc + li;
+    const bool col_ok = col < columns, work = COLS * wc < columns;
     const uint32_t tiles_at = (uint32_t)(uintptr_t)(lds_byte *)lds.tiles, row_bytes = (uint32_t)a.Hkv * (uint32_t)PITCH, head = (uint32_t)hk * (uint32_t)PITCH;
     const int c_hi = (hi - lo + 31) >> 5;                       // tiles of this part
 
@@ -432,6 +434,7 @@ __device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, L &l
 #pragma unroll
         for (int k = 0; k < STEP; ++k) next[k] = lookup(NB - STEP + k);
         int cur = 0, nxt = NB - STEP;
+        const uint32_t mine = !share ? 3u : w < NW / 2 ? 1u : 2u;      // tiles of a step that this wavefront multiplies
         for (int c = 0; c < c_hi; c += STEP) {
             asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(L::IPW * (NB - 2 * STEP)) : "memory");
 #pragma unroll
@@ -443,7 +446,7 @@ __device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, L &l
             if (work) {
 #pragma unroll
                 for (int k = 0; k < STEP; ++k)
-                    if (k == 0 || c + k < c_hi) consume(c + k, cur + k);
+                    if ((!SHARE || mine >> k & 1u) && (k == 0 || c + k < c_hi)) consume(c + k, cur + k);
             }
             cur = cur + STEP == NB ? 0 : cur + STEP;
             nxt = nxt + STEP == NB ? 0 : nxt + STEP;
@@ -455,6 +458,34 @@ __device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, L &l
         if (LG == 4) l += __shfl_xor(l, 16);
         both_halves(l, x, y);
         l = x + y;
+    }
+    if (share) {
+        // the second half's sums go to the first half, in a fixed order
+        float *const ml = (float *)lds.slots;
+        lds_byte *const sums = (lds_byte *)lds.tiles + NB * TILE + wc * (COLS * D * 4);
+        static_assert(!SHARE || (STEP == 2 && NW / 2 * COLS * D * 4 <= NB * TILE && NW * COLS * 4 <= (int)sizeof(lds.slots)), "room for the sums, behind that for turning results around");
+        __syncthreads();
+        if (w >= NW / 2) {
+            if (g == 0) ml[2 * col] = m, ml[2 * col + 1] = l;
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int v = 0; v < NA; v += 4)
+                    *(__attribute__((address_space(3))) f32x4 *)(sums + (((t * NA + v) / 4 * 64 + lane) << 4)) = (f32x4){acc[t][v], acc[t][v + 1], acc[t][v + 2], acc[t][v + 3]};
+        }
+        __syncthreads();
+        if (w >= NW / 2) return;
+        const float mo = ml[2 * col], lo2 = ml[2 * col + 1], mn = fmaxf(m, mo), ca = __builtin_amdgcn_exp2f(m - mn), cb = __builtin_amdgcn_exp2f(mo - mn);
+        m = mn;
+        l = l * ca + lo2 * cb;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int v = 0; v < NA; v += 4) {
+                const f32x4 x = *(const __attribute__((address_space(3))) f32x4 *)(sums + (((t * NA + v) / 4 * 64 + lane) << 4));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[t][v + e] = acc[t][v + e] * ca + x[e] * cb;
+            }
     }
     if (part >= 0) {
         if (col_ok) {
@@ -469,7 +500,7 @@ __device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, L &l
         return;
     }
     // columns are rows of the result: a wavefront turns its own around in the tiles, which nobody reads any more
-    __syncthreads();
+    if (!share) __syncthreads();
     if (!work) return;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     lds_byte *strip = (lds_byte *)lds.tiles + w * (COLS * L::SP);
@@ -490,11 +521,11 @@ __device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, L &l
 
 // ---- parts of a list, combined --------------------------------------------------------------------
 // One wavefront per column: parts first, first + step, ... of `columns` columns each.  head_dim / 4 lanes take a part (four elements each), the others of
-// the wavefront the next ones.
-template <int D, bool BF16>
+// the wavefront the next ones; AHEAD at once.
+template <int D, bool BF16, int AHEAD>
 __device__ __forceinline__ void combine_parts(const ListArgs &a, size_t first, size_t step, int parts, int columns, int column, size_t out_at)
 {
-    constexpr int LP = D / 4, NS = 64 / LP, AHEAD = 8;
+    constexpr int LP = D / 4, NS = 64 / LP;
     const int lane = threadIdx.x & 63, sub = lane / LP, d = lane % LP * 4;
     float M = M_FLOOR, L = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};

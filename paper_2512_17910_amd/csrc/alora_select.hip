@@ -577,8 +577,8 @@ __global__ __launch_bounds__(256, 2) void selected_matrix_kernel(SelectedArgs a)
     const SelectedItem it = selected_item(a, scratch);
     const int columns = 1 << g.lg_g, col = min((int)threadIdx.x & 15, columns - 1);
     const size_t at = ((size_t)it.t * g.Hq + ((size_t)it.hk << g.lg_g) + col) * D;
-    read_list_matrix<true, ONCE>(
-        g, it.hk, lds, it.lo, it.hi, 0x7fffffff, columns,
+    read_list_matrix<true, ONCE, false>(
+        g, it.hk, lds, it.lo, it.hi, 0x7fffffff, columns, false,
         [&](int v) { return selected_slot(g, it, v); },
         [&](int) { return 0xffffffffu; },
         at, at, it.part, columns);
@@ -591,7 +591,7 @@ __global__ __launch_bounds__(256) void selected_merge_kernel(SelectedArgs a)
     const int c = (int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), list = c >> g.lg_g;      // query head of a list in parts
     if (list >= g.T * g.Hkv - a.whole) return;
     const int G = 1 << g.lg_g;
-    combine_parts<D, BF16>(g, (size_t)list * a.parts, 1, a.parts, G, c & (G - 1), (((size_t)a.whole << g.lg_g) + c) * D);
+    combine_parts<D, BF16, 16>(g, (size_t)list * a.parts, 1, a.parts, G, c & (G - 1), (((size_t)a.whole << g.lg_g) + c) * D);
 }
 
 // ---- host -----------------------------------------------------------------------------------------

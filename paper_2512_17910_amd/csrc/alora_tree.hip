@@ -292,7 +292,7 @@ __global__ __launch_bounds__(256) void tree_vector_kernel(TreeArgs a)
 
 // 32 columns a wavefront: 128 >> lg_g rows of a sequence.
 constexpr int WAVES = 4;
-template <int D, bool ONCE>
+template <int D, bool ONCE, bool SHARE>
 __global__ __launch_bounds__(64 * WAVES, 2) void tree_matrix_kernel(TreeArgs a)
 {
     __shared__ MatrixTiles<D, WAVES, 32, 512 / D, 2, 2048> lds;      // 64 KiB of tiles: two workgroups share a CU's LDS
@@ -303,11 +303,13 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_matrix_kernel(TreeArgs a)
     TreeItem it;
     if (!find_item<WAVES>(a, item, hk, find, it)) return;
     const int32_t *bt = g.bt + (size_t)it.seq * g.max_blocks;
-    const int col = 32 * ((int)threadIdx.x >> 6) + ((int)threadIdx.x & 31), columns = it.rows << g.lg_g, row = it.row0 + (min(col, columns - 1) >> g.lg_g);
+    const int columns = it.rows << g.lg_g;
+    const bool share = SHARE && columns <= 32 * WAVES / 2;
+    const int col = 32 * (((int)threadIdx.x >> 6) & (share ? WAVES / 2 - 1 : WAVES - 1)) + ((int)threadIdx.x & 31), row = it.row0 + (min(col, columns - 1) >> g.lg_g);
     const uint32_t *bits = a.mask + (size_t)row * 2 * a.words;
     const size_t at = ((size_t)row * g.Hq + ((size_t)hk << g.lg_g) + (col & ((1 << g.lg_g) - 1))) * D;
-    read_list_matrix<false, ONCE>(
-        g, hk, lds, it.lo, it.hi, it.ctx, columns,
+    read_list_matrix<false, ONCE, SHARE>(
+        g, hk, lds, it.lo, it.hi, it.ctx, columns, share,
         [&](int v) { return slot_at(g, bt, v / g.bs, v % g.bs); },
         [&](int place) {               // the row's bits of drafts place - ctx .. + 31; what lies in front of them is seen
             const int from = place - it.ctx, i = from >> 5, s = from & 31;
@@ -323,10 +325,10 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int columns
 {
     const ListArgs &g = a.list;
     const int c = (int)blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hk = (int)blockIdx.x % g.Hkv, tile = (int)blockIdx.x / g.Hkv;
-    if (tile >= *a.n_tiles) return;
-    const TreeTile t = a.tiles[tile];
-    if (t.parts <= 1 || c >> g.lg_g >= t.rows || (long long)t.first + (long long)(t.parts - 1) * t.step >= a.max_items) return;
-    combine_parts<D, BF16>(g, (size_t)t.first * g.Hkv + hk, (size_t)t.step * g.Hkv, t.parts, columns, c,
+    const int n = *a.n_tiles;
+    const TreeTile t = a.tiles[tile];      // (both loads at once: there is room for as many as workgroups)
+    if (tile >= n || t.parts <= 1 || c >> g.lg_g >= t.rows || (long long)t.first + (long long)(t.parts - 1) * t.step >= a.max_items) return;
+    combine_parts<D, BF16, 8>(g, (size_t)t.first * g.Hkv + hk, (size_t)t.step * g.Hkv, t.parts, columns, c,
                            ((size_t)(t.row0 + (c >> g.lg_g)) * g.Hq + ((size_t)hk << g.lg_g) + (c & ((1 << g.lg_g) - 1))) * D);
 }
 
@@ -413,11 +415,17 @@ int alora_tree_attention(const void *q, const void *k_cache, const void *v_cache
     // Non-temporal copies where a sequence brings one tile on average: then its context is read once.  us, ordinary | non-temporal, 32/8 heads: 13 rows at 9000
     // positions 21.5 | 19.7, at 128000 118 | 102, 64 x 8 rows at 8192 385 | 350, 64 x 24 400 | 385, 64 x 32 430 | 427, 64 x 40 (two tiles) 702 | 739; one context of
     // 16000 for 12 sequences 101 | 97, of 8000 for 64 222 | 218.
-    const bool once = (long long)dims->n_tokens * (dims->n_q_heads / dims->n_kv_heads) <= 32ll * WAVES * dims->n_seqs;
+    const long long columns = (long long)dims->n_tokens * (dims->n_q_heads / dims->n_kv_heads);
+    const bool once = columns <= 32ll * WAVES * dims->n_seqs;
+    // Where half of the wavefronts have columns on average, the kernel that lets the other half take every second tile.  us, without | with: 13 rows at 2000
+    // positions 16.1 | 15.2, at 9000 19.4 | 17.3, 16 x 8 rows at 1000 34.2 | 27.9; at 16000 and more, where memory bounds them, the same within 2 %.  (With wider
+    // trees it loses: 48 of up to 64 rows and 8 heads a group 490 | 500.)
+    const bool share = columns <= 16ll * WAVES * dims->n_seqs;
     const auto choose = [&](auto head_dim) {
         constexpr int D = decltype(head_dim)::value;
         if (!bf16) p.columns == 4 ? go(tree_vector_kernel<D, 4, false>, tree_merge_kernel<D, false>) : go(tree_vector_kernel<D, 8, false>, tree_merge_kernel<D, false>);
-        else once ? go(tree_matrix_kernel<D, true>, tree_merge_kernel<D, true>) : go(tree_matrix_kernel<D, false>, tree_merge_kernel<D, true>);
+        else if (share) go(tree_matrix_kernel<D, true, true>, tree_merge_kernel<D, true>);
+        else once ? go(tree_matrix_kernel<D, true, false>, tree_merge_kernel<D, true>) : go(tree_matrix_kernel<D, false, false>, tree_merge_kernel<D, true>);
     };
     if (dims->head_dim == 128) choose(std::integral_constant<int, 128>{});
     else choose(std::integral_constant<int, 64>{});

@@ -295,11 +295,12 @@ def test_peaked_scores_and_scale():
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hq", [2, 8])                                 # (with two, wavefronts share the columns)
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
-def test_drafts_that_a_row_does_not_see_may_hold_anything(dtype, bad):
+def test_drafts_that_a_row_does_not_see_may_hold_anything(dtype, hq, bad):
     """Two branches; the second one's keys and values are not finite.  Rows of the first are as if it were not there."""
     def branches(value):
-        t = Tree(dtype, [70, 5], [41, 1], 1, 8, 2, 128, 16, seed=5)
+        t = Tree(dtype, [70, 5], [41, 1], 1, hq, 2, 128, 16, seed=5)
         left = np.zeros(42, bool)
         left[1: 41: 2] = True
         for i in range(41):
