@@ -28,7 +28,7 @@ __device__ __forceinline__ int slot_at(const ListArgs &a, const int32_t *bt, int
     return (unsigned)b < (unsigned)a.n_blocks ? b * a.bs + offset : -1;      // (slots are below 2^31)
 }
 
-// ---- vector arithmetic: C columns, positions on the lanes -----------------------------------------
+// ---- vector arithmetic, fp32: C columns, positions on the lanes -----------------------------------
 // head_dim / 8 lanes share a position, 8 elements each; the groups of lanes of all four wavefronts take positions in turn, each with
 // running sums of its own, merged in a fixed order at the end.
 //   lo, hi         places of the list this workgroup reads
@@ -43,15 +43,15 @@ struct VectorScratch {
     float m[4][C], l[4][C], acc[4][C][D];
 };
 
-template <int D, int C, bool BF16, class SlotOf, class Seen, class QAt, class Store>
+template <int D, int C, class SlotOf, class Seen, class QAt, class Store>
 __device__ __forceinline__ void read_list_vector(const ListArgs &a, int hk, VectorScratch<C, D> &scr, int lo, int hi, int masked_from, SlotOf slot_of, Seen seen,
                                                  QAt q_at, Store store)
 {
-    constexpr int LPP = D / 8, PPW = 64 / LPP, PPI = 4 * PPW, U = BF16 ? 4 : 2, BLK = PPI * U, WINDOW = VectorScratch<C, D>::WINDOW;
+    constexpr int LPP = D / 8, PPW = 64 / LPP, PPI = 4 * PPW, U = 2, BLK = PPI * U, WINDOW = VectorScratch<C, D>::WINDOW;
     static_assert(WINDOW % (2 * BLK) == 0, "whole blocks in a window");
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, grp = lane / LPP, ch = lane % LPP, jl = wave * PPW + grp;
     const size_t width = (size_t)a.Hkv * D, col = (size_t)hk * D + 8 * ch;
-    Raw8<BF16> qr[C];
+    Raw8<false> qr[C];
     float m[C], l[C], acc[C][8];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
@@ -63,7 +63,7 @@ __device__ __forceinline__ void read_list_vector(const ListArgs &a, int hk, Vect
         for (int e = 0; e < 8; ++e) acc[c][e] = 0.f;
     }
     int w0 = lo;
-    auto fetch = [&](int j0, Raw8<BF16> (&kr)[U], Raw8<BF16> (&vr)[U]) {
+    auto fetch = [&](int j0, Raw8<false> (&kr)[U], Raw8<false> (&vr)[U]) {
         unsigned ok = 0;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -77,7 +77,7 @@ __device__ __forceinline__ void read_list_vector(const ListArgs &a, int hk, Vect
         }
         return ok;
     };
-    auto consume = [&](int j0, const Raw8<BF16> (&kr)[U], const Raw8<BF16> (&vr)[U], unsigned ok) {
+    auto consume = [&](int j0, const Raw8<false> (&kr)[U], const Raw8<false> (&vr)[U], unsigned ok) {
         float s[U][C];
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -129,7 +129,7 @@ __device__ __forceinline__ void read_list_vector(const ListArgs &a, int hk, Vect
         for (int i = tid; i < WINDOW && w0 + i < hi; i += 256) scr.slots[i] = slot_of(w0 + i);
         __syncthreads();
         const int end = min(hi, w0 + WINDOW);
-        Raw8<BF16> kA[U], vA[U], kB[U], vB[U];
+        Raw8<false> kA[U], vA[U], kB[U], vB[U];
         unsigned okA = fetch(w0, kA, vA), okB;
         for (int j0 = w0; j0 < end; j0 += 2 * BLK) {
             okB = fetch(j0 + BLK, kB, vB);

@@ -541,7 +541,7 @@ __device__ __forceinline__ int selected_slot(const ListArgs &g, const SelectedIt
     return slot_at(g, it.bt, e, off);
 }
 
-template <int D, int G, bool BF16>
+template <int D, int G>
 __global__ __launch_bounds__(256) void selected_vector_kernel(SelectedArgs a)
 {
     __shared__ VectorScratch<G, D> scr;
@@ -549,7 +549,7 @@ __global__ __launch_bounds__(256) void selected_vector_kernel(SelectedArgs a)
     const ListArgs &g = a.list;
     const SelectedItem it = selected_item(a, scratch);
     const auto column_at = [&](int c) { return ((long long)it.t * g.Hq + it.hk * G + c) * D; };
-    read_list_vector<D, G, BF16>(
+    read_list_vector<D, G>(
         g, it.hk, scr, it.lo, it.hi, it.hi,
         [&](int v) { return selected_slot(g, it, v); },
         [&](int, int) { return true; },
@@ -561,9 +561,7 @@ __global__ __launch_bounds__(256) void selected_vector_kernel(SelectedArgs a)
                 g.o[at * D + d] = o;
                 return;
             }
-            const float y = L == 0.f ? 0.f : o / L;
-            if (BF16) ((bf16_t *)g.out)[column_at(c) + d] = (bf16_t)f32_to_bf16_bits(y);
-            else ((float *)g.out)[column_at(c) + d] = y;
+            ((float *)g.out)[column_at(c) + d] = L == 0.f ? 0.f : o / L;
         });
 }
 
@@ -769,10 +767,10 @@ int alora_selected_attention(const void *q, const void *k_cache, const void *v_c
         if constexpr (B) {
             once ? go(selected_matrix_kernel<D, true>) : go(selected_matrix_kernel<D, false>);
         } else switch (a.list.lg_g) {
-        case 0: go(selected_vector_kernel<D, 1, B>); break;
-        case 1: go(selected_vector_kernel<D, 2, B>); break;
-        case 2: go(selected_vector_kernel<D, 4, B>); break;
-        default: go(selected_vector_kernel<D, 8, B>); break;
+        case 0: go(selected_vector_kernel<D, 1>); break;
+        case 1: go(selected_vector_kernel<D, 2>); break;
+        case 2: go(selected_vector_kernel<D, 4>); break;
+        default: go(selected_vector_kernel<D, 8>); break;
         }
         if (rest) launch_kernel(selected_merge_kernel<D, B>, dim3((((unsigned)rest << a.list.lg_g) + 3) / 4), dim3(256), 0, (hipStream_t)hip_stream, a);
     };

@@ -255,7 +255,7 @@ __device__ __forceinline__ void clear_rows(const TreeArgs &a, int hk, int number
 }
 
 // C columns: C >> lg_g rows of a sequence.
-template <int D, int C, bool BF16>
+template <int D, int C>
 __global__ __launch_bounds__(256) void tree_vector_kernel(TreeArgs a)
 {
     __shared__ VectorScratch<C, D> scr;
@@ -263,7 +263,7 @@ __global__ __launch_bounds__(256) void tree_vector_kernel(TreeArgs a)
     __shared__ uint32_t bits[C][2 * ALORA_MAX_TREE_WORDS];
     const ListArgs &g = a.list;
     const int hk = (int)blockIdx.x % g.Hkv, item = (int)blockIdx.x / g.Hkv, tid = threadIdx.x;
-    if (item >= a.max_items) return clear_rows<D, BF16, 4>(a, hk, item - a.max_items, (int)(gridDim.x / g.Hkv) - a.max_items);
+    if (item >= a.max_items) return clear_rows<D, false, 4>(a, hk, item - a.max_items, (int)(gridDim.x / g.Hkv) - a.max_items);
     TreeItem it;
     if (!find_item<4>(a, item, hk, find, it)) return;
     const int G = 1 << g.lg_g;
@@ -271,7 +271,7 @@ __global__ __launch_bounds__(256) void tree_vector_kernel(TreeArgs a)
     __syncthreads();
     const int32_t *bt = g.bt + (size_t)it.seq * g.max_blocks;
     const auto column_at = [&](int c) { return (((long long)it.row0 + (c >> g.lg_g)) * g.Hq + hk * G + (c & (G - 1))) * D; };
-    read_list_vector<D, C, BF16>(
+    read_list_vector<D, C>(
         g, hk, scr, it.lo, it.hi, it.ctx,
         [&](int v) { return slot_at(g, bt, v / g.bs, v % g.bs); },
         [&](int c, int v) { return v < it.ctx || (bits[c >> g.lg_g][(v - it.ctx) >> 5] >> ((v - it.ctx) & 31) & 1u); },
@@ -284,9 +284,7 @@ __global__ __launch_bounds__(256) void tree_vector_kernel(TreeArgs a)
                 g.o[at * D + d] = o;
                 return;
             }
-            const float y = L == 0.f ? 0.f : o / L;
-            if (BF16) ((bf16_t *)g.out)[column_at(c) + d] = (bf16_t)f32_to_bf16_bits(y);
-            else ((float *)g.out)[column_at(c) + d] = y;
+            ((float *)g.out)[column_at(c) + d] = L == 0.f ? 0.f : o / L;
         });
 }
 
@@ -423,7 +421,7 @@ int alora_tree_attention(const void *q, const void *k_cache, const void *v_cache
     const bool share = columns <= 16ll * WAVES * dims->n_seqs;
     const auto choose = [&](auto head_dim) {
         constexpr int D = decltype(head_dim)::value;
-        if (!bf16) p.columns == 4 ? go(tree_vector_kernel<D, 4, false>, tree_merge_kernel<D, false>) : go(tree_vector_kernel<D, 8, false>, tree_merge_kernel<D, false>);
+        if (!bf16) p.columns == 4 ? go(tree_vector_kernel<D, 4>, tree_merge_kernel<D, false>) : go(tree_vector_kernel<D, 8>, tree_merge_kernel<D, false>);
         else if (share) go(tree_matrix_kernel<D, true, true>, tree_merge_kernel<D, true>);
         else once ? go(tree_matrix_kernel<D, true, false>, tree_merge_kernel<D, true>) : go(tree_matrix_kernel<D, false, false>, tree_merge_kernel<D, true>);
     };
