@@ -65,7 +65,7 @@ __global__ __launch_bounds__(256) void block_bounds_kernel(BoundsArgs a)
         bool fine = true;
         if (on) {
             const size_t base = (size_t)b * a.bs * width + (size_t)piece * 8;
-#pragma unroll 8
+#pragma unroll 16
             for (int r = 0; r < rows; ++r) {
                 Raw8<BF16> x;
                 float f[8];
@@ -653,7 +653,11 @@ int alora_block_bounds(const void *k_cache, const int64_t *slot_mapping, int8_t 
     const auto choose = [&](auto head_dim, auto bf16) {
         constexpr int D = decltype(head_dim)::value;
         constexpr bool B = decltype(bf16)::value;
+        // us, 2, 4, 16 rows of the call to a workgroup, bf16, 8 heads of 128: a row for each of 256 blocks 4.9, 7.5, 23.2, of 1024 7.1, 8.8, 24.9, of 2048 14.2, 14.8,
+        // 26.0, of 4096 24.1, 24.5, 28.3; chunks of whole blocks of 1024 rows 5.5, 4.9, 4.8, 2048 6.4, 5.7, 4.9, 8192 18.7, 11.6, 5.9, 65536 112, 59, 25 (what
+        // starts a workgroup is then most of it).
         if (d->n_rows <= 1024) go(block_bounds_kernel<D, B, 2>, 2);
+        else if (d->n_rows <= 4096) go(block_bounds_kernel<D, B, 4>, 4);
         else go(block_bounds_kernel<D, B, 16>, 16);
     };
     typedef std::integral_constant<int, 128> D128;

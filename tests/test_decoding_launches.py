@@ -80,7 +80,7 @@ def record(tmp_path_factory):
 
 def test_steps_and_tree_rows(record):
     one, rows, pool, most = record(["run_step", {}], ["run_step", dict(row_cap=5000)], ["run_step", dict(pool_cap=40000)], ["run_step", dict(row_cap=1 << 30, pool_cap=1 << 30)])
-    assert [l[0][2] for l in (one, rows, pool, most)] == [[1, 1, 1], [9, 1, 1], [4, 1, 1], [256, 1, 1]] and one[0][0] == "step_rows_kernel" and len(one) == 1
+    assert [l[0][2] for l in (one, rows, pool, most)] == [[1, 1, 1], [39, 1, 1], [39, 1, 1], [1024, 1, 1]] and one[0][0] == "step_rows_kernel" and len(one) == 1
     for words in (1, 2, 3, 4):
         few, many = record(["run_tree_rows", dict(words=words)], ["run_tree_rows", dict(words=words, tokens=2**31 - 1, seqs=1 << 20)])
         assert few == [["tree_rows_kernel", [words], [3, 1, 1], [64 * words, 1, 1]]] and many[0][2] == [(1 << 20) + 64, 1, 1]
@@ -126,8 +126,9 @@ def test_selected_lists_fill_the_chip(record):
 
 
 def test_bounds(record):
-    small, large, most = record(["run_bounds", dict(n_rows=1024)], ["run_bounds", dict(n_rows=1025)], ["run_bounds", dict(n_rows=1 << 27)])
-    assert small == [["block_bounds_kernel", [64, 1, 2], [512, 1, 1], [256, 1, 1]]] and large == [["block_bounds_kernel", [64, 1, 16], [65, 1, 1], [256, 1, 1]]]
+    small, some, large, most = record(*[["run_bounds", dict(n_rows=n)] for n in (1024, 1025, 4097, 1 << 27)])
+    assert some == [["block_bounds_kernel", [64, 1, 4], [257, 1, 1], [256, 1, 1]]]
+    assert small == [["block_bounds_kernel", [64, 1, 2], [512, 1, 1], [256, 1, 1]]] and large == [["block_bounds_kernel", [64, 1, 16], [257, 1, 1], [256, 1, 1]]]
     assert most[0][2] == [1 << 23, 1, 1]
 
 
@@ -138,7 +139,7 @@ def test_every_instantiation_is_reached(record):
         shape = dict(dtype=dtype, head_dim=d, n_q_heads=2 * g, n_seqs=6)
         calls += [["run_tree", dict(shape, n_tokens=6 * n // g)] for n in (30, 100, 300)]
         calls += [["run_select", dict(shape, n_tokens=n, max_blocks=m)] for n in (6, 40) for m in (100, 900)] + [["run_selected", dict(shape, n_tokens=n, budget=40)] for n in (6, 40)]
-        calls += [["run_bounds", dict(dtype=dtype, head_dim=d, n_rows=n)] for n in (60, 1300)]
+        calls += [["run_bounds", dict(dtype=dtype, head_dim=d, n_rows=n)] for n in (60, 1300, 4600)]
     calls += [["run_step", {}]] + [["run_tree_rows", dict(words=w)] for w in (1, 2, 3, 4)]
     reached = {(name, *ints) for launches in record(*calls) for name, ints, _, _ in launches}
     D, B = (64, 128), (0, 1)
@@ -147,7 +148,7 @@ def test_every_instantiation_is_reached(record):
         want |= {("tree_vector_kernel", d, c) for c in (4, 8)} | {("tree_matrix_kernel", d, *x) for x in ((1, 1), (1, 0), (0, 0))}
         want |= {("selected_vector_kernel", d, g) for g in (1, 2, 4, 8)} | {("selected_matrix_kernel", d, once) for once in B}
         for b in B:
-            want |= {("tree_merge_kernel", d, b), ("selected_merge_kernel", d, b)} | {("block_bounds_kernel", d, b, n) for n in (2, 16)}
+            want |= {("tree_merge_kernel", d, b), ("selected_merge_kernel", d, b)} | {("block_bounds_kernel", d, b, n) for n in (2, 4, 16)}
             want |= {(k, d, b, once) for k in ("block_select_kernel", "block_keys_kernel") for once in B}
     assert reached == want
     # ... and the library holds no others of them

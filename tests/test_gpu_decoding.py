@@ -356,7 +356,7 @@ def test_tree_contexts_past_the_table_are_cut():
 # ---- selected blocks ------------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("hkv,d,bs", [(8, 128, 16), (1, 64, 5), (2, 64, 16), (3, 128, 1), (16, 128, 64), (5, 64, 33)])
-@pytest.mark.parametrize("rows", [1, 60, 1300])
+@pytest.mark.parametrize("rows", [1, 60, 1300, 4600])
 def test_block_bounds(dtype, hkv, d, bs, rows):
     rng = np.random.default_rng(rows + hkv + bs)
     n = rng.multinomial(rows, np.ones(min(rows, 7)) / min(rows, 7))
