@@ -816,6 +816,7 @@ def alora_tree_attention(q, k_cache, v_cache, block_tables, row_offsets, context
 
 
 def make_bounds_dims(k_cache, slot_mapping, n_kv_heads: int, head_dim: int, block_size: int) -> AloraBoundsDims:
+    """Description of alora_block_bounds calls: k_cache [n_slots, n_kv_heads * head_dim], slot_mapping of the rows that a step wrote."""
     return AloraBoundsDims(_dtype_code(k_cache), slot_mapping.shape[0], n_kv_heads, head_dim, block_size, k_cache.shape[0])
 
 

