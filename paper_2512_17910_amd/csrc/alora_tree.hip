@@ -322,7 +322,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_matrix_kernel(TreeArgs a)
 }
 
 // One wavefront per column of a tile that has parts.  Bound by the latency of tile, sums and store where there are few (5.1 us for 31 parts of one tile).
-template <int D, bool BF16>
+template <int D, bool BF16, int AHEAD>
 __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int columns)
 {
     const ListArgs &g = a.list;
@@ -330,7 +330,7 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int columns
     const int n = *a.n_tiles;
     const TreeTile t = a.tiles[tile];      // (both loads at once: there is room for as many as workgroups)
     if (tile >= n || t.parts <= 1 || c >> g.lg_g >= t.rows || (long long)t.first + (long long)(t.parts - 1) * t.step >= a.max_items) return;
-    combine_parts<D, BF16, 8>(g, (size_t)t.first * g.Hkv + hk, (size_t)t.step * g.Hkv, t.parts, columns, c,
+    combine_parts<D, BF16, AHEAD>(g, (size_t)t.first * g.Hkv + hk, (size_t)t.step * g.Hkv, t.parts, columns, c,
                            ((size_t)(t.row0 + (c >> g.lg_g)) * g.Hq + ((size_t)hk << g.lg_g) + (c & ((1 << g.lg_g) - 1))) * D);
 }
 
@@ -423,11 +423,13 @@ int alora_tree_attention(const void *q, const void *k_cache, const void *v_cache
     // positions 16.1 | 15.2, at 9000 19.4 | 17.3, 16 x 8 rows at 1000 34.2 | 27.9; at 16000 and more, where memory bounds them, the same within 2 %.  (With wider
     // trees it loses: 48 of up to 64 rows and 8 heads a group 490 | 500.)
     const bool share = columns <= 16ll * WAVES * dims->n_seqs;
+    // Parts combined 16 at a time where a tile may have more than 16 of them (13 rows at 9001 positions 20.2 | 19.5 us; 16 x 8 rows at 4000, of fewer, 57.0 | 59.7).
+    const bool many_parts = p.tiles <= p.places / 32;
     const auto choose = [&](auto head_dim) {
         constexpr int D = decltype(head_dim)::value;
-        if (!bf16) p.columns == 4 ? go(tree_vector_kernel<D, 4>, tree_merge_kernel<D, false>) : go(tree_vector_kernel<D, 8>, tree_merge_kernel<D, false>);
-        else if (share) go(tree_matrix_kernel<D, true, true>, tree_merge_kernel<D, true>);
-        else once ? go(tree_matrix_kernel<D, true, false>, tree_merge_kernel<D, true>) : go(tree_matrix_kernel<D, false, false>, tree_merge_kernel<D, true>);
+        if (!bf16) p.columns == 4 ? go(tree_vector_kernel<D, 4>, tree_merge_kernel<D, false, 8>) : go(tree_vector_kernel<D, 8>, tree_merge_kernel<D, false, 8>);
+        else if (share) many_parts ? go(tree_matrix_kernel<D, true, true>, tree_merge_kernel<D, true, 16>) : go(tree_matrix_kernel<D, true, true>, tree_merge_kernel<D, true, 8>);
+        else once ? go(tree_matrix_kernel<D, true, false>, tree_merge_kernel<D, true, 8>) : go(tree_matrix_kernel<D, false, false>, tree_merge_kernel<D, true, 8>);
     };
     if (dims->head_dim == 128) choose(std::integral_constant<int, 128>{});
     else choose(std::integral_constant<int, 64>{});

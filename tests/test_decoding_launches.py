@@ -92,10 +92,10 @@ def test_trees(record):
     calls = [(16, "tree_matrix_kernel", [128, 1, 1]), (17, "tree_matrix_kernel", [128, 1, 0]), (32, "tree_matrix_kernel", [128, 1, 0]), (33, "tree_matrix_kernel", [128, 0, 0])]
     for (rows, name, ints), launches in zip(calls, record(*[["run_tree", dict(wide, n_tokens=5 * n)] for n, _, _ in calls])):
         items = 5 * rows // 32 + 5 + 2 * 64 + 2
-        assert launches == [[name, ints, [(items + 1 + 5 * rows // 64) * 8, 1, 1], [256, 1, 1]], ["tree_merge_kernel", [128, 1], [(5 * rows // 32 + 5) * 8, 32, 1], [256, 1, 1]]]
+        assert launches == [[name, ints, [(items + 1 + 5 * rows // 64) * 8, 1, 1], [256, 1, 1]], ["tree_merge_kernel", [128, 1, 8], [(5 * rows // 32 + 5) * 8, 32, 1], [256, 1, 1]]]
     for g, columns in ((1, 4), (2, 4), (4, 4), (8, 8)):
         l, = record(["run_tree", dict(dtype=0, n_q_heads=2 * g, n_tokens=40)])
-        assert l[0][1] == [128, columns] and l[0][2][0] == 2 * (40 * g // columns + 2 + 512 + 2 + 1) and l[1][1] == [128, 0]
+        assert l[0][1] == [128, columns] and l[0][2][0] == 2 * (40 * g // columns + 2 + 512 + 2 + 1) and l[1][1] == [128, 0, 8]
     assert record(["run_tree", dict(n_tokens=0)]) == [[]]
     record(["run_tree", dict(n_tokens=1 << 22, words=4)], ["run_tree", dict(n_tokens=1 << 21, dtype=0, n_q_heads=16)])     # (large ones fit a grid)
 
@@ -137,7 +137,7 @@ def test_every_instantiation_is_reached(record):
     calls = []
     for dtype, d, g in itertools.product((0, 1), (64, 128), (1, 2, 4, 8)):
         shape = dict(dtype=dtype, head_dim=d, n_q_heads=2 * g, n_seqs=6)
-        calls += [["run_tree", dict(shape, n_tokens=6 * n // g)] for n in (30, 100, 300)]
+        calls += [["run_tree", dict(shape, n_tokens=6 * n // g)] for n in (30, 100, 300)] + [["run_tree", dict(shape, n_tokens=3, n_seqs=1)]]
         calls += [["run_select", dict(shape, n_tokens=n, max_blocks=m)] for n in (6, 40) for m in (100, 900)] + [["run_selected", dict(shape, n_tokens=n, budget=40)] for n in (6, 40)]
         calls += [["run_bounds", dict(dtype=dtype, head_dim=d, n_rows=n)] for n in (60, 1300, 4600)]
     calls += [["run_step", {}]] + [["run_tree_rows", dict(words=w)] for w in (1, 2, 3, 4)]
@@ -148,7 +148,7 @@ def test_every_instantiation_is_reached(record):
         want |= {("tree_vector_kernel", d, c) for c in (4, 8)} | {("tree_matrix_kernel", d, *x) for x in ((1, 1), (1, 0), (0, 0))}
         want |= {("selected_vector_kernel", d, g) for g in (1, 2, 4, 8)} | {("selected_matrix_kernel", d, once) for once in B}
         for b in B:
-            want |= {("tree_merge_kernel", d, b), ("selected_merge_kernel", d, b)} | {("block_bounds_kernel", d, b, n) for n in (2, 4, 16)}
+            want |= {("tree_merge_kernel", d, b, 8), ("tree_merge_kernel", d, 1, 16), ("selected_merge_kernel", d, b)} | {("block_bounds_kernel", d, b, n) for n in (2, 4, 16)}
             want |= {(k, d, b, once) for k in ("block_select_kernel", "block_keys_kernel") for once in B}
     assert reached == want
     # ... and the library holds no others of them
