@@ -15,6 +15,13 @@ struct TreeTile {
     int row0, rows, parts, first, step, pad[3];
 };
 
+// What a workgroup (of each K/V head) is for.
+struct TreeItem {
+    int row0, rows;             // the tile's rows
+    int seq, ctx, end;          // end: of the drafts that lie in the table
+    int lo, hi, parts;          // places of the sequence it reads
+};
+
 struct TreeArgs {
     ListArgs list;
     const int32_t *offsets, *context;
@@ -22,82 +29,79 @@ struct TreeArgs {
     int words, tile_rows;       // rows of a tile
     int places;                 // workgroups per K/V head that the chip holds at once
     int least_units;            // of a part
-    int max_tiles, max_items;   // the workspace has room for (offsets that do not ascend may give more)
-    int *n_tiles;
+    int max_tiles, max_items;   // the workspace has room for
+    int *found;                 // tiles, items
     TreeTile *tiles;
+    TreeItem *items;            // of more than ALONE sequences
 };
 
 constexpr int UNIT = 32;        // positions that parts are counted in
 constexpr int GOOD_UNITS = 12;  // from which two workgroups to a compute unit are worth their parts
 
-struct TreeItem {
-    int row0, rows;             // the tile's rows
-    int seq, ctx, drafts;       // drafts: those that lie in the table
-    int lo, hi, parts, part_at; // places of the sequence this workgroup reads; number of its part's sums
-};
-
+constexpr int ALONE = 64;       // sequences up to which every wavefront finds its item by itself
 constexpr int CLASSES = 4;      // of parts by their length
 
 constexpr int CUTS = 5;
 // What a call costs in units (32 positions of a tile), by what was measured: a workgroup's start, and a part's sums.
 constexpr float START = 7.f, PART = 7.f;
 
-struct TreeScratch {
-    float sums[3 * CUTS][8];
-    int counts[8][CLASSES + 1], found[8];
+struct TreeSeq {
+    int r0, n, ctx, places, tiles, units;
 };
-
-// Which tile and part workgroup `item` (of one K/V head, NW wavefronts) is for; false: none.  The same sums, in the same order, in every workgroup of the
-// call.  A sequence's parts are equal, none longer than `per`; the longest start first (in quarters of per).  Up to 64 sequences, every wavefront
-// finds out for itself; of more, each has a share and LDS brings them together.
-template <int NW>
-__device__ __forceinline__ bool find_item(const TreeArgs &a, int item, int hk, TreeScratch &scr, TreeItem &it)
+__device__ __forceinline__ TreeSeq tree_seq(const TreeArgs &a, int s)
 {
     const ListArgs &g = a.list;
-    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n_seqs = g.n_seqs;
-    const bool alone = n_seqs <= 64;
-    const int first = alone ? lane : (int)threadIdx.x, step = alone ? 64 : 64 * NW;
-    const long long cap = min((long long)g.max_blocks * g.bs, 0x7fffffffll);
-    struct Seq { int r0, n, ctx, places, tiles, units; };
-    auto seq_of = [&](int s) {
-        Seq q = {0, 0, 0, 0, 0, 0};
-        if (s < n_seqs) {
-            q.r0 = min(max(a.offsets[s], 0), g.T);
-            q.n = min(max(a.offsets[s + 1], q.r0), g.T) - q.r0;
-            q.ctx = (int)min((long long)max(a.context[s], 0), cap);
-            q.places = (int)min((long long)q.ctx + min(q.n, 64 * a.words), cap);
-            q.tiles = (q.n + a.tile_rows - 1) / a.tile_rows;
-            q.units = (q.places + UNIT - 1) / UNIT;
-        }
-        return q;
-    };
-    auto for_each = [&](const Seq &q, auto f) {
-        f(q);
-        for (int s = first + step; s < n_seqs; s += step) f(seq_of(s));
-    };
-    // a sum over lanes 0 .. lane of every wavefront -> that over all sequences
-    auto over_all = [&](float x, float (&of_wave)[8], bool largest) {
-        x = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
-        if (alone) return x;
-        if (lane == 0) of_wave[w] = x;
-        __syncthreads();
-        x = of_wave[0];
+    TreeSeq q = {0, 0, 0, 0, 0, 0};
+    if (s < g.n_seqs) {
+        const int cap = g.max_blocks * g.bs;
+        q.r0 = min(max(a.offsets[s], 0), g.T);
+        q.n = min(max(a.offsets[s + 1], q.r0), g.T) - q.r0;
+        q.ctx = min(max(a.context[s], 0), cap);
+        q.places = min(q.ctx + min(q.n, 64 * a.words), cap);
+        q.tiles = (q.n + a.tile_rows - 1) / a.tile_rows;
+        q.units = (q.places + UNIT - 1) / UNIT;
+    }
+    return q;
+}
+
+// Units of a part: no part is longer.  Found from all sequences, NW wavefronts together (for_each calls a function for each sequence of a thread); 0: there are no tiles, or more
+// than ascending offsets give.
+template <int NW>
+struct CutScratch {
+    float sums[3 + 3 * CUTS][NW];
+};
+template <int NW, class ForEach>
+__device__ __forceinline__ int units_of_parts(const TreeArgs &a, CutScratch<NW> *scr, ForEach for_each)
+{
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // N sums, every third one a maximum: over a thread's sequences -> over all
+    auto over_all = [&](auto &x, int at) {
+        constexpr int N = sizeof(x) / sizeof(float);
+        auto over_lanes = [&](float y, bool largest) {
+            y = largest ? __int_as_float(max_upto64(__float_as_int(y))) : sum_upto64(y);
+            return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(y), 63));
+        };
 #pragma unroll
-        for (int i = 1; i < NW; ++i) x = largest ? fmaxf(x, of_wave[i]) : x + of_wave[i];
-        return x;
+        for (int i = 0; i < N; ++i) {
+            x[i] = over_lanes(x[i], i % 3 == 2);
+            if (NW > 1 && lane == 0) scr->sums[at + i][w] = x[i];
+        }
+        if (NW == 1) return;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = over_lanes(lane < NW ? scr->sums[at + i][lane] : 0.f, i % 3 == 2);
     };
     // Units of all tiles, tiles, the longest.
-    Seq q = seq_of(first);
-    float total = 0.f, tiles = 0.f, most = 0.f;
-    for_each(q, [&](const Seq &x) {
-        total += (float)x.tiles * (float)x.units;
-        tiles += (float)x.tiles;
-        most = fmaxf(most, x.tiles ? (float)x.units : 0.f);
+    float all[3] = {0.f, 0.f, 0.f};
+    for_each([&](const TreeSeq &x) {
+        all[0] += (float)x.tiles * (float)x.units;
+        all[1] += (float)x.tiles;
+        all[2] = fmaxf(all[2], x.tiles ? (float)x.units : 0.f);
     });
-    total = over_all(sum_upto64(total), scr.sums[0], false);
-    tiles = over_all(sum_upto64(tiles), scr.sums[1], false);
-    most = fmaxf(over_all(__int_as_float(max_upto64(__float_as_int(most))), scr.sums[2], true), 1.f);
-    // Units of a part.  (Reciprocals: an IEEE division is 15 instructions, and every workgroup does this before its first copy.)
+    over_all(all, 0);
+    const float total = all[0], tiles = all[1], most = fmaxf(all[2], 1.f);
+    if (tiles == 0.f || tiles > (float)a.max_tiles) return 0;
+    // (Reciprocals: an IEEE division is 15 instructions, and up to ALONE sequences every workgroup does this before its first copy.)
     auto over = [](float x, float y) { return x * __builtin_amdgcn_rcpf(y); };
     const float places = (float)a.places, share = over(total, places), room = places - tiles, half = .5f * places - tiles;
     float units = most;
@@ -111,129 +115,175 @@ __device__ __forceinline__ bool find_item(const TreeArgs &a, int item, int hk, T
     } else {
         // Many: the best of whole tiles, an equal share for every place of the chip or two thirds of it, as many parts as fit in one turn or in two.
         float cut[CUTS] = {most, share, share * (2.f / 3), over(total, room), over(total, 2.f * places - tiles)};
-        float items_of[CUTS] = {}, parts_at[CUTS] = {}, most_of[CUTS] = {}, one_over[CUTS];
+        float of[3 * CUTS] = {}, one_over[CUTS];      // items, those of them that are parts, the longest
 #pragma unroll
         for (int i = 0; i < CUTS; ++i) {
             cut[i] = cut[i] > 0.f ? fmaxf(fminf(ceilf(cut[i]), most), (float)a.least_units) : most;
             one_over[i] = __builtin_amdgcn_rcpf(cut[i]);
         }
-        for_each(q, [&](const Seq &x) {
+        for_each([&](const TreeSeq &x) {
 #pragma unroll
             for (int i = 0; i < CUTS; ++i) {
                 const float parts = fmaxf(ceilf((float)x.units * one_over[i] - 1e-3f), 1.f), n = parts * (float)x.tiles;
-                items_of[i] += n;
-                parts_at[i] += parts > 1.f ? n : 0.f;
-                most_of[i] = fmaxf(most_of[i], x.tiles ? over((float)x.units, parts) : 0.f);
+                of[3 * i] += n;
+                of[3 * i + 1] += parts > 1.f ? n : 0.f;
+                of[3 * i + 2] = fmaxf(of[3 * i + 2], x.tiles ? over((float)x.units, parts) : 0.f);
             }
         });
+        over_all(of, 3);
         float best = 3.0e38f;
 #pragma unroll
         for (int i = 0; i < CUTS; ++i) {
-            const float n = over_all(sum_upto64(items_of[i]), scr.sums[3 * i], false), p = over_all(sum_upto64(parts_at[i]), scr.sums[3 * i + 1], false);
-            const float m = over_all(__int_as_float(max_upto64(__float_as_int(most_of[i]))), scr.sums[3 * i + 2], true);
             // In units: as many turns as the chip takes, or its places filled by the longest first; a start for each turn; what parts leave and are combined from.
-            const float filled = over(n, places), turns = ceilf(filled - 1e-3f);
-            const float span = fminf(turns * m, fmaxf(m, fminf(share, filled * m) + m * (1.f / 3))), cost = span + START * turns + over(PART * p, places);
+            const float m = of[3 * i + 2], filled = over(of[3 * i], places), turns = ceilf(filled - 1e-3f);
+            const float span = fminf(turns * m, fmaxf(m, fminf(share, filled * m) + m * (1.f / 3))), cost = span + START * turns + over(PART * of[3 * i + 1], places);
             if (cost < best) best = cost, units = cut[i];
         }
     }
-    const int per = (int)fminf(units, 1.0e9f);
-    auto parts_of = [&](const Seq &x) { return max(1, (x.units + per - 1) / per); };
-    auto size_of = [&](const Seq &x, int parts) { return (x.units + parts - 1) / parts; };      // units of a part (the last one's may be fewer)
-    auto class_of = [&](int size) { return min(CLASSES - 1, (int)((float)(per - size) * (float)CLASSES * __builtin_amdgcn_rcpf((float)per))); };
-    // Where a class's items begin, and behind them the tiles: `begin` of the sequences before, of all classes where there is more than one round.
-    int begin[CLASSES + 1] = {};
-    if (n_seqs > step) {
-        int count[CLASSES] = {};
-        for_each(q, [&](const Seq &x) {
-            const int parts = parts_of(x), c = class_of(size_of(x, parts));
+    return max(1, (int)fminf(units, 1.0e9f));
+}
+
+// A sequence's parts are equal, none longer than `per`; the longest start first (in quarters of per).
+struct TreeCut {
+    int parts, size, kind;      // units of a part (the last one's may be fewer), class
+};
+__device__ __forceinline__ TreeCut tree_cut(const TreeSeq &q, int per)
+{
+    TreeCut c;
+    c.parts = max(1, (q.units + per - 1) / per);
+    c.size = (q.units + c.parts - 1) / c.parts;
+    c.kind = min(CLASSES - 1, (int)((float)(per - c.size) * (float)CLASSES * __builtin_amdgcn_rcpf((float)per)));
+    return c;
+}
+// Item `i` of a sequence (tiles of one part next to each other: they read the same rows).
+__device__ __forceinline__ TreeItem tree_item(const TreeArgs &a, int s, const TreeSeq &q, const TreeCut &c, int i)
+{
+    const int part = i / q.tiles, tile = i - part * q.tiles;
+    const long long lo = (long long)part * c.size * UNIT;
+    return {q.r0 + tile * a.tile_rows, min(a.tile_rows, q.n - tile * a.tile_rows), s, q.ctx, q.places, (int)min(lo, (long long)q.places), (int)min(lo + (long long)c.size * UNIT, (long long)q.places), c.parts};
+}
+
+// Which tile and part workgroup `item` (of one K/V head) is for; false: none.
+__device__ __forceinline__ bool find_item(const TreeArgs &a, int item, int hk, TreeItem &it)
+{
+    const int lane = threadIdx.x & 63;
+    if (a.list.n_seqs > ALONE) {
+        const int n = a.found[1];
+        const TreeItem x = a.items[item];
+        int *const to = (int *)&it, *const from = (int *)&x;
 #pragma unroll
-            for (int i = 0; i < CLASSES; ++i) count[i] += c == i ? x.tiles * parts : 0;
-        });
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < CLASSES; ++i) {
-            const int u = sum_upto64(count[i]);
-            if (lane == 63) scr.counts[w][i] = u;
-        }
-        __syncthreads();
-        int upto = 0;
-#pragma unroll
-        for (int i = 0; i < CLASSES; ++i) {
-            begin[i] = upto;
-#pragma unroll
-            for (int j = 0; j < NW; ++j) upto += scr.counts[j][i];
-        }
+        for (int i = 0; i < (int)(sizeof(TreeItem) / 4); ++i) to[i] = __builtin_amdgcn_readfirstlane(from[i]);
+        return item < n;
     }
-    int found[8] = {-1};
-    if (!alone) {
-        __syncthreads();
-        if (threadIdx.x == 0) scr.found[0] = -1;
+    // The same sums, in the same order, in every wavefront of the call.
+    const TreeSeq q = tree_seq(a, lane);
+    const int per = units_of_parts<1>(a, (CutScratch<1> *)nullptr, [&](auto f) { f(q); });
+    if (per == 0) {
+        if (item == 0 && hk == 0 && threadIdx.x == 0) a.found[0] = 0;
+        return false;
     }
-    for (int s0 = 0; s0 < n_seqs; s0 += step) {
-        if (s0) q = seq_of(s0 + first);
-        const int parts = parts_of(q), size = size_of(q, parts), c = class_of(size), items = q.tiles * parts;
-        int mine[CLASSES + 1], upto[CLASSES + 1];
+    const TreeCut c = tree_cut(q, per);
+    const int items = q.tiles * c.parts, tiles_upto = sum_upto64(q.tiles);
+    int at = 0, all = 0;
 #pragma unroll
-        for (int i = 0; i <= CLASSES; ++i) {
-            mine[i] = i == CLASSES ? q.tiles : c == i ? items : 0;
-            upto[i] = sum_upto64(mine[i]);
-            if (!alone && lane == 63) scr.counts[w][i] = upto[i];
-        }
-        if (!alone) __syncthreads();
-        int all = 0, at = 0, tile_at = 0;
-#pragma unroll
-        for (int i = 0; i <= CLASSES; ++i) {
-            int here = (n_seqs > step || i == CLASSES ? begin[i] : all) + upto[i] - mine[i];
-            if (alone) {
-                const int sum = __builtin_amdgcn_readlane(upto[i], 63);
-                if (i < CLASSES) all += sum;
-                begin[i] += sum;
-            } else {
-#pragma unroll
-                for (int j = 0; j < NW; ++j) {
-                    if (j < w) here += scr.counts[j][i];
-                    if (i < CLASSES) all += scr.counts[j][i];
-                    begin[i] += scr.counts[j][i];
-                }
-            }
-            if (i == CLASSES) tile_at = here;
-            else if (c == i) at = here;
-        }
-        const bool here = item >= at && item < at + items;
-        int mine_found[8] = {};
-        if (here) {
-            const int i = item - at, part = i / q.tiles, tile = i - part * q.tiles;      // (tiles of one part next to each other: they read the same rows)
-            const int row0 = q.r0 + tile * a.tile_rows, rows = min(a.tile_rows, q.n - tile * a.tile_rows);
-            mine_found[0] = s0 + first, mine_found[1] = row0, mine_found[2] = rows, mine_found[3] = q.ctx, mine_found[4] = q.places - q.ctx, mine_found[5] = part;
-            mine_found[6] = parts, mine_found[7] = size;
-            if (hk == 0 && part == 0 && (!alone || w == 0) && tile_at + tile < a.max_tiles) a.tiles[tile_at + tile] = {row0, rows, parts, at + tile, q.tiles, {}};
-        }
-        const unsigned long long who = __builtin_amdgcn_ballot_w64(here);
-        if (alone) {
-            if (who)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) found[i] = __builtin_amdgcn_readlane(mine_found[i], (int)__builtin_ctzll(who));
-        } else {
-            if (here)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) scr.found[i] = mine_found[i];
-            __syncthreads();
-            if (scr.found[0] >= 0 && item != 0) break;       // (workgroup 0 counts all tiles)
-        }
+    for (int i = 0; i < CLASSES; ++i) {
+        const int mine = c.kind == i ? items : 0, upto = sum_upto64(mine);
+        if (c.kind == i) at = all + upto - mine;
+        all += __builtin_amdgcn_readlane(upto, 63);
     }
-    if (item == 0 && hk == 0 && threadIdx.x == 0) *a.n_tiles = min(begin[CLASSES], a.max_tiles);
-    if (!alone) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) found[i] = __builtin_amdgcn_readfirstlane(scr.found[i]);
+    if (item == 0 && hk == 0 && threadIdx.x == 63) a.found[0] = tiles_upto;
+    const bool here = item >= at && item < at + items;
+    TreeItem mine = {};
+    if (here) {
+        mine = tree_item(a, lane, q, c, item - at);
+        const int tile = item - at;             // (of part 0)
+        if (hk == 0 && threadIdx.x < 64 && tile < q.tiles) a.tiles[tiles_upto - q.tiles + tile] = {mine.row0, mine.rows, c.parts, item, q.tiles, {}};
     }
-    if (found[0] < 0) return false;
-    it.seq = found[0], it.row0 = found[1], it.rows = found[2], it.ctx = found[3], it.drafts = found[4], it.parts = found[6];
-    const int end = it.ctx + it.drafts;
-    it.lo = (int)min((long long)found[5] * found[7] * UNIT, (long long)end);
-    it.hi = (int)min((long long)it.lo + (long long)found[7] * UNIT, (long long)end);
-    it.part_at = item;
+    const unsigned long long who = __builtin_amdgcn_ballot_w64(here);
+    if (!who) return false;
+    int *const to = (int *)&it, *const from = (int *)&mine;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(TreeItem) / 4); ++i) to[i] = __builtin_amdgcn_readlane(from[i], (int)__builtin_ctzll(who));
     return true;
+}
+
+// The same for more sequences, once for all workgroups, by one: what each item is, in the workspace.  (Done by every workgroup itself it took 6 to 7 us of each.)
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void tree_plan_kernel(TreeArgs a)
+{
+    constexpr int NW = THREADS / 64;
+    __shared__ CutScratch<NW> scr;
+    __shared__ int counts[NW][CLASSES + 1];
+    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n_seqs = a.list.n_seqs;
+    const TreeSeq q0 = tree_seq(a, tid);
+    auto for_each = [&](auto f) {
+        f(q0);
+        for (int s = tid + THREADS; s < n_seqs; s += THREADS) f(tree_seq(a, s));
+    };
+    const int per = units_of_parts<NW>(a, &scr, for_each);
+    if (per == 0) {
+        if (tid == 0) a.found[0] = a.found[1] = 0;
+        return;
+    }
+    // Where a class's items begin, and behind them the tiles: `begin` of the sequences before.
+    int begin[CLASSES + 1] = {}, n[CLASSES] = {};
+    for_each([&](const TreeSeq &x) {
+        const TreeCut c = tree_cut(x, per);
+#pragma unroll
+        for (int i = 0; i < CLASSES; ++i) n[i] += c.kind == i ? x.tiles * c.parts : 0;
+    });
+#pragma unroll
+    for (int i = 0; i < CLASSES; ++i) {
+        const int u = sum_upto64(n[i]);
+        if (lane == 63) counts[w][i] = u;
+    }
+    __syncthreads();
+    int upto = 0;
+#pragma unroll
+    for (int i = 0; i < CLASSES; ++i) {
+        begin[i] = upto;
+        upto += __builtin_amdgcn_readlane(sum_upto64(lane < NW ? counts[lane][i] : 0), 63);
+    }
+    if (tid == 0) a.found[1] = min(upto, a.max_items);
+    for (int s0 = 0; s0 < n_seqs; s0 += THREADS) {
+        const TreeSeq q = s0 ? tree_seq(a, s0 + tid) : q0;
+        const TreeCut c = tree_cut(q, per);
+        const int items = q.tiles * c.parts;
+        int mine[CLASSES + 1], sum[CLASSES + 1];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i <= CLASSES; ++i) {
+            mine[i] = i == CLASSES ? q.tiles : c.kind == i ? items : 0;
+            sum[i] = sum_upto64(mine[i]);
+            if (lane == 63) counts[w][i] = sum[i];
+        }
+        __syncthreads();
+        int at = 0, tile_at = 0;
+#pragma unroll
+        for (int i = 0; i <= CLASSES; ++i) {
+            const int of_waves = sum_upto64(lane < NW ? counts[lane][i] : 0), here = begin[i] + (w ? __builtin_amdgcn_readlane(of_waves, w - 1) : 0) + sum[i] - mine[i];
+            begin[i] += __builtin_amdgcn_readlane(of_waves, 63);
+            if (i == CLASSES) tile_at = here;
+            else if (c.kind == i) at = here;
+        }
+        // a few items by the sequence's thread, many by its wavefront
+        auto put = [&](int s, const TreeSeq &q, const TreeCut &c, int at, int tile_at, int i) {
+            const TreeItem it = tree_item(a, s, q, c, i);
+            if (at + i < a.max_items) a.items[at + i] = it;
+            if (i < q.tiles && tile_at + i < a.max_tiles) a.tiles[tile_at + i] = {it.row0, it.rows, c.parts, at + i, q.tiles, {}};
+        };
+        const bool many = items > 8;
+        if (!many)
+            for (int i = 0; i < items; ++i) put(s0 + tid, q, c, at, tile_at, i);
+        for (unsigned long long todo = __builtin_amdgcn_ballot_w64(many); todo; todo &= todo - 1) {
+            const int from = (int)__builtin_ctzll(todo);
+            auto its = [&](int x) { return __builtin_amdgcn_readlane(x, from); };
+            const TreeSeq theirs = {its(q.r0), its(q.n), its(q.ctx), its(q.places), its(q.tiles), its(q.units)};
+            const TreeCut cut = {its(c.parts), its(c.size), its(c.kind)};
+            for (int i = lane; i < its(items); i += 64) put(s0 + 64 * w + from, theirs, cut, its(at), its(tile_at), i);
+        }
+    }
+    if (tid == 0) a.found[0] = min(begin[CLASSES], a.max_tiles);
 }
 
 // Rows of no sequence: zeros.  Done by the workgroups of a K/V head behind those for items, 64 rows of the call each (as many as there may be in a batch
@@ -259,13 +309,12 @@ template <int D, int C>
 __global__ __launch_bounds__(256) void tree_vector_kernel(TreeArgs a)
 {
     __shared__ VectorScratch<C, D> scr;
-    __shared__ TreeScratch find;
     __shared__ uint32_t bits[C][2 * ALORA_MAX_TREE_WORDS];
     const ListArgs &g = a.list;
     const int hk = (int)blockIdx.x % g.Hkv, item = (int)blockIdx.x / g.Hkv, tid = threadIdx.x;
     if (item >= a.max_items) return clear_rows<D, false, 4>(a, hk, item - a.max_items, (int)(gridDim.x / g.Hkv) - a.max_items);
     TreeItem it;
-    if (!find_item<4>(a, item, hk, find, it)) return;
+    if (!find_item(a, item, hk, it)) return;
     const int G = 1 << g.lg_g;
     if (tid < 2 * a.words * it.rows) bits[tid / (2 * a.words)][tid % (2 * a.words)] = a.mask[(size_t)it.row0 * 2 * a.words + tid];
     __syncthreads();
@@ -279,7 +328,7 @@ __global__ __launch_bounds__(256) void tree_vector_kernel(TreeArgs a)
         [&](int c, int d, float M, float L, float o) {
             if (c >> g.lg_g >= it.rows) return;
             if (it.parts > 1) {
-                const size_t at = ((size_t)it.part_at * g.Hkv + hk) * C + c;
+                const size_t at = ((size_t)item * g.Hkv + hk) * C + c;
                 if (d == 0) *(f32x2 *)(g.ml + 2 * at) = (f32x2){M, L};
                 g.o[at * D + d] = o;
                 return;
@@ -298,12 +347,11 @@ template <int D, bool ONCE, bool SHARE>
 __global__ __launch_bounds__(64 * WAVES, 2) void tree_matrix_kernel(TreeArgs a)
 {
     __shared__ MatrixTiles<D, WAVES, 32, 512 / D, 2, 2048> lds;      // 64 KiB of tiles: two workgroups share a CU's LDS
-    __shared__ TreeScratch find;
     const ListArgs &g = a.list;
     const int hk = (int)blockIdx.x % g.Hkv, item = (int)blockIdx.x / g.Hkv;
     if (item >= a.max_items) return clear_rows<D, true, WAVES>(a, hk, item - a.max_items, (int)(gridDim.x / g.Hkv) - a.max_items);
     TreeItem it;
-    if (!find_item<WAVES>(a, item, hk, find, it)) return;
+    if (!find_item(a, item, hk, it)) return;
     const int32_t *bt = g.bt + (size_t)it.seq * g.max_blocks;
     const int columns = it.rows << g.lg_g;
     const bool share = SHARE && columns <= 32 * WAVES / 2;
@@ -318,20 +366,21 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_matrix_kernel(TreeArgs a)
             const uint32_t x = i < 0 ? 0xffffffffu : i < 2 * a.words ? bits[i] : 0u, y = i + 1 < 2 * a.words ? bits[i + 1] : 0u;
             return s ? x >> s | y << (32 - s) : x;
         },
-        at, at, it.parts > 1 ? (long long)it.part_at * g.Hkv + hk : -1ll, 32 * WAVES);
+        at, at, it.parts > 1 ? (long long)item * g.Hkv + hk : -1ll, 32 * WAVES);
 }
 
-// One wavefront per column of a tile that has parts.  Bound by the latency of tile, sums and store where there are few (5.1 us for 31 parts of one tile).
+// One wavefront per column of a tile that has parts, of a tile's with many tiles several.  Bound by the latency of tile, sums and store where there are few (5.1 us for 31 parts of one tile).
 template <int D, bool BF16, int AHEAD>
 __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int columns)
 {
     const ListArgs &g = a.list;
-    const int c = (int)blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hk = (int)blockIdx.x % g.Hkv, tile = (int)blockIdx.x / g.Hkv;
-    const int n = *a.n_tiles;
+    const int hk = (int)blockIdx.x % g.Hkv, tile = (int)blockIdx.x / g.Hkv;
+    const int n = a.found[0];
     const TreeTile t = a.tiles[tile];      // (both loads at once: there is room for as many as workgroups)
-    if (tile >= n || t.parts <= 1 || c >> g.lg_g >= t.rows || (long long)t.first + (long long)(t.parts - 1) * t.step >= a.max_items) return;
-    combine_parts<D, BF16, AHEAD>(g, (size_t)t.first * g.Hkv + hk, (size_t)t.step * g.Hkv, t.parts, columns, c,
-                           ((size_t)(t.row0 + (c >> g.lg_g)) * g.Hq + ((size_t)hk << g.lg_g) + (c & ((1 << g.lg_g) - 1))) * D);
+    if (tile >= n || t.parts <= 1 || (long long)t.first + (long long)(t.parts - 1) * t.step >= a.max_items) return;
+    for (int c = (int)blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); c >> g.lg_g < t.rows; c += (int)gridDim.y * 4)
+        combine_parts<D, BF16, AHEAD>(g, (size_t)t.first * g.Hkv + hk, (size_t)t.step * g.Hkv, t.parts, columns, c,
+                                      ((size_t)(t.row0 + (c >> g.lg_g)) * g.Hq + ((size_t)hk << g.lg_g) + (c & ((1 << g.lg_g) - 1))) * D);
 }
 
 // ---- host ---------------------------------------------------------------------------------------
@@ -340,7 +389,7 @@ struct TreePlan {
     bool matrix;                // instructions; else vector arithmetic
     int columns, tile_rows, places;
     long long tiles, items;
-    size_t tiles_at, ml_at, o_at, bytes;
+    size_t tiles_at, items_at, ml_at, o_at, bytes;
 };
 static TreePlan plan_tree(const alora_attn_dims *d)
 {
@@ -354,7 +403,8 @@ static TreePlan plan_tree(const alora_attn_dims *d)
     p.items = p.tiles + 2ll * p.places + 2;                                      // sum of ceil(units / per) over tiles, see find_item
     const auto up = [](size_t n) { return (n + 255) / 256 * 256; };
     p.tiles_at = 256;
-    p.ml_at = p.tiles_at + up((size_t)p.tiles * sizeof(TreeTile));
+    p.items_at = p.tiles_at + up((size_t)p.tiles * sizeof(TreeTile));
+    p.ml_at = p.items_at + (d->n_seqs > ALONE ? up((size_t)p.items * sizeof(TreeItem)) : 0);
     p.o_at = p.ml_at + up((size_t)p.items * d->n_kv_heads * p.columns * 8);
     p.bytes = p.o_at + (size_t)p.items * d->n_kv_heads * p.columns * d->head_dim * 4;
     return p;
@@ -405,12 +455,18 @@ int alora_tree_attention(const void *q, const void *k_cache, const void *v_cache
     a.mask = (const uint32_t *)tree_mask; a.words = mask_words;
     a.tile_rows = p.tile_rows; a.places = p.places; a.least_units = p.matrix ? 8 : 4;      // (fp32, 5 trees over up to 700 positions, eight columns: 2 units 22.2 us, 4 20.7, 8 23.8)
     a.max_tiles = (int)p.tiles; a.max_items = (int)p.items;
-    a.n_tiles = (int *)workspace;
+    a.found = (int *)workspace;
     a.tiles = (TreeTile *)((char *)workspace + p.tiles_at);
+    a.items = (TreeItem *)((char *)workspace + p.items_at);
     const bool bf16 = dims->dtype == ALORA_BF16;
+    // About 8192 workgroups combine parts: most tiles of a call with many have none (32 for each tile: 1000 sequences 72 us for nothing, now 5).  us, 2048, 8192, 32768
+    // workgroups: 64 x 4 rows at 300 positions 24.2, 25.7, 28.1, 16 x 8 at 4000 56.7, 56.9, 56.6; 48 ragged sequences of up to 64 rows 547, 525, 521.
     const int clearing = std::min(MOST_CLEARING, 1 + dims->n_tokens / 64);
-    const dim3 grid((unsigned)((p.items + clearing) * dims->n_kv_heads)), merge((unsigned)(p.tiles * dims->n_kv_heads), (unsigned)p.columns / 4);
+    const dim3 grid((unsigned)((p.items + clearing) * dims->n_kv_heads)), merge((unsigned)(p.tiles * dims->n_kv_heads), (unsigned)std::clamp(8192 / (p.tiles * dims->n_kv_heads), 1ll, p.columns / 4ll));
     const auto go = [&](auto kernel, auto combine) {
+        // (us, 256 | 1024 threads: 65 sequences of 300 positions 33.6 | 36.5, 256 of 1000 197 | 199, 1000 of 300 294 | 291, 3000 of 200 626 | 613)
+        if (dims->n_seqs > 512) launch_kernel(tree_plan_kernel<1024>, dim3(1), dim3(1024), 0, (hipStream_t)hip_stream, a);
+        else if (dims->n_seqs > ALONE) launch_kernel(tree_plan_kernel<256>, dim3(1), dim3(256), 0, (hipStream_t)hip_stream, a);
         launch_kernel(kernel, grid, dim3(64 * WAVES), 0, (hipStream_t)hip_stream, a);
         launch_kernel(combine, merge, dim3(256), 0, (hipStream_t)hip_stream, a, p.columns);
     };

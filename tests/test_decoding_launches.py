@@ -93,6 +93,11 @@ def test_trees(record):
     for (rows, name, ints), launches in zip(calls, record(*[["run_tree", dict(wide, n_tokens=5 * n)] for n, _, _ in calls])):
         items = 5 * rows // 32 + 5 + 2 * 64 + 2
         assert launches == [[name, ints, [(items + 1 + 5 * rows // 64) * 8, 1, 1], [256, 1, 1]], ["tree_merge_kernel", [128, 1, 8], [(5 * rows // 32 + 5) * 8, 32, 1], [256, 1, 1]]]
+    plans = [(64, []), (65, [["tree_plan_kernel", [256], [1, 1, 1], [256, 1, 1]]]), (512, [["tree_plan_kernel", [256], [1, 1, 1], [256, 1, 1]]]),
+             (513, [["tree_plan_kernel", [1024], [1, 1, 1], [1024, 1, 1]]])]
+    for (seqs, plan), launches in zip(plans, record(*[["run_tree", dict(wide, n_tokens=8 * n, n_seqs=n)] for n, _ in plans])):
+        tiles = seqs // 4 + seqs
+        assert launches[:-2] == plan and launches[-1][2] == [8 * tiles, max(1, min(32, 8192 // (8 * tiles))), 1]
     for g, columns in ((1, 4), (2, 4), (4, 4), (8, 8)):
         l, = record(["run_tree", dict(dtype=0, n_q_heads=2 * g, n_tokens=40)])
         assert l[0][1] == [128, columns] and l[0][2][0] == 2 * (40 * g // columns + 2 + 512 + 2 + 1) and l[1][1] == [128, 0, 8]
@@ -137,13 +142,13 @@ def test_every_instantiation_is_reached(record):
     calls = []
     for dtype, d, g in itertools.product((0, 1), (64, 128), (1, 2, 4, 8)):
         shape = dict(dtype=dtype, head_dim=d, n_q_heads=2 * g, n_seqs=6)
-        calls += [["run_tree", dict(shape, n_tokens=6 * n // g)] for n in (30, 100, 300)] + [["run_tree", dict(shape, n_tokens=3, n_seqs=1)]]
+        calls += [["run_tree", dict(shape, n_tokens=6 * n // g)] for n in (30, 100, 300)] + [["run_tree", dict(shape, n_tokens=3, n_seqs=n)] for n in (1, 300, 600)]
         calls += [["run_select", dict(shape, n_tokens=n, max_blocks=m)] for n in (6, 40) for m in (100, 900)] + [["run_selected", dict(shape, n_tokens=n, budget=40)] for n in (6, 40)]
         calls += [["run_bounds", dict(dtype=dtype, head_dim=d, n_rows=n)] for n in (60, 1300, 4600)]
     calls += [["run_step", {}]] + [["run_tree_rows", dict(words=w)] for w in (1, 2, 3, 4)]
     reached = {(name, *ints) for launches in record(*calls) for name, ints, _, _ in launches}
     D, B = (64, 128), (0, 1)
-    want = {("step_rows_kernel",), ("block_list_kernel", 1024), *(("tree_rows_kernel", w) for w in (1, 2, 3, 4))}
+    want = {("step_rows_kernel",), ("tree_plan_kernel", 256), ("tree_plan_kernel", 1024), ("block_list_kernel", 1024), *(("tree_rows_kernel", w) for w in (1, 2, 3, 4))}
     for d in D:
         want |= {("tree_vector_kernel", d, c) for c in (4, 8)} | {("tree_matrix_kernel", d, *x) for x in ((1, 1), (1, 0), (0, 0))}
         want |= {("selected_vector_kernel", d, g) for g in (1, 2, 4, 8)} | {("selected_matrix_kernel", d, once) for once in B}

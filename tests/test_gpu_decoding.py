@@ -287,6 +287,23 @@ def test_many_sequences_and_few(dtype):
         assert np.array_equal(raw_bits(t.run()), first)                # whatever the workspace held
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("seqs", [64, 65, 257, 513, 1100])
+@pytest.mark.parametrize("most", [3, 9])
+def test_more_sequences_than_a_wavefront_or_a_workgroup_looks_at(dtype, seqs, most):
+    """Ragged, some without a context, some without drafts; two are long, one of them with many rows: their parts and tiles are written by many threads."""
+    rng = np.random.default_rng(seqs + most)
+    ctx, n = rng.integers(0, 40, seqs), rng.integers(0, most + 1, seqs)
+    ctx[[7, seqs - 2]], n[seqs - 2] = (1900, 900), 130
+    t = Tree(dtype, ctx, n.tolist(), 3, 4, 1, 64, 16, seed=seqs, first=2, behind=3)
+    t.run()
+    t.check()
+    first = raw_bits(t.out).copy()
+    t.ws.fill_(-1e30)
+    t.out.fill_(float("nan"))
+    assert np.array_equal(raw_bits(t.run()), first)
+
+
 def test_peaked_scores_and_scale():
     for scale in (0.0, 0.3):
         t = Tree("bf16", [300, 20], [20, 30], 1, 8, 2, 128, 16, seed=4, std=6.0, scale=scale)
