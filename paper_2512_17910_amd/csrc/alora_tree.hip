@@ -4,7 +4,6 @@
 // sees of the drafts, which lie behind the context, a mask says.  The contexts are cut into parts of one length, found on the device
 // from all lengths of the call (their sum is not known on the host), so that workgroups have equal work however ragged the lengths are.
 #include <algorithm>
-#include <new>
 #include "alora_tree.h"
 #include "alora_listed.h"
 
@@ -339,7 +338,7 @@ __global__ __launch_bounds__(256) void tree_vector_kernel(TreeArgs a)
 
 // 32 columns a wavefront: 128 >> lg_g rows of a sequence.  What bounds it: with wide trees matrix and vector unit in turn (48 sequences of up to 64 drafts over up to 16000
 // positions, 64 / 8 heads, 318 GFLOP: 505 us, 0.63 PFLOP/s of products that count and 0.75 of those made; the matrix unit is busy for 30 % of the cycles, the
-// vector unit for 42), with many narrow ones memory (64 x 8 rows over 8192, 2.1 GB: 351 us, 6.1 TB/s), with one latency (13 rows over 9001, 15.6 us: to find its
+// vector unit for 47), with many narrow ones memory (64 x 8 rows over 8192, 2.1 GB: 351 us, 6.1 TB/s), with one latency (13 rows over 9001, 15.0 us: to find its
 // part 1.9, slots 1.2, first tiles 1.5, the rest two tiles at a time).  The weights are rounded once to bf16 for the product with V: twice the products, as for
 // selected blocks, cost 3 to 9 %.
 constexpr int WAVES = 4;
