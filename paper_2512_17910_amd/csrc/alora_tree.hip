@@ -9,7 +9,7 @@
 
 namespace alora {
 
-// A tile of a sequence's rows, for the kernel that combines its parts.
+// A tile of a sequence's rows, for the kernel that combines its parts: numbers first, first + step, ...
 struct TreeTile {
     int row0, rows, parts, first, step, pad[3];
 };
@@ -18,7 +18,7 @@ struct TreeTile {
 struct TreeItem {
     int row0, rows;             // the tile's rows
     int seq, ctx, end;          // end: of the drafts that lie in the table
-    int lo, hi, parts;          // places of the sequence it reads
+    int lo, hi, part;           // places of the sequence it reads; number of its part's sums, -1: the whole tile
 };
 
 struct TreeArgs {
@@ -28,7 +28,7 @@ struct TreeArgs {
     int words, tile_rows;       // rows of a tile
     int places;                 // workgroups per K/V head that the chip holds at once
     int least_units;            // of a part
-    int max_tiles, max_items;   // the workspace has room for
+    int max_tiles, max_items, max_parts;      // the workspace has room for
     int *found;                 // tiles, items
     TreeTile *tiles;
     TreeItem *items;            // of more than ALONE sequences
@@ -123,7 +123,9 @@ __device__ __forceinline__ int units_of_parts(const TreeArgs &a, CutScratch<NW> 
         for_each([&](const TreeSeq &x) {
 #pragma unroll
             for (int i = 0; i < CUTS; ++i) {
-                const float parts = fmaxf(ceilf((float)x.units * one_over[i] - 1e-3f), 1.f), n = parts * (float)x.tiles;
+                float parts = fmaxf(ceilf((float)x.units * one_over[i] - 1e-3f), 1.f);
+                if (fmaf(parts, cut[i], -(float)x.units) < 0.f) parts += 1.f;      // (exact: the parts' sums need room)
+                const float n = parts * (float)x.tiles;
                 of[3 * i] += n;
                 of[3 * i + 1] += parts > 1.f ? n : 0.f;
                 of[3 * i + 2] = fmaxf(of[3 * i + 2], x.tiles ? over((float)x.units, parts) : 0.f);
@@ -136,7 +138,7 @@ __device__ __forceinline__ int units_of_parts(const TreeArgs &a, CutScratch<NW> 
             // In units: as many turns as the chip takes, or its places filled by the longest first; a start for each turn; what parts leave and are combined from.
             const float m = of[3 * i + 2], filled = over(of[3 * i], places), turns = ceilf(filled - 1e-3f);
             const float span = fminf(turns * m, fmaxf(m, fminf(share, filled * m) + m * (1.f / 3))), cost = span + START * turns + over(PART * of[3 * i + 1], places);
-            if (cost < best) best = cost, units = cut[i];
+            if (cost < best && of[3 * i + 1] <= (float)a.max_parts) best = cost, units = cut[i];      // (whole tiles have no parts)
         }
     }
     return max(1, (int)fminf(units, 1.0e9f));
@@ -154,12 +156,12 @@ __device__ __forceinline__ TreeCut tree_cut(const TreeSeq &q, int per)
     c.kind = min(CLASSES - 1, (int)((float)(per - c.size) * (float)CLASSES * __builtin_amdgcn_rcpf((float)per)));
     return c;
 }
-// Item `i` of a sequence (tiles of one part next to each other: they read the same rows).
-__device__ __forceinline__ TreeItem tree_item(const TreeArgs &a, int s, const TreeSeq &q, const TreeCut &c, int i)
+// Item `i` of a sequence (tiles of one part next to each other: they read the same rows), whose parts' numbers begin at `part_at`.
+__device__ __forceinline__ TreeItem tree_item(const TreeArgs &a, int s, const TreeSeq &q, const TreeCut &c, int part_at, int i)
 {
     const int part = i / q.tiles, tile = i - part * q.tiles;
     const long long lo = (long long)part * c.size * UNIT;
-    return {q.r0 + tile * a.tile_rows, min(a.tile_rows, q.n - tile * a.tile_rows), s, q.ctx, q.places, (int)min(lo, (long long)q.places), (int)min(lo + (long long)c.size * UNIT, (long long)q.places), c.parts};
+    return {q.r0 + tile * a.tile_rows, min(a.tile_rows, q.n - tile * a.tile_rows), s, q.ctx, q.places, (int)min(lo, (long long)q.places), (int)min(lo + (long long)c.size * UNIT, (long long)q.places), c.parts > 1 ? part_at + i : -1};
 }
 
 // Which tile and part workgroup `item` (of one K/V head) is for; false: none.
@@ -172,7 +174,7 @@ __device__ __forceinline__ bool find_item(const TreeArgs &a, int item, int hk, T
         int *const to = (int *)&it, *const from = (int *)&x;
 #pragma unroll
         for (int i = 0; i < (int)(sizeof(TreeItem) / 4); ++i) to[i] = __builtin_amdgcn_readfirstlane(from[i]);
-        return item < n;
+        return item < n && it.part < a.max_parts;
     }
     // The same sums, in the same order, in every wavefront of the call.
     const TreeSeq q = tree_seq(a, lane);
@@ -182,7 +184,7 @@ __device__ __forceinline__ bool find_item(const TreeArgs &a, int item, int hk, T
         return false;
     }
     const TreeCut c = tree_cut(q, per);
-    const int items = q.tiles * c.parts, tiles_upto = sum_upto64(q.tiles);
+    const int items = q.tiles * c.parts, tiles_upto = sum_upto64(q.tiles), numbered = c.parts > 1 ? items : 0, part_at = sum_upto64(numbered) - numbered;
     int at = 0, all = 0;
 #pragma unroll
     for (int i = 0; i < CLASSES; ++i) {
@@ -194,16 +196,16 @@ __device__ __forceinline__ bool find_item(const TreeArgs &a, int item, int hk, T
     const bool here = item >= at && item < at + items;
     TreeItem mine = {};
     if (here) {
-        mine = tree_item(a, lane, q, c, item - at);
+        mine = tree_item(a, lane, q, c, part_at, item - at);
         const int tile = item - at;             // (of part 0)
-        if (hk == 0 && threadIdx.x < 64 && tile < q.tiles) a.tiles[tiles_upto - q.tiles + tile] = {mine.row0, mine.rows, c.parts, item, q.tiles, {}};
+        if (hk == 0 && threadIdx.x < 64 && tile < q.tiles) a.tiles[tiles_upto - q.tiles + tile] = {mine.row0, mine.rows, c.parts, part_at + tile, q.tiles, {}};
     }
     const unsigned long long who = __builtin_amdgcn_ballot_w64(here);
     if (!who) return false;
     int *const to = (int *)&it, *const from = (int *)&mine;
 #pragma unroll
     for (int i = 0; i < (int)(sizeof(TreeItem) / 4); ++i) to[i] = __builtin_amdgcn_readlane(from[i], (int)__builtin_ctzll(who));
-    return true;
+    return it.part < a.max_parts;
 }
 
 // The same for more sequences, once for all workgroups, by one: what each item is, in the workspace.  (Done by every workgroup itself it took 6 to 7 us of each.)
@@ -212,7 +214,7 @@ __global__ __launch_bounds__(THREADS) void tree_plan_kernel(TreeArgs a)
 {
     constexpr int NW = THREADS / 64;
     __shared__ CutScratch<NW> scr;
-    __shared__ int counts[NW][CLASSES + 1];
+    __shared__ int counts[NW][CLASSES + 2];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), n_seqs = a.list.n_seqs;
     const TreeSeq q0 = tree_seq(a, tid);
     auto for_each = [&](auto f) {
@@ -224,8 +226,8 @@ __global__ __launch_bounds__(THREADS) void tree_plan_kernel(TreeArgs a)
         if (tid == 0) a.found[0] = a.found[1] = 0;
         return;
     }
-    // Where a class's items begin, and behind them the tiles: `begin` of the sequences before.
-    int begin[CLASSES + 1] = {}, n[CLASSES] = {};
+    // Where a class's items begin, and the tiles, and the parts' numbers: `begin` of the sequences before.
+    int begin[CLASSES + 2] = {}, n[CLASSES] = {};
     for_each([&](const TreeSeq &x) {
         const TreeCut c = tree_cut(x, per);
 #pragma unroll
@@ -248,38 +250,39 @@ __global__ __launch_bounds__(THREADS) void tree_plan_kernel(TreeArgs a)
         const TreeSeq q = s0 ? tree_seq(a, s0 + tid) : q0;
         const TreeCut c = tree_cut(q, per);
         const int items = q.tiles * c.parts;
-        int mine[CLASSES + 1], sum[CLASSES + 1];
+        int mine[CLASSES + 2], sum[CLASSES + 2];
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i <= CLASSES; ++i) {
-            mine[i] = i == CLASSES ? q.tiles : c.kind == i ? items : 0;
+        for (int i = 0; i < CLASSES + 2; ++i) {
+            mine[i] = i == CLASSES ? q.tiles : i > CLASSES ? (c.parts > 1 ? items : 0) : c.kind == i ? items : 0;
             sum[i] = sum_upto64(mine[i]);
             if (lane == 63) counts[w][i] = sum[i];
         }
         __syncthreads();
-        int at = 0, tile_at = 0;
+        int at = 0, tile_at = 0, part_at = 0;
 #pragma unroll
-        for (int i = 0; i <= CLASSES; ++i) {
+        for (int i = 0; i < CLASSES + 2; ++i) {
             const int of_waves = sum_upto64(lane < NW ? counts[lane][i] : 0), here = begin[i] + (w ? __builtin_amdgcn_readlane(of_waves, w - 1) : 0) + sum[i] - mine[i];
             begin[i] += __builtin_amdgcn_readlane(of_waves, 63);
             if (i == CLASSES) tile_at = here;
+            else if (i > CLASSES) part_at = here;
             else if (c.kind == i) at = here;
         }
         // a few items by the sequence's thread, many by its wavefront
-        auto put = [&](int s, const TreeSeq &q, const TreeCut &c, int at, int tile_at, int i) {
-            const TreeItem it = tree_item(a, s, q, c, i);
+        auto put = [&](int s, const TreeSeq &q, const TreeCut &c, int at, int tile_at, int part_at, int i) {
+            const TreeItem it = tree_item(a, s, q, c, part_at, i);
             if (at + i < a.max_items) a.items[at + i] = it;
-            if (i < q.tiles && tile_at + i < a.max_tiles) a.tiles[tile_at + i] = {it.row0, it.rows, c.parts, at + i, q.tiles, {}};
+            if (i < q.tiles && tile_at + i < a.max_tiles) a.tiles[tile_at + i] = {it.row0, it.rows, c.parts, part_at + i, q.tiles, {}};
         };
         const bool many = items > 8;
         if (!many)
-            for (int i = 0; i < items; ++i) put(s0 + tid, q, c, at, tile_at, i);
+            for (int i = 0; i < items; ++i) put(s0 + tid, q, c, at, tile_at, part_at, i);
         for (unsigned long long todo = __builtin_amdgcn_ballot_w64(many); todo; todo &= todo - 1) {
             const int from = (int)__builtin_ctzll(todo);
             auto its = [&](int x) { return __builtin_amdgcn_readlane(x, from); };
             const TreeSeq theirs = {its(q.r0), its(q.n), its(q.ctx), its(q.places), its(q.tiles), its(q.units)};
             const TreeCut cut = {its(c.parts), its(c.size), its(c.kind)};
-            for (int i = lane; i < its(items); i += 64) put(s0 + 64 * w + from, theirs, cut, its(at), its(tile_at), i);
+            for (int i = lane; i < its(items); i += 64) put(s0 + 64 * w + from, theirs, cut, its(at), its(tile_at), its(part_at), i);
         }
     }
     if (tid == 0) a.found[0] = min(begin[CLASSES], a.max_tiles);
@@ -326,8 +329,8 @@ __global__ __launch_bounds__(256) void tree_vector_kernel(TreeArgs a)
         [&](int c) { return c >> g.lg_g < it.rows ? column_at(c) : -1ll; },
         [&](int c, int d, float M, float L, float o) {
             if (c >> g.lg_g >= it.rows) return;
-            if (it.parts > 1) {
-                const size_t at = ((size_t)item * g.Hkv + hk) * C + c;
+            if (it.part >= 0) {
+                const size_t at = ((size_t)it.part * g.Hkv + hk) * C + c;
                 if (d == 0) *(f32x2 *)(g.ml + 2 * at) = (f32x2){M, L};
                 g.o[at * D + d] = o;
                 return;
@@ -365,7 +368,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_matrix_kernel(TreeArgs a)
             const uint32_t x = i < 0 ? 0xffffffffu : i < 2 * a.words ? bits[i] : 0u, y = i + 1 < 2 * a.words ? bits[i + 1] : 0u;
             return s ? x >> s | y << (32 - s) : x;
         },
-        at, at, it.parts > 1 ? (long long)item * g.Hkv + hk : -1ll, 32 * WAVES);
+        at, at, it.part >= 0 ? (long long)it.part * g.Hkv + hk : -1ll, 32 * WAVES);
 }
 
 // One wavefront per column of a tile that has parts, of a tile's with many tiles several.  Bound by the latency of tile, sums and store where there are few (5.1 us for 31 parts of one tile).
@@ -376,7 +379,7 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int columns
     const int hk = (int)blockIdx.x % g.Hkv, tile = (int)blockIdx.x / g.Hkv;
     const int n = a.found[0];
     const TreeTile t = a.tiles[tile];      // (both loads at once: there is room for as many as workgroups)
-    if (tile >= n || t.parts <= 1 || (long long)t.first + (long long)(t.parts - 1) * t.step >= a.max_items) return;
+    if (tile >= n || t.parts <= 1 || (long long)t.first + (long long)(t.parts - 1) * t.step >= a.max_parts) return;
     for (int c = (int)blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); c >> g.lg_g < t.rows; c += (int)gridDim.y * 4)
         combine_parts<D, BF16, AHEAD>(g, (size_t)t.first * g.Hkv + hk, (size_t)t.step * g.Hkv, t.parts, columns, c,
                                       ((size_t)(t.row0 + (c >> g.lg_g)) * g.Hq + ((size_t)hk << g.lg_g) + (c & ((1 << g.lg_g) - 1))) * D);
@@ -387,7 +390,7 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int columns
 struct TreePlan {
     bool matrix;                // instructions; else vector arithmetic
     int columns, tile_rows, places;
-    long long tiles, items;
+    long long tiles, items, parts;
     size_t tiles_at, items_at, ml_at, o_at, bytes;
 };
 static TreePlan plan_tree(const alora_attn_dims *d)
@@ -399,13 +402,14 @@ static TreePlan plan_tree(const alora_attn_dims *d)
     p.tile_rows = p.columns / G;
     p.places = std::max(1, 512 / d->n_kv_heads);
     p.tiles = d->n_tokens / p.tile_rows + std::min(d->n_seqs, d->n_tokens);      // (a sequence's last tile may not be full)
-    p.items = p.tiles + 2ll * p.places + 2;                                      // sum of ceil(units / per) over tiles, see find_item
+    p.items = p.tiles + 2ll * p.places + 2;                                      // sum of ceil(units / per) over tiles, see units_of_parts
+    p.parts = std::min(p.items, 4ll * p.places + 8);                             // (few tiles have as many as there are places at most; of many tiles' cuts none with more is taken)
     const auto up = [](size_t n) { return (n + 255) / 256 * 256; };
     p.tiles_at = 256;
     p.items_at = p.tiles_at + up((size_t)p.tiles * sizeof(TreeTile));
     p.ml_at = p.items_at + (d->n_seqs > ALONE ? up((size_t)p.items * sizeof(TreeItem)) : 0);
-    p.o_at = p.ml_at + up((size_t)p.items * d->n_kv_heads * p.columns * 8);
-    p.bytes = p.o_at + (size_t)p.items * d->n_kv_heads * p.columns * d->head_dim * 4;
+    p.o_at = p.ml_at + up((size_t)p.parts * d->n_kv_heads * p.columns * 8);
+    p.bytes = p.o_at + (size_t)p.parts * d->n_kv_heads * p.columns * d->head_dim * 4;
     return p;
 }
 
@@ -453,7 +457,7 @@ int alora_tree_attention(const void *q, const void *k_cache, const void *v_cache
     a.offsets = row_offsets; a.context = context_lens;
     a.mask = (const uint32_t *)tree_mask; a.words = mask_words;
     a.tile_rows = p.tile_rows; a.places = p.places; a.least_units = p.matrix ? 8 : 4;      // (fp32, 5 trees over up to 700 positions, eight columns: 2 units 22.2 us, 4 20.7, 8 23.8)
-    a.max_tiles = (int)p.tiles; a.max_items = (int)p.items;
+    a.max_tiles = (int)p.tiles; a.max_items = (int)p.items; a.max_parts = (int)p.parts;
     a.found = (int *)workspace;
     a.tiles = (TreeTile *)((char *)workspace + p.tiles_at);
     a.items = (TreeItem *)((char *)workspace + p.items_at);

@@ -296,12 +296,27 @@ def test_more_sequences_than_a_wavefront_or_a_workgroup_looks_at(dtype, seqs, mo
     ctx, n = rng.integers(0, 40, seqs), rng.integers(0, most + 1, seqs)
     ctx[[7, seqs - 2]], n[seqs - 2] = (1900, 900), 130
     t = Tree(dtype, ctx, n.tolist(), 3, 4, 1, 64, 16, seed=seqs, first=2, behind=3)
+    t.ws[ab.alora_tree_attention_workspace_bytes(t.dims, 3) // 4:] = 7.0
     t.run()
+    assert (t.ws[ab.alora_tree_attention_workspace_bytes(t.dims, 3) // 4:] == 7.0).all()
     t.check()
     first = raw_bits(t.out).copy()
     t.ws.fill_(-1e30)
     t.out.fill_(float("nan"))
     assert np.array_equal(raw_bits(t.run()), first)
+
+
+def test_parts_of_many_ragged_sequences_have_room():
+    """Contexts of all lengths over several turns of the chip: whole tiles and parts side by side, in a workspace that has room for few of them."""
+    rng = np.random.default_rng(17)
+    for seqs, hkv, longest in ((40, 8, 3000), (63, 8, 9000), (150, 8, 4000), (90, 2, 20000)):
+        ctx = (longest * rng.random(seqs) ** 3).astype(int)
+        t = Tree("bf16", ctx, rng.integers(1, 12, seqs).tolist(), 1, 2 * hkv, hkv, 64, 16, seed=18)
+        need = ab.alora_tree_attention_workspace_bytes(t.dims, 1) // 4
+        t.ws[need:] = 7.0
+        t.run()
+        assert (t.ws[need:] == 7.0).all()
+        t.check()
 
 
 def test_peaked_scores_and_scale():
