@@ -3,7 +3,8 @@
  * the largest scores, and attention over those blocks alone (C ABI of libalora_qkv.so, gfx950).  A step of a layer calls, behind the projection,
  * alora_block_bounds for the rows it wrote, alora_block_select and alora_selected_attention.
  *
- * Conventions and limits are those of alora_qkv.h and alora_attention.h.  All pointers are DEVICE pointers.
+ * Conventions and limits are those of alora_qkv.h and alora_attention.h.  All pointers are DEVICE pointers.  block_tables may be NULL where n_seqs or
+ * max_blocks is 0.
  */
 #ifndef ALORA_SELECT_H
 #define ALORA_SELECT_H

@@ -42,6 +42,7 @@ int alora_tree_rows(const int32_t *tree_parents, const int32_t *row_offsets, con
  *
  * K_j, V_j, g(h) and scale as in alora_attention.h; any mask may be given, not only that of a tree.  A row that sees nothing, and a row of no sequence, gets zeros; a place whose
  * table entry is outside the cache is left out of the softmax.
+ *   block_tables, context_lens may be NULL where n_seqs is 0, and block_tables where max_blocks is
  *   row_offsets [n_seqs + 1] ascending, tree_mask uint64 [n_tokens, mask_words], 8-byte aligned
  *   workspace   device, 16-byte aligned, >= alora_tree_attention_workspace_bytes() bytes, contents on entry irrelevant; calls that share it must be
  *               stream-ordered.  ALORA_EWORKSPACE otherwise.

@@ -571,6 +571,9 @@ __device__ __forceinline__ void combine_parts(const ListArgs &a, size_t first, s
     else *(f32x4 *)((float *)a.out + out_at + d) = o;
 }
 
+// A table without entries may have no address.
+inline bool no_table(const alora_attn_dims *d, const int32_t *block_tables) { return !block_tables && d->n_seqs && d->max_blocks; }
+
 // dims -> what every reader of a list knows (dims checked)
 inline ListArgs list_args(const alora_attn_dims *d, const void *q, const void *kc, const void *vc, const int32_t *bt, void *out)
 {

@@ -695,7 +695,7 @@ int alora_block_select(const void *q, const int8_t *bounds, const float *scales,
     if (dims->n_tokens == 0) return ALORA_OK;
     const size_t need = select_bytes(dims);
     if (need && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < need)) return ALORA_EWORKSPACE;
-    if (!q || !bounds || !scales || !block_tables || !token_seq_ids || !token_positions || !selected) return ALORA_EINVAL;
+    if (!q || !bounds || !scales || no_table(dims, block_tables) || !token_seq_ids || !token_positions || !selected) return ALORA_EINVAL;
     if (((uintptr_t)q | (uintptr_t)bounds) & 15) return ALORA_EINVAL;
     if (((uintptr_t)scales | (uintptr_t)block_tables | (uintptr_t)token_seq_ids | (uintptr_t)token_positions | (uintptr_t)selected) & 3) return ALORA_EINVAL;
     SelectArgs a;
@@ -757,7 +757,7 @@ int alora_selected_attention(const void *q, const void *k_cache, const void *v_c
     const ListPlan plan = plan_lists(dims, budget);
     const size_t need = selected_bytes(dims, plan);
     if (need && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < need)) return ALORA_EWORKSPACE;
-    if (!q || !k_cache || !v_cache || !block_tables || !token_seq_ids || !token_positions || !selected || !out) return ALORA_EINVAL;
+    if (!q || !k_cache || !v_cache || no_table(dims, block_tables) || !token_seq_ids || !token_positions || !selected || !out) return ALORA_EINVAL;
     if (((uintptr_t)q | (uintptr_t)k_cache | (uintptr_t)v_cache | (uintptr_t)out) & 15) return ALORA_EINVAL;
     if (((uintptr_t)block_tables | (uintptr_t)token_seq_ids | (uintptr_t)token_positions | (uintptr_t)selected) & 3) return ALORA_EINVAL;
     SelectedArgs a;

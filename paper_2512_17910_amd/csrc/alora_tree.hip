@@ -447,7 +447,7 @@ int alora_tree_attention(const void *q, const void *k_cache, const void *v_cache
     if (dims->n_tokens == 0) return ALORA_OK;
     const TreePlan p = plan_tree(dims);
     if (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < p.bytes) return ALORA_EWORKSPACE;
-    if (!q || !k_cache || !v_cache || !block_tables || !row_offsets || !context_lens || !tree_mask || !out) return ALORA_EINVAL;
+    if (!q || !k_cache || !v_cache || no_table(dims, block_tables) || !row_offsets || (dims->n_seqs && !context_lens) || !tree_mask || !out) return ALORA_EINVAL;
     if (((uintptr_t)q | (uintptr_t)k_cache | (uintptr_t)v_cache | (uintptr_t)out) & 15 || (uintptr_t)tree_mask & 7) return ALORA_EINVAL;
     if (((uintptr_t)block_tables | (uintptr_t)row_offsets | (uintptr_t)context_lens) & 3) return ALORA_EINVAL;
     TreeArgs a;

@@ -622,6 +622,34 @@ def test_caches_and_bounds_past_4_gib(dtype):
     assert torch.equal(t.out, near) and torch.isfinite(near).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("seqs,columns", [(0, 4), (3, 0), (70, 0)])
+def test_rows_without_sequences_or_tables(dtype, seqs, columns):
+    """A batch padded to its size of which nothing is left, and sequences whose table has no room: zeros, no blocks."""
+    dt, n = DT[dtype], 130
+    q, kv = torch.ones((n, 512), device="cuda").to(dt), torch.full((32, 128), float("nan"), device="cuda").to(dt)
+    bt = torch.zeros((seqs, columns), dtype=torch.int32, device="cuda")
+    dims = ab.make_attn_dims(q, kv, bt, 8, 2, 64, 16)
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    off = i32(np.linspace(0, n if seqs else 0, seqs + 1).astype(int))
+    ctx, mask, pos = i32([5] * seqs), torch.full((n, 1), -1, dtype=torch.int64, device="cuda"), i32([-9] * n)
+    ws = torch.empty((ab.alora_tree_attention_workspace_bytes(dims, 1) + 16,), dtype=torch.uint8, device="cuda")
+    out = torch.full_like(q, float("nan"))
+    ab.alora_tree_attention(q, kv, kv, bt, off, ctx, mask, out, dims, ws)
+    assert not out.any()
+    ab.alora_tree_rows(i32([-1] * n), off, ctx, mask, pos)
+    assert bool(mask.any()) == bool(seqs) and pos.tolist() == [5 if seqs else 0] * n
+    seq, at = torch.arange(n, device="cuda").int() % max(1, seqs), i32([3] * n)
+    b, s = torch.zeros((2, 2, 2, 64), dtype=torch.int8, device="cuda"), torch.zeros((2, 2), device="cuda")
+    sel = torch.full((n, 2, 3), 7, dtype=torch.int32, device="cuda")
+    ab.alora_block_select(q, b, s, bt, seq, at, sel, 1, 1, dims, None)
+    assert (sel == -1).all()
+    out.fill_(float("nan"))
+    more = torch.empty((ab.alora_selected_attention_workspace_bytes(dims, 3) + 16,), dtype=torch.uint8, device="cuda")
+    ab.alora_selected_attention(q, kv, kv, bt, seq, at, torch.zeros_like(sel), out, dims, more)
+    assert not out.any()
+
+
 # ---- streams, graphs ------------------------------------------------------------------------------
 def test_another_stream_and_a_replayed_graph():
     """Tree and selection recorded once and replayed over changed data, with eager calls between the replays; two graphs, each with its workspace."""
