@@ -733,6 +733,16 @@ def _check_tensors(tensors) -> None:
         _refuse_host(**{tensors[0][0]: tensors[0][1]})
 
 
+def _check_workspace(workspace) -> None:
+    """(Of the call's tensors, which are on the current device.)"""
+    if workspace is None:
+        return
+    if not workspace.is_cuda:
+        _refuse_host(workspace=workspace)
+    if workspace.get_device() != _current_device() or not workspace.is_contiguous():
+        raise ValueError("workspace: dense memory on the current device expected")
+
+
 def _device_now() -> int:
     """The current device, -1 without any."""
     import torch
@@ -768,9 +778,9 @@ def alora_step_rows(lengths, change, kept_blocks, seq_adapters, block_tables, po
     _check_tensors((("lengths", lengths, i32, n), ("change", change, i32, n), ("block_tables", block_tables, i32, n * dims.max_blocks),
                     ("pool", pool, i32, dims.pool_cap), ("state", state, i32, 6), ("lengths_out", lengths_out, i32, n), ("state_out", state_out, i32, 6),
                     ("row_offsets", row_offsets, i32, n + 1), ("token_seq_ids", token_seq_ids, i32, rows), ("token_positions", token_positions, i32, rows),
-                    ("token_adapter_ids", token_adapter_ids, i32, rows), ("slot_mapping", slot_mapping, i64, rows)))
-    if kept_blocks is not None or seq_adapters is not None:
-        _check_tensors([(name, t, i32, n) for name, t in (("kept_blocks", kept_blocks), ("seq_adapters", seq_adapters)) if t is not None])
+                    ("token_adapter_ids", token_adapter_ids, i32, rows), ("slot_mapping", slot_mapping, i64, rows),
+                    ("kept_blocks", lengths if kept_blocks is None else kept_blocks, i32, n),
+                    ("seq_adapters", lengths if seq_adapters is None else seq_adapters, i32, n)))
     s = (_lib or lib()).alora_step_rows(lengths.data_ptr(), change.data_ptr(), _ptr(kept_blocks), _ptr(seq_adapters), block_tables.data_ptr(), pool.data_ptr(),
                                         state.data_ptr(), lengths_out.data_ptr(), state_out.data_ptr(), row_offsets.data_ptr(), token_seq_ids.data_ptr(),
                                         token_positions.data_ptr(), token_adapter_ids.data_ptr(), slot_mapping.data_ptr(), dims, _stream_handle(stream))
@@ -806,8 +816,7 @@ def alora_tree_attention(q, k_cache, v_cache, block_tables, row_offsets, context
     words = tree_mask.shape[-1]
     _check_tensors((*shared, ("row_offsets", row_offsets, i32, dims.n_seqs + 1), ("context_lens", context_lens, i32, dims.n_seqs),
                     ("tree_mask", tree_mask, i64, dims.n_tokens * words)))
-    if workspace is not None and not workspace.is_cuda:
-        _refuse_host(workspace=workspace)
+    _check_workspace(workspace)
     s = (_lib or lib()).alora_tree_attention(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_tables.data_ptr(), row_offsets.data_ptr(),
                                              context_lens.data_ptr(), tree_mask.data_ptr(), words, out.data_ptr(), dims, _ptr(workspace), _bytes(workspace),
                                              _stream_handle(stream))
@@ -860,8 +869,7 @@ def alora_block_select(q, bounds, scales, block_tables, token_seq_ids, token_pos
                     ("scales", scales, by_code[ALORA_F32], heads), ("block_tables", block_tables, i32, dims.n_seqs * dims.max_blocks),
                     ("token_seq_ids", token_seq_ids, i32, -t), ("token_positions", token_positions, i32, -t),
                     ("selected", selected, i32, t * dims.n_kv_heads * budget)))
-    if workspace is not None and not workspace.is_cuda:
-        _refuse_host(workspace=workspace)
+    _check_workspace(workspace)
     s = (_lib or lib()).alora_block_select(q.data_ptr(), bounds.data_ptr(), scales.data_ptr(), block_tables.data_ptr(), token_seq_ids.data_ptr(),
                                            token_positions.data_ptr(), selected.data_ptr(), budget, n_first, n_recent, dims, _ptr(workspace), _bytes(workspace),
                                            _stream_handle(stream))
@@ -884,8 +892,7 @@ def alora_selected_attention(q, k_cache, v_cache, block_tables, token_seq_ids, t
     i32, t, budget = _types[1], dims.n_tokens, selected.shape[-1]
     _check_tensors((*shared, ("token_seq_ids", token_seq_ids, i32, -t), ("token_positions", token_positions, i32, -t),
                     ("selected", selected, i32, t * dims.n_kv_heads * budget)))
-    if workspace is not None and not workspace.is_cuda:
-        _refuse_host(workspace=workspace)
+    _check_workspace(workspace)
     s = (_lib or lib()).alora_selected_attention(q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), block_tables.data_ptr(), token_seq_ids.data_ptr(),
                                                  token_positions.data_ptr(), selected.data_ptr(), budget, out.data_ptr(), dims, _ptr(workspace),
                                                  _bytes(workspace), _stream_handle(stream))

@@ -140,7 +140,7 @@ def test_binding_refuses_what_it_would_misread():
     for at, name in enumerate(("lengths", "change", "kept_blocks", "seq_adapters", "block_tables", "pool", "state", "lengths_out", "state_out", "row_offsets",
                                "token_seq_ids", "token_positions", "token_adapter_ids", "slot_mapping")):
         for bad in (args[at].float(), torch.cat([args[at]] * 2)):
-            with pytest.raises((TypeError, ValueError), match="on the GPU" if name in ("kept_blocks", "seq_adapters") else name):
+            with pytest.raises((TypeError, ValueError), match=name):
                 ab.alora_step_rows(*args[:at], bad, *args[at + 1:], dims)
     q, kv, bt = torch.zeros(5, 512), torch.zeros(64, 128), i(2, 4)
     attn = ab.make_attn_dims(q, kv, bt, 8, 2, 64, 16)

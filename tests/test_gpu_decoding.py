@@ -650,6 +650,18 @@ def test_rows_without_sequences_or_tables(dtype, seqs, columns):
     assert not out.any()
 
 
+def test_workspaces_that_are_not_dense_are_refused():
+    t, s = Tree("f32", [50], [3], 1, 2, 1, 64, 16), Select("f32", [900], 2, 1, 64, 1)
+    for bad in (torch.empty((1,), device="cuda").expand(1 << 28), torch.empty((1 << 23,), device="cuda")[::2]):
+        with pytest.raises(ValueError, match="workspace"):
+            ab.alora_tree_attention(t.q, t.cache.k, t.cache.v, t.bt, *t.dev, t.out, t.dims, bad)
+        sel = torch.zeros((1, 1, 9), dtype=torch.int32, device="cuda")
+        with pytest.raises(ValueError, match="workspace"):
+            ab.alora_block_select(s.q, s.b, s.s, s.bt, *s.dev, sel, 1, 1, s.dims, bad)
+        with pytest.raises(ValueError, match="workspace"):
+            ab.alora_selected_attention(s.q, s.cache.k, s.cache.v, s.bt, *s.dev, sel, torch.empty_like(s.q), s.dims, bad)
+
+
 # ---- streams, graphs ------------------------------------------------------------------------------
 def test_another_stream_and_a_replayed_graph():
     """Tree and selection recorded once and replayed over changed data, with eager calls between the replays; two graphs, each with its workspace."""
