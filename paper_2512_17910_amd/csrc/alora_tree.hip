@@ -35,7 +35,6 @@ struct TreeArgs {
 };
 
 constexpr int UNIT = 32;        // positions that parts are counted in
-constexpr int GOOD_UNITS = 12;  // from which two workgroups to a compute unit are worth their parts
 
 constexpr int ALONE = 64;       // sequences up to which every wavefront finds its item by itself
 constexpr int CLASSES = 4;      // of parts by their length
@@ -106,11 +105,13 @@ __device__ __forceinline__ int units_of_parts(const TreeArgs &a, CutScratch<NW> 
     float units = most;
     if (half >= 1.f) {
         // Few tiles: as many parts as fit the chip in one turn, or, of short contexts, half of it, a workgroup to each compute unit (a tile's last part may be
-        // short: one more for each).  us, 32/8 heads, 128, 256, 384, 512, 768 workgroups: 13 rows at 9000 positions 25.2, 21.1, 24.9, 24.8, 24.7, at 32000 59.7, 39.4,
+        // short: one more for each).  us, 32/8 heads, when every wavefront had columns of its own, 128, 256, 384, 512, 768 workgroups: 13 rows at 9000 positions 25.2, 21.1, 24.9, 24.8, 24.7, at 32000 59.7, 39.4,
         // 40.4, 37.9, 47.6, 4 x 13 rows at 16000 106, 63.5, 62.5, 53.7, 68.6; 64/8 heads, 64 rows at 64000 387, 212, 209, 181, 204.
-        units = over(total, room);
-        if (units < (float)GOOD_UNITS) units = over(total, half);
-        units = fmaxf(fminf(ceilf(units), most), (float)a.least_units);
+        // Two workgroups on a compute unit take 1.8 times as long for a position as one by itself, and leave four units' worth of parts more.  us, half | one turn: 13 rows at 14000
+        // 21.5 | 23.6, at 20000 25.7 | 28.0, at 32000 35.5 | 35.5, 8 x 8 rows at 3000 30.8 | 26.2, 16 x 8 at 1000 27.3 | 22.6.
+        auto units_for = [&](float n) { return fmaxf(fminf(ceilf(over(total, n)), most), (float)a.least_units); };
+        const float two = units_for(room), one = units_for(half);
+        units = one < 1.8f * two + 4.f ? one : two;
     } else {
         // Many: the best of whole tiles, an equal share for every place of the chip or two thirds of it, as many parts as fit in one turn or in two.
         float cut[CUTS] = {most, share, share * (2.f / 3), over(total, room), over(total, 2.f * places - tiles)};
