@@ -466,13 +466,15 @@ int alora_tree_attention(const void *q, const void *k_cache, const void *v_cache
     // About 8192 workgroups combine parts: most tiles of a call with many have none (32 for each tile: 1000 sequences 72 us for nothing, now 5).  us, 2048, 8192, 32768
     // workgroups: 64 x 4 rows at 300 positions 24.2, 25.7, 28.1, 16 x 8 at 4000 56.7, 56.9, 56.6; 48 ragged sequences of up to 64 rows 547, 525, 521.
     const int clearing = std::min(MOST_CLEARING, 1 + dims->n_tokens / 64);
-    const dim3 grid((unsigned)((p.items + clearing) * dims->n_kv_heads)), merge((unsigned)(p.tiles * dims->n_kv_heads), (unsigned)std::clamp(8192 / (p.tiles * dims->n_kv_heads), 1ll, p.columns / 4ll));
+    // (no tiles: fewer rows than one holds, and no sequence they could be of)
+    const long long merging = p.tiles * dims->n_kv_heads;
+    const dim3 grid((unsigned)((p.items + clearing) * dims->n_kv_heads)), merge((unsigned)merging, (unsigned)std::clamp(8192 / std::max(1ll, merging), 1ll, p.columns / 4ll));
     const auto go = [&](auto kernel, auto combine) {
         // (us, 256 | 1024 threads: 65 sequences of 300 positions 33.6 | 36.5, 256 of 1000 197 | 199, 1000 of 300 294 | 291, 3000 of 200 626 | 613)
         if (dims->n_seqs > 512) launch_kernel(tree_plan_kernel<1024>, dim3(1), dim3(1024), 0, (hipStream_t)hip_stream, a);
         else if (dims->n_seqs > ALONE) launch_kernel(tree_plan_kernel<256>, dim3(1), dim3(256), 0, (hipStream_t)hip_stream, a);
         launch_kernel(kernel, grid, dim3(64 * WAVES), 0, (hipStream_t)hip_stream, a);
-        launch_kernel(combine, merge, dim3(256), 0, (hipStream_t)hip_stream, a, p.columns);
+        if (merging) launch_kernel(combine, merge, dim3(256), 0, (hipStream_t)hip_stream, a, p.columns);
     };
     // Non-temporal copies where a sequence brings one tile on average: then its context is read once.  us, ordinary | non-temporal, 32/8 heads: 13 rows at 9000
     // positions 21.5 | 19.7, at 128000 118 | 102, 64 x 8 rows at 8192 385 | 350, 64 x 24 400 | 385, 64 x 32 430 | 427, 64 x 40 (two tiles) 702 | 739; one context of
