@@ -204,13 +204,18 @@ template <> struct FloatsOf<4> { typedef f32x4 type; };
 __device__ __forceinline__ f32x16 multiply(bf16x8 x, bf16x8 y, f32x16 z) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, z, 0, 0, 0); }
 __device__ __forceinline__ f32x4 multiply(bf16x8 x, bf16x8 y, f32x4 z) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, z, 0, 0, 0); }
 
+// A weight w in two bf16 numbers: its upper half, and the rest of SPLIT * w, rounded.  Both are above zero wherever w is (the rest is 2^-9 w at least), so that an infinite
+// value makes an infinity of either product; rounded to the nearest, or of w itself, the rest would be zero or below it half of the time, and the sum no number.  The factor
+// is every weight's and the sum's.  What is lost: half a step (2^-8) of a rest below (2^-7 + 2^-9) w, 1.25 * 2^-15 of w.
+constexpr float SPLIT = 1.f + 0x1p-9f;
+
 //   columns        of the workgroup that exist; a wavefront beyond them only copies
 //   share          (SHARE, two tiles a step) true, of columns for half of the wavefronts at most: the second half has the first half's, and takes every other tile
 //   masked_from    places from here on are seen by some columns only: seen(place) = 32 bits of this lane's column, place a multiple of 32 from lo on
 //   q_at, out_at   element of q and out where this lane's column begins (column COLS * wavefront + lane % COLS)
 //   part           < 0: rows of out; else number of the part whose sums are left, of room for part_columns columns
 // WHOLE: the weights go into the product with V as two bf16 numbers (their rounding then adds nothing to that of the result), for twice
-// the products.  ONCE: rows are not read again soon (non-temporal copies).
+// the products (see SPLIT).  ONCE: rows are not read again soon (non-temporal copies).
 template <bool WHOLE, bool ONCE, bool SHARE, class L, class SlotOf, class Seen>
 __device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, L &lds, int lo, int hi, int masked_from, int columns, bool may_share, SlotOf slot_of,
                                                  Seen seen, size_t q_at, size_t out_at, long long part, int part_columns)
@@ -366,8 +371,13 @@ __device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, L &l
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float x = sc[8 * s + 2 * i], y = sc[8 * s + 2 * i + 1];
-                pv[s][i] = pack_bf16(x, y);
-                if (WHOLE) pr[s][i] = pack_bf16(x - __uint_as_float(pv[s][i] << 16), y - __uint_as_float(pv[s][i] & 0xffff0000u));
+                if constexpr (WHOLE) {
+                    const uint32_t ux = __float_as_uint(x), uy = __float_as_uint(y);
+                    pv[s][i] = __builtin_amdgcn_perm(uy, ux, 0x07060302);
+                    pr[s][i] = pack_bf16(fmaf(x, SPLIT, -__uint_as_float(ux & 0xffff0000u)), fmaf(y, SPLIT, -__uint_as_float(uy & 0xffff0000u)));
+                } else {
+                    pv[s][i] = pack_bf16(x, y);
+                }
             }
         __builtin_amdgcn_s_setprio(0);
         if (some) {
@@ -458,6 +468,7 @@ __device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, L &l
         if (LG == 4) l += __shfl_xor(l, 16);
         both_halves(l, x, y);
         l = x + y;
+        if (WHOLE) l *= SPLIT;
     }
     if (share) {
         // the second half's sums go to the first half, in a fixed order
