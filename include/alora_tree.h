@@ -49,8 +49,8 @@ int alora_tree_rows(const int32_t *tree_parents, const int32_t *row_offsets, con
  * The contexts are cut into parts of equal length, which a second kernel combines in a fixed order: results do not depend on timing, but a
  * row's low bits depend on the lengths of all sequences of the call.
  * Limits as in alora_attention.h; mask_words in 1 .. ALORA_MAX_TREE_WORDS, n_seqs <= 2^20, max_blocks * block_size <= 2^30, and fewer than 2^24 workgroups: each
- * K/V head takes one for every tile of rows (128 columns in bf16, 8 in fp32 at most, n_q_heads / n_kv_heads to a row) and a few hundred (ALORA_ESHAPE).  bf16 runs on matrix instructions (weights
- * of the softmax are rounded to bf16 for the weighted sum of V; scores, maxima and sums stay fp32).
+ * K/V head takes one for every tile of rows (128 columns in bf16, 8 in fp32 at most, n_q_heads / n_kv_heads to a row) and a few hundred (ALORA_ESHAPE).  bf16 runs on matrix instructions (a
+ * weight of the softmax is two bf16 numbers in the weighted sum of V, off by 2^-14 of itself at most; scores, maxima and sums stay fp32).
  */
 int alora_tree_attention_workspace_bytes(const alora_attn_dims *dims, int32_t mask_words, size_t *out_bytes);
 int alora_tree_attention(const void *q, const void *k_cache, const void *v_cache, const int32_t *block_tables, const int32_t *row_offsets,

@@ -214,9 +214,9 @@ constexpr float SPLIT = 1.f + 0x1p-9f;
 //   masked_from    places from here on are seen by some columns only: seen(place) = 32 bits of this lane's column, place a multiple of 32 from lo on
 //   q_at, out_at   element of q and out where this lane's column begins (column COLS * wavefront + lane % COLS)
 //   part           < 0: rows of out; else number of the part whose sums are left, of room for part_columns columns
-// WHOLE: the weights go into the product with V as two bf16 numbers (their rounding then adds nothing to that of the result), for twice
-// the products (see SPLIT).  ONCE: rows are not read again soon (non-temporal copies).
-template <bool WHOLE, bool ONCE, bool SHARE, class L, class SlotOf, class Seen>
+// The weights go into the product with V as two bf16 numbers (see SPLIT): their rounding adds nothing to that of the result.  ONCE: rows are not read again
+// soon (non-temporal copies).
+template <bool ONCE, bool SHARE, class L, class SlotOf, class Seen>
 __device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, L &lds, int lo, int hi, int masked_from, int columns, bool may_share, SlotOf slot_of,
                                                  Seen seen, size_t q_at, size_t out_at, long long part, int part_columns)
 {
@@ -371,13 +371,9 @@ __device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, L &l
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float x = sc[8 * s + 2 * i], y = sc[8 * s + 2 * i + 1];
-                if constexpr (WHOLE) {
-                    const uint32_t ux = __float_as_uint(x), uy = __float_as_uint(y);
-                    pv[s][i] = __builtin_amdgcn_perm(uy, ux, 0x07060302);
-                    pr[s][i] = pack_bf16(fmaf(x, SPLIT, -__uint_as_float(ux & 0xffff0000u)), fmaf(y, SPLIT, -__uint_as_float(uy & 0xffff0000u)));
-                } else {
-                    pv[s][i] = pack_bf16(x, y);
-                }
+                const uint32_t ux = __float_as_uint(x), uy = __float_as_uint(y);
+                pv[s][i] = __builtin_amdgcn_perm(uy, ux, 0x07060302);
+                pr[s][i] = pack_bf16(fmaf(x, SPLIT, -__uint_as_float(ux & 0xffff0000u)), fmaf(y, SPLIT, -__uint_as_float(uy & 0xffff0000u)));
             }
         __builtin_amdgcn_s_setprio(0);
         if (some) {
@@ -427,7 +423,7 @@ __device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, L &l
 #pragma unroll
             for (int t = 0; t < DT; ++t) {
                 acc[t] = multiply(vf[s][t], __builtin_bit_cast(bf16x8, pv[s]), acc[t]);
-                if (WHOLE) acc[t] = multiply(vf[s][t], __builtin_bit_cast(bf16x8, pr[s]), acc[t]);
+                acc[t] = multiply(vf[s][t], __builtin_bit_cast(bf16x8, pr[s]), acc[t]);
             }
     };
     // ---- the list, STEP tiles at a time -------------------------------------------------------------
@@ -467,8 +463,7 @@ __device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, L &l
         float x, y;
         if (LG == 4) l += __shfl_xor(l, 16);
         both_halves(l, x, y);
-        l = x + y;
-        if (WHOLE) l *= SPLIT;
+        l = (x + y) * SPLIT;
     }
     if (share) {
         // the second half's sums go to the first half, in a fixed order

@@ -582,7 +582,7 @@ __global__ __launch_bounds__(256, 2) void selected_matrix_kernel(SelectedArgs a)
     const SelectedItem it = selected_item(a, scratch);
     const int columns = 1 << g.lg_g, col = min((int)threadIdx.x & 15, columns - 1);
     const size_t at = ((size_t)it.t * g.Hq + ((size_t)it.hk << g.lg_g) + col) * D;
-    read_list_matrix<true, ONCE, false>(
+    read_list_matrix<ONCE, false>(
         g, it.hk, lds, it.lo, it.hi, 0x7fffffff, columns, false,
         [&](int v) { return selected_slot(g, it, v); },
         [&](int) { return 0xffffffffu; },

@@ -341,10 +341,10 @@ __global__ __launch_bounds__(256) void tree_vector_kernel(TreeArgs a)
 }
 
 // 32 columns a wavefront: 128 >> lg_g rows of a sequence.  What bounds it: with wide trees matrix and vector unit in turn (48 sequences of up to 64 drafts over up to 16000
-// positions, 64 / 8 heads, 318 GFLOP: 505 us, 0.63 PFLOP/s of products that count and 0.75 of those made; the matrix unit is busy for 30 % of the cycles, the
-// vector unit for 47), with many narrow ones memory (64 x 8 rows over 8192, 2.1 GB: 351 us, 6.1 TB/s), with one latency (13 rows over 9001, 15.0 us: to find its
-// part 1.9, slots 1.2, first tiles 1.5, the rest two tiles at a time).  The weights are rounded once to bf16 for the product with V: twice the products, as for
-// selected blocks, cost 3 to 9 %.
+// positions, 64 / 8 heads, 318 GFLOP: 633 us with the parts combined, 0.50 PFLOP/s of products that count; 64 x 64 rows over 8192, 32 / 8 heads, whose tiles are full, 956 us, 0.58 of 0.87 made), with many narrow ones memory (64 x 8 rows over 8192, 2.1 GB: 351 us, 6.1 TB/s), with one latency (13 rows over 9001, 15.0 us: to find its
+// part 1.9, slots 1.2, first tiles 1.5, the rest two tiles at a time).  The weights are whole, as for selected blocks: the error against 64 bits is that of the result's rounding.
+// Rounded once to bf16, with two thirds of the products, they cost as much again as that rounding; us, rounded once | whole: 13 rows at 9000 positions 16.4 | 16.8, 64 x 8 rows
+// at 8192 347 | 345, 64 x 16 349 | 360, 64 x 24 390 | 468, 64 x 64 779 | 956.  (The rest's products behind or between the others', placed by hand: within 1 %.)
 constexpr int WAVES = 4;
 template <int D, bool ONCE, bool SHARE>
 __global__ __launch_bounds__(64 * WAVES, 2) void tree_matrix_kernel(TreeArgs a)
@@ -361,7 +361,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_matrix_kernel(TreeArgs a)
     const int col = 32 * (((int)threadIdx.x >> 6) & (share ? WAVES / 2 - 1 : WAVES - 1)) + ((int)threadIdx.x & 31), row = it.row0 + (min(col, columns - 1) >> g.lg_g);
     const uint32_t *bits = a.mask + (size_t)row * 2 * a.words;
     const size_t at = ((size_t)row * g.Hq + ((size_t)hk << g.lg_g) + (col & ((1 << g.lg_g) - 1))) * D;
-    read_list_matrix<false, ONCE, SHARE>(
+    read_list_matrix<ONCE, SHARE>(
         g, hk, lds, it.lo, it.hi, it.ctx, columns, share,
         [&](int v) { return slot_at(g, bt, v / g.bs, v % g.bs); },
         [&](int place) {               // the row's bits of drafts place - ctx .. + 31; what lies in front of them is seen

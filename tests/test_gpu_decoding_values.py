@@ -28,6 +28,17 @@ def whole(got, q, k, v, hq, hkv, d, dt, attention):
     assert np.all(over <= 0), (float(over.max()), np.unravel_index(int(np.argmax(over)), over.shape))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("group", [1, 4, 8])
+@pytest.mark.parametrize("ctx,n", [([0, 33, 270, 1, 95, 600], [7, 1, 40, 0, 64, 3]), ([5000, 20], [13, 2])], ids=["ragged", "parts"])
+def test_weights_of_trees(dtype, d, group, ctx, n):
+    t = Tree(dtype, ctx, n, 1, 2 * group, 2, d, 16, seed=d + group)
+    t.run()
+    q, k, v = to_f64(t.q), to_f64(t.cache.k), to_f64(t.cache.v)
+    whole(t.out, q, k, v, 2 * group, 2, d, t.dt, lambda v: od.tree_attention(q, k, v, t.cache.tables, t.off, t.ctx, t.mask, 16, 2 * group, 2, d))
+
+
 def every_block(t, budget):
     """Lists of all blocks of the rows' contexts."""
     lists = np.full((len(t.pos), t.sizes[1], budget), -1, np.int32)
@@ -113,3 +124,25 @@ def test_infinite_values_of_small_weight(dtype, score):
     t.cache.k[slot] = score / d ** 0.5
     lists = every_block(t, 20)
     spoilt(lambda: attend(t, lists), t.cache.v, [(0, slot, 0, 9, INF), (0, slot, 1, 100, -INF)], 2, 2, d, lambda r, s: True)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("hq", [2, 8, 16])                             # (with two, wavefronts share the columns of the narrow trees)
+def test_values_of_trees_that_are_not_finite(dtype, d, hq):
+    """In drafts that some rows see, in the context's places beside them, and further forward; keys are finite."""
+    ctx, n = [70, 9000, 31, 0], [41, 13, 64, 3]
+    for few in (False, True):
+        t = Tree(dtype, ctx[:2] if few else ctx, n[:2] if few else n, 1, hq, 2, d, 16, seed=hq + d)
+        t.run()
+        t.check()
+        at = [(0, 70, 0, 3, INF), (0, 75, 1, 60, -INF), (0, 80, 1, 60, INF), (0, 97, 0, 33, NAN), (0, 110, 0, 34, INF), (0, 66, 1, 8, -INF), (0, 12, 1, 9, INF), (1, 9001, 0, 0, INF), (1, 9012, 0, 0, -INF),
+              (1, 9005, 1, 17, NAN), (1, 9010, 1, 31, -INF), (1, 4321, 1, 32, INF), (1, 8999, 0, 47, INF)]
+        if not few:
+            at += [(2, 31, 0, 5, INF), (2, 40, 1, 6, INF), (2, 63, 1, 24, -INF), (2, 64, 1, 25, NAN), (2, 94, 0, 26, INF), (2, 30, 0, 13, -INF), (3, 0, 1, 14, INF), (3, 2, 0, 15, NAN)]
+        places = {slot_of(t.cache, s, p): (s, p - ctx[s]) for s, p, *_ in at}
+
+        def sees(r, slot):
+            s, j = places[slot]
+            return t.off[s] <= r < t.off[s + 1] and (j < 0 or bool(int(t.mask[r, 0]) >> j & 1))
+        spoilt(t.run, t.cache.v, [(s, slot_of(t.cache, s, p), g, c, z) for s, p, g, c, z in at], hq, 2, d, sees)
