@@ -79,6 +79,7 @@ __device__ __forceinline__ void read_list_vector(const ListArgs &a, int hk, Vect
     };
     auto consume = [&](int j0, const Raw8<false> (&kr)[U], const Raw8<false> (&vr)[U], unsigned ok) {
         float s[U][C];
+        bool on[U][C];
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -87,7 +88,10 @@ __device__ __forceinline__ void read_list_vector(const ListArgs &a, int hk, Vect
         for (int u = 0; u < U; ++u) {
             const int j = j0 + u * PPI + jl;
 #pragma unroll
-            for (int c = 0; c < C; ++c) s[u][c] = (ok >> u & 1u) && (j < masked_from || seen(c, j)) ? s[u][c] * a.scale_log2e : NEG_INF;
+            for (int c = 0; c < C; ++c) {
+                on[u][c] = (ok >> u & 1u) && (j < masked_from || seen(c, j));
+                s[u][c] = on[u][c] ? s[u][c] * a.scale_log2e : NEG_INF;
+            }
         }
         float pw[U][C];
 #pragma unroll
@@ -115,7 +119,7 @@ __device__ __forceinline__ void read_list_vector(const ListArgs &a, int hk, Vect
 #pragma unroll
                 for (int c = 0; c < C; ++c)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) acc[c][e] = pw[u][c] == 0.f ? acc[c][e] : fmaf(pw[u][c], vf[e], acc[c][e]);
+                    for (int e = 0; e < 8; ++e) acc[c][e] = on[u][c] ? fmaf(pw[u][c], vf[e], acc[c][e]) : acc[c][e];
             } else {
 #pragma unroll
                 for (int c = 0; c < C; ++c)
@@ -340,8 +344,9 @@ __device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, L &l
         for (int v = 0; v < NV; ++v) sc[v] = st[v / NA][v % NA];
         const int place = lo + 32 * c;
         const bool some = place + 31 >= masked_from;
+        uint32_t on = ok;
         if (some || ok != 0xffffffffu) {
-            const uint32_t on = some ? ok & seen(place) : ok;
+            if (some) on &= seen(place);
 #pragma unroll
             for (int v = 0; v < NV; ++v) sc[v] = on >> (4 * LG * (v >> 2) + 4 * g + (v & 3)) & 1u ? sc[v] : NEG_INF;
         }
@@ -413,7 +418,7 @@ __device__ __forceinline__ void read_list_matrix(const ListArgs &a, int hk, L &l
                         for (int v = 0; v < NA; ++v) {
                             const uint32_t d = (uint32_t)(COLS * t + 4 * LG * (v >> 2) + 4 * g + (v & 3));
                             const float z = bf16_bits_to_f32(*(const __attribute__((address_space(3))) bf16_t *)(vb + i * PITCH + (((d >> 3) ^ L::v_turn(i)) << 4) + (d & 7) * 2));
-                            if (!(fabsf(z) <= 3.402823466e38f) && !(p == 0.f)) acc[t][v] += p * z;
+                            if (!(fabsf(z) <= 3.402823466e38f) && (on >> i & 1u)) acc[t][v] += p * z;      // (seen: however small the weight)
                         }
                 }
             }

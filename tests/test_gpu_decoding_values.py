@@ -146,3 +146,27 @@ def test_values_of_trees_that_are_not_finite(dtype, d, hq):
             s, j = places[slot]
             return t.off[s] <= r < t.off[s + 1] and (j < 0 or bool(int(t.mask[r, 0]) >> j & 1))
         spoilt(t.run, t.cache.v, [(s, slot_of(t.cache, s, p), g, c, z) for s, p, g, c, z in at], hq, 2, d, sees)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("hq", [2, 16])
+@pytest.mark.parametrize("place", [10, 68, 70, 75])
+@pytest.mark.parametrize("bad", [NAN, INF, -INF])
+def test_values_of_no_weight_that_are_not_finite(dtype, hq, place, bad):
+    """A place that is seen counts however small its weight (e^-339, which fp32 does not know): the component is not finite, wherever the place lies -- far in front of
+    the drafts, beside them, among them.  Rows that do not see it are as if it were not there."""
+    d, ctx = 128, 70
+    t = Tree(dtype, [ctx], [20], 1, hq, 2, d, 16, seed=6)
+    t.q.fill_(1.0)
+    t.cache.k.zero_()
+    slot = slot_of(t.cache, 0, place)
+    t.cache.k[slot] = -30.0
+    t.cache.v[slot, 40] = 0.0
+    want = to_f64(t.run()).reshape(20, hq, d)
+    t.cache.v[slot, 40] = bad
+    got = to_f64(t.run()).reshape(20, hq, d)
+    seen = np.array([place < ctx or bool(int(m) >> (place - ctx) & 1) for m in t.mask[:, 0]])
+    assert not np.isfinite(got[seen][:, : hq // 2, 40]).any() and (bad == bad or np.isnan(got[seen][:, : hq // 2, 40]).all())
+    got[seen, : hq // 2, 40] = want[seen, : hq // 2, 40]
+    assert np.array_equal(got, want)
+    assert seen.any() and (place < 75 or not seen.all())
