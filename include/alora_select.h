@@ -52,7 +52,7 @@ int alora_block_bounds(const void *k_cache, const int64_t *slot_mapping, int8_t 
  * n_first >= 0, n_recent >= 1, n_first + n_recent <= budget, budget <= 2^20 (ALORA_EINVAL otherwise).  Limits as in alora_attention.h, and
  * n_tokens * n_kv_heads < 2^22, n_kv_heads <= 2^16, max_blocks <= 2^28 (ALORA_ESHAPE).
  *   workspace device, 16-byte aligned, >= alora_block_select_workspace_bytes() bytes (0: may be NULL), contents on entry irrelevant; calls that share
- *             it must be stream-ordered.  ALORA_EWORKSPACE otherwise.
+ *             it must be stream-ordered.  ALORA_EWORKSPACE otherwise.  What that function gives is enough for every call of fewer rows too (the other dims alike).
  */
 int alora_block_select_workspace_bytes(const alora_attn_dims *dims, size_t *out_bytes);
 int alora_block_select(const void *q, const int8_t *bounds, const float *scales, const int32_t *block_tables, const int32_t *token_seq_ids,
@@ -63,7 +63,7 @@ int alora_block_select(const void *q, const int8_t *bounds, const float *scales,
  * alora_paged_attention over the positions 0 .. p of the blocks in `selected` alone (int32 [n_tokens, n_kv_heads, budget], any list of blocks
  * of the row's table in ascending order).  An entry outside the row's context, or not above the entry before it, is left out; a row with
  * nothing left gets zeros.  Limits as above, 1 <= budget <= 2^20 (ALORA_EINVAL), budget * block_size < 2^30 (ALORA_ESHAPE).
- *   workspace as above, alora_selected_attention_workspace_bytes(): with few rows the lists are cut into parts, combined in a fixed order.
+ *   workspace as above, alora_selected_attention_workspace_bytes() (for one budget): with few rows the lists are cut into parts, combined in a fixed order.
  */
 int alora_selected_attention_workspace_bytes(const alora_attn_dims *dims, int32_t budget, size_t *out_bytes);
 int alora_selected_attention(const void *q, const void *k_cache, const void *v_cache, const int32_t *block_tables, const int32_t *token_seq_ids,

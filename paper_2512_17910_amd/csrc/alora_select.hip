@@ -611,6 +611,14 @@ static int check_select(const alora_attn_dims *d)
 static bool two_kernels(const alora_attn_dims *d) { return d->max_blocks > MOST_IN_LDS || ((long long)d->n_tokens * d->n_kv_heads < 256 && d->max_blocks > 512); }
 static size_t key_stride(const alora_attn_dims *d) { return ((size_t)d->max_blocks + 3) / 4 * 4; }
 static size_t select_bytes(const alora_attn_dims *d) { return two_kernels(d) ? (size_t)d->n_tokens * d->n_kv_heads * key_stride(d) * sizeof(uint32_t) : 0; }
+// What a call needs is not what one of fewer rows does (those may be the ones that take two kernels, or read lists in parts): the largest need of a call of
+// up to so many rows, which is what the sizes' functions give.
+static size_t select_bytes_upto(const alora_attn_dims *d)
+{
+    alora_attn_dims few = *d;
+    few.n_tokens = std::min(d->n_tokens, 255 / d->n_kv_heads);      // (the most that take two kernels for their number)
+    return std::max(select_bytes(d), select_bytes(&few));
+}
 
 constexpr int MOST_BUDGET = 1 << 20;
 
@@ -635,6 +643,16 @@ static ListPlan plan_lists(const alora_attn_dims *d, int budget)
 static size_t in_parts(const alora_attn_dims *d, const ListPlan &p) { return ((size_t)d->n_tokens * d->n_kv_heads - p.whole) * p.parts * (d->n_q_heads / d->n_kv_heads); }
 static size_t selected_ml_bytes(const alora_attn_dims *d, const ListPlan &p) { return (in_parts(d, p) * 8 + 255) / 256 * 256; }
 static size_t selected_bytes(const alora_attn_dims *d, const ListPlan &p) { return p.parts > 1 ? selected_ml_bytes(d, p) + in_parts(d, p) * d->head_dim * 4 : 0; }
+static size_t selected_bytes_upto(const alora_attn_dims *d, int budget)
+{
+    alora_attn_dims x = *d;
+    size_t most = 0;
+    for (; x.n_tokens > 0 && x.n_tokens > d->n_tokens - 512; --x.n_tokens) {      // (the lists left over repeat after 512 rows at most)
+        most = std::max(most, selected_bytes(&x, plan_lists(&x, budget)));
+        if ((d->n_tokens - x.n_tokens + 1) * (d->n_kv_heads % 512) % 512 == 0) break;
+    }
+    return most;
+}
 
 }  // namespace alora
 
@@ -681,7 +699,7 @@ int alora_block_select_workspace_bytes(const alora_attn_dims *dims, size_t *out_
     if (!out_bytes) return ALORA_EINVAL;
     const int st = check_select(dims);
     if (st) return st;
-    *out_bytes = select_bytes(dims);
+    *out_bytes = select_bytes_upto(dims);
     return ALORA_OK;
 }
 
@@ -741,7 +759,7 @@ int alora_selected_attention_workspace_bytes(const alora_attn_dims *dims, int32_
     if (!out_bytes || budget < 1 || budget > MOST_BUDGET) return ALORA_EINVAL;
     const int st = check_select(dims);
     if (st) return st;
-    *out_bytes = selected_bytes(dims, plan_lists(dims, budget));
+    *out_bytes = selected_bytes_upto(dims, budget);
     return ALORA_OK;
 }
 
