@@ -26,6 +26,7 @@ struct TreeArgs {
     const int32_t *offsets, *context;
     const uint32_t *mask;       // [T][2 * words]
     int words, tile_rows;       // rows of a tile
+    int lg_unit;
     int places;                 // workgroups per K/V head that the chip holds at once
     int least_units;            // of a part
     int max_tiles, max_items, max_parts;      // the workspace has room for
@@ -34,7 +35,7 @@ struct TreeArgs {
     TreeItem *items;            // of more than ALONE sequences
 };
 
-constexpr int UNIT = 32;        // positions that parts are counted in
+constexpr int LG_UNIT = 5;      // parts are counted in units of 32 positions; of 64 where a table has more than 2^29, so that a sequence's are 2^24 at most, which floats count
 
 constexpr int ALONE = 64;       // sequences up to which every wavefront finds its item by itself
 constexpr int CLASSES = 4;      // of parts by their length
@@ -57,7 +58,7 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeArgs &a, int s)
         q.ctx = min(max(a.context[s], 0), cap);
         q.places = min(q.ctx + min(q.n, 64 * a.words), cap);
         q.tiles = (q.n + a.tile_rows - 1) / a.tile_rows;
-        q.units = (q.places + UNIT - 1) / UNIT;
+        q.units = (q.places + (1 << a.lg_unit) - 1) >> a.lg_unit;
     }
     return q;
 }
@@ -161,8 +162,8 @@ __device__ __forceinline__ TreeCut tree_cut(const TreeSeq &q, int per)
 __device__ __forceinline__ TreeItem tree_item(const TreeArgs &a, int s, const TreeSeq &q, const TreeCut &c, int part_at, int i)
 {
     const int part = i / q.tiles, tile = i - part * q.tiles;
-    const long long lo = (long long)part * c.size * UNIT;
-    return {q.r0 + tile * a.tile_rows, min(a.tile_rows, q.n - tile * a.tile_rows), s, q.ctx, q.places, (int)min(lo, (long long)q.places), (int)min(lo + (long long)c.size * UNIT, (long long)q.places), c.parts > 1 ? part_at + i : -1};
+    const long long lo = (long long)part * c.size << a.lg_unit, hi = lo + ((long long)c.size << a.lg_unit);
+    return {q.r0 + tile * a.tile_rows, min(a.tile_rows, q.n - tile * a.tile_rows), s, q.ctx, q.places, (int)min(lo, (long long)q.places), (int)min(hi, (long long)q.places), c.parts > 1 ? part_at + i : -1};
 }
 
 // Which tile and part workgroup `item` (of one K/V head) is for; false: none.
@@ -457,7 +458,7 @@ int alora_tree_attention(const void *q, const void *k_cache, const void *v_cache
     a.list.o = (float *)((char *)workspace + p.o_at);
     a.offsets = row_offsets; a.context = context_lens;
     a.mask = (const uint32_t *)tree_mask; a.words = mask_words;
-    a.tile_rows = p.tile_rows; a.places = p.places; a.least_units = p.matrix ? 8 : 4;      // (fp32, 5 trees over up to 700 positions, eight columns: 2 units 22.2 us, 4 20.7, 8 23.8)
+    a.tile_rows = p.tile_rows; a.lg_unit = LG_UNIT + ((long long)dims->max_blocks * dims->block_size > 1 << 29); a.places = p.places; a.least_units = p.matrix ? 8 : 4;      // (fp32, 5 trees over up to 700 positions, eight columns: 2 units 22.2 us, 4 20.7, 8 23.8)
     a.max_tiles = (int)p.tiles; a.max_items = (int)p.items; a.max_parts = (int)p.parts;
     a.found = (int *)workspace;
     a.tiles = (TreeTile *)((char *)workspace + p.tiles_at);
