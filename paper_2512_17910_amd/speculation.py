@@ -220,6 +220,7 @@ def run(layers=4, prompt=1000, dtype="bf16", block_size=16, answer=40, seqs=3, s
     x = m.emb[known]
     out = torch.empty((seqs, m.hq * m.d), dtype=m.dt, device="cuda")
     dims = ab.make_attn_dims(out, m.kc[0], d.tables, m.hq, m.hkv, m.d, block_size)
+    first_layer = []
 
     def over(budget):
         chosen = torch.empty((seqs, m.hkv, budget), dtype=torch.int32, device="cuda")
@@ -229,17 +230,22 @@ def run(layers=4, prompt=1000, dtype="bf16", block_size=16, answer=40, seqs=3, s
             ab.alora_block_bounds(kc, d.slot, *bounds[i], ab.make_bounds_dims(kc, d.slot, m.hkv, m.d, block_size))
             ab.alora_block_select(q, *bounds[i], d.tables, d.seq, d.pos, chosen, 1, 2, dims, ws)
             ab.alora_selected_attention(q, kc, vc, d.tables, d.seq, d.pos, chosen, out, dims, ws)
+            if i == 0:
+                first_layer.append(out.clone())
             return out
         return _layers(m, x, d, d.pos, attend)
 
-    def whole(q, kc, vc, _):
+    def whole(q, kc, vc, i):
         ab.alora_paged_attention(q, kc, vc, d.tables, d.seq, d.pos, out, dims)
+        if i == 0:
+            first_layer.append(out.clone())
         return out
     full = _layers(m, x, d, d.pos, whole)
     most = int(d.lengths.max()) // block_size + 1
     res["all_blocks_off"] = _off(over(most), full)
+    res["all_blocks_attention_off"] = _off(first_layer[1], first_layer[0])      # (of the same queries)
     res["some_blocks"], res["of_blocks"] = max(4, most // 4), most
-    res["some_blocks_off"] = _off(over(res["some_blocks"]), full)
+    res["some_blocks_finite"] = bool(torch.isfinite(over(res["some_blocks"])).all())
     p.close()
     return res
 
