@@ -79,7 +79,6 @@ __device__ __forceinline__ void read_list_vector(const ListArgs &a, int hk, Vect
     };
     auto consume = [&](int j0, const Raw8<false> (&kr)[U], const Raw8<false> (&vr)[U], unsigned ok) {
         float s[U][C];
-        bool on[U][C];
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -88,10 +87,7 @@ __device__ __forceinline__ void read_list_vector(const ListArgs &a, int hk, Vect
         for (int u = 0; u < U; ++u) {
             const int j = j0 + u * PPI + jl;
 #pragma unroll
-            for (int c = 0; c < C; ++c) {
-                on[u][c] = (ok >> u & 1u) && (j < masked_from || seen(c, j));
-                s[u][c] = on[u][c] ? s[u][c] * a.scale_log2e : NEG_INF;
-            }
+            for (int c = 0; c < C; ++c) s[u][c] = (ok >> u & 1u) && (j < masked_from || seen(c, j)) ? s[u][c] * a.scale_log2e : NEG_INF;
         }
         float pw[U][C];
 #pragma unroll
@@ -116,10 +112,13 @@ __device__ __forceinline__ void read_list_vector(const ListArgs &a, int hk, Vect
             float vf[8];
             vr[u].widen(vf);
             if (masked) {
+                const int j = j0 + u * PPI + jl;
 #pragma unroll
-                for (int c = 0; c < C; ++c)
+                for (int c = 0; c < C; ++c) {
+                    const bool on = (ok >> u & 1u) && (j < masked_from || seen(c, j));      // (worked out again: kept, it costs the other tiles 2 to 3 %)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) acc[c][e] = on[u][c] ? fmaf(pw[u][c], vf[e], acc[c][e]) : acc[c][e];
+                    for (int e = 0; e < 8; ++e) acc[c][e] = on ? fmaf(pw[u][c], vf[e], acc[c][e]) : acc[c][e];
+                }
             } else {
 #pragma unroll
                 for (int c = 0; c < C; ++c)
