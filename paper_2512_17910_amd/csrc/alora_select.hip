@@ -624,7 +624,8 @@ constexpr int MOST_BUDGET = 1 << 20;
 
 // Lists are read whole while they fill the chip (512 workgroups: two to a compute unit), the others, behind them, in parts: as many as are done first, by what
 // was measured: a turn of workgroups takes 4 us and 0.03 for every place, the second kernel 3, each part 0.1 more.  us, 4, 8, 16, 32 parts of 8 lists of 2048
-// places: 18.8, 13.4, 11.5, 11.4.
+// places: 18.8, 13.4, 11.5, 11.4.  (Of the fp32 kernel for groups of eight heads the chip holds one to a compute unit.  fp32, 200 rows of 1500 places, heads of 128, us, and K and V at
+// 4.9 TB/s: 16/4 heads 226 (250), 32/8 422 (500), 32/4 342 (250), 64/8 614 (500).)
 struct ListPlan {
     int whole, parts;      // lists that are read whole; parts of the others
 };

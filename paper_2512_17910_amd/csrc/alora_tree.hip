@@ -27,7 +27,7 @@ struct TreeArgs {
     const uint32_t *mask;       // [T][2 * words]
     int words, tile_rows;       // rows of a tile
     int lg_unit;
-    int places;                 // workgroups per K/V head that the chip holds at once
+    int places;                 // workgroups per K/V head that the chip holds at once, two to a compute unit (of the vector kernel's with eight columns one: their turns are two)
     int least_units;            // of a part
     int max_tiles, max_items, max_parts;      // the workspace has room for
     int *found;                 // tiles, items
@@ -342,7 +342,8 @@ __global__ __launch_bounds__(256) void tree_vector_kernel(TreeArgs a)
 }
 
 // 32 columns a wavefront: 128 >> lg_g rows of a sequence.  What bounds it: with wide trees matrix and vector unit in turn (48 sequences of up to 64 drafts over up to 16000
-// positions, 64 / 8 heads, 318 GFLOP: 633 us with the parts combined, 0.50 PFLOP/s of products that count; 64 x 64 rows over 8192, 32 / 8 heads, whose tiles are full, 956 us, 0.58 of 0.87 made), with many narrow ones memory (64 x 8 rows over 8192, 2.1 GB: 351 us, 6.1 TB/s), with one latency (13 rows over 9001, 15.0 us: to find its
+// positions, 64 / 8 heads, 318 GFLOP: 631 us with the parts combined, 0.50 PFLOP/s of products that count; the matrix unit is busy for 39 % of the cycles, the vector unit for 50; 64 x 64 rows over
+// 8192, 32 / 8 heads, whose tiles are full, 950 us, 0.57 of 0.86 made), with many narrow ones memory (64 x 8 rows over 8192, 2.1 GB: 346 us, 6.2 TB/s), with one latency (13 rows over 9001, 15.4 us: to find its
 // part 1.9, slots 1.2, first tiles 1.5, the rest two tiles at a time).  The weights are whole, as for selected blocks: the error against 64 bits is that of the result's rounding.
 // Rounded once to bf16, with two thirds of the products, they cost as much again as that rounding; us, rounded once | whole: 13 rows at 9000 positions 16.4 | 16.8, 64 x 8 rows
 // at 8192 347 | 345, 64 x 16 349 | 360, 64 x 24 390 | 468, 64 x 64 779 | 956.  (The rest's products behind or between the others', placed by hand: within 1 %.)
@@ -373,7 +374,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void tree_matrix_kernel(TreeArgs a)
         at, at, it.part >= 0 ? (long long)it.part * g.Hkv + hk : -1ll, 32 * WAVES);
 }
 
-// One wavefront per column of a tile that has parts, of a tile's with many tiles several.  Bound by the latency of tile, sums and store where there are few (5.1 us for 31 parts of one tile).
+// One wavefront per column of a tile that has parts, of a tile's with many tiles several.  Bound by the latency of tile, sums and store where there are few (4.5 us for 31 parts of one tile);
+// 48 sequences of up to 64 rows 32 us for 17 MB of sums, with waves that wait for 57 % of their time.
 template <int D, bool BF16, int AHEAD>
 __global__ __launch_bounds__(256) void tree_merge_kernel(TreeArgs a, int columns)
 {
@@ -400,7 +402,7 @@ static TreePlan plan_tree(const alora_attn_dims *d)
     TreePlan p;
     const int G = d->n_q_heads / d->n_kv_heads;
     p.matrix = d->dtype == ALORA_BF16;
-    p.columns = p.matrix ? 32 * WAVES : std::max(4, G);      // (fp32, 2, 4, 8 columns, us: 30 rows at 4000 positions, 4 sequences, 72, 61, 109, 16 at 8000, 8 sequences 258, 204, 425)
+    p.columns = p.matrix ? 32 * WAVES : std::max(4, G);      // (fp32, heads of 128, 2, 4, 8 columns, us: 30 rows at 4000 positions, 4 sequences, 4/2 heads, 72, 61, 109, 16 at 8000, 8 sequences, 8/4 heads, 258, 204, 425)
     p.tile_rows = p.columns / G;
     p.places = std::max(1, 512 / d->n_kv_heads);
     p.tiles = d->n_tokens / p.tile_rows + std::min(d->n_seqs, d->n_tokens);      // (a sequence's last tile may not be full)
@@ -478,13 +480,13 @@ int alora_tree_attention(const void *q, const void *k_cache, const void *v_cache
         if (merging) launch_kernel(combine, merge, dim3(256), 0, (hipStream_t)hip_stream, a, p.columns);
     };
     // Non-temporal copies where a sequence brings one tile on average: then its context is read once.  us, ordinary | non-temporal, 32/8 heads: 13 rows at 9000
-    // positions 21.5 | 19.7, at 128000 118 | 102, 64 x 8 rows at 8192 385 | 350, 64 x 24 400 | 385, 64 x 32 430 | 427, 64 x 40 (two tiles) 702 | 739; one context of
-    // 16000 for 12 sequences 101 | 97, of 8000 for 64 222 | 218.
+    // positions 21.0 | 19.5, at 128000 118 | 113, 64 x 8 rows at 8192 381 | 352, 64 x 24 475 | 462, 64 x 32 537 | 525, 64 x 40 (two tiles) 865 | 876, 16 x 8 at 4000 54.4 | 58.5;
+    // 48 of up to 64 rows, 64/8 heads, 633 | 676.
     const long long columns = (long long)dims->n_tokens * (dims->n_q_heads / dims->n_kv_heads);
     const bool once = columns <= 32ll * WAVES * dims->n_seqs;
     // Where half of the wavefronts have columns on average, the kernel that lets the other half take every second tile.  us, without | with: 13 rows at 2000
-    // positions 16.1 | 15.2, at 9000 19.4 | 17.3, 16 x 8 rows at 1000 34.2 | 27.9; at 16000 and more, where memory bounds them, the same within 2 %.  (With wider
-    // trees it loses: 48 of up to 64 rows and 8 heads a group 490 | 500.)
+    // positions 15.7 | 15.3, at 9000 19.5 | 17.2, at 128000 113 | 101, 16 x 8 rows at 1000 24.6 | 22.8, 64 x 8 at 8192 352 | 346, 64 x 16 407 | 360.  (With wider
+    // trees it loses: 64 x 40 876 | 884, 48 of up to 64 rows and 8 heads a group 676 | 681.)
     const bool share = columns <= 16ll * WAVES * dims->n_seqs;
     // Parts combined 16 at a time where a tile may have more than 16 of them (13 rows at 9001 positions 20.2 | 19.5 us; 16 x 8 rows at 4000, of fewer, 57.0 | 59.7).
     const bool many_parts = p.tiles <= p.places / 32;
