@@ -113,9 +113,9 @@ def test_values_of_selected_blocks_that_are_not_finite(dtype, d, group, all_bloc
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("score", [0.0, -7.0, -30.0, -69.0])
+@pytest.mark.parametrize("score", [0.0, -7.0, -30.0, -69.0, -87.0])
 def test_infinite_values_of_small_weight(dtype, score):
-    """One place of 300 with a score far below the others': its weight is 2^-100 at least, and an infinity of it is one."""
+    """One place of 300 with a score far below the others': its weight is a number of fp32 (2^-126 at least; the rest of it in bf16 has fewer bits), and an infinity of it is one."""
     d = 128
     t = Select(dtype, [299], 2, 2, d, 16, seed=4)
     t.q.fill_(1.0)
